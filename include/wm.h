@@ -392,6 +392,132 @@ size_t wm_text_workspace_bytes(const wm_text_model* model, int32_t n_chunks);
 wm_status wm_encode_text(const wm_text_model* model, const int32_t* tokens, const int32_t* tok_off,
                          int32_t S, float* z0, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Sequence models of schedules ---------------------------------------
+ * Building blocks of a transition that reads whole action sequences: cross
+ * attention of action steps to a program's encoded tokens, a short causal
+ * convolution and a selective state-space scan along the steps; each with its
+ * gradient, and each with a form for one new step.  Tensors are float32
+ * (WM_FP32) or bfloat16 (WM_BF16) as `dtype` says; weights of the convolution and
+ * the scan, states, softmax statistics and all sums are float32, and a result is
+ * rounded once when it is stored (the attention's probabilities, and in its
+ * gradient the score gradients, are rounded to bfloat16 as product operands when
+ * the tensors are).  Matrices have a row stride in elements (ld_*); rows
+ * themselves are dense.  Repeated calls give identical bits. */
+
+/* Cross attention.  Segment s has the query rows q_off[s] .. q_off[s+1] and the
+ * key rows k_off[s] .. k_off[s+1] (HOST tables of S+1 entries from 0 on, S <=
+ * WM_MAX_SEGMENTS): all steps of all candidates of a program share its keys.
+ *   q [rows][heads][head_dim], k and v [rows][kv_heads][head_dim]; query head
+ *   h reads key head h / (heads / kv_heads)
+ *   o = sum_j P_j v_j,  P_j = exp(scale q . k_j - lse),  lse = log sum_j exp(scale q . k_j)
+ * over the keys of the segment with kv_mask[row] != 0 (kv_mask: one byte per
+ * key row, NULL = all).  Values of k and v in hidden rows are never used.  A row
+ * without a visible key has o = 0 and lse = -infinity.
+ * Supported: head_dim 32, 64 or 128, heads a multiple of kv_heads, scale > 0.  Pointers and
+ * row strides (in bytes) must be multiples of 16, strides at most 2^22 elements. */
+typedef struct wm_attention {
+  int32_t dtype, heads, kv_heads, head_dim, S;
+  const int32_t *q_off, *k_off;       /* HOST */
+  const void *q, *k, *v;
+  int64_t ld_q, ld_k, ld_v;
+  const uint8_t* kv_mask;             /* may be NULL */
+  float scale;
+} wm_attention;
+
+/* Bytes of workspace of the forward (grad = 0) or the gradient call (256-byte
+ * aligned, need not be cleared); 0 on a bad argument. */
+size_t wm_cross_attention_workspace_bytes(const wm_attention* a, int32_t grad);
+
+/* o [rows][heads][head_dim] out; lse [rows][heads] float32 out (may be NULL). */
+wm_status wm_cross_attention(const wm_attention* a, void* o, int64_t ld_o, float* lse,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of L given d_o = dL/do, with o and lse of the forward call: dq as q,
+ * dk and dv as k and v (summed over the rows of the segment and over the heads that
+ * share a key head; 0 for hidden keys). */
+wm_status wm_cross_attention_grad(const wm_attention* a, const void* o, int64_t ld_o, const float* lse,
+                                  const void* d_o, int64_t ld_do, void* dq, int64_t ld_dq,
+                                  void* dk, int64_t ld_dk, void* dv, int64_t ld_dv,
+                                  void* ws, size_t ws_bytes, void* stream);
+
+/* Rows of the convolution and the scan: sequence s of B has the rows off[s] ..
+ * off[s+1] (device int32 [B+1], off[0] = 0, off[B] = rows), at most T_max of them
+ * (one each for a single step).  Offsets that are not so are clamped, and reported
+ * in `status` (device int32 [64], zeroed once by the caller; may be NULL): read and
+ * clear it with wm_device_status(status, 256, stream).  Outputs are then
+ * unspecified, as are those of rows in no sequence.
+ *
+ * Causal convolution of `width` taps (2, 3 or 4) per channel:
+ *   y_t[c] = act(bias[c] + sum_j weight[c][j] x_{t - width + 1 + j}[c])
+ * act(a) = a / (1 + exp(-a)) when silu != 0, else a.  Inputs before a sequence's
+ * start come from state [B][width - 1][channels] of x's type, oldest first (NULL = 0). */
+typedef struct wm_conv {
+  int32_t dtype, B, T_max, channels, width, silu;
+  int64_t rows;
+  const int32_t* off;
+  const void* x;
+  int64_t ld_x;
+  const float *weight, *bias;         /* [channels][width], [channels] (bias may be NULL) */
+  const void* state;                  /* may be NULL */
+  int32_t* status;                    /* may be NULL */
+} wm_conv;
+
+/* y [rows][channels] out; state_out: the last width - 1 inputs of every sequence
+ * (carried-in ones where it is shorter), in the layout of state, which it may
+ * be; may be NULL. */
+wm_status wm_causal_conv(const wm_conv* a, void* y, int64_t ld_y, void* state_out, void* stream);
+
+/* Workspace bytes of wm_causal_conv_grad (0 on a bad argument). */
+size_t wm_causal_conv_workspace_bytes(const wm_conv* a);
+
+/* Gradients given dy and, if not NULL, d_state_out = dL/d(state_out): dx, dweight
+ * [channels][width], dbias [channels] (may be NULL), d_state (as state; may be NULL). */
+wm_status wm_causal_conv_grad(const wm_conv* a, const void* dy, int64_t ld_dy, const void* d_state_out,
+                              void* dx, int64_t ld_dx, float* dweight, float* dbias, void* d_state,
+                              void* ws, size_t ws_bytes, void* stream);
+
+/* Selective state-space scan with `states` (8, 16 or 32) states per channel:
+ *   dt = softplus(delta_t[c] + delta_bias[c])
+ *   h_t[c][n] = exp(dt A[c][n]) h_{t-1}[c][n] + dt Bm_t[n] u_t[c]
+ *   y_t[c] = (sum_n Cm_t[n] h_t[c][n] + D[c] u_t[c]) silu(z_t[c])
+ * from h0 [B][channels][states] float32 (NULL = 0); without z the last factor is 1.
+ * u, delta, z, y have rows of `channels`, Bm and Cm rows of `states` values (16-byte
+ * aligned rows).  A [channels][states], D and delta_bias [channels] float32. */
+typedef struct wm_scan_args {
+  int32_t dtype, B, T_max, channels, states;
+  int64_t rows;
+  const int32_t* off;
+  const void *u, *delta, *z, *Bm, *Cm;          /* z may be NULL */
+  int64_t ld_u, ld_delta, ld_z, ld_B, ld_C;
+  const float *A, *D, *delta_bias, *h0;         /* D, delta_bias and h0 may be NULL */
+  int32_t* status;                              /* may be NULL */
+} wm_scan_args;
+
+/* Workspace bytes of wm_scan (grad = 0) or wm_scan_grad, and bytes of the states
+ * that a forward call keeps for the gradient (0 on a bad argument). */
+size_t wm_scan_workspace_bytes(const wm_scan_args* a, int32_t grad);
+size_t wm_scan_checkpoint_bytes(const wm_scan_args* a);
+
+/* y [rows][channels] out; hT [B][channels][states] float32 out: the last states (h0
+ * for an empty sequence; may be NULL, may be h0); checkpoints: out for
+ * wm_scan_grad (may be NULL). */
+wm_status wm_scan(const wm_scan_args* a, void* y, int64_t ld_y, float* hT, void* checkpoints,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient outputs.  du, ddelta, dz (required with z), dB and dC have the inputs' type
+ * and layout; dA, dD, ddelta_bias are float32 (dD and ddelta_bias may be NULL); dh0
+ * [B][channels][states] float32 (may be NULL). */
+typedef struct wm_scan_grads {
+  void *du, *ddelta, *dz, *dB, *dC;
+  int64_t ld_du, ld_ddelta, ld_dz, ld_dB, ld_dC;
+  float *dA, *dD, *ddelta_bias, *dh0;
+} wm_scan_grads;
+
+/* Gradients of L given dy = dL/dy and dhT = dL/dhT (NULL = 0), with the checkpoints
+ * that wm_scan wrote for the same arguments. */
+wm_status wm_scan_grad(const wm_scan_args* a, const void* checkpoints, const void* dy, int64_t ld_dy,
+                       const float* dhT, const wm_scan_grads* grads, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronise `stream`, read and clear the workspace's device error word.
  * Returns WM_OK, or WM_ERR_INPUT_RANGE with wm_last_error() naming the
  * violation(s); WM_ERR_DEVICE if the stream reports a failure. */
@@ -405,7 +531,8 @@ const char* wm_last_error(void);
  * 2 top-k, 3 bucketing, 4 action features, 5 encoder, 6 structured action
  * features, 7 tree-ensemble scores, 8 loss forward steps, 9 step losses,
  * 10 loss backward steps, 11 weight-gradient sums, 12 encoder dense
- * products, 13 encoder attention, 14 other encoder kernels.  Enabling resets the
+ * products, 13 encoder attention, 14 other encoder kernels, 15 cross attention,
+ * 16 causal convolution, 17 scan.  Enabling resets the
  * counters; reading synchronises on the recorded events.  At most 8192
  * launches per kernel are recorded while enabled. */
 wm_status wm_timing_enable(int32_t on);

@@ -23,7 +23,8 @@ PRECISIONS = {"fp32": WM_FP32, "bf16": WM_BF16}
 NORMS = {"none": WM_NORM_NONE, "l2": WM_NORM_L2}
 KERNELS = {"rollout": 0, "score": 1, "topk": 2, "bucket": 3, "phi": 4, "encode": 5,
            "phi_struct": 6, "trees": 7, "loss_fwd": 8, "loss_steps": 9, "loss_bwd": 10,
-           "loss_grads": 11, "text_gemm": 12, "text_attn": 13, "text_other": 14}
+           "loss_grads": 11, "text_gemm": 12, "text_attn": 13, "text_other": 14,
+           "cross_attention": 15, "causal_conv": 16, "scan": 17}
 
 # Exported symbols (kept in step with include/wm.h).
 SYMBOLS = (
@@ -33,6 +34,9 @@ SYMBOLS = (
     "wm_forest_destroy", "wm_phi_struct", "wm_score_trees", "wm_evaluate_trees",
     "wm_loss_workspace_bytes", "wm_rollout_loss", "wm_text_model_create", "wm_text_model_destroy",
     "wm_text_chunks", "wm_text_workspace_bytes", "wm_encode_text", "wm_evaluate_noalloc",
+    "wm_cross_attention_workspace_bytes", "wm_cross_attention", "wm_cross_attention_grad",
+    "wm_causal_conv", "wm_causal_conv_workspace_bytes", "wm_causal_conv_grad",
+    "wm_scan_workspace_bytes", "wm_scan_checkpoint_bytes", "wm_scan", "wm_scan_grad",
 )
 
 
@@ -81,6 +85,33 @@ TEXT_WEIGHT_KEYS = ("tok_emb", "pos_emb", "ln0_g", "ln0_b", "wqkv", "bqkv", "wo"
 
 class TextWeights(ctypes.Structure):
     _fields_ = [(n, _FP) for n in TEXT_WEIGHT_KEYS]
+
+class Attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "head_dim", "S")]
+                + [(n, ctypes.c_void_p) for n in ("q_off", "k_off", "q", "k", "v")]
+                + [(n, ctypes.c_int64) for n in ("ld_q", "ld_k", "ld_v")]
+                + [("kv_mask", ctypes.c_void_p), ("scale", ctypes.c_float)])
+
+
+class Conv(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "B", "T_max", "channels", "width", "silu")]
+                + [("rows", ctypes.c_int64), ("off", ctypes.c_void_p), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("weight", "bias", "state", "status")])
+
+
+class ScanArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "B", "T_max", "channels", "states")]
+                + [("rows", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("off", "u", "delta", "z", "Bm", "Cm")]
+                + [(n, ctypes.c_int64) for n in ("ld_u", "ld_delta", "ld_z", "ld_B", "ld_C")]
+                + [(n, ctypes.c_void_p) for n in ("A", "D", "delta_bias", "h0", "status")])
+
+
+class ScanGrads(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("du", "ddelta", "dz", "dB", "dC")]
+                + [(n, ctypes.c_int64) for n in ("ld_du", "ld_ddelta", "ld_dz", "ld_dB", "ld_dC")]
+                + [(n, ctypes.c_void_p) for n in ("dA", "dD", "ddelta_bias", "dh0")])
+
 
 _lib = None
 
@@ -153,6 +184,28 @@ def load_library(path: str = LIB_PATH):
     lib.wm_text_workspace_bytes.restype = sz
     lib.wm_encode_text.argtypes = [vp, vp, vp, i32, vp, vp, sz, vp]
     lib.wm_encode_text.restype = i32
+    i64 = ctypes.c_int64
+    at, cv, sc = ctypes.POINTER(Attention), ctypes.POINTER(Conv), ctypes.POINTER(ScanArgs)
+    lib.wm_cross_attention_workspace_bytes.argtypes = [at, i32]
+    lib.wm_cross_attention_workspace_bytes.restype = sz
+    lib.wm_cross_attention.argtypes = [at, vp, i64, vp, vp, sz, vp]
+    lib.wm_cross_attention.restype = i32
+    lib.wm_cross_attention_grad.argtypes = [at, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+    lib.wm_cross_attention_grad.restype = i32
+    lib.wm_causal_conv.argtypes = [cv, vp, i64, vp, vp]
+    lib.wm_causal_conv.restype = i32
+    lib.wm_causal_conv_workspace_bytes.argtypes = [cv]
+    lib.wm_causal_conv_workspace_bytes.restype = sz
+    lib.wm_causal_conv_grad.argtypes = [cv, vp, i64, vp, vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.wm_causal_conv_grad.restype = i32
+    lib.wm_scan_workspace_bytes.argtypes = [sc, i32]
+    lib.wm_scan_workspace_bytes.restype = sz
+    lib.wm_scan_checkpoint_bytes.argtypes = [sc]
+    lib.wm_scan_checkpoint_bytes.restype = sz
+    lib.wm_scan.argtypes = [sc, vp, i64, vp, vp, vp, sz, vp]
+    lib.wm_scan.restype = i32
+    lib.wm_scan_grad.argtypes = [sc, vp, vp, i64, vp, ctypes.POINTER(ScanGrads), vp, sz, vp]
+    lib.wm_scan_grad.restype = i32
     _lib = lib
     return lib
 
@@ -454,6 +507,270 @@ def encode_text(model: TextModel, tokens, tok_off, z0=None, ws=None, stream=None
     _check(load_library().wm_encode_text(model.handle, _ptr(tokens), offp, S, _ptr(z0), _ptr(ws),
                                          ws.numel(), _stream(stream)))
     return {"z0": z0, "ws": ws}
+
+
+# ---- sequence operators ----------------------------------------------------------
+def _dtype(t):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"tensors must be float32 or bfloat16, not {t.dtype}")
+    return WM_BF16 if t.dtype == torch.bfloat16 else WM_FP32
+
+
+def _on_gpu(t):
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+
+
+def _same(like, shape, **tensors):
+    """Checks that tensors (None allowed) are on like's device with its dtype and `shape`."""
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != tuple(shape)):
+            raise ValueError(f"{name} must be {tuple(shape)} {like.dtype} on {like.device}, not {tuple(t.shape)} "
+                             f"{t.dtype} on {t.device}")
+
+
+def _f32(dev, shape, **tensors):
+    """Checks that tensors (None allowed) are dense float32 of `shape` on `dev`."""
+    import torch
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.float32 or t.device != dev or tuple(t.shape) != tuple(shape)
+                              or not t.is_contiguous()):
+            raise ValueError(f"{name} must be dense {tuple(shape)} float32 on {dev}")
+
+
+def _rows(name, t):
+    """Row stride of a matrix [rows][width] or [rows][heads][width] whose rows are dense."""
+    shape, stride = t.shape, t.stride()
+    width = 1
+    for n, st in zip(reversed(shape[1:]), reversed(stride[1:])):
+        if n > 1 and st != width:
+            raise ValueError(f"{name}: only the row stride may differ from a dense tensor's")
+        width *= n
+    return stride[0] if shape[0] > 1 else width
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(n, given, dev):
+    import torch
+    if given is not None:
+        return given, given.numel() * given.element_size()
+    return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n else (None, 0)
+
+
+def _attention(q, k, v, q_off, k_off, kv_mask, scale):
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v are [rows][heads][head_dim]")
+    if k.shape[2] != q.shape[2]:
+        raise ValueError("q and k differ in head_dim")
+    _same(q, k.shape, k=k, v=v)
+    qo, qp = _host_i32(q_off)
+    ko, kp = _host_i32(k_off)
+    if qo.ndim != 1 or len(qo) != len(ko) or len(qo) < 2:
+        raise ValueError("q_off and k_off need S + 1 entries each")
+    if qo[-1] != q.shape[0] or ko[-1] != k.shape[0]:
+        raise ValueError("q_off and k_off must end at the number of rows")
+    if kv_mask is not None:
+        if kv_mask.dtype not in (torch.uint8, torch.bool) or tuple(kv_mask.shape) != (k.shape[0],) or \
+                kv_mask.device != q.device or not kv_mask.is_contiguous():
+            raise ValueError("kv_mask must be dense uint8 or bool [key rows] on the tensors' device")
+    a = Attention(dtype=_dtype(q), heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2], S=len(qo) - 1, q_off=qp, k_off=kp,
+                  q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), ld_q=_rows("q", q), ld_k=_rows("k", k), ld_v=_rows("v", v),
+                  kv_mask=_addr(kv_mask), scale=q.shape[2] ** -0.5 if scale is None else scale)
+    a.keep = (qo, ko)
+    _on_gpu(q)
+    return a
+
+
+def cross_attention(q, k, v, q_off, k_off, *, kv_mask=None, scale=None, o=None, lse=None, need_lse=False, ws=None,
+                    stream=None):
+    """Cross attention of query rows to the key rows of their segment (wm_cross_attention).
+
+    q [rows][heads][head_dim], k and v [rows][kv_heads][head_dim], float32 or bfloat16; row strides may
+    be larger than dense.  q_off, k_off: HOST [S + 1].  kv_mask: uint8 or bool per key row (0 =
+    hidden).  scale defaults to head_dim ** -0.5.  Returns o, lse [rows][heads] (with need_lse or
+    when given; the gradient needs it) and ws.
+    """
+    import torch
+    a = _attention(q, k, v, q_off, k_off, kv_mask, scale)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _same(q, q.shape, o=o)
+    if lse is None and need_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    _f32(q.device, q.shape[:2], lse=lse)
+    lib = load_library()
+    ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 0), ws, q.device)
+    _check(lib.wm_cross_attention(a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n, _stream(stream)))
+    return {"o": o, "lse": lse, "ws": ws}
+
+
+def cross_attention_grad(do, q, k, v, o, lse, q_off, k_off, *, kv_mask=None, scale=None, dq=None, dk=None, dv=None, ws=None,
+                         stream=None):
+    """Gradients dq, dk, dv of cross_attention given do = dL/do (wm_cross_attention_grad)."""
+    import torch
+    a = _attention(q, k, v, q_off, k_off, kv_mask, scale)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+    _same(q, q.shape, o=o, do=do, dq=dq)
+    _same(q, k.shape, dk=dk, dv=dv)
+    _f32(q.device, q.shape[:2], lse=lse)
+    lib = load_library()
+    ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 1), ws, q.device)
+    _check(lib.wm_cross_attention_grad(a, o.data_ptr(), _rows("o", o), _addr(lse), do.data_ptr(), _rows("do", do), dq.data_ptr(),
+                                       _rows("dq", dq), dk.data_ptr(), _rows("dk", dk), dv.data_ptr(), _rows("dv", dv), _addr(ws),
+                                       n, _stream(stream)))
+    return {"dq": dq, "dk": dk, "dv": dv, "ws": ws}
+
+
+def _offsets_ok(off, dev):
+    import torch
+    if off.dtype != torch.int32 or off.dim() != 1 or off.numel() < 1 or off.device != dev or not off.is_contiguous():
+        raise ValueError("off must be dense int32 [B + 1] on the tensors' device")
+    return off.numel() - 1
+
+
+def _status_ok(status, dev):
+    import torch
+    if status.dtype != torch.int32 or status.numel() < 64 or status.device != dev or not status.is_contiguous():
+        raise ValueError("status must be dense int32 [64] on the tensors' device")
+
+
+def _conv(x, off, weight, bias, T_max, silu, state, status):
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x is [rows][channels], weight [channels][width]")
+    C, W = x.shape[1], weight.shape[1]
+    B = _offsets_ok(off, x.device)
+    _f32(x.device, (C, W), weight=weight)
+    _f32(x.device, (C,), bias=bias)
+    _same(x, (B, W - 1, C), state=state)
+    if state is not None and not state.is_contiguous():
+        raise ValueError("state must be dense")
+    _on_gpu(x)
+    if status is not None:
+        _status_ok(status, x.device)
+    return Conv(dtype=_dtype(x), B=B, T_max=T_max, channels=C, width=W, silu=1 if silu else 0, rows=x.shape[0], off=off.data_ptr(),
+                x=x.data_ptr(), ld_x=_rows("x", x), weight=weight.data_ptr(), bias=_addr(bias), state=_addr(state),
+                status=_addr(status))
+
+
+def causal_conv(x, off, weight, bias=None, *, T_max, silu=True, state=None, state_out=None, need_state=False, y=None,
+                status=None, stream=None):
+    """Causal convolution along packed ragged sequences (wm_causal_conv).
+
+    x [rows][channels] float32 or bfloat16, off device int32 [B + 1], T_max: the longest sequence's
+    rows, weight [channels][width] and bias [channels] float32; state [B][width - 1][channels]:
+    the inputs before every sequence.  Returns y and state (the last width - 1 inputs, with
+    need_state or state_out, which may be `state`).  status: zeroed int32 [64] for device_status.
+    """
+    import torch
+    a = _conv(x, off, weight, bias, T_max, silu, state, status)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+    if state_out is None and need_state:
+        state_out = torch.empty((a.B, a.width - 1, a.channels), dtype=x.dtype, device=x.device)
+    _same(x, x.shape, y=y)
+    _same(x, (a.B, a.width - 1, a.channels), state_out=state_out)
+    _check(load_library().wm_causal_conv(a, y.data_ptr(), _rows("y", y), _ptr(state_out), _stream(stream)))
+    return {"y": y, "state": state_out}
+
+
+def causal_conv_grad(dy, x, off, weight, bias=None, *, T_max, silu=True, state=None, d_state_out=None, need_dstate=False,
+                     status=None, ws=None, stream=None):
+    """Gradients dx, dweight, dbias and (with need_dstate) dstate of causal_conv (wm_causal_conv_grad)."""
+    import torch
+    a = _conv(x, off, weight, bias, T_max, silu, state, status)
+    dev = x.device
+    _same(x, x.shape, dy=dy)
+    shape = (a.B, a.width - 1, a.channels)
+    _same(x, shape, d_state_out=d_state_out)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    dw = torch.empty(weight.shape, dtype=torch.float32, device=dev)
+    db = torch.empty(a.channels, dtype=torch.float32, device=dev)
+    ds = torch.empty(shape, dtype=x.dtype, device=dev) if need_dstate else None
+    lib = load_library()
+    ws, n = _workspace(lib.wm_causal_conv_workspace_bytes(a), ws, dev)
+    _check(lib.wm_causal_conv_grad(a, dy.data_ptr(), _rows("dy", dy), _ptr(d_state_out), dx.data_ptr(), _rows("dx", dx),
+                                   dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n, _stream(stream)))
+    return {"dx": dx, "dweight": dw, "dbias": db, "dstate": ds, "ws": ws}
+
+
+def _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status):
+    if u.dim() != 2 or A.dim() != 2 or Bm.dim() != 2:
+        raise ValueError("u is [rows][channels], A [channels][states], Bm and Cm [rows][states]")
+    C, N = A.shape
+    B = _offsets_ok(off, u.device)
+    _same(u, (u.shape[0], C), u=u, delta=delta, z=z)
+    _same(u, (u.shape[0], N), Bm=Bm, Cm=Cm)
+    _f32(u.device, (C, N), A=A)
+    _f32(u.device, (C,), D=D, delta_bias=delta_bias)
+    _f32(u.device, (B, C, N), h0=h0)
+    lds = [_rows(n, t) if t is not None else 0 for n, t in (("u", u), ("delta", delta), ("z", z), ("Bm", Bm), ("Cm", Cm))]
+    _on_gpu(u)
+    if status is not None:
+        _status_ok(status, u.device)
+    return ScanArgs(dtype=_dtype(u), B=B, T_max=T_max, channels=C, states=N, rows=u.shape[0], off=off.data_ptr(), u=u.data_ptr(),
+                    delta=delta.data_ptr(), z=_addr(z), Bm=Bm.data_ptr(), Cm=Cm.data_ptr(), ld_u=lds[0], ld_delta=lds[1], ld_z=lds[2],
+                    ld_B=lds[3], ld_C=lds[4], A=A.data_ptr(), D=_addr(D), delta_bias=_addr(delta_bias), h0=_addr(h0),
+                    status=_addr(status))
+
+
+def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bias=None, h0=None, hT=None, need_state=False,
+                   need_checkpoints=False, checkpoints=None, y=None, status=None, ws=None, stream=None):
+    """Selective state-space scan along packed ragged sequences (wm_scan); T_max = 1 is one step.
+
+    u, delta, z [rows][channels], Bm, Cm [rows][states], float32 or bfloat16; A [channels][states], D and
+    delta_bias [channels], h0 [B][channels][states] float32; off device int32 [B + 1].  Returns y, hT
+    (with need_state, or given: may be h0) and checkpoints (with need_checkpoints, or given: what
+    selective_scan_grad needs).  status: zeroed int32 [64] for device_status.
+    """
+    import torch
+    a = _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status)
+    dev = u.device
+    lib = load_library()
+    y = torch.empty(u.shape, dtype=u.dtype, device=dev) if y is None else y
+    if hT is None and need_state:
+        hT = torch.empty((a.B, a.channels, a.states), dtype=torch.float32, device=dev)
+    if checkpoints is None and need_checkpoints:
+        checkpoints = torch.empty(lib.wm_scan_checkpoint_bytes(a), dtype=torch.uint8, device=dev)
+    _same(u, u.shape, y=y)
+    _f32(dev, (a.B, a.channels, a.states), hT=hT)
+    if checkpoints is not None and checkpoints.numel() * checkpoints.element_size() < lib.wm_scan_checkpoint_bytes(a):
+        raise ValueError("checkpoints is too small")
+    ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 0), ws, dev)
+    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _ptr(checkpoints), _addr(ws), n, _stream(stream)))
+    return {"y": y, "hT": hT, "checkpoints": checkpoints, "ws": ws}
+
+
+def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=None, z=None, delta_bias=None, h0=None, dhT=None,
+                        need_dh0=None, status=None, ws=None, stream=None):
+    """Gradients of selective_scan (wm_scan_grad): du, ddelta, dA, dB, dC, dD, ddelta_bias, dz (with z) and dh0
+    (with h0, or need_dh0), given dy, the forward call's checkpoints and dhT (None = 0)."""
+    import torch
+    a = _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status)
+    dev = u.device
+    _same(u, u.shape, dy=dy)
+    shape = (a.B, a.channels, a.states)
+    _f32(dev, shape, dhT=dhT)
+    need_dh0 = h0 is not None if need_dh0 is None else need_dh0
+    lib = load_library()
+    if checkpoints is None or checkpoints.numel() * checkpoints.element_size() < lib.wm_scan_checkpoint_bytes(a):
+        raise ValueError("checkpoints is missing or too small")
+    like = dict(dtype=u.dtype, device=dev)
+    f32 = dict(dtype=torch.float32, device=dev)
+    C, N = A.shape
+    r = {"du": torch.empty(u.shape, **like), "ddelta": torch.empty(u.shape, **like),
+         "dz": torch.empty(u.shape, **like) if z is not None else None, "dB": torch.empty(Bm.shape, **like),
+         "dC": torch.empty(Cm.shape, **like), "dA": torch.empty((C, N), **f32), "dD": torch.empty(C, **f32),
+         "ddelta_bias": torch.empty(C, **f32), "dh0": torch.empty(shape, **f32) if need_dh0 else None}
+    g = ScanGrads(ld_du=C, ld_ddelta=C, ld_dz=C, ld_dB=N, ld_dC=N, **{k: _addr(t) for k, t in r.items()})
+    ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 1), ws, dev)
+    _check(lib.wm_scan_grad(a, _ptr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _stream(stream)))
+    return {**r, "ws": ws}
 
 
 def device_status(ws, stream=None) -> int:

@@ -6,7 +6,8 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = ["csrc/wm_api.hip", "csrc/wm_kernels.hip", "csrc/wm_text.hip"]
+SOURCES = ["csrc/wm_api.hip", "csrc/wm_kernels.hip", "csrc/wm_text.hip", "csrc/wm_attend.hip",
+           "csrc/wm_scan.hip"]
 HOST_SOURCES = ["csrc/wm_pack.cpp"]      # plain C++ (the tests also build it alone)
 LIB = os.path.join(HERE, "libwm.so")
 

@@ -106,7 +106,7 @@ int rollout_lds_bytes(const DevModel& m);
 enum TimedKernel { TK_ROLLOUT = 0, TK_SCORE = 1, TK_TOPK = 2, TK_BUCKET = 3, TK_PHI = 4, TK_ENCODE = 5,
                    TK_PHI_STRUCT = 6, TK_TREES = 7, TK_TRAIN_FWD = 8, TK_LOSS = 9,
                    TK_TRAIN_BWD = 10, TK_GRADS = 11, TK_TEXT_GEMM = 12, TK_TEXT_ATTN = 13,
-                   TK_TEXT_OTHER = 14, TK_COUNT = 15 };
+                   TK_TEXT_OTHER = 14, TK_ATTEND = 15, TK_CONV = 16, TK_SCAN = 17, TK_COUNT = 18 };
 void timing_begin(int kernel, hipStream_t st);
 void timing_end(int kernel, hipStream_t st);
 

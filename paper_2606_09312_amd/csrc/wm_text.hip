@@ -396,58 +396,6 @@ struct Gemm16Args {
   const float *ln_g, *ln_b;
   int M, N, K, tiles_n, gelu, slices;
 };
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) void lds_void;
-
-// Buffer resource of `bytes` bytes at p (wave-uniform).
-__device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
-  const uint64_t a = (uint64_t)p;
-  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
-               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)),
-               (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
-}
-// 16 bytes per lane from byte vo (per lane) of a buffer into LDS at d + lane *
-// 16.  Inline assembly, because the compiler otherwise waits
-// for every outstanding copy before an LDS read of another slice of the ring;
-// the kernels wait for the copies themselves (the instruction has no register
-// output, so nothing can be overwritten while it is in flight).  s_nop 4 covers the
-// wait of a load on a scalar register that a vector instruction wrote, which the
-// compiler does not see here.  m0 is listed
-// as clobbered for the compiler's own uses of it; the warning that it is a
-// reserved register does not apply to a value nobody keeps there.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void copy16(u32x4 r, __bf16* d, uint32_t vo) {
-  const uint32_t l = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)d);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(l), "v"(vo), "s"(r) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-// Wait until at most VM vector-memory operations are outstanding, and (LGKM)
-// for every LDS read.
-template <int VM, bool LGKM>
-__device__ __forceinline__ void wait_counts() {
-  __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((LGKM ? 0 : 15) << 8) | ((VM >> 4) << 14));
-}
-// Barrier without the waits of __syncthreads; nothing moves across it.
-__device__ __forceinline__ void raw_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
-__device__ __forceinline__ void sched_fence() { __builtin_amdgcn_sched_barrier(0); }
-template <int P>
-__device__ __forceinline__ void wave_priority() { __builtin_amdgcn_s_setprio(P); }
-
-// Tile of a workgroup: workgroups go to the 8 XCDs in turn, so XCD x takes a
-// contiguous run of tiles (columns fastest) and its L2 holds one A panel and W.
-__device__ __forceinline__ int xcd_tile(int bid, int total) {
-  const int per = total >> 3, rem = total & 7, x = bid & 7, i = bid >> 3;
-  return x * per + min(x, rem) + i;
-}
-
 // Slice s of a tile's `rows` rows from row r0 of an operand of M rows.
 __device__ __forceinline__ u32x4 slice_of(const __bf16* p, int r0, int rows, int M, int s) {
   return buffer_of(p + ((size_t)s * M + r0) * GK, (uint32_t)rows * (GK * 2));

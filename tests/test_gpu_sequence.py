@@ -1,0 +1,377 @@
+"""GPU parity of the sequence operators (cross attention, causal convolution, selective scan), forward,
+gradients and single steps, against the float64 oracle on the values that the kernels are given.
+
+Comparison: ||g - o||_2 / ||o||_2 over a tensor, and the largest |g - o| against max(|o|, rms(o)).
+Tolerances, fixed from the formats: float32 results are sums of at most a few thousand products and
+an exponential whose argument (below 40 here) is rounded to 2^-24 of itself, 40 * 6e-8 = 2.4e-6 at
+the worst and a tenth of that over a tensor: 2e-6 (2-norm), 5e-5 (largest).  A bfloat16 result is
+rounded once, at most 2^-9 of itself: 2^-8.  Attention also rounds the probabilities (and the
+score gradients) to bfloat16 as product operands, up to 2^-9 each before sums that do not cancel
+them: 2^-7.  Largest elements: 16 times the 2-norm's tolerance, a result being smaller than
+what is summed for it.  Gradients that are 0 by definition are compared absolutely."""
+import numpy as np
+import pytest
+
+from oracle import sequence as Q
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+TOL = {"f32": 2e-6, "bf16": 2.0 ** -8, "bf16_attn": 2.0 ** -7}
+
+
+@pytest.fixture(scope="module")
+def wm():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2606_09312_amd as wm
+    wm.load_library()
+    return wm
+
+
+def _dt(name):
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(name, got, want, tol):
+    g, o = _np(got), np.asarray(want, np.float64)
+    assert g.shape == o.shape, name
+    fin = np.isfinite(o)
+    assert (g[~fin] == o[~fin]).all(), f"{name}: values that are not finite"
+    d = np.abs(g[fin] - o[fin])
+    norm = np.linalg.norm(o[fin])
+    if norm == 0.0:
+        assert d.max(initial=0.0) <= tol, f"{name}: {d.max()} for 0"
+        return
+    rel = np.linalg.norm(d) / norm
+    rms = norm / np.sqrt(fin.sum())
+    most = (d / np.maximum(rms, np.abs(o[fin]))).max()
+    assert rel <= tol, f"{name}: relative 2-norm {rel:.2e} > {tol:.2e}"
+    assert most <= (5e-5 if tol < 1e-4 else 16 * tol), f"{name}: largest {most:.2e}"
+
+
+def offsets(lens):
+    return [0] + list(np.cumsum(lens))
+
+
+# ---- cross attention ---------------------------------------------------------------
+def make_attn(dtype, lq, lk, Hq, Hk, dh, hidden=0.0, seed=0, q_scale=1.0, fused=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    nq, nk = sum(lq), sum(lk)
+    q = (rnd(nq, Hq, dh) * q_scale).to(_dt(dtype))
+    kv = rnd(nk, 2, Hk, dh).to(_dt(dtype))
+    mask = None
+    if hidden:
+        mask = (torch.rand(nk, generator=g, device="cuda") >= hidden).to(torch.uint8)
+    k, v = (kv[:, 0], kv[:, 1]) if fused else (kv[:, 0].contiguous(), kv[:, 1].contiguous())
+    return q, k, v, offsets(lq), offsets(lk), mask, rnd(nq, Hq, dh).to(_dt(dtype))
+
+
+def check_attn(wm, dtype, q, k, v, qo, ko, mask, do, scale=None, grad=True, poison=True):
+    sc = q.shape[2] ** -0.5 if scale is None else scale
+    clean = [_np(t) for t in (q, k, v)]
+    if mask is not None and poison:                   # what hidden rows hold is never used
+        kp, vp = k.clone(), v.clone()
+        bad = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda").to(k.dtype)
+        for t in (kp, vp):
+            rows = (mask == 0).nonzero().squeeze(-1)
+            t[rows] = bad[torch.arange(len(rows), device="cuda") % 3][:, None, None]
+        k, v = kp, vp
+    m = None if mask is None else mask.cpu().numpy()
+    f = wm.cross_attention(q, k, v, qo, ko, kv_mask=mask, scale=scale, need_lse=True)
+    o, lse = Q.attention(*clean, qo, ko, sc, m)
+    t = TOL["f32"] if dtype == "f32" else TOL["bf16_attn"]
+    close("o", f["o"], o, t)
+    close("lse", f["lse"], lse, TOL["f32"])
+    if not grad:
+        return
+    b = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko, kv_mask=mask, scale=scale)
+    for n, want in zip(("dq", "dk", "dv"), Q.attention_grad(_np(do), *clean, qo, ko, sc, m)):
+        close(n, b[n], want, t)
+    again = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko, kv_mask=mask, scale=scale)
+    for n in ("dq", "dk", "dv"):
+        assert torch.equal(b[n].view(torch.uint8), again[n].view(torch.uint8)), f"{n}: another result the second time"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("lq,lk,Hq,Hk", [
+    ([129, 31, 64], [65, 257, 33], 2, 2),              # around the tiles' edges
+    ([1, 2, 0, 3], [300, 7, 40, 0], 6, 2),             # few rows, groups of 3; no rows; no keys
+    ([40], [1500], 4, 1),                              # one segment, groups of 4, keys split
+])
+def test_attention(wm, dtype, dh, lq, lk, Hq, Hk):
+    print(f"[attn] {dtype} dh={dh} lq={lq} lk={lk} heads={Hq}/{Hk}", flush=True)
+    check_attn(wm, dtype, *make_attn(dtype, lq, lk, Hq, Hk, dh))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lq,lk", [([5, 130, 9], [70, 200, 64]), ([2, 1], [900, 40])])
+def test_attention_hidden_keys(wm, dtype, lq, lk):
+    print(f"[attn] hidden {dtype} lq={lq} lk={lk}", flush=True)
+    q, k, v, qo, ko, mask, do = make_attn(dtype, lq, lk, 4, 2, 64, hidden=0.4, seed=3)
+    mask[:ko[1]] = 0                                   # the first segment shows nothing
+    check_attn(wm, dtype, q, k, v, qo, ko, mask, do)
+    mask[:ko[1]] = 0
+    mask[ko[1] - 1] = 1                                # .. and then its last key only
+    check_attn(wm, dtype, q, k, v, qo, ko, mask.bool(), do)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_one_key(wm, dtype):
+    """With one key the weights are 1: o = v, dv sums do, and dq, dk are 0 by definition; what is left of
+    them is the rounding of two equal sums (|do . v| up to 40 here, 2^-8 of it in bfloat16's o)."""
+    q, k, v, qo, ko, _, do = make_attn(dtype, [3, 40], [1, 1], 2, 1, 64, seed=5)
+    f = wm.cross_attention(q, k, v, qo, ko, need_lse=True)
+    want = torch.cat([v[0].expand(3, 2, 64), v[1].expand(40, 2, 64)])
+    assert torch.equal(f["o"], want)
+    b = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko)
+    assert b["dq"].abs().max() < 1e-4 and b["dk"].abs().max() < 1e-3
+    close("dv", b["dv"], np.stack([_np(do)[:3].sum((0, 1)), _np(do)[3:].sum((0, 1))])[:, None], TOL["bf16_attn" if dtype == "bf16" else "f32"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_extreme_scores(wm, dtype):
+    """Scores of +-1000 (one key takes all), and rows whose scores all overflow to -infinity."""
+    q, k, v, qo, ko, _, do = make_attn(dtype, [70], [130], 2, 2, 32, seed=6)
+    q = (q.float().sign() * 12.0).to(q.dtype)
+    k = (k.float().sign() * 12.0).to(k.dtype)
+    check_attn(wm, dtype, q, k, v, qo, ko, None, do, grad=False)
+    big = torch.full_like(q[:2], 2.0 ** 126)
+    f = wm.cross_attention(big, -big[:1].expand(1, 2, 32).contiguous().repeat(5, 1, 1), v[:5].contiguous(), [0, 2], [0, 5], need_lse=True)
+    assert (f["o"] == 0).all() and (f["lse"] == -float("inf")).all()
+
+
+def test_attention_many_segments_and_scale(wm):
+    r = np.random.default_rng(7)
+    lq, lk = list(r.integers(0, 4, 400)), list(r.integers(0, 50, 400))
+    check_attn(wm, "bf16", *make_attn("bf16", lq, lk, 2, 1, 32, seed=8), scale=0.31)
+
+
+def test_attention_rows_past_32_bits(wm):
+    """Key rows 64 KiB apart: their byte offsets pass 2^32."""
+    n, ld = 70001, 32768
+    kv = torch.zeros((n, ld), dtype=torch.bfloat16, device="cuda")
+    assert n * ld * 2 > 2 ** 32
+    kv[:, :64] = torch.randn((n, 64), device="cuda", generator=torch.Generator(device="cuda").manual_seed(9)).to(torch.bfloat16)
+    k, v = kv[:, :32].unflatten(1, (1, 32)), kv[:, 32:64].unflatten(1, (1, 32))
+    q = torch.randn((3, 1, 32), device="cuda").to(torch.bfloat16)
+    f = wm.cross_attention(q, k, v, [0, 3], [0, n], need_lse=True)
+    o, lse = Q.attention(_np(q), _np(k), _np(v), [0, 3], [0, n], 32 ** -0.5)
+    close("o", f["o"], o, TOL["bf16_attn"])
+    close("lse", f["lse"], lse, TOL["f32"])
+
+
+def test_attention_gradient_against_differences(wm):
+    """The float32 gradient against central differences of the float32 forward along random directions: a
+    step of 1e-2 leaves a third-order term of about 1e-4 of the slope and rounding of 1e-5."""
+    q, k, v, qo, ko, _, do = make_attn("f32", [50, 9], [70, 33], 4, 2, 64, seed=10)
+    f = wm.cross_attention(q, k, v, qo, ko, need_lse=True)
+    b = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko)
+    loss = lambda a: (wm.cross_attention(*a, qo, ko)["o"].double() * do).sum().item()  # noqa: E731
+    for i, n in enumerate(("dq", "dk", "dv")):
+        d = torch.randn(b[n].shape, device="cuda")
+        d /= d.norm()
+        ins = [q, k.contiguous(), v.contiguous()]
+        hi, lo = list(ins), list(ins)
+        hi[i], lo[i] = ins[i] + 1e-2 * d, ins[i] - 1e-2 * d
+        slope = (loss(hi) - loss(lo)) / 2e-2
+        want = (b[n].double() * d).sum().item()
+        assert abs(slope - want) < 1e-3 * (abs(want) + b[n].norm().item() / b[n].numel() ** 0.5), (n, slope, want)
+
+
+# ---- convolution -------------------------------------------------------------------
+LENS = [[5, 0, 1, 2, 3, 17, 64, 40], [1] * 37, [333]]
+
+
+def make_conv(dtype, lens, C, W, seed, pad=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    n, B = sum(lens), len(lens)
+    x = rnd(n, C + pad).to(_dt(dtype))[:, pad // 2:pad // 2 + C]
+    off = torch.tensor(offsets(lens), dtype=torch.int32, device="cuda")
+    return (x, off, rnd(C, W), rnd(C), rnd(B, W - 1, C).to(_dt(dtype)), rnd(n, C).to(_dt(dtype)), rnd(B, W - 1, C).to(_dt(dtype)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("C,W,silu,pad", [(64, 4, True, 0), (37, 3, True, 3), (8, 2, False, 6)])
+def test_conv(wm, dtype, lens, C, W, silu, pad):
+    print(f"[conv] {dtype} lens={lens} C={C} W={W}", flush=True)
+    x, off, w, b, st, dy, ds = make_conv(dtype, lens, C, W, 20, pad)
+    status = torch.zeros(64, dtype=torch.int32, device="cuda")
+    o, T = offsets(lens), max(lens)
+    for state, bias, dso in ((None, None, None), (st, b, ds)):
+        f = wm.causal_conv(x, off, w, bias, T_max=T, silu=silu, state=state, need_state=True, status=status)
+        nps = None if state is None else _np(state)
+        nb = None if bias is None else _np(bias)
+        y, out = Q.conv(_np(x), o, _np(w), nb, silu, nps)
+        close("y", f["y"], y, TOL[dtype])
+        assert (_np(f["state"]) == out).all()          # copies
+        r = wm.causal_conv_grad(dy, x, off, w, bias, T_max=T, silu=silu, state=state, d_state_out=dso, need_dstate=True, status=status)
+        want = Q.conv_grad(_np(dy), _np(x), o, _np(w), nb, silu, nps, None if dso is None else _np(dso))
+        for n, g, t in zip(("dx", "dweight", "dbias", "dstate"), want, (TOL[dtype], TOL["f32"], TOL["f32"], TOL[dtype])):
+            close(n, r[n], g, t)
+    again = wm.causal_conv_grad(dy, x, off, w, b, T_max=T, silu=silu, state=st, d_state_out=ds, need_dstate=True)
+    for n in ("dx", "dweight", "dbias", "dstate"):
+        assert torch.equal(r[n], again[n])
+    wm.device_status(status)
+
+
+def test_conv_state_in_place_and_steps_equal_whole(wm):
+    """One step at a time, the state updated in place, gives the whole sequence's outputs bit for bit."""
+    x, off, w, b, st, _, _ = make_conv("bf16", [9, 9, 9], 40, 4, 21)
+    whole = wm.causal_conv(x, off, w, b, T_max=9, state=st, need_state=True)
+    state = st.clone()
+    one = torch.arange(4, dtype=torch.int32, device="cuda")
+    for t in range(9):
+        f = wm.causal_conv(x.view(3, 9, 40)[:, t].contiguous(), one, w, b, T_max=1, state=state, state_out=state)
+        assert torch.equal(f["y"], whole["y"].view(3, 9, 40)[:, t])
+    assert torch.equal(state, whole["state"])
+
+
+# ---- scan --------------------------------------------------------------------------
+def make_scan(dtype, lens, C, N, seed, full=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    n, B, t = sum(lens), len(lens), _dt(dtype)
+    bc = rnd(n, 2 * N).to(t)
+    uz = rnd(n, 2 * C + 1).to(t)                      # odd row stride, u and z side by side
+    a = dict(u=uz[:, 1:C + 1], delta=rnd(n, C).to(t), A=-torch.exp(rnd(C, N) * 0.7), Bm=bc[:, :N], Cm=bc[:, N:])
+    opt = dict(D=rnd(C), z=uz[:, C + 1:], delta_bias=rnd(C) - 1.0, h0=rnd(B, C, N)) if full else {}
+    off = torch.tensor(offsets(lens), dtype=torch.int32, device="cuda")
+    return a, opt, off, rnd(n, C).to(t), rnd(B, C, N)
+
+
+def check_scan(wm, dtype, lens, C, N, seed, full=True):
+    a, opt, off, dy, dhT = make_scan(dtype, lens, C, N, seed, full)
+    status = torch.zeros(64, dtype=torch.int32, device="cuda")
+    T = max(lens)
+    kw = dict(T_max=T, status=status, **opt)
+    args = (a["u"], a["delta"], a["A"], a["Bm"], a["Cm"], off)
+    f = wm.selective_scan(*args, need_state=True, need_checkpoints=True, **kw)
+    host = {n: _np(t) for n, t in {**a, **opt}.items()}
+    o = offsets(lens)
+    y, hT = Q.scan(off=o, **host)
+    close("y", f["y"], y, TOL[dtype])
+    close("hT", f["hT"], hT, TOL["f32"])
+    plain = wm.selective_scan(*args, need_state=True, **kw)      # no states kept: the same sums but for single steps
+    close("y", plain["y"], y, TOL[dtype])
+    close("hT", plain["hT"], hT, TOL["f32"])
+    for d in ((dhT, None) if full else (None,)):
+        r = wm.selective_scan_grad(dy, *args, f["checkpoints"], dhT=d, need_dh0=True, **kw)
+        want = Q.scan_grad(_np(dy), off=o, dhT=None if d is None else _np(d), **host)
+        for n, g in want.items():
+            if r[n] is not None:
+                close(n, r[n], g, TOL["f32"] if n in ("dA", "dD", "ddelta_bias", "dh0") else TOL[dtype])
+    again = wm.selective_scan_grad(dy, *args, f["checkpoints"], dhT=d, need_dh0=True, **kw)
+    for n in want:
+        assert r[n] is None or torch.equal(r[n], again[n]), n
+    wm.device_status(status)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [8, 16, 32])
+@pytest.mark.parametrize("lens,C", [([5, 0, 1, 15, 16, 17, 33], 70), ([1] * 9, 33), ([300, 129], 20), ([64, 3], 256)])
+def test_scan(wm, dtype, N, lens, C):
+    print(f"[scan] {dtype} N={N} lens={lens} C={C}", flush=True)
+    check_scan(wm, dtype, lens, C, N, 30)
+
+
+@pytest.mark.parametrize("N", [8, 16])
+def test_scan_without_options(wm, N):
+    check_scan(wm, "f32", [40, 0, 7], 19, N, 31, full=False)
+
+
+def test_scan_many_sequences(wm):
+    lens = [int(x) for x in np.random.default_rng(1).integers(0, 6, 3000)]
+    check_scan(wm, "bf16", lens, 18, 8, 32)
+
+
+def test_scan_long_cut_into_chunks(wm):
+    print("[scan] chunks", flush=True)
+    check_scan(wm, "f32", [1000, 0, 131, 700], 65, 16, 33)
+
+
+def test_scan_steps_equal_whole(wm):
+    """Single steps, the states updated in place, against the whole sequence."""
+    a, opt, off, _, _ = make_scan("f32", [11, 11, 11], 50, 16, 34)
+    whole = wm.selective_scan(a["u"], a["delta"], a["A"], a["Bm"], a["Cm"], off, T_max=11, need_state=True, **opt)
+    h = opt["h0"].clone()
+    one = torch.arange(4, dtype=torch.int32, device="cuda")
+    at = lambda x, t: x.reshape(3, 11, -1)[:, t].contiguous()  # noqa: E731
+    for t in range(11):
+        f = wm.selective_scan(at(a["u"], t), at(a["delta"], t), a["A"], at(a["Bm"], t), at(a["Cm"], t), one, T_max=1, D=opt["D"],
+                              z=at(opt["z"], t), delta_bias=opt["delta_bias"], h0=h, hT=h)
+        close(f"y {t}", f["y"], _np(at(whole["y"], t)), TOL["f32"])
+    close("hT", h, _np(whole["hT"]), TOL["f32"])
+
+
+@pytest.mark.parametrize("dtype", ["f32"])
+def test_scan_extreme_steps(wm, dtype):
+    """delta of +-60 (softplus 60 and 1e-26) and decays that underflow."""
+    a, opt, off, _, _ = make_scan(dtype, [20, 5], 16, 8, 35)
+    a["delta"] = a["delta"].sign() * 60.0
+    f = wm.selective_scan(a["u"], a["delta"], a["A"], a["Bm"], a["Cm"], off, T_max=20, need_state=True, **opt)
+    y, hT = Q.scan(off=[0, 20, 25], **{n: _np(t) for n, t in {**a, **opt}.items()})
+    close("y", f["y"], y, TOL["f32"])
+    close("hT", f["hT"], hT, TOL["f32"])
+
+
+def test_bad_offsets_are_reported(wm):
+    """Offsets outside the rows, decreasing ones and sequences past T_max: clamped and reported."""
+    a, _, off, _, _ = make_scan("f32", [6, 6], 16, 8, 36)
+    args = (a["u"], a["delta"], a["A"], a["Bm"], a["Cm"])
+    x, _, w, b, _, _, _ = make_conv("f32", [6, 6], 16, 3, 37)
+    for bad, T in (([0, 6, 99], 6), ([0, 9, 4], 12), ([-5, 6, 12], 12), ([0, 6, 12], 5)):
+        o = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        for call in (lambda st: wm.selective_scan(*args, o, T_max=T, need_checkpoints=True, status=st),
+                     lambda st: wm.causal_conv(x, o, w, b, T_max=T, status=st)):
+            status = torch.zeros(64, dtype=torch.int32, device="cuda")
+            call(status)
+            with pytest.raises(wm.WMError) as e:
+                wm.device_status(status)
+            assert e.value.status == 5
+            wm.device_status(status)                    # cleared
+
+
+# ---- streams and graphs --------------------------------------------------------------
+def test_other_stream_and_graph(wm):
+    """Calls on another stream, and captured: every replay on new inputs equals the eager call."""
+    q, k, v, qo, ko, _, do = make_attn("bf16", [70, 30], [200, 64], 4, 2, 64, seed=40)
+    a, opt, off, dy, dhT = make_scan("bf16", [30, 9], 48, 16, 41)
+
+    def calls():
+        f = wm.cross_attention(q, k, v, qo, ko, need_lse=True)
+        g = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko)
+        s = wm.selective_scan(a["u"], a["delta"], a["A"], a["Bm"], a["Cm"], off, T_max=30, need_state=True, need_checkpoints=True, **opt)
+        b = wm.selective_scan_grad(dy, a["u"], a["delta"], a["A"], a["Bm"], a["Cm"], off, s["checkpoints"], T_max=30, dhT=dhT, **opt)
+        c = wm.causal_conv(a["u"], off, opt["h0"][0, :, :4].contiguous(), opt["D"], T_max=30, need_state=True)
+        return [f["o"], f["lse"], g["dq"], g["dk"], g["dv"], s["y"], s["hT"], b["du"], b["dA"], b["dB"], c["y"], c["state"]]
+    want = [t.clone() for t in calls()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = calls()
+        for _ in range(2):
+            calls()
+    side.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    for i in range(4):
+        q.normal_()
+        a["u"].normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for x, y in zip(got, calls()):
+            assert torch.equal(x, y), f"replay {i}"
