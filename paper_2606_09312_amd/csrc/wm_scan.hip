@@ -21,7 +21,7 @@ using namespace wm;
 namespace wm {
 namespace scan {
 
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <class T>
 constexpr bool IS_BF = std::is_same<T, __bf16>::value;
@@ -30,17 +30,20 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float rcp_of(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ __forceinline__ float sigmoid(float x) { return rcp_of(1.0f + exp2_of(-x * LOG2E)); }
 
-// log(1 + e) for 0 <= e <= 1 as 2 atanh(s), s = e / (2 + e) <= 1/3: the odd series to
-// s^13 (what is left out is below 2e-8 of the value).
+// log(1 + e) for 0 <= e <= 1 as e times a polynomial of degree 9 (Lawson-weighted least
+// squares of log(1 + e) / e in float64: at most 4.8e-9 off; in float32 1.4e-7 at
+// most, 2.9e-8 on average, also where e is small, which log2(1 + e) would lose).
 __device__ __forceinline__ float log1p_unit(float e) {
-  const float s = e * rcp_of(2.0f + e), q = s * s;
-  float p = fmaf(q, 1.0f / 13.0f, 1.0f / 11.0f);
-  p = fmaf(p, q, 1.0f / 9.0f);
-  p = fmaf(p, q, 1.0f / 7.0f);
-  p = fmaf(p, q, 1.0f / 5.0f);
-  p = fmaf(p, q, 1.0f / 3.0f);
-  p = fmaf(p, q, 1.0f);
-  return 2.0f * s * p;
+  float p = fmaf(-0.0032440212089568377f, e, 0.01985144428908825f);
+  p = fmaf(p, e, -0.056959498673677444f);
+  p = fmaf(p, e, 0.10603651404380798f);
+  p = fmaf(p, e, -0.15305590629577637f);
+  p = fmaf(p, e, 0.1967593878507614f);
+  p = fmaf(p, e, -0.24954134225845337f);
+  p = fmaf(p, e, 0.3332996368408203f);
+  p = fmaf(p, e, -0.4999990165233612f);
+  p = fmaf(p, e, 1.0f);
+  return p * e;
 }
 // softplus(x) = max(x, 0) + log(1 + exp(-|x|))
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1p_unit(exp2_of(-fabsf(x) * LOG2E)); }
@@ -51,7 +54,9 @@ struct Span {
   int len;
 };
 __device__ __forceinline__ Span span_of(const int32_t* off, int s, int64_t rows, int T_max, int32_t* status, bool report) {
-  const int64_t a = off[s], b = off[s + 1];
+  // constant while a kernel runs: scalar loads where s is uniform, which no vector load waits for
+  const __attribute__((address_space(4))) int32_t* o = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)off;
+  const int64_t a = o[s], b = o[s + 1];
   const int64_t lo = a < 0 ? 0 : a > rows ? rows : a, hi = b < lo ? lo : b > rows ? rows : b;
   const int64_t n = hi - lo > T_max ? T_max : hi - lo;
   if (report && status && (lo != a || n != b - a)) atomicOr(status, ERRBIT_LEN);
@@ -348,8 +353,7 @@ __global__ __launch_bounds__(256) void conv_sum_kernel(const float* part, int gr
 // Rows of few, long sequences are also cut into chunks of `chunk` steps: every chunk's
 // end state from zero and its sum of dt first, then the states that the chunks
 // start from, then the chunks side by side.
-template <int N>
-constexpr int CK = N == 32 ? 8 : 16;          // steps between kept states (the gradient's registers hold so many)
+constexpr int CK = 8;       // steps between kept states: what the gradient's registers hold of a block
 
 struct ScanArgs {
   const int32_t* off;
@@ -366,42 +370,42 @@ struct ScanArgs {
 
 // First kept state of sequence s: ceil(len / CK) states each, so this leaves room for
 // every sequence before it.
-template <int N>
-__device__ __forceinline__ int64_t ckpt_base(const Span& sp, int s) { return sp.r0 / CK<N> + s; }
+__device__ __forceinline__ int64_t ckpt_base(const Span& sp, int s) { return sp.r0 / CK + s; }
 // Kept state i, channel c, states n ..  n + 3: quads side by side over the channels.
 template <int N>
 __device__ __forceinline__ float* ckpt_at(float* ckpt, int64_t i, int D, int c, int n) {
   return ckpt + ((i * (N / 4) + n / 4) * D + c) * 4 + (n & 3);
 }
 
-// Row t of B or C for all lanes (uniform address).
+// A row of B or C at a uniform address, kept as the 32-bit words that it is in
+// memory (scalar loads; two bf16 values a word).
 template <class T, int N>
-__device__ __forceinline__ void load_row(float (&x)[N], const T* p) {
-  if constexpr (IS_BF<T>) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+struct Row {
+  static constexpr int W = N * (int)sizeof(T) / 4;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const T* p) {
+    typedef __attribute__((address_space(4))) const uint32_t cu32;
+    const cu32* c = (const cu32*)(uintptr_t)p;
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      const uint32_t v = w[i];
-      x[2 * i] = __uint_as_float(v << 16);
-      x[2 * i + 1] = __uint_as_float(v & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = p[i];
+    for (int i = 0; i < W; ++i) w[i] = c[i];
   }
-}
+  __device__ __forceinline__ float get(int n) const {
+    if constexpr (IS_BF<T>) return __uint_as_float(n & 1 ? w[n / 2] & 0xffff0000u : w[n / 2] << 16);
+    else return __uint_as_float(w[n]);
+  }
+};
 
 // Forward over one (sequence, chunk) and 64 channels per wavefront, one per lane, all
 // N states in registers; rows of B and C are uniform (scalar loads).  LOCAL: only the
-// chunk's end state from zero and its sum of dt.
+// chunk's end state from zero and its sum of dt.  What bounds it is the vector
+// unit: per state an exponential (quarter rate) and four instructions.
 constexpr int SU = 8;       // steps whose rows are loaded together, one block ahead
-template <class T, int N, bool LOCAL>
+template <class T, int N, bool LOCAL, bool Z>
 __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int64_t item = id / a.cblocks;
-  if (item >= (int64_t)a.B * a.chunks) return;
-  const int cb = (int)(id - item * a.cblocks), s = (int)(item / a.chunks), ch = (int)(item - (int64_t)s * a.chunks);
+  const uint32_t id = blockIdx.x * 4 + wave, item = id / (uint32_t)a.cblocks;
+  if (item >= (uint32_t)a.B * (uint32_t)a.chunks) return;
+  const int cb = (int)(id - item * a.cblocks), s = (int)(item / (uint32_t)a.chunks), ch = (int)(item - (uint32_t)s * a.chunks);
   const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, !LOCAL && cb == 0 && ch == 0 && lane == 0);
   const int t0 = ch * a.chunk, t1 = min(t0 + a.chunk, sp.len);
   if (t0 >= t1 && ch > 0) return;
@@ -410,7 +414,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a) {
   float h[N], A2[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) A2[n] = a.A[(int64_t)cc * N + n] * LOG2E;
-  const float* h0 = LOCAL ? nullptr : a.chunks > 1 ? a.carry + (item * a.D + cc) * N
+  const float* h0 = LOCAL ? nullptr : a.chunks > 1 ? a.carry + ((int64_t)item * a.D + cc) * N
                                     : a.h0 ? a.h0 + ((int64_t)s * a.D + cc) * N : nullptr;
 #pragma unroll
   for (int n = 0; n < N; n += 4) {
@@ -419,63 +423,79 @@ __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a) {
     for (int i = 0; i < 4; ++i) h[n + i] = v[i];
   }
   const float bias = a.bias ? a.bias[cc] : 0.0f, Dp = a.Dp ? a.Dp[cc] : 0.0f;
-  const T* up = static_cast<const T*>(a.u) + sp.r0 * a.ld_u + cc;
-  const T* dp = static_cast<const T*>(a.delta) + sp.r0 * a.ld_delta + cc;
-  const T* zp = a.z ? static_cast<const T*>(a.z) + sp.r0 * a.ld_z + cc : nullptr;
-  const T* bp = static_cast<const T*>(a.Bm) + sp.r0 * a.ld_B;
-  const T* cp = static_cast<const T*>(a.Cm) + sp.r0 * a.ld_C;
-  T* yp = static_cast<T*>(a.y) + sp.r0 * a.ld_y + cc;
+  // row t0 of every matrix (uniform; the lane's channel is an offset)
+  const T* up = static_cast<const T*>(a.u) + (sp.r0 + t0) * a.ld_u;
+  const T* dp = static_cast<const T*>(a.delta) + (sp.r0 + t0) * a.ld_delta;
+  const T* zp = Z ? static_cast<const T*>(a.z) + (sp.r0 + t0) * a.ld_z : nullptr;
+  const T* bp = static_cast<const T*>(a.Bm) + (sp.r0 + t0) * a.ld_B;
+  const T* cp = static_cast<const T*>(a.Cm) + (sp.r0 + t0) * a.ld_C;
+  T* yp = LOCAL ? nullptr : static_cast<T*>(a.y) + (sp.r0 + t0) * a.ld_y;
   float sdt = 0.0f;
+  const int steps = t1 - t0;
+  const int64_t ck0 = LOCAL ? 0 : ckpt_base(sp, s) + t0 / CK;
   T un[SU], dn[SU], zn[SU];
-  auto load = [&](int t) {
+  auto load = [&](int t) {                     // rows t .. t + SU - 1, past the last one that one again
 #pragma unroll
     for (int i = 0; i < SU; ++i) {
-      const int64_t r = min(t + i, t1 - 1);
-      un[i] = up[r * a.ld_u];
-      dn[i] = dp[r * a.ld_delta];
-      if (!LOCAL && zp) zn[i] = zp[r * a.ld_z];
+      const int64_t r = min(t + i, steps - 1);
+      un[i] = (up + r * a.ld_u)[cc];
+      dn[i] = (dp + r * a.ld_delta)[cc];
+      if (Z) zn[i] = (zp + r * a.ld_z)[cc];
     }
   };
-  if (t0 < t1) load(t0);
-  const int64_t ck0 = LOCAL ? 0 : ckpt_base<N>(sp, s);
-  for (int tb = t0; tb < t1; tb += SU) {
+  Row<T, N> Bn, Cn;
+  auto load_bc = [&](int t) {
+    const int64_t r = min(t, steps - 1);
+    Bn.load(bp + r * a.ld_B);
+    if (!LOCAL) Cn.load(cp + r * a.ld_C);
+  };
+  auto step = [&](int t, float u, float d, float z) {
+    const Row<T, N> Br = Bn, Cr = Cn;
+    load_bc(t + 1);
+    const float du = d * u;
+    float y = Dp * u;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      h[n] = fmaf(exp2_of(d * A2[n]), h[n], du * Br.get(n));
+      if (!LOCAL) y = fmaf(Cr.get(n), h[n], y);
+    }
+    if (LOCAL) {
+      sdt += d;
+    } else {
+      if (Z) y *= z * sigmoid(z);
+      if (mine) (yp + (int64_t)t * a.ld_y)[cc] = (T)y;
+    }
+  };
+  if (steps > 0) {
+    load(0);
+    load_bc(0);
+  }
+  for (int tb = 0; tb < steps; tb += SU) {
     float u[SU], d[SU], z[SU];
 #pragma unroll
     for (int i = 0; i < SU; ++i) {
       u[i] = (float)un[i];
       d[i] = softplus((float)dn[i] + bias);
-      if (!LOCAL) z[i] = zp ? (float)zn[i] : 0.0f;
+      z[i] = Z ? (float)zn[i] : 0.0f;
     }
-    if (tb + SU < t1) load(tb + SU);
-    if (!LOCAL && a.ckpt && tb % CK<N> == 0 && mine) {
+    if (tb + SU < steps) load(tb + SU);
+    if (!LOCAL && a.ckpt && tb % CK == 0 && mine) {
 #pragma unroll
       for (int n = 0; n < N; n += 4)
-        *reinterpret_cast<f32x4*>(ckpt_at<N>(a.ckpt, ck0 + tb / CK<N>, a.D, c, n)) = f32x4{h[n], h[n + 1], h[n + 2], h[n + 3]};
+        *reinterpret_cast<f32x4*>(ckpt_at<N>(a.ckpt, ck0 + tb / CK, a.D, c, n)) = f32x4{h[n], h[n + 1], h[n + 2], h[n + 3]};
     }
+    if (tb + SU <= steps) {
 #pragma unroll
-    for (int i = 0; i < SU; ++i) {
-      if (tb + i >= t1) break;
-      float Bv[N], Cv[N];
-      load_row<T, N>(Bv, bp + (int64_t)(tb + i) * a.ld_B);
-      if (!LOCAL) load_row<T, N>(Cv, cp + (int64_t)(tb + i) * a.ld_C);
-      const float du = d[i] * u[i];
-      float y = Dp * u[i];
+      for (int i = 0; i < SU; ++i) step(tb + i, u[i], d[i], z[i]);
+    } else {
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        h[n] = fmaf(exp2_of(d[i] * A2[n]), h[n], du * Bv[n]);
-        if (!LOCAL) y = fmaf(Cv[n], h[n], y);
-      }
-      if (LOCAL) {
-        sdt += d[i];
-      } else {
-        if (zp) y *= z[i] * sigmoid(z[i]);
-        if (mine) yp[(int64_t)(tb + i) * a.ld_y] = (T)y;
-      }
+      for (int i = 0; i < SU - 1; ++i)
+        if (tb + i < steps) step(tb + i, u[i], d[i], z[i]);
     }
   }
   if (!mine) return;
-  float* out = LOCAL ? a.carry + (item * a.D + c) * N : a.hT && t1 == sp.len ? a.hT + ((int64_t)s * a.D + c) * N : nullptr;
-  if (LOCAL) a.sdt[item * a.D + c] = sdt;
+  float* out = LOCAL ? a.carry + ((int64_t)item * a.D + c) * N : a.hT && t1 == sp.len ? a.hT + ((int64_t)s * a.D + c) * N : nullptr;
+  if (LOCAL) a.sdt[(int64_t)item * a.D + c] = sdt;
   if (out)
 #pragma unroll
     for (int n = 0; n < N; n += 4) *reinterpret_cast<f32x4*>(out + n) = f32x4{h[n], h[n + 1], h[n + 2], h[n + 3]};
@@ -568,7 +588,7 @@ __global__ __launch_bounds__(256) void step_kernel(const ScanArgs a) {
 // lanes (step 4 i + q by lane q) and passed around the quad.  Sums over a
 // wavefront's channels are exchanges that halve the values each time; the
 // wavefronts' sums meet in LDS.
-constexpr int GW = 8, GC = 16 * GW;           // wavefronts and channels per workgroup
+constexpr int GW = 4, GC = 16 * GW;           // wavefronts and channels per workgroup
 
 // f(0), f(1), .. with the index as a type (register arrays and lane patterns need constants)
 template <class F, int... t>
@@ -603,17 +623,16 @@ __device__ __forceinline__ float row_sum4(float v) {
   return v;
 }
 
-// Local running gradient of a chunk (REV counterpart of scan_kernel<LOCAL>): one lane per channel.
-template <class T, int N>
+// Local running gradient of a chunk (the counterpart of scan_kernel<LOCAL>): one lane per channel.
+template <class T, int N, bool Z>
 __global__ __launch_bounds__(256) void grad_local_kernel(const ScanArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int64_t item = id / a.cblocks;
-  if (item >= (int64_t)a.B * a.chunks) return;
-  const int cb = (int)(id - item * a.cblocks), s = (int)(item / a.chunks), ch = (int)(item - (int64_t)s * a.chunks);
+  const uint32_t id = blockIdx.x * 4 + wave, item = id / (uint32_t)a.cblocks;
+  if (item >= (uint32_t)a.B * (uint32_t)a.chunks) return;
+  const int cb = (int)(id - item * a.cblocks), s = (int)(item / (uint32_t)a.chunks), ch = (int)(item - (uint32_t)s * a.chunks);
   const Span sp = span_of(a.off, s, a.rows, a.T_max, nullptr, false);
-  const int t0 = ch * a.chunk, t1 = min(t0 + a.chunk, sp.len);
-  if (t0 >= t1) return;
+  const int t0 = ch * a.chunk, t1 = min(t0 + a.chunk, sp.len), steps = t1 - t0;
+  if (steps <= 0) return;
   const int c = cb * 64 + lane, cc = min(c, a.D - 1);
   float g[N], A2[N];
 #pragma unroll
@@ -622,189 +641,351 @@ __global__ __launch_bounds__(256) void grad_local_kernel(const ScanArgs a) {
     g[n] = 0.0f;
   }
   const float bias = a.bias ? a.bias[cc] : 0.0f;
-  const T* dp = static_cast<const T*>(a.delta) + sp.r0 * a.ld_delta + cc;
-  const T* yp = static_cast<const T*>(a.dy) + sp.r0 * a.ld_dy + cc;
-  const T* zp = a.z ? static_cast<const T*>(a.z) + sp.r0 * a.ld_z + cc : nullptr;
-  const T* cp = static_cast<const T*>(a.Cm) + sp.r0 * a.ld_C;
+  const T* dp = static_cast<const T*>(a.delta) + (sp.r0 + t0) * a.ld_delta;
+  const T* yp = static_cast<const T*>(a.dy) + (sp.r0 + t0) * a.ld_dy;
+  const T* zp = Z ? static_cast<const T*>(a.z) + (sp.r0 + t0) * a.ld_z : nullptr;
+  const T* cp = static_cast<const T*>(a.Cm) + (sp.r0 + t0) * a.ld_C;
   float sdt = 0.0f;
   T dn[SU], yn[SU], zn[SU];
   auto load = [&](int t) {                    // rows t, t - 1, ..
 #pragma unroll
     for (int i = 0; i < SU; ++i) {
-      const int64_t r = max(t - i, t0);
-      dn[i] = dp[r * a.ld_delta];
-      yn[i] = yp[r * a.ld_dy];
-      if (zp) zn[i] = zp[r * a.ld_z];
+      const int64_t r = max(t - i, 0);
+      dn[i] = (dp + r * a.ld_delta)[cc];
+      yn[i] = (yp + r * a.ld_dy)[cc];
+      if (Z) zn[i] = (zp + r * a.ld_z)[cc];
     }
   };
-  load(t1 - 1);
-  for (int tb = t1 - 1; tb >= t0; tb -= SU) {
+  Row<T, N> Cn;
+  auto step = [&](int t, float d, float dy) {
+    const Row<T, N> Cr = Cn;
+    Cn.load(cp + (int64_t)max(t - 1, 0) * a.ld_C);
+#pragma unroll
+    for (int n = 0; n < N; ++n) g[n] = fmaf(Cr.get(n), dy, g[n]) * exp2_of(d * A2[n]);
+    sdt += d;
+  };
+  load(steps - 1);
+  Cn.load(cp + (int64_t)(steps - 1) * a.ld_C);
+  for (int tb = steps - 1; tb >= 0; tb -= SU) {
     float d[SU], dy[SU];
 #pragma unroll
     for (int i = 0; i < SU; ++i) {
       d[i] = softplus((float)dn[i] + bias);
       dy[i] = (float)yn[i];
-      if (zp) {
-        const float z = (float)zn[i];
-        dy[i] *= z * sigmoid(z);
-      }
+      if (Z) dy[i] *= (float)zn[i] * sigmoid((float)zn[i]);
     }
-    if (tb - SU >= t0) load(tb - SU);
+    if (tb >= SU) load(tb - SU);
+    if (tb >= SU - 1) {
 #pragma unroll
-    for (int i = 0; i < SU; ++i) {
-      if (tb - i < t0) break;
-      float Cv[N];
-      load_row<T, N>(Cv, cp + (int64_t)(tb - i) * a.ld_C);
+      for (int i = 0; i < SU; ++i) step(tb - i, d[i], dy[i]);
+    } else {
 #pragma unroll
-      for (int n = 0; n < N; ++n) g[n] = fmaf(Cv[n], dy[i], g[n]) * exp2_of(d[i] * A2[n]);
-      sdt += d[i];
+      for (int i = 0; i < SU - 1; ++i)
+        if (tb - i >= 0) step(tb - i, d[i], dy[i]);
     }
   }
   if (c >= a.D) return;
-  a.sdt[item * a.D + c] = sdt;
-  float* out = a.carry + (item * a.D + c) * N;
+  a.sdt[(int64_t)item * a.D + c] = sdt;
+  float* out = a.carry + ((int64_t)item * a.D + c) * N;
 #pragma unroll
   for (int n = 0; n < N; n += 4) *reinterpret_cast<f32x4*>(out + n) = f32x4{g[n], g[n + 1], g[n + 2], g[n + 3]};
 }
 
-template <class T, int N>
-__global__ __launch_bounds__(64 * GW) void grad_kernel(const ScanArgs a) {
-  constexpr int L = N / 4, K = CK<N>, I = K / 4;      // states per lane, steps per block, steps a lane prepares
-  __shared__ __attribute__((aligned(16))) float rows[2][K][N];        // B and C of the block's steps
-  __shared__ float sums[GW][K][2 * N];                                 // a wavefront's dB, dC
+template <class T, int N, bool Z>
+__global__ __launch_bounds__(64 * GW, 2) void grad_kernel(const ScanArgs a) {
+  constexpr int L = N / 4, K = CK, I = K / 4;      // states per lane, steps per block, steps a lane prepares
+  constexpr int E = 16 / (int)sizeof(T), UN = K * N / E;               // staging of B, C: values and units of 16 bytes
+  static_assert(2 * UN <= 64 * GW, "one unit per thread");
+  __shared__ __attribute__((aligned(16))) float rows_buf[2][2][K][N];      // B and C of the block's steps
+  __shared__ __attribute__((aligned(16))) float sums_buf[2][GW][K][2 * N]; // a wavefront's dB, dC
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q = lane & 3, cb = blockIdx.x % a.cblocks, group = blockIdx.x / a.cblocks;
   const int c = cb * GC + wave * 16 + (lane >> 2), cc = min(c, a.D - 1);
   const bool mine = c < a.D;
-  float A[L], dA[L], dD = 0.0f, dbias = 0.0f;
+  float A2[L], dA[L], dD = 0.0f, dbias = 0.0f;
 #pragma unroll
   for (int n = 0; n < L; ++n) {
-    A[n] = a.A[(int64_t)cc * N + q * L + n];
+    A2[n] = a.A[(int64_t)cc * N + q * L + n] * LOG2E;
     dA[n] = 0.0f;
   }
   const float bias = a.bias ? a.bias[cc] : 0.0f, Dp = a.Dp ? a.Dp[cc] : 0.0f;
-  const int64_t items = (int64_t)a.B * a.chunks;
-  for (int64_t item = group; item < items; item += a.groups) {
-    const int s = (int)(item / a.chunks), ch = (int)(item - (int64_t)s * a.chunks);
-    const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, cb == 0 && ch == 0 && tid == 0);
-    const int t0 = ch * a.chunk, t1 = min(t0 + a.chunk, sp.len);
-    float g[L];
-    const float* gin = a.chunks > 1 ? a.carry + item * a.D * N : a.dhT ? a.dhT + (int64_t)s * a.D * N : nullptr;
+  // where this lane's sum of a step goes: lanes 0..31 dB, 32..63 dC; odd rows of 16 the
+  // odd state of a pair; bit 2 the pair (with two states per lane there is one)
+  const int to = (lane >> 5) * N + q * L + ((lane >> 4) & 1) + (L > 2 ? ((lane >> 2) & 1) * 2 : 0);
+  const int items = a.B * a.chunks;
+  // The blocks are walked one after another over the items; a block's inputs are
+  // loaded while the block before it is computed.
+  struct Block {
+    int item, s, t0, t1, tb;
+    int64_t r0;
+    bool first;                                // the item's first chunk: its gradient leaves through dh0
+  };
+  // the block in scalar registers (what the compiler takes for divergent it would address per lane)
+  auto uniform = [&](int sq, int item, int t0, int t1, int tb, int64_t r0) {
+    auto u = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    Block k = {};
+    k.s = u(sq);
+    k.item = u(item);
+    k.t0 = u(t0);
+    k.t1 = u(t1);
+    k.tb = u(tb);
+    k.r0 = (int64_t)u((int)r0);                // rows < 2^31
+    return k;
+  };
+  const bool have_in = a.chunks > 1 || a.dhT;
+  const float* const in_base = a.chunks > 1 ? a.carry : a.dhT;
+  // what reaches an item's last state from later (without any, and where not wanted,
+  // some values of A, which the caller ignores: loads are unconditional, because
+  // registers that are loaded on one path only are waited for there)
+  auto grad_in = [&](const Block& k, bool wanted, float (&x)[L]) {
+    const float* p = (wanted && have_in ? in_base + (int64_t)(a.chunks > 1 ? k.item : k.s) * a.D * N : a.A) + (uint32_t)cc * N + q * L;
+    constexpr int V = L < 4 ? L : 4;
 #pragma unroll
-    for (int n = 0; n < L; ++n) g[n] = gin && (t0 < t1 || ch == 0) ? gin[(int64_t)cc * N + q * L + n] : 0.0f;
-    const int64_t ck0 = ckpt_base<N>(sp, s);
-    const int last = (t1 - 1) / K;                     // chunks are whole blocks
-    for (int blk = last; blk >= t0 / K && t0 < t1; --blk) {
-      const int tb = blk * K, steps = min(K, t1 - tb);
-      __syncthreads();
-      for (int i = tid; i < 2 * K * N; i += 64 * GW) {
-        const int m = i / (K * N), t = i / N % K, n = i % N;
-        const T* p = m ? static_cast<const T*>(a.Cm) + (sp.r0 + tb + t) * a.ld_C : static_cast<const T*>(a.Bm) + (sp.r0 + tb + t) * a.ld_B;
-        rows[m][t][n] = t < steps ? (float)p[n] : 0.0f;
+    for (int n = 0; n < L; n += V) {
+      const Vec<float, V> v = *reinterpret_cast<const Vec<float, V>*>(p + n);
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[n + i] = v[i];
+    }
+  };
+  auto grad_out = [&](const Block& k, const float (&x)[L]) {
+    if (a.dh0 && k.first && mine)
+#pragma unroll
+      for (int n = 0; n < L; ++n) a.dh0[((int64_t)k.s * a.D + c) * N + q * L + n] = x[n];
+  };
+  // the last block of the first item from `item` on that has any (item = items: none); the
+  // gradient of an empty sequence's state passes through
+  auto open = [&](int item) {
+    Block k = {};
+    for (k.item = item; k.item < items; k.item += a.groups) {
+      k.s = a.chunks > 1 ? k.item / a.chunks : k.item;
+      const int ch = k.item - k.s * a.chunks;
+      const Span sp = span_of(a.off, k.s, a.rows, a.T_max, a.status, cb == 0 && ch == 0 && tid == 0);
+      k.r0 = sp.r0;
+      k.first = ch == 0;
+      k.t0 = ch * a.chunk;
+      k.t1 = min(k.t0 + a.chunk, sp.len);
+      if (k.t0 < k.t1) {
+        k.tb = (k.t1 - 1) / K * K;             // chunks are whole blocks
+        break;
       }
-      // this lane's steps 4 i + q; steps past the end have dt = 0 and dy = 0: the
-      // state stays and the gradient passes
-      float dt[I], u[I], dy[I], z[I], dout[I], sg[I], yg[I], s1[I], s2[I];
+      if (k.first && a.dh0) {
+        float x[L];
+        grad_in(k, true, x);
 #pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const int t = 4 * i + q;
-        const int64_t r = sp.r0 + tb + min(t, steps - 1);
-        const bool in = t < steps;
-        u[i] = in ? (float)static_cast<const T*>(a.u)[r * a.ld_u + cc] : 0.0f;
-        dout[i] = in ? (float)static_cast<const T*>(a.dy)[r * a.ld_dy + cc] : 0.0f;
-        const float raw = (float)static_cast<const T*>(a.delta)[r * a.ld_delta + cc] + bias;
-        z[i] = a.z ? (float)static_cast<const T*>(a.z)[r * a.ld_z + cc] : 0.0f;
-        const float e = exp2_of(-fabsf(raw) * LOG2E);
-        dt[i] = in ? fmaxf(raw, 0.0f) + log1p_unit(e) : 0.0f;
-        sg[i] = (raw >= 0.0f ? 1.0f : e) * rcp_of(1.0f + e);
-        dy[i] = a.z ? dout[i] * z[i] * sigmoid(z[i]) : dout[i];
-        yg[i] = s1[i] = s2[i] = 0.0f;
-      }
-      float hs[L];
-      {
-        const float* kept = ckpt_at<N>(a.ckpt, ck0 + blk, a.D, cc, q * L);
-#pragma unroll
-        for (int n = 0; n < L; ++n) hs[n] = (L < 4 || n < 4) ? kept[n] : kept[(int64_t)(n / 4) * a.D * 4 + (n & 3)];
-      }
-      __syncthreads();
-      float h[K][L], e[K][L];
-      auto forward = [&](auto tv) {
-        constexpr int t = decltype(tv)::value;
-        const float d = quad_get<(t & 3)>(dt[t / 4]), du = d * quad_get<(t & 3)>(u[t / 4]);
-        float y = 0.0f;
-#pragma unroll
-        for (int n = 0; n < L; ++n) {
-          e[t][n] = exp2_of(d * A[n] * LOG2E);
-          h[t][n] = fmaf(e[t][n], t ? h[t ? t - 1 : 0][n] : hs[n], du * rows[0][t][q * L + n]);
-          if (a.z) y = fmaf(rows[1][t][q * L + n], h[t][n], y);
-        }
-        if (a.z) {
-          y = quad_sum(y);
-          if (q == (t & 3)) yg[t / 4] = y;
-        }
-      };
-      auto backward = [&](auto tv) {
-        constexpr int t = decltype(tv)::value;
-        const float d = quad_get<(t & 3)>(dt[t / 4]), du = d * quad_get<(t & 3)>(u[t / 4]), y = quad_get<(t & 3)>(dy[t / 4]);
-        float x1 = 0.0f, x2 = 0.0f, db[L], dc[L];
-#pragma unroll
-        for (int n = 0; n < L; ++n) {
-          g[n] = fmaf(rows[1][t][q * L + n], y, g[n]);
-          dc[n] = mine ? y * h[t][n] : 0.0f;
-          db[n] = mine ? g[n] * du : 0.0f;
-          x1 = fmaf(g[n], rows[0][t][q * L + n], x1);
-          g[n] *= e[t][n];
-          const float w = g[n] * (t ? h[t ? t - 1 : 0][n] : hs[n]);
-          x2 = fmaf(w, A[n], x2);
-          dA[n] = fmaf(w, d, dA[n]);
-        }
-        x1 = quad_sum(x1);
-        x2 = quad_sum(x2);
-        if (q == (t & 3)) {
-          s1[t / 4] = x1;
-          s2[t / 4] = x2;
-        }
-        // lanes 0..31 dB, lanes 32..63 dC; then rows of 16 lanes: two states each
-        float f[L];
-#pragma unroll
-        for (int n = 0; n < L; ++n) f[n] = fold32(db[n], dc[n]);
-#pragma unroll
-        for (int n = 0; n < L; n += 2) {
-          const float v = row_sum4(fold16(f[n], f[n + 1]));
-          if ((lane & 12) == 0) sums[wave][t][(lane >> 5) * N + q * L + n + ((lane >> 4) & 1)] = v;
-        }
-      };
-      each_step(forward, std::make_integer_sequence<int, K>{});
-      each_step([&](auto tv) { backward(std::integral_constant<int, K - 1 - decltype(tv)::value>{}); }, std::make_integer_sequence<int, K>{});
-      // this lane's steps: du, ddelta, dz
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const int t = 4 * i + q;
-        if (t >= steps || !mine) continue;
-        const int64_t r = sp.r0 + tb + t;
-        static_cast<T*>(a.du)[r * a.ld_du + c] = (T)fmaf(dt[i], s1[i], Dp * dy[i]);
-        const float dd = fmaf(u[i], s1[i], s2[i]) * sg[i];
-        static_cast<T*>(a.ddelta)[r * a.ld_ddelta + c] = (T)dd;
-        dbias += dd;
-        dD = fmaf(dy[i], u[i], dD);
-        if (a.z) {
-          const float sz = sigmoid(z[i]), yv = fmaf(Dp, u[i], yg[i]);
-          static_cast<T*>(a.dz)[r * a.ld_dz + c] = (T)(dout[i] * yv * sz * fmaf(z[i], 1.0f - sz, 1.0f));
-        }
-      }
-      __syncthreads();
-      for (int i = tid; i < steps * 2 * N; i += 64 * GW) {
-        const int t = i / (2 * N), n = i % (2 * N);
-        float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < GW; ++w) v += sums[w][t][n];
-        a.pbc[((int64_t)cb * a.rows + sp.r0 + tb + t) * (2 * N) + n] = v;
+        for (int n = 0; n < L; ++n) x[n] = have_in ? x[n] : 0.0f;
+        grad_out(k, x);
       }
     }
-    if (a.dh0 && ch == 0 && mine)
+    return k;
+  };
+  T ur[I], dr[I], yr[I], zr[I];                // this lane's steps 4 i + q; steps past the end read the last one
+  float hs[L], g[L], gn[L];                    // the kept state; the running gradient, an item's first
+  u32x4 row_x;                                 // 16 bytes of B or C, as they are (converting them here would wait for them)
+  // this thread's 16 bytes of B or C
+  const int rm = tid / UN & 1, rt = tid % UN / (N / E), rn = tid % (N / E) * E;
+  const uintptr_t pb = (uintptr_t)a.Bm, pc = (uintptr_t)a.Cm;          // values: a choice of arguments would load them again
+  const T* const rp = reinterpret_cast<const T*>(rm ? pc : pb) + rn;
+  const int64_t lb = a.ld_B, lc = a.ld_C;
+  const int64_t rl = rm ? lc : lb;
+  auto load = [&](const Block& k, bool fresh, T (&u)[I], T (&d)[I], T (&y)[I], T (&z)[I], float (&h)[L], u32x4& x) {
+    const int steps = min(K, k.t1 - k.tb);
+    const int64_t rb = k.r0 + k.tb;
+    auto row = [&](const void* p, int64_t ld) { return static_cast<const T*>(p) + rb * ld; };     // uniform
 #pragma unroll
-      for (int n = 0; n < L; ++n) a.dh0[((int64_t)s * a.D + c) * N + q * L + n] = g[n];
+    for (int i = 0; i < I; ++i) {
+      const uint32_t t = min(4 * i + q, steps - 1);
+      d[i] = row(a.delta, a.ld_delta)[t * (uint32_t)a.ld_delta + cc];
+      u[i] = row(a.u, a.ld_u)[t * (uint32_t)a.ld_u + cc];
+      y[i] = row(a.dy, a.ld_dy)[t * (uint32_t)a.ld_dy + cc];
+      if (Z) z[i] = row(a.z, a.ld_z)[t * (uint32_t)a.ld_z + cc];
+    }
+    const float* kept = ckpt_at<N>(a.ckpt, ckpt_base({k.r0, 0}, k.s) + k.tb / K, a.D, 0, 0);      // uniform
+    const uint32_t at = ((uint32_t)(q * L / 4) * a.D + cc) * 4 + (q * L & 3);
+    constexpr int V = L < 4 ? L : 4;
+#pragma unroll
+    for (int n = 0; n < L; n += V) {
+      const Vec<float, V> v = *reinterpret_cast<const Vec<float, V>*>(kept + at + (uint32_t)(n / 4) * a.D * 4);
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[n + i] = v[i];
+    }
+    x = *reinterpret_cast<const u32x4*>(rp + (rb + min(rt, steps - 1)) * rl);      // threads past the rows: unused
+    grad_in(k, fresh, gn);
+  };
+  Block cur = open(group);
+  if (cur.item < items) {
+    load(cur, true, ur, dr, yr, zr, hs, row_x);
+#pragma unroll
+    for (int n = 0; n < L; ++n) g[n] = have_in ? gn[n] : 0.0f;
   }
+  // Results of a block are stored in the next block's turn, before its successor's loads are
+  // issued: waiting for loads also waits for the stores before them, which then have
+  // had a block's time.  One barrier per block: rows and sums alternate between two buffers.
+  T duo[I], ddo[I], dzo[I];
+  Block prev = {};
+  prev.item = items;                           // none yet
+  auto store = [&](const Block& k, const float (&sums)[GW][K][2 * N]) {
+    const int steps = min(K, k.t1 - k.tb);
+    const int64_t rb = k.r0 + k.tb;
+    auto out = [&](void* p, int64_t ld) { return static_cast<T*>(p) + rb * ld; };
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const uint32_t t = 4 * i + q;
+      if ((int)t >= steps || !mine) continue;
+      out(a.du, a.ld_du)[t * (uint32_t)a.ld_du + c] = duo[i];
+      out(a.ddelta, a.ld_ddelta)[t * (uint32_t)a.ld_ddelta + c] = ddo[i];
+      if (Z) out(a.dz, a.ld_dz)[t * (uint32_t)a.ld_dz + c] = dzo[i];
+    }
+    float* pbc = a.pbc + ((int64_t)cb * a.rows + rb) * (2 * N);
+    for (int i = tid; i < steps * 2 * N; i += 64 * GW) {
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < GW; ++w) v += (&sums[w][0][0])[i];
+      pbc[i] = v;
+    }
+  };
+  int buf = 0;
+  for (; cur.item < items; buf ^= 1) {
+    const int tb = cur.tb, steps = min(K, cur.t1 - tb);
+    auto& rows = rows_buf[buf];
+    auto& sums = sums_buf[buf];
+    Block nxt = cur;
+    nxt.tb -= K;
+    const bool fresh = nxt.tb < cur.t0;
+    if (fresh) nxt = open(cur.item + a.groups);
+    const bool more = nxt.item < items;
+    const Block ahead = uniform(more ? nxt.s : cur.s, more ? nxt.item : cur.item, more ? nxt.t0 : cur.t0, more ? nxt.t1 : cur.t1,
+                                more ? nxt.tb : cur.tb, more ? nxt.r0 : cur.r0);
+    if (tid < 2 * UN) {                        // rows past the end as zero
+      const Vec<T, E> v = __builtin_bit_cast(Vec<T, E>, row_x);
+#pragma unroll
+      for (int i = 0; i < E; i += 4) {
+        f32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = rt < steps ? (float)v[i + j] : 0.0f;
+        *reinterpret_cast<f32x4*>(&rows[rm][rt][rn + i]) = x;
+      }
+    }
+    // steps past the end have dt = 0 and dy = 0: the state stays and the gradient passes;
+    // lanes past the last channel have u = 0 and dy = 0, so that they add nothing to dB, dC
+    float dt[I], du[I], dy[I], yg[I], s1[I], s2[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const bool in = 4 * i + q < steps;
+      dt[i] = in ? softplus((float)dr[i] + bias) : 0.0f;
+      du[i] = mine ? dt[i] * (float)ur[i] : 0.0f;
+      float d = (float)yr[i];
+      if (Z) d *= (float)zr[i] * sigmoid((float)zr[i]);
+      dy[i] = in && mine ? d : 0.0f;
+      yg[i] = s1[i] = s2[i] = 0.0f;
+    }
+    __syncthreads();
+    if (prev.item < items) store(prev, sums_buf[buf ^ 1]);
+    T un[I], dn[I], yn[I], zn[I];
+    float hn[L];
+    u32x4 row_n;
+    load(ahead, fresh, un, dn, yn, zn, hn, row_n);
+    float h[K][L], e[K][L];
+    auto get_row = [&](float (&x)[L], int m, int t, int lq) {       // states lq L .. of a step's B or C
+      constexpr int V = L < 4 ? L : 4;
+      const Vec<float, V>* p = reinterpret_cast<const Vec<float, V>*>(&rows[m][t][0]) + lq * (L / V);
+#pragma unroll
+      for (int n = 0; n < L; ++n) x[n] = p[n / V][n % V];
+    };
+    auto forward = [&](auto tv) {
+      constexpr int t = decltype(tv)::value;
+      const float d = quad_get<(t & 3)>(dt[t / 4]), x = quad_get<(t & 3)>(du[t / 4]);
+      float y = 0.0f, Br[L], Cr[L];
+      get_row(Br, 0, t, q);
+      if (Z) get_row(Cr, 1, t, q);
+#pragma unroll
+      for (int n = 0; n < L; ++n) {
+        e[t][n] = exp2_of(d * A2[n]);
+        h[t][n] = fmaf(e[t][n], t ? h[t ? t - 1 : 0][n] : hs[n], x * Br[n]);
+        if (Z) y = fmaf(Cr[n], h[t][n], y);
+      }
+      if (Z) {
+        y = quad_sum(y);
+        yg[t / 4] = q == (t & 3) ? y : yg[t / 4];
+      }
+    };
+    int at = q;
+    auto backward = [&](auto tv) {
+      constexpr int t = decltype(tv)::value;
+      const float d = quad_get<(t & 3)>(dt[t / 4]), x = quad_get<(t & 3)>(du[t / 4]), y = quad_get<(t & 3)>(dy[t / 4]);
+      float x1 = 0.0f, x2 = 0.0f, f[L], Br[L], Cr[L];
+      get_row(Br, 0, t, at);
+      get_row(Cr, 1, t, at);
+#pragma unroll
+      for (int n = 0; n < L; ++n) {
+        g[n] = fmaf(Cr[n], y, g[n]);
+        f[n] = fold32(g[n] * x, y * h[t][n]);
+        x1 = fmaf(g[n], Br[n], x1);
+        g[n] *= e[t][n];
+        const float w = g[n] * (t ? h[t ? t - 1 : 0][n] : hs[n]);
+        x2 = fmaf(w, A2[n], x2);
+        dA[n] = fmaf(w, d, dA[n]);
+      }
+      x1 = quad_sum(x1);
+      x2 = quad_sum(x2);
+      s1[t / 4] = q == (t & 3) ? x1 : s1[t / 4];
+      s2[t / 4] = q == (t & 3) ? x2 : s2[t / 4];
+      float v[L / 2];
+#pragma unroll
+      for (int n = 0; n < L; n += 2) v[n / 2] = row_sum4(fold16(f[n], f[n + 1]));
+      // lanes that hold the same sum write it to the same place
+      if constexpr (L == 2) {
+        sums[wave][t][to] = v[0];
+      } else {
+#pragma unroll
+        for (int n = 0; n < L / 2; n += 2) {
+          const float even = v[n], odd = v[n + 1];       // values: a choice of elements would go through memory
+          sums[wave][t][to + 2 * n] = lane & 4 ? odd : even;
+        }
+      }
+    };
+    each_step(forward, std::make_integer_sequence<int, K>{});
+    // values that the compiler cannot see through: the walk back reads the rows and passes
+    // the steps' values again (keeping them from the walk forward takes 2 K (L + 1)
+    // registers, which spill)
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int i = 0; i < I; ++i) asm volatile("" : "+v"(dt[i]), "+v"(du[i]));
+    each_step([&](auto tv) { backward(std::integral_constant<int, K - 1 - decltype(tv)::value>{}); }, std::make_integer_sequence<int, K>{});
+    // this lane's steps: du, ddelta, dz
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const bool in = 4 * i + q < steps;
+      const float u = (float)ur[i], raw = (float)dr[i] + bias;
+      duo[i] = (T)fmaf(dt[i], s1[i], Dp * dy[i]);
+      const float dd = in ? fmaf(u, s1[i], s2[i] * LN2) * sigmoid(raw) : 0.0f;
+      ddo[i] = (T)dd;
+      dbias += dd;
+      dD = fmaf(dy[i], u, dD);
+      if (Z) {
+        const float z = (float)zr[i], sz = sigmoid(z), yv = fmaf(Dp, u, yg[i]);
+        dzo[i] = (T)((float)yr[i] * yv * sz * fmaf(z, 1.0f - sz, 1.0f));
+      }
+    }
+    if (fresh) {
+      grad_out(cur, g);
+#pragma unroll
+      for (int n = 0; n < L; ++n) g[n] = have_in ? gn[n] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      ur[i] = un[i];
+      dr[i] = dn[i];
+      yr[i] = yn[i];
+      if (Z) zr[i] = zn[i];
+    }
+#pragma unroll
+    for (int n = 0; n < L; ++n) hs[n] = hn[n];
+    row_x = row_n;
+    prev = cur;
+    cur = nxt;
+  }
+  __syncthreads();
+  if (prev.item < items) store(prev, sums_buf[buf ^ 1]);
   dD = quad_sum(dD);
   dbias = quad_sum(dbias);
   if (!mine) return;
@@ -854,7 +1035,8 @@ wm_status check_rows(int32_t dtype, int32_t B, int32_t T_max, int64_t rows, int3
   if (B > 0 && !off) return bad("off is NULL");
   return WM_OK;
 }
-bool mat_ok(const void* p, int64_t ld, int64_t rows, int64_t width) { return rows == 0 || (p && ld >= width); }
+// row strides up to 2^24 elements: the kernels take rows of a block by 32-bit offsets
+bool mat_ok(const void* p, int64_t ld, int64_t rows, int64_t width) { return rows == 0 || (p && ld >= width && ld <= (1 << 24)); }
 
 struct ConvPlan {
   int runs, groups, vec;
@@ -901,7 +1083,6 @@ struct ScanPlan {
   int chunk, chunks, groups, cblocks, gblocks;    // gblocks: channel blocks of the gradient
   size_t o_carry, o_sdt, o_pbc, o_pad, bytes;
 };
-int ck_of(int N) { return N == 32 ? 8 : 16; }
 
 wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
   if (!a) return bad("scan arguments are NULL");
@@ -910,7 +1091,7 @@ wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
   if (a->states != 8 && a->states != 16 && a->states != 32) return set_error(WM_ERR_UNSUPPORTED, "states must be 8, 16 or 32");
   if (!a->A) return bad("A is NULL");
   if (!mat_ok(a->u, a->ld_u, a->rows, a->channels) || !mat_ok(a->delta, a->ld_delta, a->rows, a->channels) ||
-      (a->z && a->ld_z < a->channels))
+      (a->z && (a->ld_z < a->channels || a->ld_z > (1 << 24))))
     return bad("u, delta or z is NULL or its row stride is below channels");
   const int64_t e = a->dtype == WM_BF16 ? 2 : 4;
   if (!mat_ok(a->Bm, a->ld_B, a->rows, a->states) || !mat_ok(a->Cm, a->ld_C, a->rows, a->states) ||
@@ -932,7 +1113,7 @@ wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
       p->chunks = (int)cdiv(a->T_max, c);
     }
   }
-  if ((int64_t)a->B * p->chunks > INT32_MAX / 4) return set_error(WM_ERR_UNSUPPORTED, "B x T_max is too large");
+  if ((int64_t)a->B * p->chunks * p->cblocks > INT32_MAX / 4) return set_error(WM_ERR_UNSUPPORTED, "B x T_max is too large");
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   p->o_carry = p->o_sdt = p->o_pbc = p->o_pad = 0;
@@ -943,7 +1124,7 @@ wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
   }
   p->groups = 1;
   if (grad) {
-    p->groups = (int)std::max<int64_t>(1, std::min<int64_t>(items, cdiv(1024, p->gblocks)));
+    p->groups = (int)std::max<int64_t>(1, std::min<int64_t>(items, cdiv(4096, p->gblocks)));
     p->o_pbc = take((size_t)p->gblocks * a->rows * 2 * N * 4);
     p->o_pad = take((size_t)p->groups * a->channels * (N + 2) * 4);
   }
@@ -1063,7 +1244,7 @@ size_t wm_scan_workspace_bytes(const wm_scan_args* w, int32_t grad) {
 size_t wm_scan_checkpoint_bytes(const wm_scan_args* w) {
   ScanPlan p;
   if (check_scan(w, &p, false) != WM_OK) return 0;
-  return al256((size_t)(w->rows / ck_of(w->states) + w->B + 1) * w->channels * w->states * 4);
+  return al256((size_t)(w->rows / CK + w->B + 1) * w->channels * w->states * 4);
 }
 
 wm_status wm_scan(const wm_scan_args* w, void* y, int64_t ld_y, float* hT, void* checkpoints, void* ws, size_t ws_bytes,
@@ -1088,10 +1269,11 @@ wm_status wm_scan(const wm_scan_args* w, void* y, int64_t ld_y, float* hT, void*
     }
     const dim3 grid((unsigned)cdiv((int64_t)w->B * p.chunks * p.cblocks, 4));
     if (p.chunks > 1) {
-      hipLaunchKernelGGL((scan_kernel<T, N, true>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((scan_kernel<T, N, true, false>), grid, dim3(256), 0, st, a);
       hipLaunchKernelGGL((carry_kernel<N, false>), dim3((unsigned)cdiv((int64_t)w->B * w->channels * N, 256)), dim3(256), 0, st, a);
     }
-    hipLaunchKernelGGL((scan_kernel<T, N, false>), grid, dim3(256), 0, st, a);
+    if (a.z) hipLaunchKernelGGL((scan_kernel<T, N, false, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((scan_kernel<T, N, false, false>), grid, dim3(256), 0, st, a);
   };
   WM_ST(TK_SCAN, scan_typed(w, go));
   return clear_error();
@@ -1109,6 +1291,7 @@ wm_status wm_scan_grad(const wm_scan_args* w, const void* checkpoints, const voi
   if (!mat_ok(g->dB, g->ld_dB, w->rows, w->states) || !mat_ok(g->dC, g->ld_dC, w->rows, w->states))
     return bad("dB or dC is NULL or its row stride is below states");
   if (!g->dA || !checkpoints) return bad("dA or checkpoints is NULL");
+  if ((uintptr_t)dhT % 16 || (uintptr_t)checkpoints % 16) return bad("dhT and checkpoints must be 16-byte aligned");
   if (!ws || (uintptr_t)ws % 256 || ws_bytes < p.bytes) return bad("workspace is NULL, not 256-byte aligned or too small");
   hipStream_t st = static_cast<hipStream_t>(stream);
   uint8_t* w8 = static_cast<uint8_t*>(ws);
@@ -1123,12 +1306,15 @@ wm_status wm_scan_grad(const wm_scan_args* w, const void* checkpoints, const voi
     using T = decltype(t);
     constexpr int N = decltype(nv)::value;
     if (p.chunks > 1) {
-      hipLaunchKernelGGL((grad_local_kernel<T, N>), dim3((unsigned)cdiv((int64_t)w->B * p.chunks * p.cblocks, 4)), dim3(256), 0, st, a);
+      const dim3 grid((unsigned)cdiv((int64_t)w->B * p.chunks * p.cblocks, 4));
+      if (a.z) hipLaunchKernelGGL((grad_local_kernel<T, N, true>), grid, dim3(256), 0, st, a);
+      else hipLaunchKernelGGL((grad_local_kernel<T, N, false>), grid, dim3(256), 0, st, a);
       hipLaunchKernelGGL((carry_kernel<N, true>), dim3((unsigned)cdiv((int64_t)w->B * w->channels * N, 256)), dim3(256), 0, st, a);
     }
     ScanArgs b = a;
     b.cblocks = p.gblocks;
-    hipLaunchKernelGGL((grad_kernel<T, N>), dim3(p.groups * p.gblocks), dim3(64 * GW), 0, st, b);
+    if (a.z) hipLaunchKernelGGL((grad_kernel<T, N, true>), dim3(p.groups * p.gblocks), dim3(64 * GW), 0, st, b);
+    else hipLaunchKernelGGL((grad_kernel<T, N, false>), dim3(p.groups * p.gblocks), dim3(64 * GW), 0, st, b);
     if (w->rows > 0)
       hipLaunchKernelGGL((bc_sum_kernel<T, N>), dim3((unsigned)cdiv(w->rows * 2 * N, 256)), dim3(256), 0, st, a.pbc, p.gblocks,
                          w->rows, static_cast<T*>(g->dB), g->ld_dB, static_cast<T*>(g->dC), g->ld_dC);

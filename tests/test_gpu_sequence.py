@@ -169,16 +169,17 @@ def test_attention_rows_past_32_bits(wm):
 
 
 def test_attention_gradient_against_differences(wm):
-    """The float32 gradient against central differences of the float32 forward along random directions: a
-    step of 1e-2 leaves a third-order term of about 1e-4 of the slope and rounding of 1e-5."""
+    """The float32 gradient against central differences of the float64 definition along random directions (the
+    float32 forward cannot serve: the rounding of its 15,104 outputs, 3e-7 of 0.2 each, adds up to
+    7e-6 in the loss and 4e-4 in the slope).  A step of 1e-2 leaves a third-order term below 1e-4."""
     q, k, v, qo, ko, _, do = make_attn("f32", [50, 9], [70, 33], 4, 2, 64, seed=10)
     f = wm.cross_attention(q, k, v, qo, ko, need_lse=True)
     b = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko)
-    loss = lambda a: (wm.cross_attention(*a, qo, ko)["o"].double() * do).sum().item()  # noqa: E731
+    loss = lambda a: (Q.attention(*(_np(t) for t in a), qo, ko, 64 ** -0.5)[0] * _np(do)).sum()  # noqa: E731
     for i, n in enumerate(("dq", "dk", "dv")):
-        d = torch.randn(b[n].shape, device="cuda")
+        d = torch.randn(b[n].shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(11 + i)).double()
         d /= d.norm()
-        ins = [q, k.contiguous(), v.contiguous()]
+        ins = [q.double(), k.double(), v.double()]
         hi, lo = list(ins), list(ins)
         hi[i], lo[i] = ins[i] + 1e-2 * d, ins[i] - 1e-2 * d
         slope = (loss(hi) - loss(lo)) / 2e-2
