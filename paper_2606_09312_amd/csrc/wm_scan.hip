@@ -90,9 +90,11 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[V]) {
 }
 
 // --------------------------------------------------------------------------
-// Convolution.  A thread takes V neighbouring channels and runs of RUN rows of a
-// sequence, the taps' window in registers.
-constexpr int RUN = 16;
+// Convolution.  A lane takes V neighbouring channels and a run of RUN rows of a
+// sequence, the taps' window in registers; the rows of SUB steps are loaded together, one
+// block ahead (bytes bound it: what counts is loads in flight).  A wavefront takes 2^lp
+// lanes' channels of 64 >> lp runs, so that narrow rows fill it too.
+constexpr int RUN = 16, SUB = 8;
 
 struct ConvArgs {
   const int32_t* off;
@@ -102,7 +104,7 @@ struct ConvArgs {
   float* part;              // [groups][W + 1][D]
   int32_t* status;
   int64_t ld_x, ld_y, ld_dy, ld_dx, rows;
-  int B, T_max, D, runs, silu, groups;
+  int B, T_max, D, runs, silu, groups, lp;
 };
 
 // the input `t` of a sequence: before its start the carried state (zero without one)
@@ -131,37 +133,73 @@ struct Taps {
   }
 };
 
+// This lane's slot (a run or a group of runs) of `slots` and its first channel; false past the end.
+template <int V>
+__device__ __forceinline__ bool conv_slot(const ConvArgs& a, uint32_t slots, uint32_t& slot, int& c) {
+  const uint32_t CG = a.D / V, blocks = (CG + (1u << a.lp) - 1) >> a.lp;
+  const uint32_t wave = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, row = wave / blocks;
+  slot = row * (64u >> a.lp) + (lane >> a.lp);
+  const uint32_t cg = ((wave - row * blocks) << a.lp) + (lane & ((1u << a.lp) - 1));
+  c = (int)cg * V;
+  return slot < slots && cg < CG;
+}
+template <class T, int V>
+using Raw = std::conditional_t<V == 1, T, Vec<T, V == 1 ? 2 : V>>;
+template <class T, int V>
+__device__ __forceinline__ float elem(const Raw<T, V>& r, int i) {
+  if constexpr (V == 1) return (float)r;
+  else return (float)r[i];
+}
+// rows first .. first + SUB - 1 of a matrix, past `last` that one again
+template <class T, int V>
+__device__ __forceinline__ void load_rows(Raw<T, V> (&x)[SUB], const T* p, int64_t ld, int first, int last) {
+#pragma unroll
+  for (int i = 0; i < SUB; ++i) x[i] = *reinterpret_cast<const Raw<T, V>*>(p + min(first + i, last) * ld);
+}
+
 template <class T, int V, int W>
 __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a) {
-  const int CG = a.D / V;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t item = id / CG;
-  if (item >= (int64_t)a.B * a.runs) return;
-  const int c = (int)(id - item * CG) * V, s = (int)(item / a.runs), run = (int)(item - (int64_t)s * a.runs);
+  uint32_t item;
+  int c;
+  if (!conv_slot<V>(a, (uint32_t)a.B * a.runs, item, c)) return;
+  const int s = item / (uint32_t)a.runs, run = item - s * a.runs;
   const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, c == 0 && run == 0);
   const int t0 = run * RUN, t1 = min(t0 + RUN, sp.len);
   if (t0 < t1) {
-    Taps<V, W> k;
-    k.load(a, c);
+    const T* xp = static_cast<const T*>(a.x) + sp.r0 * a.ld_x + c;
+    T* yp = static_cast<T*>(a.y) + sp.r0 * a.ld_y + c;
+    Raw<T, V> next[SUB];
+    load_rows<T, V>(next, xp, a.ld_x, t0, t1 - 1);
     float win[W][V];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) conv_in<T, V, W>(win[j], a, sp, s, t0 - (W - 1) + j, c);
-#pragma unroll 4
-    for (int t = t0; t < t1; ++t) {
-      load_vec<T, V>(win[W - 1], static_cast<const T*>(a.x) + (sp.r0 + t) * a.ld_x + c);
-      float y[V];
+    Taps<V, W> k;
+    k.load(a, c);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float v = k.b[i];
+    for (int tb = 0; tb < RUN; tb += SUB) {
+      if (t0 + tb >= t1) break;
+      Raw<T, V> x[SUB];
 #pragma unroll
-        for (int j = 0; j < W; ++j) v = fmaf(k.w[j][i], win[j][i], v);
-        y[i] = a.silu ? v * sigmoid(v) : v;
+      for (int i = 0; i < SUB; ++i) x[i] = next[i];
+      if (tb + SUB < RUN) load_rows<T, V>(next, xp, a.ld_x, t0 + tb + SUB, t1 - 1);
+#pragma unroll
+      for (int i = 0; i < SUB; ++i) {
+        const int t = t0 + tb + i;
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          win[W - 1][e] = elem<T, V>(x[i], e);
+          float v = k.b[e];
+#pragma unroll
+          for (int j = 0; j < W; ++j) v = fmaf(k.w[j][e], win[j][e], v);
+          y[e] = a.silu ? v * sigmoid(v) : v;
+        }
+        if (t < t1) store_vec<T, V>(yp + t * a.ld_y, y);
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+          for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e];
       }
-      store_vec<T, V>(static_cast<T*>(a.y) + (sp.r0 + t) * a.ld_y + c, y);
-#pragma unroll
-      for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) win[j][i] = win[j + 1][i];
     }
   }
   if (a.state_out && run == 0) {          // may be the state itself: this thread alone reads and writes its channels
@@ -174,20 +212,27 @@ __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a) {
 }
 
 // dx, dstate and partial sums of dw and db.  da_t = dy_t act'(a_t) is formed again from
-// the inputs; dx_t = sum_j w_j da_{t + W - 1 - j}.  A thread owns V channels and the items
+// the inputs; dx_t = sum_j w_j da_{t + W - 1 - j}.  A lane owns V channels and the runs
 // group, group + groups, ..; each row's share of dw is counted by the run that holds it.
 template <class T, int V, int W>
 __global__ __launch_bounds__(256) void conv_grad_kernel(const ConvArgs a) {
-  const int CG = a.D / V;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int group = (int)(id / CG);
-  if (group >= a.groups) return;
-  const int c = (int)(id - (int64_t)group * CG) * V;
+  uint32_t group;
+  int c;
+  if (!conv_slot<V>(a, a.groups, group, c)) return;
   Taps<V, W> k;
   k.load(a, c);
   float dw[W][V] = {}, db[V] = {};
-  for (int64_t item = group; item < (int64_t)a.B * a.runs; item += a.groups) {
-    const int s = (int)(item / a.runs), run = (int)(item - (int64_t)s * a.runs);
+  // dL/da of a row with inputs x[0 .. W - 1] and output gradient g
+  auto grad = [&](const float (&x)[W][V], int e, float g) {
+    float v = k.b[e];
+#pragma unroll
+    for (int j = 0; j < W; ++j) v = fmaf(k.w[j][e], x[j][e], v);
+    if (!a.silu) return g;
+    const float sg = sigmoid(v);
+    return g * sg * fmaf(v, 1.0f - sg, 1.0f);
+  };
+  for (uint32_t item = group; item < (uint32_t)a.B * a.runs; item += a.groups) {
+    const int s = item / (uint32_t)a.runs, run = item - s * a.runs;
     const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, c == 0 && run == 0);
     const int t0 = run * RUN, t1 = min(t0 + RUN, sp.len);
     // the gradient of the carried-out state reaches the last W - 1 inputs (and, in a
@@ -202,65 +247,62 @@ __global__ __launch_bounds__(256) void conv_grad_kernel(const ConvArgs a) {
       }
     };
     if (t0 < t1) {
-      float win[W][V], da[W][V];            // da[j]: of row t - (W - 1) + j
-#pragma unroll
-      for (int j = 0; j < W - 1; ++j) conv_in<T, V, W>(win[j], a, sp, s, t0 - (W - 1) + j, c);
-#pragma unroll
-      for (int j = 0; j < W; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) da[j][i] = 0.0f;
+      const T* xp = static_cast<const T*>(a.x) + sp.r0 * a.ld_x + c;
+      const T* gp = static_cast<const T*>(a.dy) + sp.r0 * a.ld_dy + c;
+      T* dp = static_cast<T*>(a.dx) + sp.r0 * a.ld_dx + c;
       // rows t0 .. t1 - 1 and the W - 1 after them; dx of row t - (W - 1) is complete at row t
       const int end = t1 + W - 1;
-#pragma unroll 2
-      for (int t = t0; t < end; ++t) {
-        float g[V];
-        if (t < sp.len) {
-          load_vec<T, V>(win[W - 1], static_cast<const T*>(a.x) + (sp.r0 + t) * a.ld_x + c);
-          load_vec<T, V>(g, static_cast<const T*>(a.dy) + (sp.r0 + t) * a.ld_dy + c);
+      Raw<T, V> xn[SUB], gn[SUB];
+      load_rows<T, V>(xn, xp, a.ld_x, t0, sp.len - 1);
+      load_rows<T, V>(gn, gp, a.ld_dy, t0, sp.len - 1);
+      float win[W][V], da[W][V] = {};       // da[j]: of row t - (W - 1) + j
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            float v = k.b[i];
+      for (int j = 0; j < W - 1; ++j) conv_in<T, V, W>(win[j], a, sp, s, t0 - (W - 1) + j, c);
+      for (int tb = t0; tb < end; tb += SUB) {
+        Raw<T, V> x[SUB], g[SUB];
 #pragma unroll
-            for (int j = 0; j < W; ++j) v = fmaf(k.w[j][i], win[j][i], v);
-            if (a.silu) {
-              const float sg = sigmoid(v);
-              g[i] *= sg * fmaf(v, 1.0f - sg, 1.0f);
-            }
-          }
-          if (t < t1) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              db[i] += g[i];
-#pragma unroll
-              for (int j = 0; j < W; ++j) dw[j][i] = fmaf(g[i], win[j][i], dw[j][i]);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) g[i] = 0.0f;
+        for (int i = 0; i < SUB; ++i) {
+          x[i] = xn[i];
+          g[i] = gn[i];
+        }
+        if (tb + SUB < end) {
+          load_rows<T, V>(xn, xp, a.ld_x, tb + SUB, sp.len - 1);
+          load_rows<T, V>(gn, gp, a.ld_dy, tb + SUB, sp.len - 1);
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) da[W - 1][i] = g[i];
-        const int u = t - (W - 1);          // u's last reader of da is row t
-        if (u >= t0) {
-          float d[V];
+        for (int i = 0; i < SUB; ++i) {
+          const int t = tb + i;
+          if (t >= end) break;
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            float v = 0.0f;
+          for (int e = 0; e < V; ++e) win[W - 1][e] = elem<T, V>(x[i], e);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v = fmaf(k.w[W - 1 - j][i], da[j][i], v);
-            d[i] = v;
+          for (int e = 0; e < V; ++e) {
+            const float d = t < sp.len ? grad(win, e, elem<T, V>(g[i], e)) : 0.0f, own = t < t1 ? d : 0.0f;
+            da[W - 1][e] = d;
+            db[e] += own;
+#pragma unroll
+            for (int j = 0; j < W; ++j) dw[j][e] = fmaf(own, win[j][e], dw[j][e]);
           }
-          from_state(u, d);
-          store_vec<T, V>(static_cast<T*>(a.dx) + (sp.r0 + u) * a.ld_dx + c, d);
+          const int u = t - (W - 1);        // u's last reader of da is row t
+          if (u >= t0) {
+            float d[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              d[e] = 0.0f;
+#pragma unroll
+              for (int j = 0; j < W; ++j) d[e] = fmaf(k.w[W - 1 - j][e], da[j][e], d[e]);
+            }
+            from_state(u, d);
+            store_vec<T, V>(dp + u * a.ld_dx, d);
+          }
+#pragma unroll
+          for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              win[j][e] = win[j + 1][e];
+              da[j][e] = da[j + 1][e];
+            }
         }
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            win[j][i] = win[j + 1][i];
-            da[j][i] = da[j + 1][i];
-          }
       }
     }
     if (a.d_state && run == 0) {
@@ -271,20 +313,12 @@ __global__ __launch_bounds__(256) void conv_grad_kernel(const ConvArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) first[t][i] = 0.0f;
         if (t < sp.len) {
-          float x[W][V];
+          float x[W][V], g[V];
 #pragma unroll
           for (int j = 0; j < W; ++j) conv_in<T, V, W>(x[j], a, sp, s, t - (W - 1) + j, c);
-          load_vec<T, V>(first[t], static_cast<const T*>(a.dy) + (sp.r0 + t) * a.ld_dy + c);
+          load_vec<T, V>(g, static_cast<const T*>(a.dy) + (sp.r0 + t) * a.ld_dy + c);
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            float v = k.b[i];
-#pragma unroll
-            for (int j = 0; j < W; ++j) v = fmaf(k.w[j][i], x[j][i], v);
-            if (a.silu) {
-              const float sg = sigmoid(v);
-              first[t][i] *= sg * fmaf(v, 1.0f - sg, 1.0f);
-            }
-          }
+          for (int i = 0; i < V; ++i) first[t][i] = grad(x, i, g[i]);
         }
       }
 #pragma unroll
@@ -535,46 +569,53 @@ __global__ __launch_bounds__(256) void carry_kernel(const ScanArgs a) {
   if (used == 0) x[0] = h;                   // an empty sequence's only chunk
 }
 
-// One step (T_max = 1): four lanes per channel, N / 4 states each, so that the
-// states pass as whole 16-byte quads.
+// One step (T_max = 1): a workgroup takes 64 channels of a sequence, four lanes per
+// channel with N / 4 states each, so that the states pass as whole 16-byte quads.
+// Bytes bound it: 8 N of a channel's 8 N + 8 are its states, in and out.
 template <class T, int N>
 __global__ __launch_bounds__(256) void step_kernel(const ScanArgs a) {
-  constexpr int L = N / 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int q = (int)(id & 3);
-  const int64_t sc = id >> 2;
-  if (sc >= (int64_t)a.B * a.D) return;      // whole quads
-  const int s = (int)(sc / a.D), c = (int)(sc - (int64_t)s * a.D);
-  const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, c == 0 && q == 0);
-  float h[L];
-  const int64_t at = sc * N + q * L;
+  constexpr int L = N / 4, V = L < 4 ? L : 4;
+  typedef Vec<float, V> FV;
+  const uint32_t s = blockIdx.x / (uint32_t)a.cblocks, cb = blockIdx.x - s * a.cblocks;
+  const int q = threadIdx.x & 3, c = cb * 64 + (threadIdx.x >> 2);
+  const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, cb == 0 && threadIdx.x == 0);
+  if (c >= a.D) return;                      // whole quads
+  FV h[L / V], A[L / V];
+  const int64_t at = ((int64_t)s * a.D + c) * N + q * L;
 #pragma unroll
-  for (int n = 0; n < L; ++n) h[n] = a.h0 ? a.h0[at + n] : 0.0f;
+  for (int i = 0; i < L / V; ++i) {
+    h[i] = a.h0 ? *reinterpret_cast<const FV*>(a.h0 + at + i * V) : FV{};
+    A[i] = *reinterpret_cast<const FV*>(a.A + (int64_t)c * N + q * L + i * V);
+  }
   if (sp.len > 0) {
-    const float u = (float)static_cast<const T*>(a.u)[sp.r0 * a.ld_u + c];
-    const float d = softplus((float)static_cast<const T*>(a.delta)[sp.r0 * a.ld_delta + c] + (a.bias ? a.bias[c] : 0.0f));
+    const float u = (float)(static_cast<const T*>(a.u) + sp.r0 * a.ld_u)[c];
+    const float d = softplus((float)(static_cast<const T*>(a.delta) + sp.r0 * a.ld_delta)[c] + (a.bias ? a.bias[c] : 0.0f));
     const T* b = static_cast<const T*>(a.Bm) + sp.r0 * a.ld_B + q * L;
     const T* cr = static_cast<const T*>(a.Cm) + sp.r0 * a.ld_C + q * L;
     float y = 0.0f;
 #pragma unroll
-    for (int n = 0; n < L; ++n) {
-      h[n] = fmaf(exp2_of(d * a.A[(int64_t)c * N + q * L + n] * LOG2E), h[n], d * u * (float)b[n]);
-      y = fmaf((float)cr[n], h[n], y);
+    for (int i = 0; i < L / V; ++i) {
+      const Vec<T, V> bv = *reinterpret_cast<const Vec<T, V>*>(b + i * V), cv = *reinterpret_cast<const Vec<T, V>*>(cr + i * V);
+#pragma unroll
+      for (int n = 0; n < V; ++n) {
+        h[i][n] = fmaf(exp2_of(d * A[i][n] * LOG2E), h[i][n], d * u * (float)bv[n]);
+        y = fmaf((float)cv[n], h[i][n], y);
+      }
     }
     y += __shfl_xor(y, 1);
     y += __shfl_xor(y, 2);
     y = fmaf(a.Dp ? a.Dp[c] : 0.0f, u, y);
     if (q == 0) {
       if (a.z) {
-        const float z = (float)static_cast<const T*>(a.z)[sp.r0 * a.ld_z + c];
+        const float z = (float)(static_cast<const T*>(a.z) + sp.r0 * a.ld_z)[c];
         y *= z * sigmoid(z);
       }
-      static_cast<T*>(a.y)[sp.r0 * a.ld_y + c] = (T)y;
+      (static_cast<T*>(a.y) + sp.r0 * a.ld_y)[c] = (T)y;
     }
   }
   if (a.hT)
 #pragma unroll
-    for (int n = 0; n < L; ++n) a.hT[at + n] = h[n];
+    for (int i = 0; i < L / V; ++i) *reinterpret_cast<FV*>(a.hT + at + i * V) = h[i];
 }
 
 // --------------------------------------------------------------------------
@@ -1039,7 +1080,7 @@ wm_status check_rows(int32_t dtype, int32_t B, int32_t T_max, int64_t rows, int3
 bool mat_ok(const void* p, int64_t ld, int64_t rows, int64_t width) { return rows == 0 || (p && ld >= width && ld <= (1 << 24)); }
 
 struct ConvPlan {
-  int runs, groups, vec;
+  int runs, groups;
   size_t bytes;
 };
 wm_status check_conv(const wm_conv* a, ConvPlan* p) {
@@ -1051,11 +1092,9 @@ wm_status check_conv(const wm_conv* a, ConvPlan* p) {
   if (!mat_ok(a->x, a->ld_x, a->rows, a->channels)) return bad("x is NULL or its row stride is below channels");
   p->runs = std::max<int>(1, (int)cdiv(a->T_max, RUN));
   const int64_t items = (int64_t)a->B * p->runs;
-  if (items > INT32_MAX || items * a->channels > ((int64_t)1 << 39)) return set_error(WM_ERR_UNSUPPORTED, "B x T_max is too large");
+  if (items > INT32_MAX / 2 || items * cdiv(a->channels, 64) > INT32_MAX / 2) return set_error(WM_ERR_UNSUPPORTED, "B x T_max is too large");
   // groups of the gradient: about eight wavefronts per SIMD when vectors can be used
-  const int v = a->dtype == WM_BF16 ? 8 : 4;
-  p->vec = a->channels % v == 0 ? v : 1;
-  const int64_t cg = a->channels / p->vec;
+  const int64_t cg = a->channels % 4 == 0 ? a->channels / 4 : a->channels;
   p->groups = (int)std::max<int64_t>(1, std::min<int64_t>(items, cdiv(256 * 4 * 4 * 64, cg)));
   p->bytes = al256((size_t)p->groups * (a->width + 1) * a->channels * 4);
   return WM_OK;
@@ -1066,9 +1105,19 @@ bool vec_ok(int v, int32_t dtype, const void* p, int64_t ld) {
   return !p || ((uintptr_t)p % (v * e) == 0 && ld % v == 0);
 }
 
-template <class T, class F>
+// Lanes per run (a power of two) and workgroups of a launch over `slots` runs or groups.
+unsigned conv_grid(ConvArgs& a, int vec, int64_t slots) {
+  const int64_t cg = a.D / vec;
+  a.lp = 0;
+  while (a.lp < 6 && (1 << a.lp) < cg) ++a.lp;
+  const int64_t waves = cdiv(slots, 64 >> a.lp) * cdiv(cg, 1 << a.lp);
+  return (unsigned)cdiv(waves, 4);
+}
+
+// The gradient takes four channels per lane in both types (eight in bf16 need more
+// registers than a wavefront may have twice per SIMD).
+template <class T, int V, class F>
 hipError_t conv_typed(int vec, int width, F f) {
-  constexpr int V = IS_BF<T> ? 8 : 4;
   auto by_width = [&](auto vv) {
     if (width == 2) f(T{}, vv, std::integral_constant<int, 2>{});
     else if (width == 3) f(T{}, vv, std::integral_constant<int, 3>{});
@@ -1193,16 +1242,15 @@ wm_status wm_causal_conv(const wm_conv* w, void* y, int64_t ld_y, void* state_ou
   a.w = w->weight; a.b = w->bias; a.status = w->status;
   a.ld_x = w->ld_x; a.ld_y = ld_y; a.rows = w->rows;
   a.B = w->B; a.T_max = w->T_max; a.D = w->channels; a.runs = p.runs; a.silu = w->silu;
-  int vec = p.vec;
-  if (!vec_ok(vec, w->dtype, w->x, w->ld_x) || !vec_ok(vec, w->dtype, y, ld_y) || !vec_ok(vec, w->dtype, w->state, 0) ||
+  int vec = w->dtype == WM_BF16 ? 8 : 4;
+  if (w->channels % vec || !vec_ok(vec, w->dtype, w->x, w->ld_x) || !vec_ok(vec, w->dtype, y, ld_y) || !vec_ok(vec, w->dtype, w->state, 0) ||
       !vec_ok(vec, w->dtype, state_out, 0))
     vec = 1;
-  const int64_t threads = (int64_t)w->B * p.runs * (w->channels / vec);
+  const unsigned grid = conv_grid(a, vec, (int64_t)w->B * p.runs);
   auto go = [&](auto t, auto v, auto wd) {
-    hipLaunchKernelGGL((conv_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3((unsigned)cdiv(threads, 256)),
-                       dim3(256), 0, st, a);
+    hipLaunchKernelGGL((conv_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3(grid), dim3(256), 0, st, a);
   };
-  WM_ST(TK_CONV, w->dtype == WM_BF16 ? conv_typed<__bf16>(vec, w->width, go) : conv_typed<float>(vec, w->width, go));
+  WM_ST(TK_CONV, (w->dtype == WM_BF16 ? conv_typed<__bf16, 8>(vec, w->width, go) : conv_typed<float, 4>(vec, w->width, go)));
   return clear_error();
 }
 
@@ -1222,17 +1270,16 @@ wm_status wm_causal_conv_grad(const wm_conv* w, const void* dy, int64_t ld_dy, c
   a.part = static_cast<float*>(ws);
   a.ld_x = w->ld_x; a.ld_dy = ld_dy; a.ld_dx = ld_dx; a.rows = w->rows;
   a.B = w->B; a.T_max = w->T_max; a.D = w->channels; a.runs = p.runs; a.silu = w->silu; a.groups = p.groups;
-  int vec = p.vec;
+  int vec = w->channels % 4 ? 1 : 4;
   for (const auto& m : {std::pair<const void*, int64_t>{w->x, w->ld_x}, {dy, ld_dy}, {dx, ld_dx}, {w->state, 0}, {d_state_out, 0}, {d_state, 0}})
     if (!vec_ok(vec, w->dtype, m.first, m.second)) vec = 1;
-  const int64_t threads = (int64_t)p.groups * (w->channels / vec);
+  const unsigned grid = conv_grid(a, vec, p.groups);
   auto go = [&](auto t, auto v, auto wd) {
-    hipLaunchKernelGGL((conv_grad_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3((unsigned)cdiv(threads, 256)),
-                       dim3(256), 0, st, a);
+    hipLaunchKernelGGL((conv_grad_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3(grid), dim3(256), 0, st, a);
     hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)cdiv((int64_t)(w->width + 1) * w->channels, 16)), dim3(256), 0, st,
                        a.part, a.groups, w->width, w->channels, dweight, dbias);
   };
-  WM_ST(TK_CONV, w->dtype == WM_BF16 ? conv_typed<__bf16>(vec, w->width, go) : conv_typed<float>(vec, w->width, go));
+  WM_ST(TK_CONV, (w->dtype == WM_BF16 ? conv_typed<__bf16, 4>(vec, w->width, go) : conv_typed<float, 4>(vec, w->width, go)));
   return clear_error();
 }
 
@@ -1264,7 +1311,7 @@ wm_status wm_scan(const wm_scan_args* w, void* y, int64_t ld_y, float* hT, void*
     using T = decltype(t);
     constexpr int N = decltype(nv)::value;
     if (w->T_max <= 1 && !checkpoints) {
-      hipLaunchKernelGGL((step_kernel<T, N>), dim3((unsigned)cdiv((int64_t)w->B * w->channels * 4, 256)), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((step_kernel<T, N>), dim3((unsigned)(w->B * p.cblocks)), dim3(256), 0, st, a);
       return;
     }
     const dim3 grid((unsigned)cdiv((int64_t)w->B * p.chunks * p.cblocks, 4));
