@@ -29,16 +29,24 @@ using namespace wm;
 namespace wm {
 namespace attend {
 
-constexpr int MAX_SEGS = 256;               // segments per launch (the tables are kernel arguments)
+constexpr int MAX_SEGS = 128;               // segments per launch (the table is a kernel argument)
+constexpr int XCDS = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-// A new maximum replaces the one in use only when it passes it by this much (units of
-// log2): sums then stay below 2^8 of their usual size and the accumulators are
-// seldom rescaled.
-constexpr float MAX_SLACK = 8.0f;
+// Weights against a maximum that is out of date are fine until a row's sum over one
+// step passes this: the accumulators are seldom rescaled, and the maximum is seldom
+// looked for (half an instruction per score, and a branch).
+constexpr float SUM_LIMIT = 1024.0f;
 
+// Segments of a launch, those with the longest loops first.  A segment's (key head,
+// tile) pairs are dealt out evenly over the XCDs (workgroups go to them in turn), in
+// runs that share a head's keys in an XCD's L2: dealing whole segments to XCDs
+// left some with twice the work of others where key counts differ.
 struct Table {
   int32_t n;
-  int32_t q_off[MAX_SEGS + 1], k_off[MAX_SEGS + 1], tile_off[MAX_SEGS + 1];
+  struct {
+    int32_t q0, lq, k0, lk;
+  } seg[MAX_SEGS];
+  int32_t off[MAX_SEGS + 1];                // pairs per XCD, summed
 };
 
 struct Args {
@@ -218,31 +226,32 @@ __device__ __forceinline__ void copy_tile(u32x4 buf, T* tile, int tid, Off offse
   }
 }
 
-__device__ __forceinline__ int segment_of_tile(const Table& t, int tile, int per) {
+// The problem of a workgroup: segment, key head, tile, split of its loop.
+struct Prob {
+  int q0, R, k0, Lk, hk, tile, split;
+};
+// false: none (a segment's pairs need not divide by the XCDs).  rows_per_tile: of the tiled axis (R, or Lk
+// for keys).
+template <bool KEYS>
+__device__ __forceinline__ bool problem(const Table& t, const Args& a, int rows_per_tile, Prob& p) {
+  const int x = blockIdx.x % XCDS, i = blockIdx.x / XCDS;
   int lo = 0, hi = t.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (t.tile_off[mid] * per <= tile) lo = mid; else hi = mid - 1;
+    if (t.off[mid] <= i) lo = mid; else hi = mid - 1;
   }
-  return lo;
-}
-
-// The problem of a workgroup: segment, key head, tile.
-struct Prob {
-  int q0, R, k0, Lk, hk, tile;
-};
-__device__ __forceinline__ Prob problem(const Table& t, const Args& a, int bid, int total) {
-  const int id = xcd_tile(bid, total);
-  const int s = segment_of_tile(t, id, a.kv_heads);
-  const int local = id - t.tile_off[s] * a.kv_heads, nt = t.tile_off[s + 1] - t.tile_off[s];
-  Prob p;
-  p.q0 = t.q_off[s];
-  p.R = (t.q_off[s + 1] - p.q0) * a.G;
-  p.k0 = t.k_off[s];
-  p.Lk = t.k_off[s + 1] - p.k0;
-  p.hk = local / nt;
-  p.tile = local % nt;
-  return p;
+  p.q0 = t.seg[lo].q0;
+  p.R = t.seg[lo].lq * a.G;
+  p.k0 = t.seg[lo].k0;
+  p.Lk = t.seg[lo].lk;
+  const int tiles = ((KEYS ? p.Lk : p.R) + rows_per_tile - 1) / rows_per_tile;
+  // XCD x's share, another first XCD for every segment so that the shares' remainders spread
+  const int n = tiles * a.kv_heads * a.splits, y = (x + 3 * lo) % XCDS, at = (int)((int64_t)n * y / XCDS) + i - t.off[lo];
+  const int pair = at / a.splits;
+  p.split = at - pair * a.splits;
+  p.hk = pair / tiles;
+  p.tile = pair - p.hk * tiles;
+  return at < (int)((int64_t)n * (y + 1) / XCDS);
 }
 
 // Which of the `n` keys from `key` on are seen, one bit each (64 at most).
@@ -280,7 +289,8 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   T* const vs = lds + 2 * KB * DH;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, wr = wave % WR, wk = wave / WR;
-  const Prob p = problem(t, a, blockIdx.x, gridDim.x);
+  Prob p;
+  if (!problem<false>(t, a, 32 * WR, p)) return;
   const int row = p.tile * (32 * WR) + wr * 32 + (lane & 31);       // may pass R: computed, not stored
   const int rr = min(row, p.R - 1), head = p.hk * a.G + rr % a.G;
   const int64_t qrow = (int64_t)p.q0 + rr / a.G;
@@ -288,7 +298,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
   TL::scale_op(qf, a.c2);
 
-  const int tiles = (p.Lk + KB - 1) / KB, split = blockIdx.y;
+  const int tiles = (p.Lk + KB - 1) / KB, split = p.split;
   const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
   const uint8_t* mask = a.mask ? a.mask + p.k0 : nullptr;
   auto mask_byte = [&](int tile, int w) -> int {
@@ -319,7 +329,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
   float mx = -INFINITY, sum = 0.0f;
-  const float slack = IS_BF<T> ? MAX_SLACK / a.c2 : MAX_SLACK;
+  bool started = false;                       // every row has a maximum
   if (t0 < t1) {
     look(t0, vis, true);
     copy(t0, vis);
@@ -339,41 +349,63 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     }
     const T* kt = ks + (ti & 1) * KB * DH;
     const T* vt = vs + (ti & 1) * KB * DH;
+    // The keys of this wavefront in the tile, 32 at a time; weights are formed
+    // against the maximum in use, and only where their sum grows past 2^10 (or a
+    // key is hidden, or there is no maximum yet) the maximum is looked for.
+    constexpr int NB = KB / 32 / WK;
+    f32x16 s[NB];
+    uint32_t seen[NB];
+    bool plain = started;
 #pragma unroll
-    for (int kb = 0; kb < KB / 32 / WK; ++kb) {
+    for (int kb = 0; kb < NB; ++kb) {
       const int base = 32 * (kb * WK + wk);
-      const uint32_t seen = (uint32_t)(vis[NV > 1 ? base >> 6 : 0] >> (base & 63));
-      if (seen == 0) continue;
-      f32x16 s = TL::mm_row(kt, base, qf, lane);
-      if (seen != ~0u) {
-        const uint32_t m = seen >> (4 * h);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : -INFINITY;
-      }
-      float bm = s[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) bm = fmaxf(bm, s[r]);
-      bm = pair_max(bm);
-      if (__any(bm > mx + slack)) {
-        const float nm = bm > mx + slack ? bm : mx;
-        const float f = nm > mx ? exp2_of(log2_units<T>(mx - nm, a.c2)) : 1.0f;
-        sum *= f;
-#pragma unroll
-        for (int b = 0; b < DB; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[b][r] *= f;
-        mx = nm;
-      }
-      const float mc = mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2);    // only keys of weight 0 so far
-      float bs = 0.0f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = weight<T>(s[r], a.c2, mc);
-        bs += s[r];
-      }
-      sum += bs;
-      TL::mm_col(vt, base, s, acc, lane);
+      seen[kb] = (uint32_t)(vis[NV > 1 ? base >> 6 : 0] >> (base & 63));
+      plain = plain && seen[kb] == ~0u;
     }
+    float bs = INFINITY;
+    auto scores = [&]() {
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) s[kb] = TL::mm_row(kt, 32 * (kb * WK + wk), qf, lane);
+    };
+    auto weights = [&](float mc) {                // in the scores' place
+      bs = 0.0f;
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[kb][r] = weight<T>(s[kb][r], a.c2, mc);
+          bs += s[kb][r];
+        }
+    };
+    if (plain) {
+      scores();
+      weights(log2_units<T>(mx, a.c2));
+    }
+    if (__any(!(bs <= SUM_LIMIT))) {
+      scores();                                   // again: keeping them takes as many registers as the weights
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        const uint32_t m = seen[kb] >> (4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] = (m >> acc_row(0, r)) & 1 ? s[kb][r] : -INFINITY;
+      }
+      float bm = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, s[kb][r]);
+      bm = pair_max(bm);
+      const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, a.c2)) : 1.0f;
+      sum *= f;
+#pragma unroll
+      for (int b = 0; b < DB; ++b) acc[b] *= f;
+      mx = bm > mx ? bm : mx;
+      started = !__any(mx == -INFINITY);
+      weights(mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2));      // only keys of weight 0 so far
+    }
+    sum += bs;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) TL::mm_col(vt, 32 * (kb * WK + wk), s[kb], acc, lane);
 #pragma unroll
     for (int w = 0; w < NV; ++w) vis[w] = next[w];
   }
@@ -477,7 +509,8 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   T* const vs = lds + 2 * KB * DH;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
-  const Prob p = problem(t, a, blockIdx.x, gridDim.x);
+  Prob p;
+  if (!problem<false>(t, a, 128, p)) return;
   const int row = p.tile * 128 + wave * 32 + (lane & 31);
   const int rr = min(row, p.R - 1), head = p.hk * a.G + rr % a.G;
   const int64_t qrow = (int64_t)p.q0 + rr / a.G, orow = qrow * a.heads + head;
@@ -494,7 +527,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const float lse = a.lse[orow];
   // a row without a visible key has lse = -inf: its P is 0
   const float l2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
-  const int split = blockIdx.y;
+  const int split = p.split;
   if (split == 0 && h == 0 && row < p.R) {
     a.stat[2 * orow] = l2;
     a.stat[2 * orow + 1] = delta;
@@ -546,6 +579,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * (dp[r] - delta);
       if (seen != ~0u) {
+        asm volatile("");                       // a branch: seldom taken, 32 instructions
         const uint32_t m = seen >> (4 * h);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : 0.0f;
@@ -571,7 +605,8 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
   T* const gs = lds + 2 * RB * DH;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
-  const Prob p = problem(t, a, blockIdx.x, gridDim.x);
+  Prob p;
+  if (!problem<true>(t, a, 128, p)) return;
   const int key = p.tile * 128 + wave * 32 + (lane & 31), kc = min(key, p.Lk - 1);
   const int64_t krow = (int64_t)p.k0 + kc;
   const bool seen = !a.mask || a.mask[krow] != 0;
@@ -579,7 +614,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
   TL::load_op(kf, static_cast<const T*>(a.k) + krow * a.ld_k + p.hk * DH, h);
   TL::load_op(vf, static_cast<const T*>(a.v) + krow * a.ld_v + p.hk * DH, h);
   TL::scale_op(kf, a.c2);
-  const int tiles = (p.R + RB - 1) / RB, split = blockIdx.y;
+  const int tiles = (p.R + RB - 1) / RB, split = p.split;
   const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
   auto copy = [&](int tile) {
     const int r0 = tile * RB, first = r0 / a.G;            // the tile's first query
@@ -687,12 +722,22 @@ struct Plan {
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Splits of a long axis of `units` steps so that about two workgroups per compute unit
-// exist; each keeps at least `least` steps.
-int splits_for(int64_t blocks, int64_t units, int64_t least) {
-  if (blocks <= 0) return 1;
-  const int64_t want = cdiv(512, blocks), most = std::max<int64_t>(1, units / least);
-  return (int)std::min<int64_t>({want, most, 64});
+// Into how many splits the loops of `blocks` workgroups, `units` steps of unit_us each on
+// average (`longest` at most), are cut: the number of rounds that 256 x per_cu
+// places take times a split's length, plus what the partial sums cost (part_us a
+// split; a launch that joins them).  Every split keeps at least `least` steps.
+// One split of 520 workgroups on 512 places took 400 us (a second round of eight), four 290.
+int splits_for(int64_t blocks, double units, int64_t longest, int64_t least, int per_cu, double unit_us, double part_us) {
+  int best = 1;
+  double cost = 1e30;
+  for (int s = 1; s <= 64 && (s == 1 || s <= longest / least); ++s) {
+    const double c = (double)cdiv(blocks * s, 256 * per_cu) * std::ceil(units / s) * unit_us + (s > 1 ? s * part_us + 4.0 : 0.0);
+    if (c < 0.98 * cost) {
+      cost = c;
+      best = s;
+    }
+  }
+  return best;
 }
 
 wm_status check(const wm_attention* a, Plan* p, bool grad) {
@@ -726,23 +771,49 @@ wm_status check(const wm_attention* a, Plan* p, bool grad) {
       !rows_ok(a->k, a->ld_k, p->nk, (int64_t)a->kv_heads * a->head_dim) ||
       !rows_ok(a->v, a->ld_v, p->nk, (int64_t)a->kv_heads * a->head_dim))
     return bad("q, k and v need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
-  // rows and blocks of the three kernels, over all segments
-  int64_t row_tiles = 0, few_tiles = 0, key_tiles = 0;
-  const bool wide32 = a->dtype == WM_FP32 && a->head_dim == 128;
+  // tiles of the kernels and steps of their loops, over all segments
+  const bool bf = a->dtype == WM_BF16;
+  const int dh = a->head_dim, wi = dh == 32 ? 0 : dh == 64 ? 1 : 2;
+  const bool wide32 = !bf && dh == 128;
   const int few_rows = wide32 ? 64 : 32, few_keys = wide32 ? 64 : 128, tile = wide32 ? 32 : 64;
+  int64_t row_tiles = 0, few_tiles = 0, key_tiles = 0;
+  double row_steps = 0, few_steps = 0, key_steps = 0;
   for (int s = 0; s < a->S; ++s) {
     const int64_t r = ((int64_t)a->q_off[s + 1] - a->q_off[s]) * G, lk = (int64_t)a->k_off[s + 1] - a->k_off[s];
     row_tiles += cdiv(r, 128);
     few_tiles += cdiv(r, few_rows);
     key_tiles += cdiv(lk, 128);
+    row_steps += (double)cdiv(r, 128) * cdiv(lk, tile);
+    few_steps += (double)cdiv(r, few_rows) * cdiv(lk, few_keys);
+    key_steps += (double)cdiv(lk, 128) * cdiv(r, tile);
   }
-  if (row_tiles * a->kv_heads > INT32_MAX / 8 || few_tiles * a->kv_heads > INT32_MAX / 8 || key_tiles * a->kv_heads > INT32_MAX / 8)
-    return set_error(WM_ERR_UNSUPPORTED, "too many row tiles");
+  const int64_t most = INT32_MAX / 64 / 8;               // 64: splits
+  if (row_tiles * a->kv_heads > most || few_tiles * a->kv_heads > most || key_tiles * a->kv_heads > most)
+    return set_error(WM_ERR_UNSUPPORTED, "too many row or key tiles");
+  const int64_t rows_all = p->nq * a->heads, kv_all = p->nk * a->kv_heads;
+  // workgroups that share a compute unit (registers, LDS), us of a step when they do (rates that the
+  // kernels reach: 600 TFLOP/s in bf16, 90 in float32, a step of the few-row form its bytes at 4.5 TB/s; not
+  // below 1 us), us to write and read a split's partial sums
+  static const int fwd_cu[2][3] = {{3, 2, 2}, {4, 3, 2}}, few_cu[2][3] = {{2, 1, 1}, {4, 2, 1}};
+  static const int dq_cu[2][3] = {{2, 2, 1}, {4, 3, 1}}, dkv_cu[2][3] = {{2, 1, 1}, {3, 2, 1}};
+  auto step_us = [&](int products, int per_cu) {
+    return std::max(1.0, products * 2.0 * 128 * tile * dh * 256 * per_cu / (bf ? 600e6 : 90e6));
+  };
+  auto part_us = [&](int64_t values) { return 2.0 * values * dh * 4 / 4.5e6; };
+  auto avg = [](double steps, int64_t tiles) { return tiles ? steps / tiles : 0.0; };
   p->few = p->max_r <= few_rows;
-  p->fwd_splits = p->few ? splits_for(few_tiles * a->kv_heads, cdiv(p->max_lk, few_keys), 2)
-                         : splits_for(row_tiles * a->kv_heads, cdiv(p->max_lk, tile), 4);
-  p->dq_splits = splits_for(row_tiles * a->kv_heads, cdiv(p->max_lk, tile), 4);
-  p->dkv_splits = splits_for(key_tiles * a->kv_heads, cdiv(p->max_r, tile), 4);
+  if (p->few) {
+    const int cu = few_cu[bf][wi];
+    p->fwd_splits = splits_for(few_tiles * a->kv_heads, avg(few_steps, few_tiles), cdiv(p->max_lk, few_keys), 2, cu,
+                               std::max(1.0, 2.0 * few_keys * dh * e * 256 * cu / 4.5e6), part_us(rows_all));
+  } else {
+    const int cu = fwd_cu[bf][wi];
+    p->fwd_splits = splits_for(row_tiles * a->kv_heads, avg(row_steps, row_tiles), cdiv(p->max_lk, tile), 2, cu, step_us(2, cu), part_us(rows_all));
+  }
+  p->dq_splits = splits_for(row_tiles * a->kv_heads, avg(row_steps, row_tiles), cdiv(p->max_lk, tile), 2, dq_cu[bf][wi],
+                            step_us(3, dq_cu[bf][wi]), part_us(rows_all));
+  p->dkv_splits = splits_for(key_tiles * a->kv_heads, avg(key_steps, key_tiles), cdiv(p->max_r, tile), 2, dkv_cu[bf][wi],
+                             step_us(4, dkv_cu[bf][wi]), part_us(2 * kv_all));
   const int64_t rows = p->nq * a->heads, kv = p->nk * a->kv_heads;
   size_t at = 0;
   p->o_part = p->o_ml = p->o_stat = 0;
@@ -774,21 +845,18 @@ Args base_args(const wm_attention* w) {
   return a;
 }
 
-// Calls go(table, number of tiles) for runs of at most MAX_SEGS segments.
+// Calls go(table, workgroups) for runs of at most MAX_SEGS segments, sorted by the length of their
+// workgroups' loops; tiles(lq, lk) is a segment's number of tiles.
 template <class Tiles, class Go>
-hipError_t each_run(const wm_attention* a, Tiles tiles, Go go) {
+hipError_t each_run(const wm_attention* a, bool keys, int splits, Tiles tiles, Go go) {
   for (int s0 = 0; s0 < a->S; s0 += MAX_SEGS) {
-    Table t;
-    t.n = std::min(MAX_SEGS, a->S - s0);
-    t.tile_off[0] = 0;
-    for (int i = 0; i <= t.n; ++i) {
-      t.q_off[i] = a->q_off[s0 + i];
-      t.k_off[i] = a->k_off[s0 + i];
-      if (i) t.tile_off[i] = t.tile_off[i - 1] + (int32_t)tiles(t.q_off[i] - t.q_off[i - 1], t.k_off[i] - t.k_off[i - 1]);
-    }
-    for (int i = t.n + 1; i <= MAX_SEGS; ++i) t.q_off[i] = t.k_off[i] = t.tile_off[i] = 0;
-    if (t.tile_off[t.n] == 0) continue;
-    go(t, t.tile_off[t.n]);
+    Table t = {};
+    for (int i = s0; i < std::min(a->S, s0 + MAX_SEGS); ++i)
+      t.seg[t.n++] = {a->q_off[i], a->q_off[i + 1] - a->q_off[i], a->k_off[i], a->k_off[i + 1] - a->k_off[i]};
+    std::stable_sort(t.seg, t.seg + t.n, [&](const auto& x, const auto& y) { return keys ? x.lq > y.lq : x.lk > y.lk; });
+    for (int i = 0; i < t.n; ++i) t.off[i + 1] = t.off[i] + (int32_t)cdiv(tiles(t.seg[i].lq, t.seg[i].lk) * a->kv_heads * splits, XCDS);
+    if (t.off[t.n] == 0) continue;
+    go(t, t.off[t.n] * XCDS);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -813,9 +881,9 @@ hipError_t forward(const wm_attention* w, const Plan& p, const Args& a, hipStrea
     constexpr int DH = decltype(dh)::value;
     constexpr int WK = (!IS_BF<T> && DH == 128) ? 2 : 4;
     const int rows = p.few ? 128 / WK : 128;
-    hipError_t e = each_run(w, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, rows); },
-                            [&](const Table& t, int tiles) {
-                              const dim3 grid(tiles * a.kv_heads, a.splits);
+    hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, rows); },
+                            [&](const Table& t, int blocks) {
+                              const dim3 grid(blocks);
                               if (p.few) hipLaunchKernelGGL((forward_kernel<T, DH, WK>), grid, dim3(256), 0, st, t, a);
                               else hipLaunchKernelGGL((forward_kernel<T, DH, 1>), grid, dim3(256), 0, st, t, a);
                             });
@@ -830,9 +898,9 @@ hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStr
   return typed(w, [&](auto tv, auto dh) {
     using T = decltype(tv);
     constexpr int DH = decltype(dh)::value;
-    hipError_t e = each_run(w, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, 128); },
-                            [&](const Table& t, int tiles) {
-                              hipLaunchKernelGGL((dq_kernel<T, DH>), dim3(tiles * a.kv_heads, a.splits), dim3(256), 0, st, t, a);
+    hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, 128); },
+                            [&](const Table& t, int blocks) {
+                              hipLaunchKernelGGL((dq_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.nq * a.heads;
@@ -846,9 +914,9 @@ hipError_t grad_keys(const wm_attention* w, const Plan& p, const Args& a, hipStr
   return typed(w, [&](auto tv, auto dh) {
     using T = decltype(tv);
     constexpr int DH = decltype(dh)::value;
-    hipError_t e = each_run(w, [&](int64_t, int64_t lk) { return cdiv(lk, 128); },
-                            [&](const Table& t, int tiles) {
-                              hipLaunchKernelGGL((dkv_kernel<T, DH>), dim3(tiles * a.kv_heads, a.splits), dim3(256), 0, st, t, a);
+    hipError_t e = each_run(w, true, a.splits, [&](int64_t, int64_t lk) { return cdiv(lk, 128); },
+                            [&](const Table& t, int blocks) {
+                              hipLaunchKernelGGL((dkv_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.nk * a.kv_heads;
