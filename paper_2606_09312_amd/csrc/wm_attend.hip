@@ -355,53 +355,53 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     constexpr int NB = KB / 32 / WK;
     f32x16 s[NB];
     uint32_t seen[NB];
-    bool plain = started;
+    bool all = true;
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb) {
       const int base = 32 * (kb * WK + wk);
       seen[kb] = (uint32_t)(vis[NV > 1 ? base >> 6 : 0] >> (base & 63));
-      plain = plain && seen[kb] == ~0u;
+      all = all && seen[kb] == ~0u;
     }
-    float bs = INFINITY;
-    auto scores = [&]() {
+    float bs;
+    bool look_for_max = !started || !all;
+    // a second time, scores and all, with the maximum that the first lacked
+    for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb) s[kb] = TL::mm_row(kt, 32 * (kb * WK + wk), qf, lane);
-    };
-    auto weights = [&](float mc) {                // in the scores' place
+      if (!all) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+          uint32_t m = seen[kb] >> (4 * h);
+          asm volatile("" : "+v"(m));               // keeps this a branch: seldom taken, 48 instructions
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = (m >> acc_row(0, r)) & 1 ? s[kb][r] : -INFINITY;
+        }
+      }
+      if (look_for_max) {
+        float bm = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) bm = fmaxf(bm, s[kb][r]);
+        bm = pair_max(bm);
+        const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, a.c2)) : 1.0f;
+        sum *= f;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) acc[b] *= f;
+        mx = bm > mx ? bm : mx;
+        started = !__any(mx == -INFINITY);
+      }
+      const float mc = mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2);      // only keys of weight 0 so far
       bs = 0.0f;
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 16; ++r) {             // weights in the scores' place
           s[kb][r] = weight<T>(s[kb][r], a.c2, mc);
           bs += s[kb][r];
         }
-    };
-    if (plain) {
-      scores();
-      weights(log2_units<T>(mx, a.c2));
-    }
-    if (__any(!(bs <= SUM_LIMIT))) {
-      scores();                                   // again: keeping them takes as many registers as the weights
-#pragma unroll
-      for (int kb = 0; kb < NB; ++kb) {
-        const uint32_t m = seen[kb] >> (4 * h);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] = (m >> acc_row(0, r)) & 1 ? s[kb][r] : -INFINITY;
-      }
-      float bm = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, s[kb][r]);
-      bm = pair_max(bm);
-      const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, a.c2)) : 1.0f;
-      sum *= f;
-#pragma unroll
-      for (int b = 0; b < DB; ++b) acc[b] *= f;
-      mx = bm > mx ? bm : mx;
-      started = !__any(mx == -INFINITY);
-      weights(mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2));      // only keys of weight 0 so far
+      if (!__any(bs > SUM_LIMIT)) break;           // infinite or NaN scores stay what they are
+      look_for_max = true;
     }
     sum += bs;
 #pragma unroll
@@ -579,8 +579,8 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * (dp[r] - delta);
       if (seen != ~0u) {
-        asm volatile("");                       // a branch: seldom taken, 32 instructions
-        const uint32_t m = seen >> (4 * h);
+        uint32_t m = seen >> (4 * h);
+        asm volatile("" : "+v"(m));             // keeps this a branch: seldom taken, 48 instructions
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : 0.0f;
       }
