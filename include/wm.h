@@ -425,7 +425,8 @@ typedef struct wm_attention {
 } wm_attention;
 
 /* Bytes of workspace of the forward (grad = 0) or the gradient call (256-byte
- * aligned, need not be cleared); 0 on a bad argument. */
+ * aligned, need not be cleared); 0 on a bad argument, 256 where none is needed
+ * (NULL may be passed then). */
 size_t wm_cross_attention_workspace_bytes(const wm_attention* a, int32_t grad);
 
 /* o [rows][heads][head_dim] out; lse [rows][heads] float32 out (may be NULL). */
@@ -494,7 +495,8 @@ typedef struct wm_scan_args {
 } wm_scan_args;
 
 /* Workspace bytes of wm_scan (grad = 0) or wm_scan_grad, and bytes of the states
- * that a forward call keeps for the gradient (0 on a bad argument). */
+ * that a forward call keeps for the gradient (0 on a bad argument; workspaces as
+ * above). */
 size_t wm_scan_workspace_bytes(const wm_scan_args* a, int32_t grad);
 size_t wm_scan_checkpoint_bytes(const wm_scan_args* a);
 

@@ -510,11 +510,19 @@ def encode_text(model: TextModel, tokens, tok_off, z0=None, ws=None, stream=None
 
 
 # ---- sequence operators ----------------------------------------------------------
+# The checks run on every call of a step-by-step rollout, whose kernels take some 10 us: they
+# compare shapes, types and devices directly and build the argument blocks positionally.
+_DTYPES = {}
+
+
 def _dtype(t):
-    import torch
-    if t.dtype not in (torch.bfloat16, torch.float32):
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: WM_BF16, torch.float32: WM_FP32})
+    d = _DTYPES.get(t.dtype)
+    if d is None:
         raise ValueError(f"tensors must be float32 or bfloat16, not {t.dtype}")
-    return WM_BF16 if t.dtype == torch.bfloat16 else WM_FP32
+    return d
 
 
 def _on_gpu(t):
@@ -524,18 +532,16 @@ def _on_gpu(t):
 
 def _same(like, shape, **tensors):
     """Checks that tensors (None allowed) are on like's device with its dtype and `shape`."""
+    dtype, dev = like.dtype, like.device
     for name, t in tensors.items():
-        if t is not None and (t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != tuple(shape)):
-            raise ValueError(f"{name} must be {tuple(shape)} {like.dtype} on {like.device}, not {tuple(t.shape)} "
-                             f"{t.dtype} on {t.device}")
+        if t is not None and (t.shape != shape or t.dtype != dtype or t.device != dev):
+            raise ValueError(f"{name} must be {tuple(shape)} {dtype} on {dev}, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
 def _f32(dev, shape, **tensors):
     """Checks that tensors (None allowed) are dense float32 of `shape` on `dev`."""
-    import torch
     for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.float32 or t.device != dev or tuple(t.shape) != tuple(shape)
-                              or not t.is_contiguous()):
+        if t is not None and (t.shape != shape or _DTYPES.get(t.dtype) != WM_FP32 or t.device != dev or not t.is_contiguous()):
             raise ValueError(f"{name} must be dense {tuple(shape)} float32 on {dev}")
 
 
@@ -543,8 +549,9 @@ def _rows(name, t):
     """Row stride of a matrix [rows][width] or [rows][heads][width] whose rows are dense."""
     shape, stride = t.shape, t.stride()
     width = 1
-    for n, st in zip(reversed(shape[1:]), reversed(stride[1:])):
-        if n > 1 and st != width:
+    for i in range(len(shape) - 1, 0, -1):
+        n = shape[i]
+        if n > 1 and stride[i] != width:
             raise ValueError(f"{name}: only the row stride may differ from a dense tensor's")
         width *= n
     return stride[0] if shape[0] > 1 else width
@@ -555,10 +562,16 @@ def _addr(t):
 
 
 def _workspace(n, given, dev):
+    """The workspace and its bytes; the least size that the library answers, 256, means that it needs none."""
     import torch
     if given is not None:
         return given, given.numel() * given.element_size()
-    return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n else (None, 0)
+    return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n > 256 else (None, 0)
+
+
+def _stream_on(stream, dev):
+    import torch
+    return (torch.cuda.current_stream(dev.index) if stream is None else stream).cuda_stream
 
 
 def _attention(q, k, v, q_off, k_off, kv_mask, scale):
@@ -567,9 +580,10 @@ def _attention(q, k, v, q_off, k_off, kv_mask, scale):
         raise ValueError("q, k and v are [rows][heads][head_dim]")
     if k.shape[2] != q.shape[2]:
         raise ValueError("q and k differ in head_dim")
+    _dtype(q)
     _same(q, k.shape, k=k, v=v)
-    qo, qp = _host_i32(q_off)
-    ko, kp = _host_i32(k_off)
+    qo, ko = np.ascontiguousarray(q_off, dtype=np.int32), np.ascontiguousarray(k_off, dtype=np.int32)
+    qp, kp = qo.ctypes.data, ko.ctypes.data
     if qo.ndim != 1 or len(qo) != len(ko) or len(qo) < 2:
         raise ValueError("q_off and k_off need S + 1 entries each")
     if qo[-1] != q.shape[0] or ko[-1] != k.shape[0]:
@@ -578,9 +592,9 @@ def _attention(q, k, v, q_off, k_off, kv_mask, scale):
         if kv_mask.dtype not in (torch.uint8, torch.bool) or tuple(kv_mask.shape) != (k.shape[0],) or \
                 kv_mask.device != q.device or not kv_mask.is_contiguous():
             raise ValueError("kv_mask must be dense uint8 or bool [key rows] on the tensors' device")
-    a = Attention(dtype=_dtype(q), heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2], S=len(qo) - 1, q_off=qp, k_off=kp,
-                  q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), ld_q=_rows("q", q), ld_k=_rows("k", k), ld_v=_rows("v", v),
-                  kv_mask=_addr(kv_mask), scale=q.shape[2] ** -0.5 if scale is None else scale)
+    # in the order of Attention's fields
+    a = Attention(_dtype(q), q.shape[1], k.shape[1], q.shape[2], len(qo) - 1, qp, kp, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                  _rows("q", q), _rows("k", k), _rows("v", v), _addr(kv_mask), q.shape[2] ** -0.5 if scale is None else scale)
     a.keep = (qo, ko)
     _on_gpu(q)
     return a
@@ -605,7 +619,7 @@ def cross_attention(q, k, v, q_off, k_off, *, kv_mask=None, scale=None, o=None, 
     _f32(q.device, q.shape[:2], lse=lse)
     lib = load_library()
     ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 0), ws, q.device)
-    _check(lib.wm_cross_attention(a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n, _stream(stream)))
+    _check(lib.wm_cross_attention(a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n, _stream_on(stream, q.device)))
     return {"o": o, "lse": lse, "ws": ws}
 
 
@@ -624,7 +638,7 @@ def cross_attention_grad(do, q, k, v, o, lse, q_off, k_off, *, kv_mask=None, sca
     ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 1), ws, q.device)
     _check(lib.wm_cross_attention_grad(a, o.data_ptr(), _rows("o", o), _addr(lse), do.data_ptr(), _rows("do", do), dq.data_ptr(),
                                        _rows("dq", dq), dk.data_ptr(), _rows("dk", dk), dv.data_ptr(), _rows("dv", dv), _addr(ws),
-                                       n, _stream(stream)))
+                                       n, _stream_on(stream, q.device)))
     return {"dq": dq, "dk": dk, "dv": dv, "ws": ws}
 
 
@@ -646,6 +660,7 @@ def _conv(x, off, weight, bias, T_max, silu, state, status):
         raise ValueError("x is [rows][channels], weight [channels][width]")
     C, W = x.shape[1], weight.shape[1]
     B = _offsets_ok(off, x.device)
+    _dtype(x)
     _f32(x.device, (C, W), weight=weight)
     _f32(x.device, (C,), bias=bias)
     _same(x, (B, W - 1, C), state=state)
@@ -654,9 +669,9 @@ def _conv(x, off, weight, bias, T_max, silu, state, status):
     _on_gpu(x)
     if status is not None:
         _status_ok(status, x.device)
-    return Conv(dtype=_dtype(x), B=B, T_max=T_max, channels=C, width=W, silu=1 if silu else 0, rows=x.shape[0], off=off.data_ptr(),
-                x=x.data_ptr(), ld_x=_rows("x", x), weight=weight.data_ptr(), bias=_addr(bias), state=_addr(state),
-                status=_addr(status))
+    # in the order of Conv's fields
+    return Conv(_dtype(x), B, T_max, C, W, 1 if silu else 0, x.shape[0], off.data_ptr(), x.data_ptr(), _rows("x", x),
+                weight.data_ptr(), _addr(bias), _addr(state), _addr(status))
 
 
 def causal_conv(x, off, weight, bias=None, *, T_max, silu=True, state=None, state_out=None, need_state=False, y=None,
@@ -675,7 +690,7 @@ def causal_conv(x, off, weight, bias=None, *, T_max, silu=True, state=None, stat
         state_out = torch.empty((a.B, a.width - 1, a.channels), dtype=x.dtype, device=x.device)
     _same(x, x.shape, y=y)
     _same(x, (a.B, a.width - 1, a.channels), state_out=state_out)
-    _check(load_library().wm_causal_conv(a, y.data_ptr(), _rows("y", y), _ptr(state_out), _stream(stream)))
+    _check(load_library().wm_causal_conv(a, y.data_ptr(), _rows("y", y), _ptr(state_out), _stream_on(stream, x.device)))
     return {"y": y, "state": state_out}
 
 
@@ -695,7 +710,7 @@ def causal_conv_grad(dy, x, off, weight, bias=None, *, T_max, silu=True, state=N
     lib = load_library()
     ws, n = _workspace(lib.wm_causal_conv_workspace_bytes(a), ws, dev)
     _check(lib.wm_causal_conv_grad(a, dy.data_ptr(), _rows("dy", dy), _ptr(d_state_out), dx.data_ptr(), _rows("dx", dx),
-                                   dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n, _stream(stream)))
+                                   dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n, _stream_on(stream, dev)))
     return {"dx": dx, "dweight": dw, "dbias": db, "dstate": ds, "ws": ws}
 
 
@@ -704,6 +719,7 @@ def _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status):
         raise ValueError("u is [rows][channels], A [channels][states], Bm and Cm [rows][states]")
     C, N = A.shape
     B = _offsets_ok(off, u.device)
+    _dtype(u)
     _same(u, (u.shape[0], C), u=u, delta=delta, z=z)
     _same(u, (u.shape[0], N), Bm=Bm, Cm=Cm)
     _f32(u.device, (C, N), A=A)
@@ -713,10 +729,9 @@ def _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status):
     _on_gpu(u)
     if status is not None:
         _status_ok(status, u.device)
-    return ScanArgs(dtype=_dtype(u), B=B, T_max=T_max, channels=C, states=N, rows=u.shape[0], off=off.data_ptr(), u=u.data_ptr(),
-                    delta=delta.data_ptr(), z=_addr(z), Bm=Bm.data_ptr(), Cm=Cm.data_ptr(), ld_u=lds[0], ld_delta=lds[1], ld_z=lds[2],
-                    ld_B=lds[3], ld_C=lds[4], A=A.data_ptr(), D=_addr(D), delta_bias=_addr(delta_bias), h0=_addr(h0),
-                    status=_addr(status))
+    # in the order of ScanArgs' fields
+    return ScanArgs(_dtype(u), B, T_max, C, N, u.shape[0], off.data_ptr(), u.data_ptr(), delta.data_ptr(), _addr(z), Bm.data_ptr(),
+                    Cm.data_ptr(), *lds, A.data_ptr(), _addr(D), _addr(delta_bias), _addr(h0), _addr(status))
 
 
 def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bias=None, h0=None, hT=None, need_state=False,
@@ -741,8 +756,8 @@ def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bia
     _f32(dev, (a.B, a.channels, a.states), hT=hT)
     if checkpoints is not None and checkpoints.numel() * checkpoints.element_size() < lib.wm_scan_checkpoint_bytes(a):
         raise ValueError("checkpoints is too small")
-    ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 0), ws, dev)
-    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _ptr(checkpoints), _addr(ws), n, _stream(stream)))
+    ws, n = (None, 0) if T_max <= 1 and ws is None else _workspace(lib.wm_scan_workspace_bytes(a, 0), ws, dev)
+    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _ptr(checkpoints), _addr(ws), n, _stream_on(stream, dev)))
     return {"y": y, "hT": hT, "checkpoints": checkpoints, "ws": ws}
 
 
@@ -769,7 +784,7 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
          "ddelta_bias": torch.empty(C, **f32), "dh0": torch.empty(shape, **f32) if need_dh0 else None}
     g = ScanGrads(ld_du=C, ld_ddelta=C, ld_dz=C, ld_dB=N, ld_dC=N, **{k: _addr(t) for k, t in r.items()})
     ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 1), ws, dev)
-    _check(lib.wm_scan_grad(a, _ptr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _stream(stream)))
+    _check(lib.wm_scan_grad(a, _ptr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _stream_on(stream, dev)))
     return {**r, "ws": ws}
 
 

@@ -1285,7 +1285,7 @@ wm_status wm_causal_conv_grad(const wm_conv* w, const void* dy, int64_t ld_dy, c
 
 size_t wm_scan_workspace_bytes(const wm_scan_args* w, int32_t grad) {
   ScanPlan p;
-  return check_scan(w, &p, grad != 0) == WM_OK ? std::max<size_t>(p.bytes, 256) : 0;
+  return check_scan(w, &p, grad != 0) == WM_OK ? std::max<size_t>(p.bytes, 256) : 0;      // 0: refused
 }
 
 size_t wm_scan_checkpoint_bytes(const wm_scan_args* w) {
