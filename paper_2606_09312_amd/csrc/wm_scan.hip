@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256) void carry_kernel(const ScanArgs a) {
   float h = start ? start[i] : 0.0f;
   float* x = a.carry + (int64_t)s * a.chunks * per + cn;
   const float* sd = a.sdt + (int64_t)s * a.chunks * a.D + c;
-  constexpr int U = 8;
+  constexpr int U = 16;
   for (int k0 = 0; k0 < used; k0 += U) {
     float e[U], f[U];
 #pragma unroll
@@ -1156,7 +1156,7 @@ wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
   p->chunk = std::max(1, a->T_max);
   p->chunks = 1;
   if (waves > 0 && waves < 1024 && a->T_max >= 128) {
-    const int64_t c = std::max<int64_t>(64, cdiv(cdiv((int64_t)a->T_max * waves, 4096), 32) * 32);
+    const int64_t c = std::max<int64_t>(32, cdiv(cdiv((int64_t)a->T_max * waves, 4096), 32) * 32);
     if (c < a->T_max) {
       p->chunk = (int)c;
       p->chunks = (int)cdiv(a->T_max, c);
