@@ -8,10 +8,10 @@ package is the thin Python binding over it.
 """
 from .binding import (  # noqa: F401
     GRAD_KEYS, KERNELS, NORMS, PRECISIONS, SYMBOLS, WMError, Forest, Model, TextModel,
-    causal_conv, causal_conv_grad, cross_attention, cross_attention_grad, device_status, encode_init, encode_text, evaluate, evaluate_noalloc, grad_shapes, load_library,
-    loss_workspace,
-    phi_struct, rollout, rollout_loss, score, score_trees,
-    selective_scan, selective_scan_grad, timing_enable, timing_read, topk,
+    causal_conv, causal_conv_grad, cross_attention, cross_attention_grad, device_status, encode_init,
+    encode_text, evaluate, evaluate_noalloc, grad_shapes, load_library, loss_workspace, phi_struct,
+    rollout, rollout_loss, score, score_trees, selective_scan, selective_scan_grad, timing_enable,
+    timing_read, topk,
 )
 
 

@@ -274,8 +274,14 @@ __device__ __forceinline__ void store_cols(T* row, const f32x16 (&acc)[DB], floa
 
 // --------------------------------------------------------------------------
 // Forward.  A workgroup of 4 wavefronts takes 128 / WK rows (32 per wavefront);
-// WK wavefronts share rows and take every WK-th block of 32 keys.  Tiles of K and V
-// are staged two deep by copies straight to LDS; softmax online.
+// WK wavefronts share rows and take every WK-th block of 32 keys (the form for at
+// most 32 rows per key head, where a wavefront of its own per 32 rows would leave three idle:
+// 16 streams of one query over 10k keys, 645 MB, 157 us, 4.1 TB/s, what a
+// large read reaches here).  Tiles of K and V are staged two deep by copies straight
+// to LDS; softmax online.  Long forms are bound by the vector unit, an
+// exponential (quarter rate) and 2.5 instructions per score, which is busy 64% of the
+// time at three wavefronts per SIMD: 32k rows on 256 to 2048 keys, 12 heads of 64
+// in bf16, 100 GFLOP, 142 us (709 TFLOP/s).
 template <class T, int DH, int WK>
 constexpr int FWD_PER_CU = 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 template <class T, int DH, int WK>
@@ -499,7 +505,9 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t row0, i
 // owns keys (dk, dv).
 
 // dq, and every row's (lse log2 e, delta) for the other kernel.  As the forward
-// kernel with 128 rows per workgroup.
+// kernel with 128 rows per workgroup: three products of which two are formed again,
+// against one that would have to pass dS through memory.  28k rows on 1024 to 2048 keys,
+// 12 heads of 64 in bf16, 161 GFLOP: 199 us.
 template <class T, int DH>
 __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
@@ -594,7 +602,10 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
 }
 
 // dk and dv of 128 keys (32 per wavefront, in registers as row operands); the
-// rows' q and do pass through LDS.
+// rows' q and do pass through LDS.  Matrix unit, vector unit and LDS each need about
+// the same time per block (512 cycles at a head width of 64), and two
+// wavefronts per SIMD overlap them in part: the same rows and keys, 214 GFLOP,
+// 328 us and 22 to add four splits' sums.
 template <class T, int DH>
 __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
