@@ -168,6 +168,28 @@ def test_attention_rows_past_32_bits(wm):
     close("lse", f["lse"], lse, TOL["f32"])
 
 
+@pytest.mark.parametrize("lq", [[3, 2], [150, 40]])
+def test_attention_outputs_into_wider_rows(wm, lq):
+    """Outputs that are slices of wider rows: the values of dense outputs, and nothing beside them is written;
+    the same with a workspace of the caller's that holds garbage."""
+    q, k, v, qo, ko, mask, do = make_attn("bf16", lq, [700, 90], 4, 2, 64, hidden=0.2, seed=12)
+    f = wm.cross_attention(q, k, v, qo, ko, kv_mask=mask, need_lse=True)
+    b = wm.cross_attention_grad(do, q, k, v, f["o"], f["lse"], qo, ko, kv_mask=mask)
+
+    def wide(t):
+        x = torch.full((t.shape[0], t.shape[1] + 2, t.shape[2]), 7.0, dtype=t.dtype, device="cuda")
+        return x, x[:, 1:-1]
+    (bo, o), (bq, dq), (bk, dk), (bv, dv) = (wide(t) for t in (q, q, k, v))
+    ws = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")       # NaN as float32
+    wm.cross_attention(q, k, v, qo, ko, kv_mask=mask, o=o, need_lse=True, ws=ws)
+    ws.fill_(255)
+    wm.cross_attention_grad(do, q, k, v, o, f["lse"], qo, ko, kv_mask=mask, dq=dq, dk=dk, dv=dv, ws=ws)
+    for got, want in ((o, f["o"]), (dq, b["dq"]), (dk, b["dk"]), (dv, b["dv"])):
+        assert torch.equal(got, want)
+    for whole in (bo, bq, bk, bv):
+        assert (whole[:, 0] == 7).all() and (whole[:, -1] == 7).all()
+
+
 def test_attention_gradient_against_differences(wm):
     """The float32 gradient against central differences of the float64 definition along random directions (the
     float32 forward cannot serve: the rounding of its 15,104 outputs, 3e-7 of 0.2 each, adds up to
@@ -298,6 +320,24 @@ def test_scan_many_sequences(wm):
 def test_scan_long_cut_into_chunks(wm):
     print("[scan] chunks", flush=True)
     check_scan(wm, "f32", [1000, 0, 131, 700], 65, 16, 33)
+
+
+def test_scan_garbage_workspace_and_odd_rows(wm):
+    """A caller's workspace and kept states that hold garbage, y in rows of odd stride: nothing else changes."""
+    a, opt, off, dy, dhT = make_scan("f32", [400, 3, 150], 37, 16, 38)
+    args = (a["u"], a["delta"], a["A"], a["Bm"], a["Cm"], off)
+    f = wm.selective_scan(*args, T_max=400, need_state=True, need_checkpoints=True, **opt)
+    g = wm.selective_scan_grad(dy, *args, f["checkpoints"], T_max=400, dhT=dhT, **opt)
+    ws = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+    kept = torch.full_like(f["checkpoints"], 255)
+    wide = torch.full((553, 41), 7.0, device="cuda")
+    r = wm.selective_scan(*args, T_max=400, need_state=True, checkpoints=kept, y=wide[:, 3:40], ws=ws, **opt)
+    assert torch.equal(r["y"], f["y"]) and torch.equal(r["hT"], f["hT"])
+    assert (wide[:, :3] == 7).all() and (wide[:, 40:] == 7).all()
+    ws.fill_(255)
+    b = wm.selective_scan_grad(dy, *args, kept, T_max=400, dhT=dhT, ws=ws, **opt)
+    for n in ("du", "ddelta", "dz", "dA", "dB", "dC", "dD", "ddelta_bias", "dh0"):
+        assert torch.equal(b[n], g[n]), n
 
 
 def test_scan_steps_equal_whole(wm):
