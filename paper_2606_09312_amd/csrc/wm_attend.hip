@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t row0, i
 // dq, and every row's (lse log2 e, delta) for the other kernel.  As the forward
 // kernel with 128 rows per workgroup: three products of which two are formed again,
 // against one that would have to pass dS through memory.  28k rows on 1024 to 2048 keys,
-// 12 heads of 64 in bf16, 161 GFLOP: 199 us.
+// 12 heads of 64 in bf16, 161 GFLOP: 193 us.
 template <class T, int DH>
 __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
 // rows' q and do pass through LDS.  Matrix unit, vector unit and LDS each need about
 // the same time per block (512 cycles at a head width of 64), and two
 // wavefronts per SIMD overlap them in part: the same rows and keys, 214 GFLOP,
-// 328 us and 22 to add four splits' sums.
+// 310 us (689 TFLOP/s) and 21 to add four splits' sums.
 template <class T, int DH>
 __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
@@ -740,7 +740,8 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // average (`longest` at most), are cut: the number of rounds that 256 x per_cu
 // places take times a split's length, plus what the partial sums cost (part_us a
 // split; a launch that joins them).  Every split keeps at least `least` steps.
-// One split of 520 workgroups on 512 places took 400 us (a second round of eight), four 290.
+// One split of 520 workgroups on 512 places took 400 us (a second round of eight), four
+// 310 and 21 for the sums.
 int splits_for(int64_t blocks, double units, int64_t longest, int64_t least, int per_cu, double unit_us, double part_us) {
   int best = 1;
   double cost = 1e30;
