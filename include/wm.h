@@ -426,7 +426,7 @@ typedef struct wm_attention {
 
 /* Bytes of workspace of the forward (grad = 0) or the gradient call (256-byte
  * aligned, need not be cleared); 0 on a bad argument, 256 where none is needed
- * (NULL may be passed then). */
+ * (NULL may be passed then), more than 256 where one is. */
 size_t wm_cross_attention_workspace_bytes(const wm_attention* a, int32_t grad);
 
 /* o [rows][heads][head_dim] out; lse [rows][heads] float32 out (may be NULL). */
@@ -468,7 +468,8 @@ typedef struct wm_conv {
  * be; may be NULL. */
 wm_status wm_causal_conv(const wm_conv* a, void* y, int64_t ld_y, void* state_out, void* stream);
 
-/* Workspace bytes of wm_causal_conv_grad (0 on a bad argument). */
+/* Workspace bytes of wm_causal_conv_grad (0 on a bad argument, else more than 256: it
+ * always needs one). */
 size_t wm_causal_conv_workspace_bytes(const wm_conv* a);
 
 /* Gradients given dy and, if not NULL, d_state_out = dL/d(state_out): dx, dweight

@@ -562,7 +562,7 @@ def _addr(t):
 
 
 def _workspace(n, given, dev):
-    """The workspace and its bytes; the least size that the library answers, 256, means that it needs none."""
+    """The workspace and its bytes; the library answers 256 where it needs none, more where it does."""
     import torch
     if given is not None:
         return given, given.numel() * given.element_size()

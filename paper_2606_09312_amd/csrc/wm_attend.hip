@@ -845,7 +845,7 @@ wm_status check(const wm_attention* a, Plan* p, bool grad) {
     if (p->dkv_splits > 1) part = std::max(part, (size_t)p->dkv_splits * 2 * kv * a->head_dim * 4);
     if (part) p->o_part = take(part);
   }
-  p->bytes = at;
+  p->bytes = workspace_of(at);
   return WM_OK;
 }
 
@@ -963,7 +963,7 @@ extern "C" {
 
 size_t wm_cross_attention_workspace_bytes(const wm_attention* a, int32_t grad) {
   Plan p;
-  return check(a, &p, grad != 0) == WM_OK ? std::max<size_t>(p.bytes, 256) : 0;
+  return check(a, &p, grad != 0) == WM_OK ? std::max(p.bytes, NO_WORKSPACE) : 0;
 }
 
 wm_status wm_cross_attention(const wm_attention* w, void* o, int64_t ld_o, float* lse, void* ws, size_t ws_bytes,

@@ -110,6 +110,11 @@ enum TimedKernel { TK_ROLLOUT = 0, TK_SCORE = 1, TK_TOPK = 2, TK_BUCKET = 3, TK_
 void timing_begin(int kernel, hipStream_t st);
 void timing_end(int kernel, hipStream_t st);
 
+// Workspaces of the sequence operators.  Their size queries answer 256 where none is needed (0 is a
+// refusal), so one that is needed has more, however few of its bytes are used.
+constexpr size_t NO_WORKSPACE = 256;
+inline size_t workspace_of(size_t bytes) { return bytes > 0 && bytes <= NO_WORKSPACE ? 2 * NO_WORKSPACE : bytes; }
+
 // Thread-local last-error message of the C ABI (wm_api.hip).
 wm_status set_error(wm_status st, const std::string& msg);
 wm_status clear_error();

@@ -1104,7 +1104,7 @@ wm_status check_conv(const wm_conv* a, ConvPlan* p) {
   // groups of the gradient: about eight wavefronts per SIMD when vectors can be used
   const int64_t cg = a->channels % 4 == 0 ? a->channels / 4 : a->channels;
   p->groups = (int)std::max<int64_t>(1, std::min<int64_t>(items, cdiv(256 * 4 * 4 * 64, cg)));
-  p->bytes = al256((size_t)p->groups * (a->width + 1) * a->channels * 4);
+  p->bytes = workspace_of(al256((size_t)p->groups * (a->width + 1) * a->channels * 4));
   return WM_OK;
 }
 // whether V-wide accesses of rows are aligned
@@ -1187,7 +1187,7 @@ wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
     p->o_pbc = take((size_t)p->gblocks * a->rows * 2 * N * 4);
     p->o_pad = take((size_t)p->groups * a->channels * (N + 2) * 4);
   }
-  p->bytes = at;
+  p->bytes = workspace_of(at);
   return WM_OK;
 }
 
@@ -1295,7 +1295,7 @@ wm_status wm_causal_conv_grad(const wm_conv* w, const void* dy, int64_t ld_dy, c
 
 size_t wm_scan_workspace_bytes(const wm_scan_args* w, int32_t grad) {
   ScanPlan p;
-  return check_scan(w, &p, grad != 0) == WM_OK ? std::max<size_t>(p.bytes, 256) : 0;      // 0: refused
+  return check_scan(w, &p, grad != 0) == WM_OK ? std::max(p.bytes, NO_WORKSPACE) : 0;
 }
 
 size_t wm_scan_checkpoint_bytes(const wm_scan_args* w) {
