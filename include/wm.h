@@ -443,10 +443,11 @@ wm_status wm_cross_attention_grad(const wm_attention* a, const void* o, int64_t 
 
 /* Rows of the convolution and the scan: sequence s of B has the rows off[s] ..
  * off[s+1] (device int32 [B+1], off[0] = 0, off[B] = rows), at most T_max of them
- * (one each for a single step).  Offsets that are not so are clamped, and reported
+ * (one each for a single step; no sequences, no rows).  Offsets that are not so, also
+ * those that leave rows out at either end, are clamped and reported
  * in `status` (device int32 [64], zeroed once by the caller; may be NULL): read and
  * clear it with wm_device_status(status, 256, stream).  Outputs are then
- * unspecified, as are those of rows in no sequence.
+ * unspecified.
  *
  * Causal convolution of `width` taps (2, 3 or 4) per channel:
  *   y_t[c] = act(bias[c] + sum_j weight[c][j] x_{t - width + 1 + j}[c])

@@ -682,6 +682,7 @@ wm_status wm_device_status(void* ws, size_t ws_bytes, void* stream) {
   if (word & ERRBIT_TYPE) msg += " an action type outside [0, n_kinds);";
   if (word & ERRBIT_PARAM) msg += " an action parameter < 1;";
   if (word & ERRBIT_TOKEN) msg += " a token id outside [0, vocab);";
+  if (word & ERRBIT_ROWS) msg += " offsets that do not run from 0 to the rows;";
   return fail(WM_ERR_INPUT_RANGE, msg);
 }
 

@@ -250,7 +250,7 @@ inline size_t bucket_words(int B, int T_max) {
 }
 
 // Device error bits (workspace error word).
-enum : int { ERRBIT_LEN = 1, ERRBIT_TYPE = 2, ERRBIT_PARAM = 4, ERRBIT_TOKEN = 8 };
+enum : int { ERRBIT_LEN = 1, ERRBIT_TYPE = 2, ERRBIT_PARAM = 4, ERRBIT_TOKEN = 8, ERRBIT_ROWS = 16 };
 
 struct SegTable {
   int32_t n;                              // S

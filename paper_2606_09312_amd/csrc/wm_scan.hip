@@ -2,7 +2,8 @@
 // selective state-space scan, forward, gradients and single steps.
 //
 // Sequence s has rows [off[s], off[s+1]) (device offsets; a length past T_max
-// or offsets outside the rows set the error word and are clamped).  Every sum
+// or offsets outside the rows set the error word and are clamped; offsets that
+// leave rows out at either end set it too).  Every sum
 // over rows, sequences or channels is in a fixed order.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -48,18 +49,22 @@ __device__ __forceinline__ float log1p_unit(float e) {
 // softplus(x) = max(x, 0) + log(1 + exp(-|x|))
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1p_unit(exp2_of(-fabsf(x) * LOG2E)); }
 
-// Rows of a sequence, clamped to what exists.
+// Rows of a sequence, clamped to what exists (`report`: what does not fit sets the error word).
 struct Span {
   int64_t r0;
   int len;
 };
-__device__ __forceinline__ Span span_of(const int32_t* off, int s, int64_t rows, int T_max, int32_t* status, bool report) {
+template <class Args>
+__device__ __forceinline__ Span span_of(const Args& g, int s, bool report) {
   // constant while a kernel runs: scalar loads where s is uniform, which no vector load waits for
-  const __attribute__((address_space(4))) int32_t* o = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)off;
+  const __attribute__((address_space(4))) int32_t* o = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)g.off;
   const int64_t a = o[s], b = o[s + 1];
-  const int64_t lo = a < 0 ? 0 : a > rows ? rows : a, hi = b < lo ? lo : b > rows ? rows : b;
-  const int64_t n = hi - lo > T_max ? T_max : hi - lo;
-  if (report && status && (lo != a || n != b - a)) atomicOr(status, ERRBIT_LEN);
+  const int64_t lo = a < 0 ? 0 : a > g.rows ? g.rows : a, hi = b < lo ? lo : b > g.rows ? g.rows : b;
+  const int64_t n = hi - lo > g.T_max ? g.T_max : hi - lo;
+  if (report && g.status) {
+    if (lo != a || n != b - a) atomicOr(g.status, ERRBIT_LEN);
+    if ((s == 0 && a != 0) || (s == g.B - 1 && b != g.rows)) atomicOr(g.status, ERRBIT_ROWS);
+  }
   return {lo, (int)n};
 }
 
@@ -164,7 +169,7 @@ __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a) {
   int c;
   if (!conv_slot<V>(a, (uint32_t)a.B * a.runs, item, c)) return;
   const int s = item / (uint32_t)a.runs, run = item - s * a.runs;
-  const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, c == 0 && run == 0);
+  const Span sp = span_of(a, s, c == 0 && run == 0);
   const int t0 = run * RUN, t1 = min(t0 + RUN, sp.len);
   if (t0 < t1) {
     const T* xp = static_cast<const T*>(a.x) + sp.r0 * a.ld_x + c;
@@ -234,7 +239,7 @@ __global__ __launch_bounds__(256) void conv_grad_kernel(const ConvArgs a) {
   };
   for (uint32_t item = group; item < (uint32_t)a.B * a.runs; item += a.groups) {
     const int s = item / (uint32_t)a.runs, run = item - s * a.runs;
-    const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, c == 0 && run == 0);
+    const Span sp = span_of(a, s, c == 0 && run == 0);
     const int t0 = run * RUN, t1 = min(t0 + RUN, sp.len);
     // the gradient of the carried-out state reaches the last W - 1 inputs (and, in a
     // sequence shorter than that, the carried-in state)
@@ -443,7 +448,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a) {
   const uint32_t id = blockIdx.x * 4 + wave, item = id / (uint32_t)a.cblocks;
   if (item >= (uint32_t)a.B * (uint32_t)a.chunks) return;
   const int cb = (int)(id - item * a.cblocks), s = (int)(item / (uint32_t)a.chunks), ch = (int)(item - (uint32_t)s * a.chunks);
-  const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, !LOCAL && cb == 0 && ch == 0 && lane == 0);
+  const Span sp = span_of(a, s, !LOCAL && cb == 0 && ch == 0 && lane == 0);
   const int t0 = ch * a.chunk, t1 = min(t0 + a.chunk, sp.len);
   if (t0 >= t1 && ch > 0) return;
   const int c = cb * 64 + lane, cc = min(c, a.D - 1);
@@ -546,7 +551,7 @@ __global__ __launch_bounds__(256) void carry_kernel(const ScanArgs a) {
   if (i >= a.B * per) return;
   const int s = (int)(i / per);
   const int64_t cn = i - s * per, c = cn / N;
-  const Span sp = span_of(a.off, s, a.rows, a.T_max, nullptr, false);
+  const Span sp = span_of(a, s, false);
   const int used = (sp.len + a.chunk - 1) / a.chunk;
   const float A2 = a.A[cn] * LOG2E;
   const float* start = REV ? a.dhT : a.h0;
@@ -582,7 +587,7 @@ __global__ __launch_bounds__(256) void step_kernel(const ScanArgs a) {
   typedef Vec<float, V> FV;
   const uint32_t s = blockIdx.x / (uint32_t)a.cblocks, cb = blockIdx.x - s * a.cblocks;
   const int q = threadIdx.x & 3, c = cb * 64 + (threadIdx.x >> 2);
-  const Span sp = span_of(a.off, s, a.rows, a.T_max, a.status, cb == 0 && threadIdx.x == 0);
+  const Span sp = span_of(a, s, cb == 0 && threadIdx.x == 0);
   if (c >= a.D) return;                      // whole quads
   FV h[L / V], A[L / V];
   const int64_t at = ((int64_t)s * a.D + c) * N + q * L;
@@ -679,7 +684,7 @@ __global__ __launch_bounds__(256) void grad_local_kernel(const ScanArgs a) {
   const uint32_t id = blockIdx.x * 4 + wave, item = id / (uint32_t)a.cblocks;
   if (item >= (uint32_t)a.B * (uint32_t)a.chunks) return;
   const int cb = (int)(id - item * a.cblocks), s = (int)(item / (uint32_t)a.chunks), ch = (int)(item - (uint32_t)s * a.chunks);
-  const Span sp = span_of(a.off, s, a.rows, a.T_max, nullptr, false);
+  const Span sp = span_of(a, s, false);
   const int t0 = ch * a.chunk, t1 = min(t0 + a.chunk, sp.len), steps = t1 - t0;
   if (steps <= 0) return;
   const int c = cb * 64 + lane, cc = min(c, a.D - 1);
@@ -808,7 +813,7 @@ __global__ __launch_bounds__(64 * GW, 2) void grad_kernel(const ScanArgs a) {
     for (k.item = item; k.item < items; k.item += a.groups) {
       k.s = a.chunks > 1 ? k.item / a.chunks : k.item;
       const int ch = k.item - k.s * a.chunks;
-      const Span sp = span_of(a.off, k.s, a.rows, a.T_max, a.status, cb == 0 && ch == 0 && tid == 0);
+      const Span sp = span_of(a, k.s, cb == 0 && ch == 0 && tid == 0);
       k.r0 = sp.r0;
       k.first = ch == 0;
       k.t0 = ch * a.chunk;
@@ -1082,6 +1087,7 @@ wm_status check_rows(int32_t dtype, int32_t B, int32_t T_max, int64_t rows, int3
   if (B < 0 || T_max < 0 || rows < 0 || rows > INT32_MAX) return bad("B, T_max and rows must be non-negative, rows below 2^31");
   if (channels < 1 || channels > (1 << 20)) return bad("channels must be in [1, 2^20]");
   if (B > 0 && !off) return bad("off is NULL");
+  if (B == 0 && rows > 0) return bad("rows without a sequence");
   return WM_OK;
 }
 // row strides up to 2^24 elements: the kernels take rows of a block by 32-bit offsets

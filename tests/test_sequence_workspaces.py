@@ -51,3 +51,11 @@ def test_none_needed():
     lib = wm.load_library()
     assert lib.wm_cross_attention_workspace_bytes(attention(), 0) == 256 == lib.wm_scan_workspace_bytes(scan(), 0)
     assert B._workspace(256, None, "cpu") == (None, 0)
+
+
+def test_rows_without_a_sequence_are_refused():
+    lib = wm.load_library()
+    assert lib.wm_causal_conv_workspace_bytes(conv(B=0, rows=8)) == 0 == lib.wm_scan_workspace_bytes(scan(B=0, rows=8), 1)
+    assert lib.wm_scan(scan(B=0, rows=8), FAKE, 16, None, None, None, 0, None) == BAD
+    assert lib.wm_causal_conv(conv(B=0, rows=8), FAKE, 16, None, None) == BAD
+    assert lib.wm_causal_conv_workspace_bytes(conv(B=0, rows=0)) > 0 and lib.wm_scan_workspace_bytes(scan(B=0, rows=0), 1) > 0
