@@ -7,6 +7,8 @@ torch's current stream unless one is given.  A missing library raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 from typing import Dict, Optional
 
@@ -569,9 +571,38 @@ def _workspace(n, given, dev):
     return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n > 256 else (None, 0)
 
 
-def _stream_on(stream, dev):
+def _current_stream(dev):
     import torch
-    return (torch.cuda.current_stream(dev.index) if stream is None else stream).cuda_stream
+    return torch.cuda.current_stream(dev.index).cuda_stream
+
+
+def _on_stream(fn):
+    """Gives fn, which allocates and launches on the current stream, the keyword `stream`.
+
+    The call then runs with that stream current, so that what it allocates (workspaces that are
+    dropped on return above all) belongs to the stream's pool and is reused in the stream's order only.
+    Results are kept from that reuse while the caller's stream uses them, and the caller's tensors
+    from their own pool's while `stream` does.
+    """
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        import torch
+        here = torch.cuda.current_stream(stream.device)
+        if stream == here:
+            return fn(*args, **kw)
+        with torch.cuda.stream(stream):
+            r = fn(*args, **kw)
+        for on, values in ((stream, (*args, *kw.values())), (here, r.values())):
+            for t in values:
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(on)
+        return r
+    sig = inspect.signature(fn)
+    call.__signature__ = sig.replace(parameters=[*sig.parameters.values(),
+                                                 inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
+    return call
 
 
 def _attention(q, k, v, q_off, k_off, kv_mask, scale):
@@ -600,8 +631,8 @@ def _attention(q, k, v, q_off, k_off, kv_mask, scale):
     return a
 
 
-def cross_attention(q, k, v, q_off, k_off, *, kv_mask=None, scale=None, o=None, lse=None, need_lse=False, ws=None,
-                    stream=None):
+@_on_stream
+def cross_attention(q, k, v, q_off, k_off, *, kv_mask=None, scale=None, o=None, lse=None, need_lse=False, ws=None):
     """Cross attention of query rows to the key rows of their segment (wm_cross_attention).
 
     q [rows][heads][head_dim], k and v [rows][kv_heads][head_dim], float32 or bfloat16; row strides may
@@ -619,12 +650,12 @@ def cross_attention(q, k, v, q_off, k_off, *, kv_mask=None, scale=None, o=None, 
     _f32(q.device, q.shape[:2], lse=lse)
     lib = load_library()
     ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 0), ws, q.device)
-    _check(lib.wm_cross_attention(a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n, _stream_on(stream, q.device)))
+    _check(lib.wm_cross_attention(a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n, _current_stream(q.device)))
     return {"o": o, "lse": lse, "ws": ws}
 
 
-def cross_attention_grad(do, q, k, v, o, lse, q_off, k_off, *, kv_mask=None, scale=None, dq=None, dk=None, dv=None, ws=None,
-                         stream=None):
+@_on_stream
+def cross_attention_grad(do, q, k, v, o, lse, q_off, k_off, *, kv_mask=None, scale=None, dq=None, dk=None, dv=None, ws=None):
     """Gradients dq, dk, dv of cross_attention given do = dL/do (wm_cross_attention_grad)."""
     import torch
     a = _attention(q, k, v, q_off, k_off, kv_mask, scale)
@@ -638,7 +669,7 @@ def cross_attention_grad(do, q, k, v, o, lse, q_off, k_off, *, kv_mask=None, sca
     ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 1), ws, q.device)
     _check(lib.wm_cross_attention_grad(a, o.data_ptr(), _rows("o", o), _addr(lse), do.data_ptr(), _rows("do", do), dq.data_ptr(),
                                        _rows("dq", dq), dk.data_ptr(), _rows("dk", dk), dv.data_ptr(), _rows("dv", dv), _addr(ws),
-                                       n, _stream_on(stream, q.device)))
+                                       n, _current_stream(q.device)))
     return {"dq": dq, "dk": dk, "dv": dv, "ws": ws}
 
 
@@ -674,8 +705,9 @@ def _conv(x, off, weight, bias, T_max, silu, state, status):
                 weight.data_ptr(), _addr(bias), _addr(state), _addr(status))
 
 
+@_on_stream
 def causal_conv(x, off, weight, bias=None, *, T_max, silu=True, state=None, state_out=None, need_state=False, y=None,
-                status=None, stream=None):
+                status=None):
     """Causal convolution along packed ragged sequences (wm_causal_conv).
 
     x [rows][channels] float32 or bfloat16, off device int32 [B + 1], T_max: the longest sequence's
@@ -690,12 +722,13 @@ def causal_conv(x, off, weight, bias=None, *, T_max, silu=True, state=None, stat
         state_out = torch.empty((a.B, a.width - 1, a.channels), dtype=x.dtype, device=x.device)
     _same(x, x.shape, y=y)
     _same(x, (a.B, a.width - 1, a.channels), state_out=state_out)
-    _check(load_library().wm_causal_conv(a, y.data_ptr(), _rows("y", y), _ptr(state_out), _stream_on(stream, x.device)))
+    _check(load_library().wm_causal_conv(a, y.data_ptr(), _rows("y", y), _ptr(state_out), _current_stream(x.device)))
     return {"y": y, "state": state_out}
 
 
+@_on_stream
 def causal_conv_grad(dy, x, off, weight, bias=None, *, T_max, silu=True, state=None, d_state_out=None, need_dstate=False,
-                     status=None, ws=None, stream=None):
+                     status=None, ws=None):
     """Gradients dx, dweight, dbias and (with need_dstate) dstate of causal_conv (wm_causal_conv_grad)."""
     import torch
     a = _conv(x, off, weight, bias, T_max, silu, state, status)
@@ -710,7 +743,7 @@ def causal_conv_grad(dy, x, off, weight, bias=None, *, T_max, silu=True, state=N
     lib = load_library()
     ws, n = _workspace(lib.wm_causal_conv_workspace_bytes(a), ws, dev)
     _check(lib.wm_causal_conv_grad(a, dy.data_ptr(), _rows("dy", dy), _ptr(d_state_out), dx.data_ptr(), _rows("dx", dx),
-                                   dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n, _stream_on(stream, dev)))
+                                   dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n, _current_stream(dev)))
     return {"dx": dx, "dweight": dw, "dbias": db, "dstate": ds, "ws": ws}
 
 
@@ -734,8 +767,9 @@ def _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status):
                     Cm.data_ptr(), *lds, A.data_ptr(), _addr(D), _addr(delta_bias), _addr(h0), _addr(status))
 
 
+@_on_stream
 def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bias=None, h0=None, hT=None, need_state=False,
-                   need_checkpoints=False, checkpoints=None, y=None, status=None, ws=None, stream=None):
+                   need_checkpoints=False, checkpoints=None, y=None, status=None, ws=None):
     """Selective state-space scan along packed ragged sequences (wm_scan); T_max = 1 is one step.
 
     u, delta, z [rows][channels], Bm, Cm [rows][states], float32 or bfloat16; A [channels][states], D and
@@ -757,12 +791,13 @@ def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bia
     if checkpoints is not None and checkpoints.numel() * checkpoints.element_size() < lib.wm_scan_checkpoint_bytes(a):
         raise ValueError("checkpoints is too small")
     ws, n = (None, 0) if T_max <= 1 and ws is None else _workspace(lib.wm_scan_workspace_bytes(a, 0), ws, dev)
-    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _ptr(checkpoints), _addr(ws), n, _stream_on(stream, dev)))
+    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _ptr(checkpoints), _addr(ws), n, _current_stream(dev)))
     return {"y": y, "hT": hT, "checkpoints": checkpoints, "ws": ws}
 
 
+@_on_stream
 def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=None, z=None, delta_bias=None, h0=None, dhT=None,
-                        need_dh0=None, status=None, ws=None, stream=None):
+                        need_dh0=None, status=None, ws=None):
     """Gradients of selective_scan (wm_scan_grad): du, ddelta, dA, dB, dC, dD, ddelta_bias, dz (with z) and dh0
     (with h0, or need_dh0), given dy, the forward call's checkpoints and dhT (None = 0)."""
     import torch
@@ -784,7 +819,7 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
          "ddelta_bias": torch.empty(C, **f32), "dh0": torch.empty(shape, **f32) if need_dh0 else None}
     g = ScanGrads(ld_du=C, ld_ddelta=C, ld_dz=C, ld_dB=N, ld_dC=N, **{k: _addr(t) for k, t in r.items()})
     ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 1), ws, dev)
-    _check(lib.wm_scan_grad(a, _ptr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _stream_on(stream, dev)))
+    _check(lib.wm_scan_grad(a, _ptr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _current_stream(dev)))
     return {**r, "ws": ws}
 
 
