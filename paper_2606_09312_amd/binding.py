@@ -563,11 +563,18 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
+def _given(name, t, dev):
+    """Bytes of a caller's workspace or kept states."""
+    if t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be dense on {dev}")
+    return t.numel() * t.element_size()
+
+
 def _workspace(n, given, dev):
     """The workspace and its bytes; the library answers 256 where it needs none, more where it does."""
     import torch
     if given is not None:
-        return given, given.numel() * given.element_size()
+        return given, _given("ws", given, dev)
     return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n > 256 else (None, 0)
 
 
@@ -788,10 +795,10 @@ def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bia
         checkpoints = torch.empty(lib.wm_scan_checkpoint_bytes(a), dtype=torch.uint8, device=dev)
     _same(u, u.shape, y=y)
     _f32(dev, (a.B, a.channels, a.states), hT=hT)
-    if checkpoints is not None and checkpoints.numel() * checkpoints.element_size() < lib.wm_scan_checkpoint_bytes(a):
+    if checkpoints is not None and _given("checkpoints", checkpoints, dev) < lib.wm_scan_checkpoint_bytes(a):
         raise ValueError("checkpoints is too small")
     ws, n = (None, 0) if T_max <= 1 and ws is None else _workspace(lib.wm_scan_workspace_bytes(a, 0), ws, dev)
-    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _ptr(checkpoints), _addr(ws), n, _current_stream(dev)))
+    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _addr(checkpoints), _addr(ws), n, _current_stream(dev)))
     return {"y": y, "hT": hT, "checkpoints": checkpoints, "ws": ws}
 
 
@@ -808,7 +815,7 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
     _f32(dev, shape, dhT=dhT)
     need_dh0 = h0 is not None if need_dh0 is None else need_dh0
     lib = load_library()
-    if checkpoints is None or checkpoints.numel() * checkpoints.element_size() < lib.wm_scan_checkpoint_bytes(a):
+    if checkpoints is None or _given("checkpoints", checkpoints, dev) < lib.wm_scan_checkpoint_bytes(a):
         raise ValueError("checkpoints is missing or too small")
     like = dict(dtype=u.dtype, device=dev)
     f32 = dict(dtype=torch.float32, device=dev)
@@ -819,7 +826,7 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
          "ddelta_bias": torch.empty(C, **f32), "dh0": torch.empty(shape, **f32) if need_dh0 else None}
     g = ScanGrads(ld_du=C, ld_ddelta=C, ld_dz=C, ld_dB=N, ld_dC=N, **{k: _addr(t) for k, t in r.items()})
     ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 1), ws, dev)
-    _check(lib.wm_scan_grad(a, _ptr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _current_stream(dev)))
+    _check(lib.wm_scan_grad(a, _addr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _current_stream(dev)))
     return {**r, "ws": ws}
 
 

@@ -1,0 +1,32 @@
+"""What the binding of the sequence operators asks of a workspace and of kept states that the caller passes: device
+memory beside the tensors, dense; and of a stream: the tensors' device (no GPU needed)."""
+import pytest
+
+import paper_2606_09312_amd as wm
+from test_sequence_streams import Library, Stream, all_calls, torch, world  # noqa: F401
+
+WITH_WS = [n for n in all_calls() if n != "causal_conv"]
+META = torch.device("meta")
+
+
+@pytest.mark.parametrize("name", WITH_WS)
+@pytest.mark.parametrize("ws", [torch.zeros(8192, dtype=torch.uint8, device=META),       # another device than the tensors'
+                                torch.zeros(8192, 2, dtype=torch.uint8)[:, 0]], ids=["device", "strided"])
+def test_workspace(world, name, ws):  # noqa: F811
+    args, kw = all_calls()[name]
+    with pytest.raises(ValueError, match="ws must be dense"):
+        getattr(wm, name)(*args, ws=ws, **kw)
+    assert not [c for c in world.lib.calls if not c[0].endswith("_bytes")]
+    getattr(wm, name)(*args, ws=torch.zeros(8192, dtype=torch.uint8), **kw)
+
+
+@pytest.mark.parametrize("kept", [torch.zeros(8192, dtype=torch.uint8, device=META),
+                                  torch.zeros(8192, 2, dtype=torch.uint8)[:, 0], torch.zeros(4095, dtype=torch.uint8)],
+                         ids=["device", "strided", "short"])
+def test_checkpoints(world, kept):  # noqa: F811
+    (x, _, A, b, _, off), _ = all_calls()["selective_scan"]
+    with pytest.raises(ValueError, match="checkpoints"):
+        wm.selective_scan(x, x, A, b, b, off, T_max=4, checkpoints=kept)
+    with pytest.raises(ValueError, match="checkpoints"):
+        wm.selective_scan_grad(x, x, x, A, b, b, off, kept, T_max=4)
+    assert not [c for c in world.lib.calls if not c[0].endswith("_bytes")]
