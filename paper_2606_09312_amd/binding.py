@@ -578,9 +578,15 @@ def _workspace(n, given, dev):
     return (torch.empty(n, dtype=torch.uint8, device=dev), n) if n > 256 else (None, 0)
 
 
-def _current_stream(dev):
+def _launch(fn, dev, *args):
+    """A library call on the current stream of dev, which is the current device meanwhile."""
     import torch
-    return torch.cuda.current_stream(dev.index).cuda_stream
+    stream = torch.cuda.current_stream(dev.index).cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(*args, stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, stream))
 
 
 def _on_stream(fn):
@@ -597,14 +603,18 @@ def _on_stream(fn):
             return fn(*args, **kw)
         import torch
         here = torch.cuda.current_stream(stream.device)
+        given = [t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor) and t.is_cuda]
+        if any(t.device != stream.device for t in given):
+            raise ValueError(f"stream is on {stream.device}, tensors are not")
         if stream == here:
             return fn(*args, **kw)
         with torch.cuda.stream(stream):
             r = fn(*args, **kw)
-        for on, values in ((stream, (*args, *kw.values())), (here, r.values())):
-            for t in values:
-                if isinstance(t, torch.Tensor) and t.is_cuda:
-                    t.record_stream(on)
+        for t in given:
+            t.record_stream(stream)
+        for t in r.values():
+            if t is not None:
+                t.record_stream(here)
         return r
     sig = inspect.signature(fn)
     call.__signature__ = sig.replace(parameters=[*sig.parameters.values(),
@@ -657,7 +667,7 @@ def cross_attention(q, k, v, q_off, k_off, *, kv_mask=None, scale=None, o=None, 
     _f32(q.device, q.shape[:2], lse=lse)
     lib = load_library()
     ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 0), ws, q.device)
-    _check(lib.wm_cross_attention(a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n, _current_stream(q.device)))
+    _launch(lib.wm_cross_attention, q.device, a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n)
     return {"o": o, "lse": lse, "ws": ws}
 
 
@@ -674,9 +684,8 @@ def cross_attention_grad(do, q, k, v, o, lse, q_off, k_off, *, kv_mask=None, sca
     _f32(q.device, q.shape[:2], lse=lse)
     lib = load_library()
     ws, n = _workspace(lib.wm_cross_attention_workspace_bytes(a, 1), ws, q.device)
-    _check(lib.wm_cross_attention_grad(a, o.data_ptr(), _rows("o", o), _addr(lse), do.data_ptr(), _rows("do", do), dq.data_ptr(),
-                                       _rows("dq", dq), dk.data_ptr(), _rows("dk", dk), dv.data_ptr(), _rows("dv", dv), _addr(ws),
-                                       n, _current_stream(q.device)))
+    _launch(lib.wm_cross_attention_grad, q.device, a, o.data_ptr(), _rows("o", o), _addr(lse), do.data_ptr(), _rows("do", do),
+            dq.data_ptr(), _rows("dq", dq), dk.data_ptr(), _rows("dk", dk), dv.data_ptr(), _rows("dv", dv), _addr(ws), n)
     return {"dq": dq, "dk": dk, "dv": dv, "ws": ws}
 
 
@@ -729,7 +738,7 @@ def causal_conv(x, off, weight, bias=None, *, T_max, silu=True, state=None, stat
         state_out = torch.empty((a.B, a.width - 1, a.channels), dtype=x.dtype, device=x.device)
     _same(x, x.shape, y=y)
     _same(x, (a.B, a.width - 1, a.channels), state_out=state_out)
-    _check(load_library().wm_causal_conv(a, y.data_ptr(), _rows("y", y), _ptr(state_out), _current_stream(x.device)))
+    _launch(load_library().wm_causal_conv, x.device, a, y.data_ptr(), _rows("y", y), _ptr(state_out))
     return {"y": y, "state": state_out}
 
 
@@ -749,8 +758,8 @@ def causal_conv_grad(dy, x, off, weight, bias=None, *, T_max, silu=True, state=N
     ds = torch.empty(shape, dtype=x.dtype, device=dev) if need_dstate else None
     lib = load_library()
     ws, n = _workspace(lib.wm_causal_conv_workspace_bytes(a), ws, dev)
-    _check(lib.wm_causal_conv_grad(a, dy.data_ptr(), _rows("dy", dy), _ptr(d_state_out), dx.data_ptr(), _rows("dx", dx),
-                                   dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n, _current_stream(dev)))
+    _launch(lib.wm_causal_conv_grad, dev, a, dy.data_ptr(), _rows("dy", dy), _ptr(d_state_out), dx.data_ptr(), _rows("dx", dx),
+            dw.data_ptr(), db.data_ptr(), _addr(ds), _addr(ws), n)
     return {"dx": dx, "dweight": dw, "dbias": db, "dstate": ds, "ws": ws}
 
 
@@ -798,7 +807,7 @@ def selective_scan(u, delta, A, Bm, Cm, off, *, T_max, D=None, z=None, delta_bia
     if checkpoints is not None and _given("checkpoints", checkpoints, dev) < lib.wm_scan_checkpoint_bytes(a):
         raise ValueError("checkpoints is too small")
     ws, n = (None, 0) if T_max <= 1 and ws is None else _workspace(lib.wm_scan_workspace_bytes(a, 0), ws, dev)
-    _check(lib.wm_scan(a, y.data_ptr(), _rows("y", y), _addr(hT), _addr(checkpoints), _addr(ws), n, _current_stream(dev)))
+    _launch(lib.wm_scan, dev, a, y.data_ptr(), _rows("y", y), _addr(hT), _addr(checkpoints), _addr(ws), n)
     return {"y": y, "hT": hT, "checkpoints": checkpoints, "ws": ws}
 
 
@@ -826,7 +835,7 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
          "ddelta_bias": torch.empty(C, **f32), "dh0": torch.empty(shape, **f32) if need_dh0 else None}
     g = ScanGrads(ld_du=C, ld_ddelta=C, ld_dz=C, ld_dB=N, ld_dC=N, **{k: _addr(t) for k, t in r.items()})
     ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 1), ws, dev)
-    _check(lib.wm_scan_grad(a, _addr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n, _current_stream(dev)))
+    _launch(lib.wm_scan_grad, dev, a, _addr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n)
     return {**r, "ws": ws}
 
 

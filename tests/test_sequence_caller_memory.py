@@ -30,3 +30,35 @@ def test_checkpoints(world, kept):  # noqa: F811
     with pytest.raises(ValueError, match="checkpoints"):
         wm.selective_scan_grad(x, x, x, A, b, b, off, kept, T_max=4)
     assert not [c for c in world.lib.calls if not c[0].endswith("_bytes")]
+
+
+@pytest.mark.parametrize("name", list(all_calls()))
+def test_tensors_on_another_device_than_the_current_one(world, monkeypatch, name):  # noqa: F811
+    """The tensors' device is current for the launch, and only for it."""
+    current = []
+
+    class Device:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.was, world.device = world.device, self.dev.index
+
+        def __exit__(self, *_):
+            world.device = self.was
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(world, "device", 3)
+    monkeypatch.setattr(Library, "__getattr__", lambda lib, n: lambda *a: current.append((n, world.device)) or
+                        (4096 if n.endswith("_bytes") else 0))
+    args, kw = all_calls()[name]
+    getattr(wm, name)(*args, **kw)
+    assert [d for n, d in current if not n.endswith("_bytes")] == [None]           # the tensors' index here
+    assert world.device == 3
+
+
+@pytest.mark.parametrize("name", list(all_calls()))
+def test_stream_of_another_device(world, name):  # noqa: F811
+    args, kw = all_calls()[name]
+    with pytest.raises(ValueError, match="stream is on"):
+        getattr(wm, name)(*args, stream=Stream("there", 9, torch.device("cuda", 1)), **kw)
+    assert not world.lib.calls

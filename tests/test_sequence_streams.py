@@ -33,6 +33,7 @@ def world(monkeypatch):
     class World:
         main, side = Stream("main", 1), Stream("side", 2)
         now, lib, born, recorded = [main], Library(), [], []
+        device = None                        # the current one; the CPU tensors' index is None too
 
         @staticmethod
         @contextlib.contextmanager
@@ -52,6 +53,7 @@ def world(monkeypatch):
     monkeypatch.setattr(torch, "empty", new)
     monkeypatch.setattr(torch.cuda, "stream", w.stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: w.now[-1])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: w.device)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: w.recorded.append((t.data_ptr(), s.name)), raising=False)
     return w
 
