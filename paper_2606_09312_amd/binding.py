@@ -623,12 +623,11 @@ def _on_stream(fn):
 
 
 def _attention(q, k, v, q_off, k_off, kv_mask, scale):
-    import torch
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q, k and v are [rows][heads][head_dim]")
     if k.shape[2] != q.shape[2]:
         raise ValueError("q and k differ in head_dim")
-    _dtype(q)
+    dtype = _dtype(q)
     _same(q, k.shape, k=k, v=v)
     qo, ko = np.ascontiguousarray(q_off, dtype=np.int32), np.ascontiguousarray(k_off, dtype=np.int32)
     qp, kp = qo.ctypes.data, ko.ctypes.data
@@ -637,11 +636,12 @@ def _attention(q, k, v, q_off, k_off, kv_mask, scale):
     if qo[-1] != q.shape[0] or ko[-1] != k.shape[0]:
         raise ValueError("q_off and k_off must end at the number of rows")
     if kv_mask is not None:
+        import torch
         if kv_mask.dtype not in (torch.uint8, torch.bool) or tuple(kv_mask.shape) != (k.shape[0],) or \
                 kv_mask.device != q.device or not kv_mask.is_contiguous():
             raise ValueError("kv_mask must be dense uint8 or bool [key rows] on the tensors' device")
     # in the order of Attention's fields
-    a = Attention(_dtype(q), q.shape[1], k.shape[1], q.shape[2], len(qo) - 1, qp, kp, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    a = Attention(dtype, q.shape[1], k.shape[1], q.shape[2], len(qo) - 1, qp, kp, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                   _rows("q", q), _rows("k", k), _rows("v", v), _addr(kv_mask), q.shape[2] ** -0.5 if scale is None else scale)
     a.keep = (qo, ko)
     _on_gpu(q)
@@ -707,7 +707,7 @@ def _conv(x, off, weight, bias, T_max, silu, state, status):
         raise ValueError("x is [rows][channels], weight [channels][width]")
     C, W = x.shape[1], weight.shape[1]
     B = _offsets_ok(off, x.device)
-    _dtype(x)
+    dtype = _dtype(x)
     _f32(x.device, (C, W), weight=weight)
     _f32(x.device, (C,), bias=bias)
     _same(x, (B, W - 1, C), state=state)
@@ -717,7 +717,7 @@ def _conv(x, off, weight, bias, T_max, silu, state, status):
     if status is not None:
         _status_ok(status, x.device)
     # in the order of Conv's fields
-    return Conv(_dtype(x), B, T_max, C, W, 1 if silu else 0, x.shape[0], off.data_ptr(), x.data_ptr(), _rows("x", x),
+    return Conv(dtype, B, T_max, C, W, 1 if silu else 0, x.shape[0], off.data_ptr(), x.data_ptr(), _rows("x", x),
                 weight.data_ptr(), _addr(bias), _addr(state), _addr(status))
 
 
@@ -768,7 +768,7 @@ def _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status):
         raise ValueError("u is [rows][channels], A [channels][states], Bm and Cm [rows][states]")
     C, N = A.shape
     B = _offsets_ok(off, u.device)
-    _dtype(u)
+    dtype = _dtype(u)
     _same(u, (u.shape[0], C), u=u, delta=delta, z=z)
     _same(u, (u.shape[0], N), Bm=Bm, Cm=Cm)
     _f32(u.device, (C, N), A=A)
@@ -779,7 +779,7 @@ def _scan(u, delta, A, Bm, Cm, off, T_max, D, z, delta_bias, h0, status):
     if status is not None:
         _status_ok(status, u.device)
     # in the order of ScanArgs' fields
-    return ScanArgs(_dtype(u), B, T_max, C, N, u.shape[0], off.data_ptr(), u.data_ptr(), delta.data_ptr(), _addr(z), Bm.data_ptr(),
+    return ScanArgs(dtype, B, T_max, C, N, u.shape[0], off.data_ptr(), u.data_ptr(), delta.data_ptr(), _addr(z), Bm.data_ptr(),
                     Cm.data_ptr(), *lds, A.data_ptr(), _addr(D), _addr(delta_bias), _addr(h0), _addr(status))
 
 
