@@ -237,6 +237,40 @@ def _stream(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _on_stream(fn):
+    """Gives fn, which allocates and launches on the current stream, the keyword `stream`.
+
+    The call then runs with that stream current, so that what it allocates (workspaces that are
+    dropped on return above all) belongs to the stream's pool and is reused in the stream's order only.
+    Results are kept from that reuse while the caller's stream uses them, and the caller's tensors
+    from their own pool's while `stream` does.
+    """
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        import torch
+        here = torch.cuda.current_stream(stream.device)
+        given = [t for v in (*args, *kw.values()) for t in (v.values() if isinstance(v, dict) else (v,))
+                 if isinstance(t, torch.Tensor) and t.is_cuda]
+        if any(t.device != stream.device for t in given):
+            raise ValueError(f"stream is on {stream.device}, tensors are not")
+        if stream == here:
+            return fn(*args, **kw)
+        with torch.cuda.stream(stream):
+            r = fn(*args, **kw)
+        for t in given:
+            t.record_stream(stream)
+        for t in r.values():
+            if t is not None:
+                t.record_stream(here)
+        return r
+    sig = inspect.signature(fn)
+    call.__signature__ = sig.replace(parameters=[*sig.parameters.values(),
+                                                 inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
+    return call
+
+
 class Model:
     """Device copy of the evaluator's weights (wm_model_create)."""
 
@@ -349,8 +383,9 @@ def score_trees(forest: Forest, zT, phi_s, hw, scores, stream=None):
                                          hw.shape[1], _ptr(scores), _stream(stream)))
 
 
+@_on_stream
 def evaluate(model: Model, init, seg_off, types, params, lens, hw, k, *, init_is_feats=False,
-             scores=None, zT=None, idx=None, val=None, ws=None, stream=None, forest=None):
+             scores=None, zT=None, idx=None, val=None, ws=None, forest=None):
     """Fused [encode,] rollout, score and top-k (wm_evaluate) on device tensors;
     with a Forest, the tree-ensemble ranker on structured action features
     (wm_evaluate_trees).
@@ -371,7 +406,7 @@ def evaluate(model: Model, init, seg_off, types, params, lens, hw, k, *, init_is
         ws = model.workspace(B, T_max, S, n_hw, device=dev)
     args = (_ptr(init), 1 if init_is_feats else 0, segp, S, _ptr(types), _ptr(params),
             _ptr(lens), B, T_max, _ptr(hw), n_hw, k, _ptr(scores), _ptr(zT), _ptr(idx), _ptr(val),
-            _ptr(ws), ws.numel(), _stream(stream))
+            _ptr(ws), ws.numel(), _stream(None))
     if forest is None:
         _check(load_library().wm_evaluate(model.handle, *args))
     else:
@@ -414,9 +449,9 @@ def loss_workspace(model: Model, B: int, T_max: int, device="cuda"):
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
+@_on_stream
 def rollout_loss(model: Model, z0, seg_off, types, params, lens, targets, negatives, lam: float,
-                 gamma: float, *, grads=True, dz0=True, loss=None, total=None, out=None, ws=None,
-                 stream=None):
+                 gamma: float, *, grads=True, dz0=True, loss=None, total=None, out=None, ws=None):
     """Rollout loss and its gradients (wm_rollout_loss) on device tensors.
 
     targets [B][T_max][d], negatives [B][T_max][n_neg][d].  Returns a dict
@@ -451,7 +486,7 @@ def rollout_loss(model: Model, z0, seg_off, types, params, lens, targets, negati
         model.handle, _ptr(z0), segp, S, _ptr(types), _ptr(params), _ptr(lens), B, T_max,
         _ptr(targets), _ptr(negatives), negatives.shape[2] if negatives.dim() == 4 else 0,
         float(lam), float(gamma), _ptr(loss), _ptr(total), gp, _ptr(ws), ws.numel(),
-        _stream(stream)))
+        _stream(None)))
     return res
 
 
@@ -498,6 +533,11 @@ class TextModel:
 
 def encode_text(model: TextModel, tokens, tok_off, z0=None, ws=None, stream=None):
     """z0 [S][d] from concatenated token ids (device int32) and HOST tok_off [S+1]."""
+    return _encode_text(model, tokens, tok_off, z0, ws, stream=stream)
+
+
+@_on_stream
+def _encode_text(model, tokens, tok_off, z0, ws):
     import torch
     off, offp = _host_i32(tok_off)
     S = len(off) - 1
@@ -507,7 +547,7 @@ def encode_text(model: TextModel, tokens, tok_off, z0=None, ws=None, stream=None
     if ws is None:
         ws = model.workspace(off, device=dev)
     _check(load_library().wm_encode_text(model.handle, _ptr(tokens), offp, S, _ptr(z0), _ptr(ws),
-                                         ws.numel(), _stream(stream)))
+                                         ws.numel(), _stream(None)))
     return {"z0": z0, "ws": ws}
 
 
@@ -587,39 +627,6 @@ def _launch(fn, dev, *args):
     else:
         with torch.cuda.device(dev):
             _check(fn(*args, stream))
-
-
-def _on_stream(fn):
-    """Gives fn, which allocates and launches on the current stream, the keyword `stream`.
-
-    The call then runs with that stream current, so that what it allocates (workspaces that are
-    dropped on return above all) belongs to the stream's pool and is reused in the stream's order only.
-    Results are kept from that reuse while the caller's stream uses them, and the caller's tensors
-    from their own pool's while `stream` does.
-    """
-    @functools.wraps(fn)
-    def call(*args, stream=None, **kw):
-        if stream is None:
-            return fn(*args, **kw)
-        import torch
-        here = torch.cuda.current_stream(stream.device)
-        given = [t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor) and t.is_cuda]
-        if any(t.device != stream.device for t in given):
-            raise ValueError(f"stream is on {stream.device}, tensors are not")
-        if stream == here:
-            return fn(*args, **kw)
-        with torch.cuda.stream(stream):
-            r = fn(*args, **kw)
-        for t in given:
-            t.record_stream(stream)
-        for t in r.values():
-            if t is not None:
-                t.record_stream(here)
-        return r
-    sig = inspect.signature(fn)
-    call.__signature__ = sig.replace(parameters=[*sig.parameters.values(),
-                                                 inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
-    return call
 
 
 def _attention(q, k, v, q_off, k_off, kv_mask, scale):
