@@ -1082,6 +1082,9 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 wm_status bad(const char* m) { return set_error(WM_ERR_INVALID_ARGUMENT, m); }
 
+// A launch holds fewer than 2^32 threads: workgroups of 256.
+constexpr int64_t MAX_GROUPS = UINT32_MAX / 256;
+
 wm_status check_rows(int32_t dtype, int32_t B, int32_t T_max, int64_t rows, int32_t channels, const int32_t* off) {
   if (dtype != WM_FP32 && dtype != WM_BF16) return bad("dtype must be WM_FP32 or WM_BF16");
   if (B < 0 || T_max < 0 || rows < 0 || rows > INT32_MAX) return bad("B, T_max and rows must be non-negative, rows below 2^31");
@@ -1120,12 +1123,12 @@ bool vec_ok(int v, int32_t dtype, const void* p, int64_t ld) {
 }
 
 // Lanes per run (a power of two) and workgroups of a launch over `slots` runs or groups.
-unsigned conv_grid(ConvArgs& a, int vec, int64_t slots) {
+int64_t conv_grid(ConvArgs& a, int vec, int64_t slots) {
   const int64_t cg = a.D / vec;
   a.lp = 0;
   while (a.lp < 6 && (1 << a.lp) < cg) ++a.lp;
   const int64_t waves = cdiv(slots, 64 >> a.lp) * cdiv(cg, 1 << a.lp);
-  return (unsigned)cdiv(waves, 4);
+  return cdiv(waves, 4);
 }
 
 // The gradient takes four channels per lane in both types (eight in bf16 need more
@@ -1178,7 +1181,8 @@ wm_status check_scan(const wm_scan_args* a, ScanPlan* p, bool grad) {
       p->chunks = (int)cdiv(a->T_max, c);
     }
   }
-  if ((int64_t)a->B * p->chunks * p->cblocks > INT32_MAX / 4) return set_error(WM_ERR_UNSUPPORTED, "B x T_max is too large");
+  if (cdiv((int64_t)a->B * p->chunks * p->cblocks, 4) > MAX_GROUPS || (grad && cdiv(a->rows * 2 * N, 256) > MAX_GROUPS))
+    return set_error(WM_ERR_UNSUPPORTED, "B x channels or rows x states is too large");
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   p->o_carry = p->o_sdt = p->o_pbc = p->o_pad = 0;
@@ -1262,9 +1266,10 @@ wm_status wm_causal_conv(const wm_conv* w, void* y, int64_t ld_y, void* state_ou
   if (w->channels % vec || !vec_ok(vec, w->dtype, w->x, w->ld_x) || !vec_ok(vec, w->dtype, y, ld_y) || !vec_ok(vec, w->dtype, w->state, 0) ||
       !vec_ok(vec, w->dtype, state_out, 0))
     vec = 1;
-  const unsigned grid = conv_grid(a, vec, (int64_t)w->B * p.runs);
+  const int64_t grid = conv_grid(a, vec, (int64_t)w->B * p.runs);
+  if (grid > MAX_GROUPS) return set_error(WM_ERR_UNSUPPORTED, "B x T_max x channels is too large");
   auto go = [&](auto t, auto v, auto wd) {
-    hipLaunchKernelGGL((conv_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((conv_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3((unsigned)grid), dim3(256), 0, st, a);
   };
   WM_ST(TK_CONV, (w->dtype == WM_BF16 ? conv_typed<__bf16, 8>(vec, w->width, go) : conv_typed<float, 4>(vec, w->width, go)));
   return clear_error();
@@ -1289,9 +1294,9 @@ wm_status wm_causal_conv_grad(const wm_conv* w, const void* dy, int64_t ld_dy, c
   int vec = w->channels % 4 ? 1 : 4;
   for (const auto& m : {std::pair<const void*, int64_t>{w->x, w->ld_x}, {dy, ld_dy}, {dx, ld_dx}, {w->state, 0}, {d_state_out, 0}, {d_state, 0}})
     if (!vec_ok(vec, w->dtype, m.first, m.second)) vec = 1;
-  const unsigned grid = conv_grid(a, vec, p.groups);
+  const int64_t grid = conv_grid(a, vec, p.groups);      // some 4096 wavefronts
   auto go = [&](auto t, auto v, auto wd) {
-    hipLaunchKernelGGL((conv_grad_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3(grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((conv_grad_kernel<decltype(t), decltype(v)::value, decltype(wd)::value>), dim3((unsigned)grid), dim3(256), 0, st, a);
     hipLaunchKernelGGL(conv_sum_kernel, dim3((unsigned)cdiv((int64_t)(w->width + 1) * w->channels, 16)), dim3(256), 0, st,
                        a.part, a.groups, w->width, w->channels, dweight, dbias);
   };
@@ -1326,7 +1331,7 @@ wm_status wm_scan(const wm_scan_args* w, void* y, int64_t ld_y, float* hT, void*
   auto go = [&](auto t, auto nv) {
     using T = decltype(t);
     constexpr int N = decltype(nv)::value;
-    if (w->T_max <= 1 && !checkpoints) {
+    if (w->T_max <= 1 && !checkpoints && (int64_t)w->B * p.cblocks <= MAX_GROUPS) {    // more: four to a workgroup below
       hipLaunchKernelGGL((step_kernel<T, N>), dim3((unsigned)(w->B * p.cblocks)), dim3(256), 0, st, a);
       return;
     }
