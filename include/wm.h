@@ -413,7 +413,7 @@ wm_status wm_encode_text(const wm_text_model* model, const int32_t* tokens, cons
  * over the keys of the segment with kv_mask[row] != 0 (kv_mask: one byte per
  * key row, NULL = all).  Values of k and v in hidden rows are never used.  A row
  * without a visible key has o = 0 and lse = -infinity.
- * Supported: head_dim 32, 64 or 128, heads a multiple of kv_heads, scale > 0.  Pointers and
+ * Supported: head_dim 32, 64 or 128, heads a multiple of kv_heads, 0 < scale < 2e38.  Pointers and
  * row strides (in bytes) must be multiples of 16, strides at most 2^22 elements. */
 typedef struct wm_attention {
   int32_t dtype, heads, kv_heads, head_dim, S;

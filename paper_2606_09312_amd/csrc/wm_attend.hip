@@ -763,7 +763,7 @@ wm_status check(const wm_attention* a, Plan* p, bool grad) {
   if (a->heads > 1024) return set_error(WM_ERR_UNSUPPORTED, "more than 1024 heads");
   if (a->head_dim != 32 && a->head_dim != 64 && a->head_dim != 128)
     return set_error(WM_ERR_UNSUPPORTED, "head_dim must be 32, 64 or 128");
-  if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("scale must be positive and finite");
+  if (!(a->scale > 0.0f) || !std::isfinite(a->scale * LOG2E)) return bad("scale must be positive and below 2e38");
   if (a->S < 1 || a->S > WM_MAX_SEGMENTS) return bad("S must be in [1, WM_MAX_SEGMENTS]");
   if (!a->q_off || !a->k_off) return bad("q_off/k_off is NULL");
   if (a->q_off[0] != 0 || a->k_off[0] != 0) return bad("q_off and k_off must start at 0");

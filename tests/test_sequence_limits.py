@@ -1,9 +1,11 @@
-"""Sizes past what a launch can hold are refused before anything is enqueued (no GPU needed)."""
+"""Sizes past what a launch can hold and scales past float32 are refused before anything is enqueued (no GPU needed)."""
+import ctypes
+
 import pytest
 
 import paper_2606_09312_amd as wm
 from paper_2606_09312_amd import binding as B
-from test_sequence_refusals import FAKE, conv, scan
+from test_sequence_refusals import FAKE, attention, conv, scan
 
 MANY = 2 ** 26            # wavefronts: 2^32 threads, one more than a launch may have
 
@@ -33,3 +35,13 @@ def test_scan():
     assert lib.wm_scan_grad(a, FAKE, FAKE, 16, None, g, FAKE, 1 << 40, None) == B.WM_ERR_UNSUPPORTED
     assert lib.wm_scan_workspace_bytes(a, 1) == 0 and lib.wm_scan_workspace_bytes(a, 0) > 0
     assert lib.wm_scan_workspace_bytes(scan(rows=2 ** 27 - 8), 1) > 0
+
+
+def test_attention_scale():
+    """scale log2(e), which the kernels work with, has to be finite too."""
+    lib = wm.load_library()
+    for scale in (3e38, 2.4e38):
+        a = attention(scale=scale)
+        assert lib.wm_cross_attention(a, FAKE, 256, None, ctypes.c_void_p(FAKE), 1 << 30, None) == B.WM_ERR_INVALID_ARGUMENT
+        assert lib.wm_cross_attention_workspace_bytes(a, 1) == 0
+    assert lib.wm_cross_attention_workspace_bytes(attention(scale=2.3e38), 1) > 0
