@@ -471,11 +471,11 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
 
 // Joins the key splits of every row: 16-byte quads of a row's features, one per thread.
 template <class T, int DH>
-__global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t row0, int64_t rows) {
+__global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
   constexpr int Q = DH / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= rows * Q) return;
-  const int64_t r = row0 + i / Q;
+  const int64_t r = i / Q;
   const int d = (int)(i % Q) * 4;
   float top = -INFINITY;
   for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[2 * (s * a.part_rows + r)]);
@@ -755,6 +755,12 @@ int splits_for(int64_t blocks, double units, int64_t longest, int64_t least, int
   return best;
 }
 
+// whether a matrix of n rows [heads][head_dim] has rows that the kernels can take
+bool rows_ok(const wm_attention* a, const void* p, int64_t ld, int64_t n, int heads) {
+  const int64_t e = a->dtype == WM_BF16 ? 2 : 4;
+  return n == 0 || (p && (uintptr_t)p % 16 == 0 && ld >= (int64_t)heads * a->head_dim && ld * e % 16 == 0 && ld <= (1 << 22));
+}
+
 wm_status check(const wm_attention* a, Plan* p, bool grad) {
   auto bad = [](const char* m) { return set_error(WM_ERR_INVALID_ARGUMENT, m); };
   if (!a) return bad("attention arguments are NULL");
@@ -779,12 +785,8 @@ wm_status check(const wm_attention* a, Plan* p, bool grad) {
   p->nq = a->q_off[a->S];
   p->nk = a->k_off[a->S];
   const int64_t e = a->dtype == WM_BF16 ? 2 : 4;
-  auto rows_ok = [&](const void* ptr, int64_t ld, int64_t n, int64_t width) {
-    return n == 0 || (ptr && (uintptr_t)ptr % 16 == 0 && ld >= width && ld * e % 16 == 0 && ld <= (1 << 22));
-  };
-  if (!rows_ok(a->q, a->ld_q, p->nq, (int64_t)a->heads * a->head_dim) ||
-      !rows_ok(a->k, a->ld_k, p->nk, (int64_t)a->kv_heads * a->head_dim) ||
-      !rows_ok(a->v, a->ld_v, p->nk, (int64_t)a->kv_heads * a->head_dim))
+  if (!rows_ok(a, a->q, a->ld_q, p->nq, a->heads) || !rows_ok(a, a->k, a->ld_k, p->nk, a->kv_heads) ||
+      !rows_ok(a, a->v, a->ld_v, p->nk, a->kv_heads))
     return bad("q, k and v need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
   // tiles of the kernels and steps of their loops, over all segments
   const bool bf = a->dtype == WM_BF16;
@@ -829,20 +831,19 @@ wm_status check(const wm_attention* a, Plan* p, bool grad) {
                             step_us(3, dq_cu[bf][wi]), part_us(rows_all));
   p->dkv_splits = splits_for(key_tiles * a->kv_heads, avg(key_steps, key_tiles), cdiv(p->max_r, tile), 2, dkv_cu[bf][wi],
                              step_us(4, dkv_cu[bf][wi]), part_us(2 * kv_all));
-  const int64_t rows = p->nq * a->heads, kv = p->nk * a->kv_heads;
   size_t at = 0;
   p->o_part = p->o_ml = p->o_stat = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   if (!grad) {
     if (p->fwd_splits > 1) {
-      p->o_part = take((size_t)p->fwd_splits * rows * a->head_dim * 4);
-      p->o_ml = take((size_t)p->fwd_splits * rows * 8);
+      p->o_part = take((size_t)p->fwd_splits * rows_all * a->head_dim * 4);
+      p->o_ml = take((size_t)p->fwd_splits * rows_all * 8);
     }
   } else {
-    p->o_stat = take((size_t)rows * 8);
+    p->o_stat = take((size_t)rows_all * 8);
     size_t part = 0;              // dq's and then dk's and dv's, one after the other on the stream
-    if (p->dq_splits > 1) part = (size_t)p->dq_splits * rows * a->head_dim * 4;
-    if (p->dkv_splits > 1) part = std::max(part, (size_t)p->dkv_splits * 2 * kv * a->head_dim * 4);
+    if (p->dq_splits > 1) part = (size_t)p->dq_splits * rows_all * a->head_dim * 4;
+    if (p->dkv_splits > 1) part = std::max(part, (size_t)p->dkv_splits * 2 * kv_all * a->head_dim * 4);
     if (part) p->o_part = take(part);
   }
   p->bytes = workspace_of(at);
@@ -904,7 +905,7 @@ hipError_t forward(const wm_attention* w, const Plan& p, const Args& a, hipStrea
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.nq * a.heads;
-    hipLaunchKernelGGL((join_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256)), dim3(256), 0, st, a, (int64_t)0, n);
+    hipLaunchKernelGGL((join_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256)), dim3(256), 0, st, a, n);
     return hipGetLastError();
   });
 }
@@ -941,11 +942,6 @@ hipError_t grad_keys(const wm_attention* w, const Plan& p, const Args& a, hipStr
   });
 }
 
-bool row_major_ok(const wm_attention* a, const void* p, int64_t ld, int64_t n, int heads) {
-  const int64_t e = a->dtype == WM_BF16 ? 2 : 4;
-  return n == 0 || (p && (uintptr_t)p % 16 == 0 && ld >= (int64_t)heads * a->head_dim && ld * e % 16 == 0 && ld <= (1 << 22));
-}
-
 }  // namespace attend
 }  // namespace wm
 
@@ -971,7 +967,7 @@ wm_status wm_cross_attention(const wm_attention* w, void* o, int64_t ld_o, float
   Plan p;
   const wm_status s = check(w, &p, false);
   if (s != WM_OK) return s;
-  if (!row_major_ok(w, o, ld_o, p.nq, w->heads)) return set_error(WM_ERR_INVALID_ARGUMENT, "o needs 16-byte aligned rows");
+  if (!rows_ok(w, o, ld_o, p.nq, w->heads)) return set_error(WM_ERR_INVALID_ARGUMENT, "o needs 16-byte aligned rows");
   if (p.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < p.bytes))
     return set_error(WM_ERR_INVALID_ARGUMENT, "workspace is NULL, not 256-byte aligned or too small");
   if (p.nq == 0) return clear_error();
@@ -995,9 +991,9 @@ wm_status wm_cross_attention_grad(const wm_attention* w, const void* o, int64_t 
   Plan p;
   const wm_status s = check(w, &p, true);
   if (s != WM_OK) return s;
-  if (!row_major_ok(w, o, ld_o, p.nq, w->heads) || !row_major_ok(w, d_o, ld_do, p.nq, w->heads) ||
-      !row_major_ok(w, dq, ld_dq, p.nq, w->heads) || !row_major_ok(w, dk, ld_dk, p.nk, w->kv_heads) ||
-      !row_major_ok(w, dv, ld_dv, p.nk, w->kv_heads))
+  if (!rows_ok(w, o, ld_o, p.nq, w->heads) || !rows_ok(w, d_o, ld_do, p.nq, w->heads) ||
+      !rows_ok(w, dq, ld_dq, p.nq, w->heads) || !rows_ok(w, dk, ld_dk, p.nk, w->kv_heads) ||
+      !rows_ok(w, dv, ld_dv, p.nk, w->kv_heads))
     return set_error(WM_ERR_INVALID_ARGUMENT, "o, d_o, dq, dk and dv need 16-byte aligned rows");
   if (p.nq > 0 && !lse) return set_error(WM_ERR_INVALID_ARGUMENT, "lse is NULL");
   if (p.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < p.bytes))
