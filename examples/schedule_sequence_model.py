@@ -132,7 +132,7 @@ def run(programs=4, per_program=64, T=24, d=64, train_steps=20, dtype=torch.floa
     B = programs * per_program
     tok = [int(n) for n in r.integers(40, 200, programs)]
     k_off = np.concatenate([[0], np.cumsum(tok)])
-    tokens = torch.randn(int(k_off[-1]), d, device=dev).to(dtype)                # the encoder's token states
+    tokens = torch.randn(int(k_off[-1]), d, device=dev).to(dtype)                # in place of an encoder's token states
     off = torch.arange(0, B * T + 1, T, dtype=torch.int32, device=dev)
     q_off = np.arange(programs + 1) * per_program * T
     x = torch.randn(B * T, d, device=dev).to(dtype)                              # action embeddings

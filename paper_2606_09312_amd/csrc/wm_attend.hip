@@ -84,7 +84,7 @@ __device__ __forceinline__ float pair_sum(float v) {
 }
 
 // Scores leave the products in units of log2 in float32 (an operand is scaled when it is
-// loaded, and the largest score's weight is exactly 1), unscaled in bf16 (a
+// loaded, and a score that is the maximum in use weighs exactly 1), unscaled in bf16 (a
 // scaled operand would be rounded once more).
 template <class T>
 __device__ __forceinline__ float log2_units(float s, float c2) { return IS_BF<T> ? s * c2 : s; }
@@ -165,7 +165,10 @@ struct Tile {
     }
     return acc;
   }
-  // acc[b] += sum over tile rows base + acc_row(h, r) of column 32 b + c of the tile and p[r]
+  // acc[b] += sum over tile rows base + acc_row(h, r) of column 32 b + c of the tile and p[r].
+  // bf16: p (probabilities, score gradients) is rounded to bf16 to be a matrix operand; float32
+  // products run at a seventh of the rate.  It costs the second of two roundings: results are
+  // 1.9e-3 to 2.4e-3 off (2-norm), where the rounding of the result alone gives 1.7e-3.
   static __device__ __forceinline__ void mm_col(const T* tile, int base, const f32x16& p, f32x16 (&acc)[DB], int lane) {
     const int h = lane >> 5;
     if constexpr (IS_BF<T>) {
@@ -276,12 +279,12 @@ __device__ __forceinline__ void store_cols(T* row, const f32x16 (&acc)[DB], floa
 // Forward.  A workgroup of 4 wavefronts takes 128 / WK rows (32 per wavefront);
 // WK wavefronts share rows and take every WK-th block of 32 keys (the form for at
 // most 32 rows per key head, where a wavefront of its own per 32 rows would leave three idle:
-// 16 streams of one query over 10k keys, 645 MB, 157 us, 4.1 TB/s, what a
+// 16 streams of one query over 10k keys, 645 MB, 158 us, 4.1 TB/s, what a
 // large read reaches here).  Tiles of K and V are staged two deep by copies straight
-// to LDS; softmax online.  Long forms are bound by the vector unit, an
-// exponential (quarter rate) and 2.5 instructions per score, which is busy 64% of the
-// time at three wavefronts per SIMD: 32k rows on 256 to 2048 keys, 12 heads of 64
-// in bf16, 100 GFLOP, 142 us (709 TFLOP/s).
+// to LDS; softmax online.  Long forms are bound by the vector unit: an exponential (as
+// long as two instructions) and six instructions per score keep it busy 69% of the
+// time, the matrix cores 33%, at 2.6 wavefronts per SIMD: 32k rows on 256 to 2048
+// keys, 12 heads of 64 in bf16, 100 GFLOP, 141 us (711 TFLOP/s).
 template <class T, int DH, int WK>
 constexpr int FWD_PER_CU = 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 template <class T, int DH, int WK>
@@ -506,8 +509,8 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
 
 // dq, and every row's (lse log2 e, delta) for the other kernel.  As the forward
 // kernel with 128 rows per workgroup: three products of which two are formed again,
-// against one that would have to pass dS through memory.  28k rows on 1024 to 2048 keys,
-// 12 heads of 64 in bf16, 161 GFLOP: 193 us.
+// against one that would have to pass dS through memory.  Vector unit busy 57% of the time, matrix
+// cores 42%: 28k rows on 1024 to 2048 keys, 12 heads of 64 in bf16, 161 GFLOP, 190 us.
 template <class T, int DH>
 __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
@@ -602,10 +605,9 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
 }
 
 // dk and dv of 128 keys (32 per wavefront, in registers as row operands); the
-// rows' q and do pass through LDS.  Matrix unit, vector unit and LDS each need about
-// the same time per block (512 cycles at a head width of 64), and two
-// wavefronts per SIMD overlap them in part: the same rows and keys, 214 GFLOP,
-// 310 us (689 TFLOP/s) and 21 to add four splits' sums.
+// rows' q and do pass through LDS.  Vector unit busy 49% of the time, matrix cores 33%, LDS
+// 25%, which 1.6 wavefronts per SIMD overlap in part: the same rows and keys, 214 GFLOP,
+// 311 us (688 TFLOP/s) and 21 to add four splits' sums.
 template <class T, int DH>
 __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
@@ -739,7 +741,9 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Into how many splits the loops of `blocks` workgroups, `units` steps of unit_us each on
 // average (`longest` at most), are cut: the number of rounds that 256 x per_cu
 // places take times a split's length, plus what the partial sums cost (part_us a
-// split; a launch that joins them).  Every split keeps at least `least` steps.
+// split; a launch that joins them).  A split of the longest loop keeps at least
+// `least` steps; all loops are cut alike, so that splits of short ones may be empty,
+// and a long loop among many short ones gets the splits of the average.
 // One split of 520 workgroups on 512 places took 400 us (a second round of eight), four
 // 310 and 21 for the sums.
 int splits_for(int64_t blocks, double units, int64_t longest, int64_t least, int per_cu, double unit_us, double part_us) {

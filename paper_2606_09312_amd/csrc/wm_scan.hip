@@ -32,8 +32,9 @@ __device__ __forceinline__ float rcp_of(float x) { return __builtin_amdgcn_rcpf(
 __device__ __forceinline__ float sigmoid(float x) { return rcp_of(1.0f + exp2_of(-x * LOG2E)); }
 
 // log(1 + e) for 0 <= e <= 1 as e times a polynomial of degree 9 (Lawson-weighted least
-// squares of log(1 + e) / e in float64: at most 4.8e-9 off; in float32 1.4e-7 at
-// most, 2.9e-8 on average, also where e is small, which log2(1 + e) would lose).
+// squares of log(1 + e) / e in float64; with its coefficients in float32 at most 3.4e-8
+// of itself off, evaluated in float32 1.6e-7 at most and 2.4e-8 on average, also where e
+// is small, which log2(1 + e) would lose).
 __device__ __forceinline__ float log1p_unit(float e) {
   float p = fmaf(-0.0032440212089568377f, e, 0.01985144428908825f);
   p = fmaf(p, e, -0.056959498673677444f);
@@ -438,9 +439,10 @@ struct Row {
 // Forward over one (sequence, chunk) and 64 channels per wavefront, one per lane, all
 // N states in registers; rows of B and C are uniform (scalar loads).  LOCAL: only the
 // chunk's end state from zero and its sum of dt.  What bounds it is the vector
-// unit: per state an exponential (quarter rate) and four instructions.  8192 sequences of
-// up to 64 steps (187k rows), 256 channels, 16 states, gate, bf16: 256 us, 2.0 TB/s of
-// the 522 MB; with rows of B and C by vector loads 349.
+// unit, busy 70% of the time: per step and channel 129 instructions at 16 states, 19 of
+// them exponentials and reciprocals (as long as two).  8192 sequences of up to 64
+// steps (184k rows), 256 channels, 16 states, gate, bf16: 255 us, 2.0 TB/s of the
+// 522 MB; with rows of B and C by vector loads 349.
 constexpr int SU = 8;       // steps whose rows are loaded together, one block ahead
 template <class T, int N, bool LOCAL, bool Z>
 __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a) {
@@ -637,11 +639,11 @@ __global__ __launch_bounds__(256) void step_kernel(const ScanArgs a) {
 // in registers.  Per-step values of a channel are computed by one of its four
 // lanes (step 4 i + q by lane q) and passed around the quad.  Sums over a
 // wavefront's channels are exchanges that halve the values each time; the
-// wavefronts' sums meet in LDS.  The vector unit bounds it (about 20 instructions per
-// state and step, busy 60% of the time): 2048 sequences of up to 32 steps (34k rows), 512
-// channels, 16 states, gate, bf16: 390 us.  Blocks of 16 steps would keep half as many
-// states in memory, but spill 50 registers and use 69% instead of 82% of these
-// sequences' blocks.
+// wavefronts' sums meet in LDS.  The vector unit bounds it (35 instructions per
+// state and step, 29 where the blocks' padding counts as steps; busy 75% of the
+// time): 2048 sequences of up to 32 steps (34k rows), 512 channels, 16 states, gate,
+// bf16: 386 us.  Blocks of 16 steps would keep half as many states in memory, but
+// spill 50 registers and use 69% instead of 82% of these sequences' blocks.
 constexpr int GW = 4, GC = 16 * GW;           // wavefronts and channels per workgroup
 
 // f(0), f(1), .. with the index as a type (register arrays and lane patterns need constants)
