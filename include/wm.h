@@ -522,6 +522,122 @@ typedef struct wm_scan_grads {
 wm_status wm_scan_grad(const wm_scan_args* a, const void* checkpoints, const void* dy, int64_t ld_dy,
                        const float* dhT, const wm_scan_grads* grads, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Attention over a shared prefix ---------------------------------------
+ * Operators of a causal sequence model of schedules: the candidates of a program
+ * share the program's keys and values (their prefix, computed once for all) and
+ * have the keys of their own steps behind them, all under one softmax.  Training and
+ * scoring whole sequences: wm_rotate and wm_prefix_attention on packed rows.  Step by
+ * step: wm_cache_append and wm_cached_attention on a paged cache.  Types, sums, row
+ * strides, offsets, `status` and repeated calls as above.  Queries, keys and values need 16-byte
+ * aligned rows (pointers and strides in bytes multiples of 16, strides at most 2^22
+ * elements).
+ *
+ * Rotation by position: pair i of the first `rot` features of a head (features i and
+ * i + rot / 2, or 2 i and 2 i + 1 where interleaved != 0) is turned by the angle
+ * position x freq[i], freq [rot / 2] float32:
+ *   (a, b) -> (a cos - b sin, a sin + b cos)
+ * Other features stay.  Angles are reduced in 64 bits: they are right to 2e-7 at every int32 position. */
+
+/* x [rows][heads][head_dim], head_dim a multiple of 8 up to 512, rot even, 2 <= rot <= head_dim.  Row
+ * off[s] + i is at position first[s] + i (first: device int32 [B], NULL = 0).  inverse != 0 turns
+ * back, which is the gradient: dx = wm_rotate(dy) with the other sign. */
+typedef struct wm_rotation {
+  int32_t dtype, B, T_max, heads, head_dim, rot, interleaved, inverse;
+  int64_t rows;
+  const int32_t *off, *first;
+  const float* freq;
+  const void* x;
+  int64_t ld_x;
+  int32_t* status;                      /* may be NULL */
+} wm_rotation;
+
+/* y [rows][heads][head_dim] out; may be x with the same stride.  Rows behind the last sequence stay. */
+wm_status wm_rotate(const wm_rotation* a, void* y, int64_t ld_y, void* stream);
+
+/* A pool of pages, k and v [n_pages][kv_heads][page][head_dim]; page: 16, 32, 64, 128 or 256 slots;
+ * head_dim 32, 64 or 128.  Sequence s of B has its keys 0 .. lens[s] - 1 (device int32 [B]) in the pages
+ * pages[s][0], pages[s][1], ... (device int32 [B][max_pages]), `page` in each; a table's entries past a
+ * length are never read.  lens counts the rows of the present call: a step first raises lens, then
+ * appends and attends with it.  A page outside [0, n_pages) and a length that does not fit are
+ * reported in `status`; nothing is read or written there. */
+typedef struct wm_cache {
+  int32_t dtype, kv_heads, head_dim, page, n_pages, B, max_pages;
+  void *k, *v;                          /* 16-byte aligned */
+  const int32_t *pages, *lens;
+} wm_cache;
+
+/* Appends rows [rows][kv_heads][head_dim] of k and v: row i of the n of sequence s goes to slot
+ * lens[s] - n + i, at position first[s] + slot.  Keys are rotated on the way (freq NULL: as they are, rot
+ * and interleaved without meaning), values are copied.  q [rows][heads][head_dim] (may be NULL, heads 0) is rotated alike
+ * to q_out.  Slots that the rows do not name stay.  Two rows of a call must not name the same
+ * slot of one page. */
+typedef struct wm_append {
+  wm_cache cache;
+  int32_t T_max, heads, rot, interleaved;
+  int64_t rows;
+  const int32_t *off, *first;           /* first may be NULL = 0 */
+  const float* freq;
+  const void *k, *v, *q;
+  int64_t ld_k, ld_v, ld_q;
+  int32_t* status;                      /* may be NULL */
+} wm_append;
+
+/* q_out: as q (may be q); NULL without q. */
+wm_status wm_cache_append(const wm_append* a, void* q_out, int64_t ld_q_out, void* stream);
+
+/* Attention of new rows to cached keys.  Row i of the n of sequence s sees the sequence's keys 0 .. lens[s] - n + i (none
+ * where that is negative) and, with S > 0 programs, all prefix_lens[p] keys of its program p: the sequences
+ * seg_off[p] .. seg_off[p + 1] (HOST [S + 1] from 0 to B) share them, in pages prefix_pages[p] of the same pool
+ * (device int32 [S][prefix_max_pages], [S]).  len_max and prefix_max: no length is greater (the work is
+ * divided by them; they need not be exact).  A row that sees no key has o = 0 and lse = -infinity.  Rows
+ * behind the last sequence stay.  heads a multiple of kv_heads, at most 1024; scale as in wm_attention. */
+typedef struct wm_cached {
+  wm_cache cache;
+  int32_t T_max, len_max, heads, S, prefix_max_pages, prefix_max;
+  int64_t rows;
+  const int32_t* off;
+  const int32_t* seg_off;               /* HOST */
+  const int32_t *prefix_pages, *prefix_lens;
+  const void* q;
+  int64_t ld_q;
+  float scale;
+  int32_t* status;                      /* may be NULL */
+} wm_cached;
+
+/* Workspace rules as for wm_cross_attention. */
+size_t wm_cached_attention_workspace_bytes(const wm_cached* a);
+
+/* o [rows][heads][head_dim] out; lse [rows][heads] float32 out (may be NULL). */
+wm_status wm_cached_attention(const wm_cached* a, void* o, int64_t ld_o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* The same on packed rows.  `shared`: q, the programs' rows q_off and their keys k, v at k_off, with kv_mask
+ * over them, as in wm_cross_attention; k and v here: own keys, one for every query row, [rows][kv_heads][head_dim].
+ * A row sees its program's (shown) keys and own keys from its sequence's first row to itself.  off as above with B
+ * sequences (a sequence that crosses the border of two programs is cut there). */
+typedef struct wm_prefix {
+  wm_attention shared;
+  const void *k, *v;
+  int64_t ld_k, ld_v;
+  int32_t B, T_max;
+  const int32_t* off;
+  int32_t* status;                      /* may be NULL */
+} wm_prefix;
+
+size_t wm_prefix_attention_workspace_bytes(const wm_prefix* a, int32_t grad);
+
+wm_status wm_prefix_attention(const wm_prefix* a, void* o, int64_t ld_o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient outputs: dq, dk, dv as q, k, v; dpk and dpv as the programs' keys and values (summed over all rows of
+ * the program and the heads that share a key head; 0 for hidden keys). */
+typedef struct wm_prefix_grads {
+  void *dq, *dk, *dv, *dpk, *dpv;
+  int64_t ld_dq, ld_dk, ld_dv, ld_dpk, ld_dpv;
+} wm_prefix_grads;
+
+/* Gradients given d_o = dL/do, with o and lse of the forward call. */
+wm_status wm_prefix_attention_grad(const wm_prefix* a, const void* o, int64_t ld_o, const float* lse, const void* d_o, int64_t ld_do,
+                                   const wm_prefix_grads* grads, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronise `stream`, read and clear the workspace's device error word.
  * Returns WM_OK, or WM_ERR_INPUT_RANGE with wm_last_error() naming the
  * violation(s); WM_ERR_DEVICE if the stream reports a failure. */
@@ -536,9 +652,10 @@ const char* wm_last_error(void);
  * features, 7 tree-ensemble scores, 8 loss forward steps, 9 step losses,
  * 10 loss backward steps, 11 weight-gradient sums, 12 encoder dense
  * products, 13 encoder attention, 14 other encoder kernels, 15 cross attention,
- * 16 causal convolution, 17 scan.  Enabling resets the
- * counters; reading synchronises on the recorded events.  At most 8192
- * launches per kernel are recorded while enabled. */
+ * 16 causal convolution, 17 scan, 18 rotation, 19 cache append, 20 cached
+ * attention, 21 attention over a shared prefix.  Enabling resets the counters;
+ * reading synchronises on the recorded events.  At most 8192 launches per kernel
+ * are recorded while enabled. */
 wm_status wm_timing_enable(int32_t on);
 wm_status wm_timing_read(int32_t kernel, double* total_ms, int64_t* launches);
 

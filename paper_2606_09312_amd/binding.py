@@ -26,7 +26,8 @@ NORMS = {"none": WM_NORM_NONE, "l2": WM_NORM_L2}
 KERNELS = {"rollout": 0, "score": 1, "topk": 2, "bucket": 3, "phi": 4, "encode": 5,
            "phi_struct": 6, "trees": 7, "loss_fwd": 8, "loss_steps": 9, "loss_bwd": 10,
            "loss_grads": 11, "text_gemm": 12, "text_attn": 13, "text_other": 14,
-           "cross_attention": 15, "causal_conv": 16, "scan": 17}
+           "cross_attention": 15, "causal_conv": 16, "scan": 17, "rotate": 18, "cache_append": 19,
+           "cached_attention": 20, "prefix_attention": 21}
 
 # Exported symbols (kept in step with include/wm.h).
 SYMBOLS = (
@@ -39,6 +40,8 @@ SYMBOLS = (
     "wm_cross_attention_workspace_bytes", "wm_cross_attention", "wm_cross_attention_grad",
     "wm_causal_conv", "wm_causal_conv_workspace_bytes", "wm_causal_conv_grad",
     "wm_scan_workspace_bytes", "wm_scan_checkpoint_bytes", "wm_scan", "wm_scan_grad",
+    "wm_rotate", "wm_cache_append", "wm_cached_attention_workspace_bytes", "wm_cached_attention",
+    "wm_prefix_attention_workspace_bytes", "wm_prefix_attention", "wm_prefix_attention_grad",
 )
 
 
@@ -113,6 +116,39 @@ class ScanGrads(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_void_p) for n in ("du", "ddelta", "dz", "dB", "dC")]
                 + [(n, ctypes.c_int64) for n in ("ld_du", "ld_ddelta", "ld_dz", "ld_dB", "ld_dC")]
                 + [(n, ctypes.c_void_p) for n in ("dA", "dD", "ddelta_bias", "dh0")])
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "B", "T_max", "heads", "head_dim", "rot", "interleaved", "inverse")]
+                + [("rows", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("off", "first", "freq", "x")]
+                + [("ld_x", ctypes.c_int64), ("status", ctypes.c_void_p)])
+
+
+class Cache(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "kv_heads", "head_dim", "page", "n_pages", "B", "max_pages")]
+                + [(n, ctypes.c_void_p) for n in ("k", "v", "pages", "lens")])
+
+
+class Append(ctypes.Structure):
+    _fields_ = ([("cache", Cache)] + [(n, ctypes.c_int32) for n in ("T_max", "heads", "rot", "interleaved")]
+                + [("rows", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("off", "first", "freq", "k", "v", "q")]
+                + [(n, ctypes.c_int64) for n in ("ld_k", "ld_v", "ld_q")] + [("status", ctypes.c_void_p)])
+
+
+class Cached(ctypes.Structure):
+    _fields_ = ([("cache", Cache)] + [(n, ctypes.c_int32) for n in ("T_max", "len_max", "heads", "S", "prefix_max_pages", "prefix_max")]
+                + [("rows", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("off", "seg_off", "prefix_pages", "prefix_lens", "q")]
+                + [("ld_q", ctypes.c_int64), ("scale", ctypes.c_float), ("status", ctypes.c_void_p)])
+
+
+class Prefix(ctypes.Structure):
+    _fields_ = ([("shared", Attention)] + [(n, ctypes.c_void_p) for n in ("k", "v")] + [(n, ctypes.c_int64) for n in ("ld_k", "ld_v")]
+                + [(n, ctypes.c_int32) for n in ("B", "T_max")] + [(n, ctypes.c_void_p) for n in ("off", "status")])
+
+
+class PrefixGrads(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("dq", "dk", "dv", "dpk", "dpv")]
+                + [(n, ctypes.c_int64) for n in ("ld_dq", "ld_dk", "ld_dv", "ld_dpk", "ld_dpv")])
 
 
 _lib = None
@@ -208,6 +244,21 @@ def load_library(path: str = LIB_PATH):
     lib.wm_scan.restype = i32
     lib.wm_scan_grad.argtypes = [sc, vp, vp, i64, vp, ctypes.POINTER(ScanGrads), vp, sz, vp]
     lib.wm_scan_grad.restype = i32
+    ro, ap, ca, pr = (ctypes.POINTER(c) for c in (Rotation, Append, Cached, Prefix))
+    lib.wm_rotate.argtypes = [ro, vp, i64, vp]
+    lib.wm_rotate.restype = i32
+    lib.wm_cache_append.argtypes = [ap, vp, i64, vp]
+    lib.wm_cache_append.restype = i32
+    lib.wm_cached_attention_workspace_bytes.argtypes = [ca]
+    lib.wm_cached_attention_workspace_bytes.restype = sz
+    lib.wm_cached_attention.argtypes = [ca, vp, i64, vp, vp, sz, vp]
+    lib.wm_cached_attention.restype = i32
+    lib.wm_prefix_attention_workspace_bytes.argtypes = [pr, i32]
+    lib.wm_prefix_attention_workspace_bytes.restype = sz
+    lib.wm_prefix_attention.argtypes = [pr, vp, i64, vp, vp, sz, vp]
+    lib.wm_prefix_attention.restype = i32
+    lib.wm_prefix_attention_grad.argtypes = [pr, vp, i64, vp, vp, i64, ctypes.POINTER(PrefixGrads), vp, sz, vp]
+    lib.wm_prefix_attention_grad.restype = i32
     _lib = lib
     return lib
 
@@ -843,6 +894,217 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
     g = ScanGrads(ld_du=C, ld_ddelta=C, ld_dz=C, ld_dB=N, ld_dC=N, **{k: _addr(t) for k, t in r.items()})
     ws, n = _workspace(lib.wm_scan_workspace_bytes(a, 1), ws, dev)
     _launch(lib.wm_scan_grad, dev, a, _addr(checkpoints), dy.data_ptr(), _rows("dy", dy), _addr(dhT), g, _addr(ws), n)
+    return {**r, "ws": ws}
+
+
+# ---- attention over a shared prefix ------------------------------------------------
+def _i32(dev, shape, **tensors):
+    """Checks that tensors (None allowed) are dense int32 of `shape` on `dev`."""
+    import torch
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.int32 or t.shape != shape or t.device != dev or not t.is_contiguous()):
+            raise ValueError(f"{name} must be dense int32 {tuple(shape)} on {dev}")
+
+
+def _heads(**tensors):
+    for name, t in tensors.items():
+        if t.dim() != 3:
+            raise ValueError(f"{name} is [rows][heads][head_dim]")
+
+
+def _frequencies(freq, dev):
+    if freq.dim() != 1:
+        raise ValueError("freq is [rot / 2]")
+    _f32(dev, freq.shape, freq=freq)
+    return 2 * freq.shape[0]
+
+
+@_on_stream
+def rotate(x, off, freq, *, T_max, first=None, interleaved=False, inverse=False, y=None, status=None):
+    """Rotation of packed rows by position (wm_rotate): pair i of a head by position * freq[i].
+
+    x [rows][heads][head_dim] float32 or bfloat16, off device int32 [B + 1], T_max: the longest sequence's
+    rows; freq [rot / 2] float32 turns the first rot features of a head: features i and i + rot / 2, or 2 i and
+    2 i + 1 (interleaved).  Row i of sequence s is at position first[s] + i (first: device int32 [B], None = 0).
+    inverse turns back: the gradient of a rotation is the rotation of its gradient with the other sign.  Returns
+    y (given: may be x).  status: zeroed int32 [64] for device_status.
+    """
+    import torch
+    _heads(x=x)
+    dtype = _dtype(x)
+    B = _offsets_ok(off, x.device)
+    _i32(x.device, (B,), first=first)
+    rot = _frequencies(freq, x.device)
+    _on_gpu(x)
+    if status is not None:
+        _status_ok(status, x.device)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+    _same(x, x.shape, y=y)
+    # in the order of Rotation's fields
+    a = Rotation(dtype, B, T_max, x.shape[1], x.shape[2], rot, 1 if interleaved else 0, 1 if inverse else 0, x.shape[0], off.data_ptr(),
+                 _addr(first), freq.data_ptr(), x.data_ptr(), _rows("x", x), _addr(status))
+    _launch(load_library().wm_rotate, x.device, a, y.data_ptr(), _rows("y", y))
+    return {"y": y}
+
+
+def _cache(k_cache, v_cache, pages, lens):
+    if k_cache.dim() != 4 or pages.dim() != 2:
+        raise ValueError("caches are [n_pages][kv_heads][page][head_dim], pages [B][max_pages]")
+    dtype, dev = _dtype(k_cache), k_cache.device
+    _same(k_cache, k_cache.shape, v_cache=v_cache)
+    if not k_cache.is_contiguous() or not v_cache.is_contiguous():
+        raise ValueError("k_cache and v_cache must be dense")
+    B = pages.shape[0]
+    _i32(dev, pages.shape, pages=pages)
+    _i32(dev, (B,), lens=lens)
+    n, heads, page, dim = k_cache.shape
+    _on_gpu(k_cache)
+    # in the order of Cache's fields
+    return Cache(dtype, heads, dim, page, n, B, pages.shape[1], k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), lens.data_ptr())
+
+
+@_on_stream
+def cache_append(k, v, k_cache, v_cache, pages, lens, off, *, T_max, first=None, freq=None, interleaved=False, q=None, q_out=None,
+                 status=None):
+    """Appends keys and values to a paged cache, the keys rotated on the way (wm_cache_append).
+
+    k, v [rows][kv_heads][head_dim] (q [rows][heads][head_dim]) of the caches' type; k_cache, v_cache
+    [n_pages][kv_heads][page][head_dim], changed in place; pages int32 [B][max_pages], lens int32 [B], off int32 [B + 1]
+    on the device.  lens counts the new rows: row i of the n of sequence s goes to slot lens[s] - n + i, at position
+    first[s] + slot.  freq and interleaved as in rotate; without freq nothing is rotated.  Returns q (rotated alike;
+    q_out may be q), k_cache and v_cache.  status: zeroed int32 [64] for device_status.
+    """
+    import torch
+    _heads(k=k)
+    c = _cache(k_cache, v_cache, pages, lens)
+    dev = k_cache.device
+    shape = (k.shape[0], c.kv_heads, c.head_dim)
+    _same(k_cache, shape, k=k, v=v)
+    if _offsets_ok(off, dev) != c.B:
+        raise ValueError("off needs an entry more than pages has rows")
+    _i32(dev, (c.B,), first=first)
+    rot = 0 if freq is None else _frequencies(freq, dev)
+    if status is not None:
+        _status_ok(status, dev)
+    heads = 0
+    if q is not None:
+        _heads(q=q)
+        heads = q.shape[1]
+        shape = (k.shape[0], heads, c.head_dim)
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q_out is None else q_out
+        _same(k_cache, shape, q=q, q_out=q_out)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    # in the order of Append's fields
+    a = Append(c, T_max, heads, rot, 1 if interleaved else 0, k.shape[0], off.data_ptr(), _addr(first), _addr(freq), k.data_ptr(), v.data_ptr(),
+               _addr(q), _rows("k", k), _rows("v", v), _rows("q", q) if heads else 0, _addr(status))
+    _launch(load_library().wm_cache_append, dev, a, _addr(q_out), _rows("q_out", q_out) if heads else 0)
+    return {"q": q_out, "k_cache": k_cache, "v_cache": v_cache}
+
+
+@_on_stream
+def cached_attention(q, k_cache, v_cache, pages, lens, off, *, T_max, len_max=None, seg_off=None, prefix_pages=None, prefix_lens=None,
+                     prefix_max=None, scale=None, o=None, lse=None, need_lse=False, status=None, ws=None):
+    """Attention of new rows to their sequence's cached keys and to those that its program's sequences share
+    (wm_cached_attention).
+
+    q [rows][heads][head_dim]; caches, pages, lens and off as in cache_append: row i of the n of sequence s sees the
+    sequence's keys 0 .. lens[s] - n + i.  With seg_off (HOST [S + 1], from 0 to B), the sequences of program p also see
+    its prefix_lens[p] keys (device int32 [S]) in the pages prefix_pages[p] (device int32 [S][...]) of the same pool.  len_max and
+    prefix_max: no length is greater (default: what the tables hold; closer bounds divide the work better).  scale
+    defaults to head_dim ** -0.5.  Returns o, lse [rows][heads] (with need_lse or when given) and ws.  status: zeroed int32
+    [64] for device_status.
+    """
+    import torch
+    _heads(q=q)
+    c = _cache(k_cache, v_cache, pages, lens)
+    dev = k_cache.device
+    _same(k_cache, (q.shape[0], q.shape[1], c.head_dim), q=q)
+    if _offsets_ok(off, dev) != c.B:
+        raise ValueError("off needs an entry more than pages has rows")
+    len_max = c.max_pages * c.page if len_max is None else len_max
+    S = shared_pages = 0
+    seg = segp = None
+    if seg_off is None:
+        if prefix_pages is not None or prefix_lens is not None:
+            raise ValueError("prefix_pages and prefix_lens need seg_off")
+    else:
+        if prefix_pages is None or prefix_lens is None or prefix_pages.dim() != 2:
+            raise ValueError("seg_off needs prefix_pages [S][...] and prefix_lens [S]")
+        seg = np.ascontiguousarray(seg_off, dtype=np.int32)
+        S = len(seg) - 1
+        if seg.ndim != 1 or S < 1 or seg[-1] != c.B:
+            raise ValueError("seg_off must end at the number of sequences")
+        segp, shared_pages = seg.ctypes.data, prefix_pages.shape[1]
+        _i32(dev, (S, shared_pages), prefix_pages=prefix_pages)
+        _i32(dev, (S,), prefix_lens=prefix_lens)
+    prefix_max = shared_pages * c.page if prefix_max is None else prefix_max
+    if status is not None:
+        _status_ok(status, dev)
+    o = torch.empty(q.shape, dtype=q.dtype, device=dev) if o is None else o
+    _same(q, q.shape, o=o)
+    if lse is None and need_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+    _f32(dev, q.shape[:2], lse=lse)
+    # in the order of Cached's fields
+    a = Cached(c, T_max, len_max, q.shape[1], S, shared_pages, prefix_max, q.shape[0], off.data_ptr(), segp, _addr(prefix_pages),
+               _addr(prefix_lens), q.data_ptr(), _rows("q", q), q.shape[2] ** -0.5 if scale is None else scale, _addr(status))
+    lib = load_library()
+    ws, n = _workspace(lib.wm_cached_attention_workspace_bytes(a), ws, dev)
+    _launch(lib.wm_cached_attention, dev, a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n)
+    return {"o": o, "lse": lse, "ws": ws}
+
+
+def _prefix(q, k, v, pk, pv, off, q_off, p_off, T_max, kv_mask, scale, status):
+    _heads(k=k, pk=pk)
+    a = _attention(q, pk, pv, q_off, p_off, kv_mask, scale)
+    _same(q, (q.shape[0],) + tuple(pk.shape[1:]), k=k, v=v)
+    B = _offsets_ok(off, q.device)
+    if status is not None:
+        _status_ok(status, q.device)
+    # in the order of Prefix's fields
+    p = Prefix(a, k.data_ptr(), v.data_ptr(), _rows("k", k), _rows("v", v), B, T_max, off.data_ptr(), _addr(status))
+    p.keep = a.keep
+    return p
+
+
+@_on_stream
+def prefix_attention(q, k, v, pk, pv, off, q_off, p_off, *, T_max, kv_mask=None, scale=None, o=None, lse=None, need_lse=False,
+                     status=None, ws=None):
+    """Causal attention of packed sequences whose programs' keys come first (wm_prefix_attention).
+
+    q [rows][heads][head_dim], own keys k, v [rows][kv_heads][head_dim], the programs' keys pk, pv
+    [program rows][kv_heads][head_dim], float32 or bfloat16; row strides may be larger than dense.  off: device int32
+    [B + 1], the sequences' rows (at most T_max each); q_off, p_off: HOST [S + 1], the programs' query rows and keys.  A
+    row sees its program's keys (those with kv_mask != 0) and own keys from its sequence's first row to itself.  Returns o, lse
+    [rows][heads] (with need_lse or when given; the gradient needs it) and ws.  status: zeroed int32 [64] for device_status.
+    """
+    import torch
+    a = _prefix(q, k, v, pk, pv, off, q_off, p_off, T_max, kv_mask, scale, status)
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if o is None else o
+    _same(q, q.shape, o=o)
+    if lse is None and need_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    _f32(q.device, q.shape[:2], lse=lse)
+    lib = load_library()
+    ws, n = _workspace(lib.wm_prefix_attention_workspace_bytes(a, 0), ws, q.device)
+    _launch(lib.wm_prefix_attention, q.device, a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n)
+    return {"o": o, "lse": lse, "ws": ws}
+
+
+@_on_stream
+def prefix_attention_grad(do, q, k, v, pk, pv, o, lse, off, q_off, p_off, *, T_max, kv_mask=None, scale=None, status=None, ws=None):
+    """Gradients dq, dk, dv, dpk and dpv of prefix_attention given do = dL/do (wm_prefix_attention_grad)."""
+    import torch
+    a = _prefix(q, k, v, pk, pv, off, q_off, p_off, T_max, kv_mask, scale, status)
+    dev = q.device
+    _same(q, q.shape, o=o, do=do)
+    _f32(dev, q.shape[:2], lse=lse)
+    r = {"d" + n: torch.empty(t.shape, dtype=t.dtype, device=dev) for n, t in (("q", q), ("k", k), ("v", v), ("pk", pk), ("pv", pv))}
+    g = PrefixGrads(*[_addr(t) for t in r.values()], *[_rows(n, t) for n, t in r.items()])
+    lib = load_library()
+    ws, n = _workspace(lib.wm_prefix_attention_workspace_bytes(a, 1), ws, dev)
+    _launch(lib.wm_prefix_attention_grad, dev, a, o.data_ptr(), _rows("o", o), _addr(lse), do.data_ptr(), _rows("do", do), g, _addr(ws), n)
     return {**r, "ws": ws}
 
 

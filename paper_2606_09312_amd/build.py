@@ -7,7 +7,7 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SOURCES = ["csrc/wm_api.hip", "csrc/wm_kernels.hip", "csrc/wm_text.hip", "csrc/wm_attend.hip",
-           "csrc/wm_scan.hip"]
+           "csrc/wm_scan.hip", "csrc/wm_cache.hip", "csrc/wm_prefix.hip"]
 HOST_SOURCES = ["csrc/wm_pack.cpp"]      # plain C++ (the tests also build it alone)
 LIB = os.path.join(HERE, "libwm.so")
 

@@ -683,6 +683,8 @@ wm_status wm_device_status(void* ws, size_t ws_bytes, void* stream) {
   if (word & ERRBIT_PARAM) msg += " an action parameter < 1;";
   if (word & ERRBIT_TOKEN) msg += " a token id outside [0, vocab);";
   if (word & ERRBIT_ROWS) msg += " offsets that do not run from 0 to the rows;";
+  if (word & ERRBIT_KEYS) msg += " a number of keys that its page table or the new rows do not fit;";
+  if (word & ERRBIT_PAGE) msg += " a page outside [0, n_pages);";
   return fail(WM_ERR_INPUT_RANGE, msg);
 }
 

@@ -106,7 +106,8 @@ int rollout_lds_bytes(const DevModel& m);
 enum TimedKernel { TK_ROLLOUT = 0, TK_SCORE = 1, TK_TOPK = 2, TK_BUCKET = 3, TK_PHI = 4, TK_ENCODE = 5,
                    TK_PHI_STRUCT = 6, TK_TREES = 7, TK_TRAIN_FWD = 8, TK_LOSS = 9,
                    TK_TRAIN_BWD = 10, TK_GRADS = 11, TK_TEXT_GEMM = 12, TK_TEXT_ATTN = 13,
-                   TK_TEXT_OTHER = 14, TK_ATTEND = 15, TK_CONV = 16, TK_SCAN = 17, TK_COUNT = 18 };
+                   TK_TEXT_OTHER = 14, TK_ATTEND = 15, TK_CONV = 16, TK_SCAN = 17,
+                   TK_ROTATE = 18, TK_APPEND = 19, TK_CACHED = 20, TK_PREFIX = 21, TK_COUNT = 22 };
 void timing_begin(int kernel, hipStream_t st);
 void timing_end(int kernel, hipStream_t st);
 
@@ -114,6 +115,14 @@ void timing_end(int kernel, hipStream_t st);
 // refusal), so one that is needed has more, however few of its bytes are used.
 constexpr size_t NO_WORKSPACE = 256;
 inline size_t workspace_of(size_t bytes) { return bytes > 0 && bytes <= NO_WORKSPACE ? 2 * NO_WORKSPACE : bytes; }
+
+// Host checks of a paged cache (wm_cache.hip), log2 of a page's slots.
+wm_status check_cache(const wm_cache* c);
+inline int page_bits(int page) {
+  int n = 0;
+  while ((1 << n) < page) ++n;
+  return n;
+}
 
 // Thread-local last-error message of the C ABI (wm_api.hip).
 wm_status set_error(wm_status st, const std::string& msg);

@@ -1,0 +1,1163 @@
+// Attention to the keys of a program and to the sequence's own keys, under one softmax: all rows of
+// packed sequences at once with gradients (dense rows), and single steps or chunks over a paged cache.
+//
+// As in the cross attention (wm_attend.hip) the G query heads of a key head are stacked, so a
+// workgroup has rows of one (program, key head) or (sequence, key head).  Its keys come in two runs,
+// cut into tiles one after the other: the program's, which every row sees, and own keys, of which a
+// row sees an interval [lo, hi) (its sequence's rows up to itself).  In packed rows the intervals of
+// neighbouring rows are neighbours, so a workgroup's own keys are one run as well, also where it
+// holds many short sequences.
+#include <string>
+
+#include "wm_attend.h"
+
+using namespace wm;
+
+namespace wm {
+namespace prefix {
+
+using namespace wm::attend;
+
+struct Args {
+  const void *q, *k, *v, *pk, *pv, *o, *d_o;
+  int64_t ld_q, ld_k, ld_v, ld_pk, ld_pv, ld_o, ld_do;
+  const uint8_t* mask;                      // of the program's keys (dense)
+  const int32_t* off;                       // [B + 1] rows of the sequences
+  int32_t* status;
+  int64_t rows;
+  int B, T_max;
+  float c2, scale;                          // scale log2(e), scale
+  int heads, kv_heads, G, splits;
+  void *out, *out2;                         // o; dq; dk and dv
+  int64_t ld_out, ld_out2;
+  float* lse;                               // forward: out (may be null); gradient: in
+  float* stat;                              // gradient: [rows heads][2] (lse log2 e, delta)
+  float* part;                              // partial sums [parts][rows heads][DH] (dkv: [splits][2][rows kv_heads][DH])
+  float* part_ml;                           // forward: [parts][rows heads][2] maximum (log2 units), sum
+  int64_t part_rows;
+  int part0, parts;                         // this launch's first part (cached), all parts (join)
+  // cached
+  const int32_t *pages, *lens, *ppages, *plens;
+  int max_pages, max_ppages, len_max, plen_max, n_pages, lps;      // lps: log2 of a page's slots
+  int seq0, nseq, row_tiles;                // a launch by sequences; 0 row tiles: by programs
+};
+
+// Offsets (and key counts) that do not fit are reported by the launch's threads together, once.
+__device__ __forceinline__ void check_rows(const Args& a, int tid) {
+  if (!a.status) return;
+  for (int64_t s = (int64_t)blockIdx.x * 256 + tid; s <= a.B; s += (int64_t)gridDim.x * 256) {
+    const int64_t x = a.off[s];
+    if ((s == 0 && x != 0) || (s == a.B && x != a.rows)) atomicOr(a.status, ERRBIT_ROWS);
+    if (s < a.B) {
+      const int64_t n = a.off[s + 1] - x;
+      if (n < 0 || n > a.T_max) atomicOr(a.status, ERRBIT_LEN);
+      if (a.lens && (a.lens[s] < 0 || a.lens[s] > a.len_max)) atomicOr(a.status, ERRBIT_KEYS);
+    }
+  }
+}
+
+// The last sequence of [lo, hi] that starts at `row` or before, looked for by a wavefront's lanes together (the
+// search never leaves [lo, hi], whatever the offsets are).
+__device__ __forceinline__ int last_start(const int32_t* off, int lo, int hi, int row, int lane) {
+  while (lo < hi) {
+    const int step = (hi - lo + 63) >> 6, at = lo + step * (lane + 1);
+    const int n = __popcll(__ballot(at <= hi && off[min(at, hi)] <= row));
+    lo += step * n;
+    hi = min(hi, lo + step - 1);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Bounds of the sequence of a row, within [first, end): a wavefront's rows ascend by lane.
+// `from`: a sequence that starts at the wavefront's first row or before.
+__device__ __forceinline__ int2 bounds_of(const Args& a, int from, int row, int last_row, int first, int end, int lane) {
+  int hi = last_start(a.off, from, a.B - 1, last_row, lane), lo = from;
+  while (__any(lo < hi)) {
+    const int mid = (int)(((int64_t)lo + hi + 1) >> 1);
+    if (lo < hi) {
+      if (a.off[mid] <= row) lo = mid; else hi = mid - 1;
+    }
+  }
+  return make_int2(min(max(a.off[lo], first), row), max(min(a.off[lo + 1], end), row + 1));
+}
+
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+__device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// A weight of 0 does not hide a value that is not finite from a product, and in a block of own keys that only some of the
+// rows see, the others' weights are 0.  So where sums come out that are not finite, the workgroup
+// goes through its loop a second time with mm_rows in mm_col's place for own keys.
+template <int DB>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
+  float z = 0.0f;
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = fmaf(acc[b][r], 0.0f, z);
+  return z != 0.0f;
+}
+// Tile::mm_col one row after the other, a lane's column taking those of m (bit acc_row(0, r) of its half).
+template <class T, int DH>
+__device__ __forceinline__ void mm_rows(const T* tile, int base, const f32x16& p, uint32_t m, f32x16 (&acc)[DH / 32], int lane) {
+  using TL = Tile<T, DH>;
+  const int h = lane >> 5;
+#pragma unroll 1
+  for (int row = 0; row < 32; ++row) {
+    const int half = (row >> 2) & 1, reg = (row & 3) | ((row >> 3) << 2);
+    float w = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w = reg == r ? p[r] : w;
+    int use = (m >> acc_row(0, reg)) & 1;
+    const float w2 = __shfl_xor(w, 32);
+    const int use2 = __shfl_xor(use, 32);
+    w = h == half ? w : w2;
+    use = h == half ? use : use2;
+    if constexpr (IS_BF<T>) w = (float)(__bf16)w;
+    typedef T t4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int b = 0; b < DH / 32; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int f = 32 * b + acc_row(h, 4 * q);
+        const t4 x = *reinterpret_cast<const t4*>(tile + (base + row) * DH + ((f / TL::E) ^ TL::swz(base + row)) * TL::E + f % TL::E);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[b][4 * q + i] = use ? fmaf(w, (float)x[i], acc[b][4 * q + i]) : acc[b][4 * q + i];
+      }
+  }
+}
+
+// Page of a table, checked; lanes past the tile's pages have none.
+__device__ __forceinline__ int page_id(const Args& a, const int32_t* table, int entry, bool used) {
+  if (!used) return -1;
+  const int id = table[entry];
+  if (id >= 0 && id < a.n_pages) return id;
+  if (a.status) atomicOr(a.status, ERRBIT_PAGE);
+  return -1;
+}
+
+// Keys [first, first + ROWS) of a page table, of which the first `len` exist, into a tile.  A page has at least 16
+// slots and a tile starts at a multiple of its length, so the 16 or fewer rows that one
+// instruction copies lie in one page, whose end (or the last key) bounds the buffer: rows past it
+// read as zero.  ids: lane l has the tile's l-th page.
+template <class T, int DH, int ROWS, int NT>
+__device__ __forceinline__ void copy_pages(const Args& a, const void* cache, int hk, T* tile, int first, int len, int ids, int tid) {
+  using TL = Tile<T, DH>;
+  constexpr int N = ROWS * TL::UPR / NT, RPI = 64 / TL::UPR;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int slots = 1 << a.lps;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r0 = (i * NT + wave * 64) / TL::UPR;                   // the instruction's first row
+    const int id = lane_of(ids, r0 >> a.lps);
+    const int n = id < 0 ? 0 : min(max(len - first - r0, 0), RPI);
+    const int64_t at = ((int64_t)max(id, 0) * a.kv_heads + hk) * slots + ((first + r0) & (slots - 1));
+    const u32x4 buf = buffer_of(static_cast<const T*>(cache) + at * DH, (uint32_t)(n * DH * sizeof(T)));
+    const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(r0 + r);
+    copy16(buf, tile + (size_t)(i * NT + wave * 64) * TL::E, (uint32_t)(r * DH * sizeof(T) + unit * 16));
+  }
+}
+
+// --------------------------------------------------------------------------
+// Forward.  A workgroup of 4 wavefronts takes 128 / WK rows (32 per wavefront); WK wavefronts share
+// rows and take every WK-th block of 32 keys.  Tiles of K and V are staged two deep; softmax online
+// (wm_attend.hip).  PAGED: the launch goes by programs (the rows of all its sequences, the program's keys
+// only) or by sequences (row_tiles > 0: its own keys, after the program's if it has any).
+template <class T, int DH, int WK>
+constexpr int FWD_PER_CU = 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
+template <class T, int DH, int WK, bool PAGED>
+__global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(const Table t, const Args a) {
+  using TL = Tile<T, DH>;
+  constexpr int WR = 4 / WK, DB = TL::DB;
+  constexpr int KB = WK > 1 ? 32 * WK : TILE_ROWS<T, DH>;     // keys per tile
+  constexpr int NV = (KB + 63) / 64;                          // visibility words per tile
+  constexpr int NB = KB / 32 / WK;                            // blocks of 32 keys of a wavefront in a tile
+  __shared__ __attribute__((aligned(16))) T lds[4 * KB * DH];
+  T* const ks = lds;                                          // [2][KB][DH]
+  T* const vs = lds + 2 * KB * DH;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, wr = wave % WR, wk = wave / WR;
+  if (a.part0 == 0) check_rows(a, tid);
+
+  // The workgroup's rows, the program's keys, own keys [o0, o1) and the interval of them that a lane's row sees.
+  int64_t q0;
+  int R, hk, tile, split, P, o0 = 0, o1 = 0, lo = 0, hi = 0, seg = 0;
+  int64_t p0 = 0;
+  const int32_t *own_table = nullptr, *shared_table = nullptr;
+  if constexpr (!PAGED) {
+    Prob p;
+    if (!problem<false>(t, a, 32 * WR, p)) return;
+    q0 = p.q0; R = p.R; hk = p.hk; split = p.split; P = p.Lk; p0 = p.k0;
+    tile = (R + 32 * WR - 1) / (32 * WR) - 1 - p.tile;        // the longest loops first
+  } else {
+    int64_t n;
+    if (a.row_tiles) {
+      int at = xcd_tile(blockIdx.x, gridDim.x);
+      split = at % a.splits; at /= a.splits;
+      tile = a.row_tiles - 1 - at % a.row_tiles; at /= a.row_tiles;
+      const int s = a.seq0 + at % a.nseq;
+      hk = at / a.nseq;
+      const int64_t x = a.off[s], y = a.off[s + 1];
+      q0 = min(max(x, (int64_t)0), a.rows);
+      n = min(min(max(y, q0), a.rows) - q0, (int64_t)a.T_max);
+      int g = 0, gh = t.n - 1;                                // the sequence's program
+      while (g < gh) {
+        const int mid = (g + gh + 1) >> 1;
+        if (t.seg[mid].q0 <= s) g = mid; else gh = mid - 1;
+      }
+      seg = t.n > 0 ? t.seg[g].k0 : -1;
+      own_table = a.pages + (int64_t)s * a.max_pages;
+      const int L = min(max(a.lens[s], 0), a.len_max);
+      // (hi is formed below; o1 holds what the row before the first sees)
+      o1 = L - (int)n;
+    } else {
+      Prob p;
+      if (!problem<false>(t, a, 32 * WR, p)) return;
+      hk = p.hk; tile = p.tile; split = p.split; seg = p.k0;
+      const int64_t x = a.off[p.q0], y = a.off[p.q0 + p.R / a.G / a.T_max];
+      q0 = min(max(x, (int64_t)0), a.rows);
+      n = min(min(max(y, q0), a.rows) - q0, (int64_t)(p.R / a.G));
+    }
+    R = (int)n * a.G;
+    if (tile * 32 * WR >= R) return;
+    P = 0;
+    if (seg >= 0 && a.plens) {
+      const int x = a.plens[seg];
+      P = min(max(x, 0), a.plen_max);
+      if (x != P && a.status && tid == 0) atomicOr(a.status, ERRBIT_KEYS);
+      shared_table = a.ppages + (int64_t)seg * a.max_ppages;
+    }
+  }
+  const int row = tile * (32 * WR) + wr * 32 + (lane & 31);   // may pass R: computed, not stored
+  const int rr = min(row, R - 1), head = hk * a.G + rr % a.G;
+  const int64_t qrow = q0 + rr / a.G;
+  const int last = (min((tile + 1) * (32 * WR), R) - 1) / a.G;         // the tile's last query
+  typename TL::Op qf;
+  TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
+  TL::scale_op(qf, a.c2);
+  if constexpr (!PAGED) {
+    const int first = (int)q0 + tile * (32 * WR) / a.G, end = (int)q0 + R / a.G;
+    const int s = last_start(a.off, 0, a.B - 1, first, lane);
+    const int2 b = bounds_of(a, s, (int)qrow, lane_of((int)qrow, 31), (int)q0, end, lane);
+    lo = b.x;
+    hi = (int)qrow + 1;
+    o0 = min(max(a.off[s], (int)q0), first);
+    o1 = (int)q0 + last + 1;
+  } else if (a.row_tiles) {
+    hi = max(o1 + rr / a.G + 1, 0);
+    o1 = max(o1 + last + 1, 0);
+  }
+  const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
+
+  const int nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
+  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const uint8_t* mask = !PAGED && a.mask ? a.mask + p0 : nullptr;
+  // What a tile's copy needs from memory, loaded a tile ahead: mask bytes, or page numbers (lane l: page l).
+  int pre[NV];
+  auto look_ahead = [&](int ti) {
+    if constexpr (PAGED) {
+      const bool own = ti >= nP;
+      const int first = (own ? ti - nP : ti) * KB, len = own ? o1 : P;
+      const int entry = (first >> a.lps) + lane;
+      pre[0] = page_id(a, own ? own_table : shared_table, entry, lane < max(KB >> a.lps, 1) && ((int64_t)entry << a.lps) < len);
+    } else if (mask && ti < nP) {
+#pragma unroll
+      for (int w = 0; w < NV; ++w) {
+        const int key = ti * KB + 64 * w + lane;
+        pre[w] = (KB >= 64 || lane < KB) && key < P ? mask[key] : 0;
+      }
+    }
+  };
+  uint64_t vis[NV], next[NV];                                 // keys of the program that exist and are shown
+  auto look = [&](int ti, uint64_t (&v)[NV]) {
+#pragma unroll
+    for (int w = 0; w < NV; ++w)
+      v[w] = mask && ti < nP ? __ballot(pre[w] != 0) : in_range(min((ti < nP ? P - ti * KB : o1 - o0 - (ti - nP) * KB) - 64 * w, KB));
+  };
+  auto copy = [&](int ti, const uint64_t (&v)[NV]) {
+    T* const kt = ks + (ti & 1) * KB * DH;
+    T* const vt = vs + (ti & 1) * KB * DH;
+    const bool own = ti >= nP;
+    if constexpr (PAGED) {
+      const int first = (own ? ti - nP : ti) * KB, len = own ? o1 : P;
+      copy_pages<T, DH, KB, 256>(a, a.k, hk, kt, first, len, pre[0], tid);
+      copy_pages<T, DH, KB, 256>(a, a.v, hk, vt, first, len, pre[0], tid);
+    } else {
+      const int64_t first = own ? (int64_t)o0 + (ti - nP) * KB : p0 + (int64_t)ti * KB;
+      const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
+      const u32x4 kb = buffer_of(static_cast<const T*>(own ? a.k : a.pk) + first * lk + hk * DH, BAD - 1);
+      const u32x4 vb = buffer_of(static_cast<const T*>(own ? a.v : a.pv) + first * lv + hk * DH, BAD - 1);
+      auto seen = [&](int r) { return (v[NV > 1 ? r >> 6 : 0] >> (r & 63)) & 1; };
+      copy_tile<T, DH, KB, 256>(kb, kt, tid, [&](int r) { return seen(r) ? (uint32_t)(r * lk * sizeof(T)) : BAD; });
+      copy_tile<T, DH, KB, 256>(vb, vt, tid, [&](int r) { return seen(r) ? (uint32_t)(r * lv * sizeof(T)) : BAD; });
+    }
+  };
+
+  f32x16 acc[DB];
+  float mx, sum;
+  bool careful = false;
+again:
+#pragma unroll
+  for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
+  mx = -INFINITY;
+  sum = 0.0f;
+  bool started = false;                       // every row has a maximum
+  if (t0 < t1) {
+    look_ahead(t0);
+    look(t0, vis);
+    copy(t0, vis);
+    if (t0 + 1 < t1) look_ahead(t0 + 1);
+  }
+  for (int ti = t0; ti < t1; ++ti) {
+    wait_counts<0, true>();
+    raw_barrier();
+    if (ti + 1 < t1) {
+      look(ti + 1, next);
+      copy(ti + 1, next);
+      if (ti + 2 < t1) look_ahead(ti + 2);
+    }
+    const T* kt = ks + (ti & 1) * KB * DH;
+    const T* vt = vs + (ti & 1) * KB * DH;
+    // Keys of the wavefront's blocks that a lane's row sees; own keys are skipped where no row sees any.
+    const bool own = ti >= nP;
+    const int at = own ? o0 + (ti - nP) * KB : 0;             // the tile's first own key
+    uint32_t seen[NB];
+    bool all = true, none = true;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      const int base = 32 * (kb * WK + wk);
+      if (own) {
+        seen[kb] = below(hi - at - base) & ~below(lo - at - base);
+        all = all && lo_z <= at + base && hi_a >= at + base + 32;
+        none = none && (lo_a >= at + base + 32 || hi_z <= at + base);
+      } else {
+        seen[kb] = (uint32_t)(vis[NV > 1 ? base >> 6 : 0] >> (base & 63));
+        all = all && seen[kb] == ~0u;
+        none = none && seen[kb] == 0u;
+      }
+    }
+    if (!none) {
+      f32x16 s[NB];
+      float bs;
+      bool look_for_max = !started || !all;
+      // a second time, scores and all, with the maximum that the first lacked
+      for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) s[kb] = TL::mm_row(kt, 32 * (kb * WK + wk), qf, lane);
+        if (!all) {
+#pragma unroll
+          for (int kb = 0; kb < NB; ++kb) {
+            uint32_t m = seen[kb] >> (4 * h);
+            asm volatile("" : "+v"(m));               // keeps this a branch: seldom taken, 48 instructions
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kb][r] = (m >> acc_row(0, r)) & 1 ? s[kb][r] : -INFINITY;
+          }
+        }
+        if (look_for_max) {
+          float bm = s[0][0];
+#pragma unroll
+          for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) bm = fmaxf(bm, s[kb][r]);
+          bm = pair_max(bm);
+          const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, a.c2)) : 1.0f;
+          sum *= f;
+#pragma unroll
+          for (int b = 0; b < DB; ++b) acc[b] *= f;
+          mx = bm > mx ? bm : mx;
+          started = !__any(mx == -INFINITY);
+        }
+        const float mc = mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2);    // only keys of weight 0 so far
+        bs = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {             // weights in the scores' place
+            s[kb][r] = weight<T>(s[kb][r], a.c2, mc);
+            bs += s[kb][r];
+          }
+        if (!__any(bs > SUM_LIMIT)) break;           // infinite or NaN scores stay what they are
+        look_for_max = true;
+      }
+      sum += bs;
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        if (careful && own) mm_rows<T, DH>(vt, 32 * (kb * WK + wk), s[kb], seen[kb] >> (4 * h), acc, lane);
+        else TL::mm_col(vt, 32 * (kb * WK + wk), s[kb], acc, lane);
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < NV; ++w) vis[w] = next[w];
+  }
+  if (t1 > nP && !careful && __syncthreads_or(not_finite<DB>(acc))) {
+    careful = true;
+    goto again;
+  }
+  sum = pair_sum(sum);
+  float m2 = mx == -INFINITY ? -INFINITY : log2_units<T>(mx, a.c2);
+  if constexpr (WK > 1) {       // join the wavefronts that share rows
+    __syncthreads();
+    constexpr int LW = DH + 4;
+    float* x = reinterpret_cast<float*>(lds);                 // [4][32][LW]
+    float* ml = x + 4 * 32 * LW;                              // [4][32][2]
+    static_assert((4 * 32 * LW + 256) * 4 <= sizeof(lds), "the exchange takes the tiles' place");
+    if (wk > 0) {
+      store_cols<float, DB>(x + (wave * 32 + (lane & 31)) * LW, acc, 1.0f, h);
+      if (h == 0) {
+        ml[(wave * 32 + lane) * 2] = m2;
+        ml[(wave * 32 + lane) * 2 + 1] = sum;
+      }
+    }
+    __syncthreads();
+    if (wk > 0) return;
+    float top = m2;
+#pragma unroll
+    for (int k = 1; k < WK; ++k) top = fmaxf(top, ml[((wr + WR * k) * 32 + (lane & 31)) * 2]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float f = exp2_of(m2 - ref);
+    sum *= f;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) acc[b] *= f;
+#pragma unroll
+    for (int k = 1; k < WK; ++k) {
+      const int w = (wr + WR * k) * 32 + (lane & 31);
+      f = exp2_of(ml[2 * w] - ref);
+      sum = fmaf(ml[2 * w + 1], f, sum);
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const f32x16 y = load_acc(x + w * LW + 32 * b, h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][r] = fmaf(y[r], f, acc[b][r]);
+      }
+    }
+    m2 = top;
+  }
+  if (row >= R) return;
+  const int64_t orow = qrow * a.heads + head;
+  if (a.parts > 1) {
+    const int64_t prow = (int64_t)(a.part0 + split) * a.part_rows + orow;
+    if (sum != 0.0f) store_cols<float, DB>(a.part + prow * DH, acc, 1.0f, h);           // else no part
+    if (h == 0) {
+      a.part_ml[2 * prow] = m2;
+      a.part_ml[2 * prow + 1] = sum;
+    }
+    return;
+  }
+  store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, sum == 0.0f ? 0.0f : 1.0f / sum, h);
+  if (a.lse && h == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : (m2 + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// Joins the parts of every row that some sequence has: 16-byte quads of a row's features, one per thread.
+template <class T, int DH>
+__global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
+  constexpr int Q = DH / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * Q) return;
+  const int64_t r = i / Q;
+  if (r / a.heads >= a.off[a.B]) return;                      // behind the last sequence
+  const int d = (int)(i % Q) * 4;
+  float top = -INFINITY;
+  for (int s = 0; s < a.parts; ++s) top = fmaxf(top, a.part_ml[2 * (s * a.part_rows + r)]);
+  float sum = 0.0f;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < a.parts; ++s) {
+    const int64_t p = s * a.part_rows + r;
+    const float l = a.part_ml[2 * p + 1];
+    if (l == 0.0f) continue;
+    const float f = exp2_of(a.part_ml[2 * p] - top);
+    sum = fmaf(l, f, sum);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + p * DH + d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = fmaf(x[j], f, acc[j]);
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  t4 y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = (T)(acc[j] * inv);
+  *reinterpret_cast<t4*>(static_cast<T*>(a.out) + (r / a.heads) * a.ld_out + (r % a.heads) * DH + d) = y;
+  if (a.lse && d == 0) a.lse[r] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// --------------------------------------------------------------------------
+// Gradients, as in wm_attend.hip: P = exp(S - lse) is formed again; delta = do . o; dS = P (do . v - delta).
+// One kernel owns rows (dq; it also writes every row's statistics), one owns own keys, and the
+// program's keys take the cross attention's.
+
+template <class T, int DH>
+__global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel(const Table t, const Args a) {
+  using TL = Tile<T, DH>;
+  constexpr int DB = TL::DB, KB = TILE_ROWS<T, DH>;
+  __shared__ __attribute__((aligned(16))) T lds[4 * KB * DH];
+  T* const ks = lds;
+  T* const vs = lds + 2 * KB * DH;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5;
+  check_rows(a, tid);
+  Prob p;
+  if (!problem<false>(t, a, 128, p)) return;
+  const int tile = (p.R + 127) / 128 - 1 - p.tile;            // the longest loops first
+  const int row = tile * 128 + wave * 32 + (lane & 31);
+  const int rr = min(row, p.R - 1), head = p.hk * a.G + rr % a.G;
+  const int64_t qrow = (int64_t)p.q0 + rr / a.G, orow = qrow * a.heads + head;
+  typename TL::Op qf, gf;
+  TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
+  TL::scale_op(qf, a.c2);
+  TL::load_op(gf, static_cast<const T*>(a.d_o) + qrow * a.ld_do + head * DH, h);
+  float delta;
+  {
+    typename TL::Op of;
+    TL::load_op(of, static_cast<const T*>(a.o) + qrow * a.ld_o + head * DH, h);
+    delta = TL::dot_cols(of, gf, lane);
+  }
+  const float lse = a.lse[orow];
+  // a row that saw only keys of weight 0 has lse = -inf: its P is 0
+  const float l2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
+  const int split = p.split;
+  if (split == 0 && h == 0 && row < p.R) {
+    a.stat[2 * orow] = l2;
+    a.stat[2 * orow + 1] = delta;
+  }
+  const int first = p.q0 + tile * 128 / a.G, end = p.q0 + p.R / a.G, last = (min((tile + 1) * 128, p.R) - 1) / a.G;
+  const int s0 = last_start(a.off, 0, a.B - 1, first, lane);
+  const int lo = bounds_of(a, s0, (int)qrow, lane_of((int)qrow, 31), p.q0, end, lane).x, hi = (int)qrow + 1;
+  const int o0 = min(max(a.off[s0], p.q0), first), o1 = p.q0 + last + 1;
+  const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
+
+  const int P = p.Lk, nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
+  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const uint8_t* mask = a.mask ? a.mask + p.k0 : nullptr;
+  auto mask_byte = [&](int ti) -> int {
+    const int key = ti * KB + lane;
+    return mask && (KB >= 64 || lane < KB) && key < P ? mask[key] : 0;
+  };
+  auto look = [&](int ti, int mb) -> uint64_t {
+    return mask && ti < nP ? __ballot(mb != 0) : in_range(min(ti < nP ? P - ti * KB : o1 - o0 - (ti - nP) * KB, KB));
+  };
+  auto copy = [&](int ti, uint64_t v) {
+    const bool own = ti >= nP;
+    const int64_t at = own ? (int64_t)o0 + (ti - nP) * KB : (int64_t)p.k0 + (int64_t)ti * KB;
+    const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
+    const u32x4 kb = buffer_of(static_cast<const T*>(own ? a.k : a.pk) + at * lk + p.hk * DH, BAD - 1);
+    const u32x4 vb = buffer_of(static_cast<const T*>(own ? a.v : a.pv) + at * lv + p.hk * DH, BAD - 1);
+    copy_tile<T, DH, KB, 256>(kb, ks + (ti & 1) * KB * DH, tid, [&](int r) { return (v >> r) & 1 ? (uint32_t)(r * lk * sizeof(T)) : BAD; });
+    copy_tile<T, DH, KB, 256>(vb, vs + (ti & 1) * KB * DH, tid, [&](int r) { return (v >> r) & 1 ? (uint32_t)(r * lv * sizeof(T)) : BAD; });
+  };
+  f32x16 acc[DB];
+  uint64_t vis = 0, next = 0;
+  int mb = 0;
+  bool careful = false;
+again:
+#pragma unroll
+  for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
+  if (t0 < t1) {
+    vis = look(t0, mask_byte(t0));
+    copy(t0, vis);
+    if (t0 + 1 < t1) mb = mask_byte(t0 + 1);
+  }
+  for (int ti = t0; ti < t1; ++ti) {
+    wait_counts<0, true>();
+    raw_barrier();
+    if (ti + 1 < t1) {
+      next = look(ti + 1, mb);
+      copy(ti + 1, next);
+      if (ti + 2 < t1) mb = mask_byte(ti + 2);
+    }
+    const T* kt = ks + (ti & 1) * KB * DH;
+    const T* vt = vs + (ti & 1) * KB * DH;
+    const bool own = ti >= nP;
+    const int at = own ? o0 + (ti - nP) * KB : 0;
+#pragma unroll
+    for (int kb = 0; kb < KB / 32; ++kb) {
+      uint32_t seen = (uint32_t)(vis >> (32 * kb));
+      bool all = seen == ~0u, none = seen == 0u;
+      if (own) {
+        const int k0 = at + 32 * kb;
+        seen = below(hi - k0) & ~below(lo - k0);
+        all = lo_z <= k0 && hi_a >= k0 + 32;
+        none = lo_a >= k0 + 32 || hi_z <= k0;
+      }
+      if (none) continue;
+      f32x16 s = TL::mm_row(kt, 32 * kb, qf, lane);
+      const f32x16 dp = TL::mm_row(vt, 32 * kb, gf, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * (dp[r] - delta);
+      if (!all) {
+        uint32_t m = seen >> (4 * h);
+        asm volatile("" : "+v"(m));             // keeps this a branch: seldom taken, 48 instructions
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : 0.0f;
+      }
+      if (careful && own) mm_rows<T, DH>(kt, 32 * kb, s, seen >> (4 * h), acc, lane);
+      else TL::mm_col(kt, 32 * kb, s, acc, lane);
+    }
+    vis = next;
+  }
+  if (t1 > nP && !careful && __syncthreads_or(not_finite<DB>(acc))) {
+    careful = true;
+    goto again;
+  }
+  if (row >= p.R) return;
+  if (a.splits > 1) store_cols<float, DB>(a.part + (split * a.part_rows + orow) * DH, acc, a.scale, h);
+  else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
+}
+
+// dk and dv of 128 own keys (32 per wavefront, in registers as row operands): key j is seen by the rows from its
+// own to its sequence's last.
+template <class T, int DH>
+__global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kernel(const Table t, const Args a) {
+  using TL = Tile<T, DH>;
+  constexpr int DB = TL::DB, RB = TILE_ROWS<T, DH>;
+  __shared__ __attribute__((aligned(16))) T lds[4 * RB * DH];
+  __shared__ __attribute__((aligned(16))) float st[2][2][RB];      // [buffer][lse log2 e, delta][row]
+  T* const qs = lds;
+  T* const gs = lds + 2 * RB * DH;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5;
+  Prob p;
+  if (!problem<true>(t, a, 128, p)) return;
+  const int key = p.tile * 128 + wave * 32 + (lane & 31), kc = min(key, p.Lk - 1);
+  const int krow = p.q0 + kc;
+  typename TL::Op kf, vf;
+  TL::load_op(kf, static_cast<const T*>(a.k) + krow * a.ld_k + p.hk * DH, h);
+  TL::load_op(vf, static_cast<const T*>(a.v) + krow * a.ld_v + p.hk * DH, h);
+  TL::scale_op(kf, a.c2);
+  // stacked rows of the segment that see a lane's key: [lo, hi); of the workgroup's keys: [x0, x1)
+  const int first = p.tile * 128, lastk = min(first + 128, p.Lk) - 1, end = p.q0 + p.Lk;
+  const int s0 = last_start(a.off, 0, a.B - 1, p.q0 + first, lane);
+  const int s1 = last_start(a.off, s0, a.B - 1, p.q0 + lastk, lane);
+  const int2 b = bounds_of(a, s0, krow, lane_of(krow, 31), p.q0, end, lane);
+  const int lo = kc * a.G, hi = (b.y - p.q0) * a.G;
+  const int x0 = first * a.G, x1 = (max(min(a.off[s1 + 1], end), p.q0 + lastk + 1) - p.q0) * a.G;
+  const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
+
+  const int tiles = (x1 - x0 + RB - 1) / RB, split = p.split;
+  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+  auto copy = [&](int ti) {
+    const int r0 = x0 + ti * RB, q1 = r0 / a.G;              // the tile's first query
+    const u32x4 qb = buffer_of(static_cast<const T*>(a.q) + ((int64_t)p.q0 + q1) * a.ld_q + p.hk * a.G * DH, BAD - 1);
+    const u32x4 gb = buffer_of(static_cast<const T*>(a.d_o) + ((int64_t)p.q0 + q1) * a.ld_do + p.hk * a.G * DH, BAD - 1);
+    auto off = [&](int r, int64_t ld) {
+      const int x = r0 + r, qi = x / a.G;
+      return x < x1 ? (uint32_t)(((qi - q1) * ld + (x - qi * a.G) * DH) * sizeof(T)) : BAD;
+    };
+    copy_tile<T, DH, RB, 256>(qb, qs + (ti & 1) * RB * DH, tid, [&](int r) { return off(r, a.ld_q); });
+    copy_tile<T, DH, RB, 256>(gb, gs + (ti & 1) * RB * DH, tid, [&](int r) { return off(r, a.ld_do); });
+  };
+  float2 sv = make_float2(INFINITY, 0.0f);
+  auto load_stat = [&](int ti) {
+    sv = make_float2(INFINITY, 0.0f);                        // rows past the end: P = 0
+    const int x = x0 + ti * RB + tid;
+    if (tid < RB && x < x1) {
+      const int qi = x / a.G;
+      sv = *reinterpret_cast<const float2*>(a.stat + 2 * (((int64_t)p.q0 + qi) * a.heads + p.hk * a.G + x - qi * a.G));
+    }
+  };
+  auto put_stat = [&](int ti) {
+    if (tid < RB) {
+      st[ti & 1][0][tid] = sv.x;
+      st[ti & 1][1][tid] = sv.y;
+    }
+  };
+  f32x16 dk[DB], dv[DB];
+  bool careful = false;
+again:
+#pragma unroll
+  for (int i = 0; i < DB; ++i) dk[i] = dv[i] = f32x16{};
+  if (t0 < t1) {
+    copy(t0);
+    load_stat(t0);
+    put_stat(t0);
+  }
+  for (int ti = t0; ti < t1; ++ti) {
+    wait_counts<0, true>();
+    raw_barrier();
+    if (ti + 1 < t1) {
+      copy(ti + 1);
+      load_stat(ti + 1);
+    }
+    const T* qt = qs + (ti & 1) * RB * DH;
+    const T* gt = gs + (ti & 1) * RB * DH;
+#pragma unroll
+    for (int rb = 0; rb < RB / 32; ++rb) {
+      const int r0 = x0 + ti * RB + 32 * rb;
+      if (lo_a >= r0 + 32 || hi_z <= r0) continue;           // no key is seen by these rows
+      f32x16 s = TL::mm_row(qt, 32 * rb, kf, lane);
+      f32x16 dp = TL::mm_row(gt, 32 * rb, vf, lane);
+      const f32x16 l2 = load_acc(&st[ti & 1][0][32 * rb], h), de = load_acc(&st[ti & 1][1][32 * rb], h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = weight<T>(s[r], a.c2, l2[r]);
+        dp[r] -= de[r];
+      }
+      const uint32_t m = (below(hi - r0) & ~below(lo - r0)) >> (4 * h);
+      if (lo_z > r0 || hi_a < r0 + 32) {
+        uint32_t see = m;
+        asm volatile("" : "+v"(see));             // keeps this a branch
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = (see >> acc_row(0, r)) & 1 ? s[r] : 0.0f;
+          dp[r] = (see >> acc_row(0, r)) & 1 ? dp[r] : 0.0f;
+        }
+      }
+      if (careful) mm_rows<T, DH>(gt, 32 * rb, s, m, dv, lane);
+      else TL::mm_col(gt, 32 * rb, s, dv, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] *= dp[r];
+      if (careful) mm_rows<T, DH>(qt, 32 * rb, s, m, dk, lane);
+      else TL::mm_col(qt, 32 * rb, s, dk, lane);
+    }
+    if (ti + 1 < t1) put_stat(ti + 1);
+  }
+  if (!careful && __syncthreads_or(not_finite<DB>(dk) || not_finite<DB>(dv))) {
+    careful = true;
+    goto again;
+  }
+  if (key >= p.Lk) return;
+  if (a.splits > 1) {
+    const int64_t prow = (int64_t)krow * a.kv_heads + p.hk;
+    store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
+    store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
+  } else {
+    store_cols<T, DB>(static_cast<T*>(a.out) + krow * a.ld_out + p.hk * DH, dk, a.scale, h);
+    store_cols<T, DB>(static_cast<T*>(a.out2) + krow * a.ld_out2 + p.hk * DH, dv, 1.0f, h);
+  }
+}
+
+// out[row] = sum of the splits' rows, in order; blockIdx.y picks dk or dv.
+template <class T, int DH>
+__global__ __launch_bounds__(256) void add_kernel(const float* part, int64_t rows, int splits, int sets, int heads,
+                                                  void* out0, int64_t ld0, void* out1, int64_t ld1) {
+  constexpr int Q = DH / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * Q) return;
+  const int set = blockIdx.y;
+  const int64_t r = i / Q, ld = set ? ld1 : ld0;
+  const int d = (int)(i % Q) * 4;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < splits; ++s) acc += *reinterpret_cast<const f32x4*>(part + (((int64_t)s * sets + set) * rows + r) * DH + d);
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  t4 y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = (T)acc[j];
+  *reinterpret_cast<t4*>(static_cast<T*>(set ? out1 : out0) + (r / heads) * ld + (r % heads) * DH + d) = y;
+}
+
+// --------------------------------------------------------------------------
+// Host side.
+
+constexpr int64_t MOST_TILES = INT32_MAX / 64 / XCDS;        // 64: splits
+// Rates that the kernels reach: TFLOP/s of the products, bytes of the few-row form (wm_attend.hip).
+double step_us(bool bf, int products, int64_t rows, int64_t keys, int dh, int per_cu) {
+  return std::max(1.0, products * 2.0 * rows * keys * dh * 256 * per_cu / (bf ? 600e6 : 90e6));
+}
+double few_us(bool bf, int64_t keys, int dh, int per_cu) {
+  return std::max(1.0, 2.0 * keys * dh * (bf ? 2 : 4) * 256 * per_cu / 4.5e6);
+}
+double part_us(int64_t values, int dh) { return 2.0 * values * dh * 4 / 4.5e6; }
+
+// Rows and keys per tile, workgroups that share a compute unit (registers, LDS).
+struct Shape {
+  bool bf;
+  int few_rows, few_keys, tile, few_cu, fwd_cu, dq_cu, dkv_cu;
+};
+Shape shape_of(int dtype, int dh) {
+  const bool bf = dtype == WM_BF16, wide32 = !bf && dh == 128;
+  const int wi = dh == 32 ? 0 : dh == 64 ? 1 : 2;
+  static const int few[2][3] = {{2, 1, 1}, {4, 2, 1}}, fwd[2][3] = {{3, 2, 2}, {4, 3, 2}};
+  static const int dq[2][3] = {{2, 2, 1}, {4, 3, 1}}, dkv[2][3] = {{2, 1, 1}, {3, 2, 1}};
+  return {bf, wide32 ? 64 : 32, wide32 ? 64 : 128, wide32 ? 32 : 64, few[bf][wi], fwd[bf][wi], dq[bf][wi], dkv[bf][wi]};
+}
+
+wm_status bad(const char* m) { return set_error(WM_ERR_INVALID_ARGUMENT, m); }
+// the launches that join parts have a thread per 4 features, and a launch at most 2^32 threads
+bool too_wide(int64_t rows_all, int dh) { return rows_all > (int64_t)UINT32_MAX / (dh / 4) - 256; }
+
+// ---- dense rows --------------------------------------------------------------
+struct Plan {
+  Shared sh;
+  bool few;
+  int fwd_splits, dq_splits, dkv_splits;
+  size_t o_part, o_ml, o_stat, bytes;
+};
+
+wm_status check(const wm_prefix* a, Plan* p, bool grad) {
+  if (!a) return bad("prefix attention arguments are NULL");
+  const wm_attention* w = &a->shared;
+  const wm_status s = check_shared(w, &p->sh);
+  if (s != WM_OK) return s;
+  if (a->B < 0 || a->T_max < 0) return bad("B and T_max must not be negative");
+  const int64_t nq = p->sh.nq;
+  if (nq > 0 && (a->B < 1 || a->T_max < 1 || !a->off)) return bad("rows need sequences: B and T_max at least 1, off not NULL");
+  if (!rows_ok(w, a->k, a->ld_k, nq, w->kv_heads) || !rows_ok(w, a->v, a->ld_v, nq, w->kv_heads))
+    return bad("k and v need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
+  const Shape f = shape_of(w->dtype, w->head_dim);
+  const int G = w->heads / w->kv_heads, dh = w->head_dim;
+  int64_t row_tiles = 0, few_tiles = 0, key_tiles = 0, longest = 0, longest_rows = 0;
+  double row_steps = 0, few_steps = 0, key_steps = 0;
+  for (int i = 0; i < w->S; ++i) {
+    const int64_t lq = (int64_t)w->q_off[i + 1] - w->q_off[i], P = (int64_t)w->k_off[i + 1] - w->k_off[i];
+    if (lq == 0) continue;
+    // own keys of a tile's rows: their own and those before them, half a sequence on average
+    const int64_t T = std::min<int64_t>(a->T_max, lq), own = std::min(lq, 128 / G + T / 2 + 1), few_own = std::min(lq, f.few_rows / G + T / 2 + 1);
+    const int64_t seen = std::min(lq, 128 + T / 2) * G;
+    row_tiles += cdiv(lq * G, 128);
+    few_tiles += cdiv(lq * G, f.few_rows);
+    key_tiles += cdiv(lq, 128);
+    row_steps += (double)cdiv(lq * G, 128) * (cdiv(P, f.tile) + cdiv(own, f.tile));
+    few_steps += (double)cdiv(lq * G, f.few_rows) * (cdiv(P, f.few_keys) + cdiv(few_own, f.few_keys));
+    key_steps += (double)cdiv(lq, 128) * cdiv(seen, f.tile);
+    longest = std::max(longest, P + std::min(lq, 128 / G + T));
+    longest_rows = std::max(longest_rows, std::min(lq, 128 + T) * G);
+  }
+  if (row_tiles * w->kv_heads > MOST_TILES || few_tiles * w->kv_heads > MOST_TILES || key_tiles * w->kv_heads > MOST_TILES)
+    return set_error(WM_ERR_UNSUPPORTED, "too many row or key tiles");
+  const int64_t rows_all = nq * w->heads, kv_all = nq * w->kv_heads;
+  auto avg = [](double steps, int64_t tiles) { return tiles ? steps / tiles : 0.0; };
+  p->few = p->sh.max_r <= f.few_rows;
+  if (p->few)
+    p->fwd_splits = splits_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu,
+                               few_us(f.bf, f.few_keys, dh, f.few_cu), part_us(rows_all, dh));
+  else
+    p->fwd_splits = splits_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.fwd_cu,
+                               step_us(f.bf, 2, 128, f.tile, dh, f.fwd_cu), part_us(rows_all, dh));
+  p->dq_splits = splits_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.dq_cu,
+                            step_us(f.bf, 3, 128, f.tile, dh, f.dq_cu), part_us(rows_all, dh));
+  p->dkv_splits = splits_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu,
+                             step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh));
+  if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
+  size_t at = 0;
+  p->o_part = p->o_ml = p->o_stat = 0;
+  auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
+  if (!grad) {
+    if (p->fwd_splits > 1) {
+      p->o_part = take((size_t)p->fwd_splits * rows_all * dh * 4);
+      p->o_ml = take((size_t)p->fwd_splits * rows_all * 8);
+    }
+  } else {
+    p->o_stat = take((size_t)rows_all * 8);
+    size_t part = p->sh.part_bytes;              // dq's, own keys' and the programs' keys', one after the other on the stream
+    if (p->dq_splits > 1) part = std::max(part, (size_t)p->dq_splits * rows_all * dh * 4);
+    if (p->dkv_splits > 1) part = std::max(part, (size_t)p->dkv_splits * 2 * kv_all * dh * 4);
+    if (part) p->o_part = take(part);
+  }
+  p->bytes = workspace_of(at);
+  return WM_OK;
+}
+
+Args base_args(const wm_prefix* x, const Plan& p) {
+  const wm_attention* w = &x->shared;
+  Args a = {};
+  a.q = w->q; a.pk = w->k; a.pv = w->v; a.k = x->k; a.v = x->v;
+  a.ld_q = w->ld_q; a.ld_pk = w->ld_k; a.ld_pv = w->ld_v; a.ld_k = x->ld_k; a.ld_v = x->ld_v;
+  a.mask = w->kv_mask;
+  a.off = x->off; a.status = x->status; a.rows = p.sh.nq; a.B = x->B; a.T_max = x->T_max;
+  a.scale = w->scale;
+  a.c2 = w->scale * LOG2E;
+  a.heads = w->heads; a.kv_heads = w->kv_heads; a.G = w->heads / w->kv_heads;
+  return a;
+}
+
+template <class T, int DH>
+hipError_t join(const Args& a, int64_t n, hipStream_t st) {
+  hipLaunchKernelGGL((join_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256)), dim3(256), 0, st, a, n);
+  return hipGetLastError();
+}
+
+hipError_t forward(const wm_attention* w, const Plan& p, const Args& a, hipStream_t st) {
+  return typed(w, [&](auto tv, auto dh) {
+    using T = decltype(tv);
+    constexpr int DH = decltype(dh)::value;
+    constexpr int WK = (!IS_BF<T> && DH == 128) ? 2 : 4;
+    const int rows = p.few ? 128 / WK : 128;
+    hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, rows); },
+                            [&](const Table& t, int blocks) {
+                              const dim3 grid(blocks);
+                              if (p.few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, false>), grid, dim3(256), 0, st, t, a);
+                              else hipLaunchKernelGGL((forward_kernel<T, DH, 1, false>), grid, dim3(256), 0, st, t, a);
+                            });
+    if (e != hipSuccess || a.parts == 1) return e;
+    return join<T, DH>(a, p.sh.nq * a.heads, st);
+  });
+}
+
+hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStream_t st) {
+  return typed(w, [&](auto tv, auto dh) {
+    using T = decltype(tv);
+    constexpr int DH = decltype(dh)::value;
+    hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, 128); },
+                            [&](const Table& t, int blocks) {
+                              hipLaunchKernelGGL((dq_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
+                            });
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t n = p.sh.nq * a.heads;
+    hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 1), dim3(256), 0, st, a.part, n,
+                       a.splits, 1, a.heads, a.out, a.ld_out, nullptr, (int64_t)0);
+    return hipGetLastError();
+  });
+}
+
+hipError_t grad_own_keys(const wm_attention* w, const Plan& p, const Args& a, hipStream_t st) {
+  wm_attention own = *w;          // its keys are the rows themselves
+  own.k_off = w->q_off;
+  return typed(w, [&](auto tv, auto dh) {
+    using T = decltype(tv);
+    constexpr int DH = decltype(dh)::value;
+    hipError_t e = each_run(&own, true, a.splits, [&](int64_t, int64_t lk) { return cdiv(lk, 128); },
+                            [&](const Table& t, int blocks) {
+                              hipLaunchKernelGGL((dkv_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
+                            });
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t n = p.sh.nq * a.kv_heads;
+    hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 2), dim3(256), 0, st, a.part, n,
+                       a.splits, 2, a.kv_heads, a.out, a.ld_out, a.out2, a.ld_out2);
+    return hipGetLastError();
+  });
+}
+
+// ---- paged cache -----------------------------------------------------------------
+struct CachedPlan {
+  wm_attention w;                 // types and widths
+  bool joint;                     // one launch by sequences (their program's keys among them), no launch by programs
+  bool few, shared_few;           // rows of 32 per workgroup, its wavefronts sharing them
+  int splits, shared_splits;
+  int64_t most_rows;              // stacked rows of a program, at most
+  size_t o_part, o_ml, bytes;
+};
+
+wm_status check(const wm_cached* a, CachedPlan* p) {
+  if (!a) return bad("cached attention arguments are NULL");
+  const wm_status s = check_cache(&a->cache);
+  if (s != WM_OK) return s;
+  const wm_cache& c = a->cache;
+  if (a->heads < 1 || a->heads % c.kv_heads) return bad("heads must be a positive multiple of kv_heads");
+  if (a->heads > 1024) return set_error(WM_ERR_UNSUPPORTED, "more than 1024 heads");
+  if (!(a->scale > 0.0f) || !std::isfinite(a->scale * LOG2E)) return bad("scale must be positive and below 2e38");
+  if (a->rows < 0 || a->rows > INT32_MAX || a->T_max < 0) return bad("rows must be in [0, 2^31), T_max not negative");
+  if (a->rows > 0 && (c.B < 1 || a->T_max < 1)) return bad("rows need sequences: B and T_max at least 1");
+  if (c.B > 0 && !a->off) return bad("off is NULL");
+  if (a->len_max < 0 || a->len_max > (int64_t)c.max_pages * c.page) return bad("len_max must be in [0, max_pages page]");
+  p->w = {};
+  p->w.dtype = c.dtype; p->w.heads = a->heads; p->w.kv_heads = c.kv_heads; p->w.head_dim = c.head_dim;
+  if (!rows_ok(&p->w, a->q, a->ld_q, a->rows, a->heads))
+    return bad("q needs 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
+  if (a->S < 0 || a->S > WM_MAX_SEGMENTS) return bad("S must be in [0, WM_MAX_SEGMENTS]");
+  const int G = a->heads / c.kv_heads, dh = c.head_dim;
+  const int64_t seq_rows = std::min<int64_t>(a->T_max, std::max<int64_t>(a->rows, 1)) * G;
+  int64_t most_seqs = 0, shared_tiles = 0, shared_few_tiles = 0;
+  const Shape f = shape_of(c.dtype, dh);
+  if (a->S > 0) {
+    if (!a->seg_off || a->seg_off[0] != 0 || a->seg_off[a->S] != c.B) return bad("seg_off must run from 0 to B");
+    for (int i = 0; i < a->S; ++i) {
+      const int64_t n = (int64_t)a->seg_off[i + 1] - a->seg_off[i];
+      if (n < 0) return bad("seg_off must not decrease");
+      most_seqs = std::max(most_seqs, n);
+      shared_tiles += cdiv(n * a->T_max * G, 128);
+      shared_few_tiles += cdiv(n * a->T_max * G, f.few_rows);
+    }
+    if (a->prefix_max < 0 || a->prefix_max > (int64_t)a->prefix_max_pages * c.page) return bad("prefix_max must be in [0, prefix_max_pages page]");
+    if (!a->prefix_lens || (a->prefix_max_pages > 0 && !a->prefix_pages)) return bad("prefix_lens/prefix_pages is NULL");
+  }
+  if (most_seqs * a->T_max * G > INT32_MAX) return set_error(WM_ERR_UNSUPPORTED, "a program has more than 2^31 rows of one key head");
+  const int P = a->S > 0 ? a->prefix_max : 0;
+  p->few = seq_rows <= f.few_rows;
+  p->most_rows = most_seqs * a->T_max * G;
+  p->shared_few = p->most_rows <= f.few_rows;
+  // Sequences of many rows fill a tile by themselves and read the program's keys along with their own.
+  p->joint = P == 0 || most_seqs <= 1 || seq_rows >= 64;
+  const int rows = p->few ? f.few_rows : 128, keys = p->few ? f.few_keys : f.tile, cu = p->few ? f.few_cu : f.fwd_cu;
+  const int64_t tiles = c.B * cdiv(seq_rows, rows) * c.kv_heads, rows_all = a->rows * a->heads;
+  if (tiles > MOST_TILES || shared_few_tiles * c.kv_heads > MOST_TILES) return set_error(WM_ERR_UNSUPPORTED, "too many row tiles");
+  auto us = [&](bool few, int k, int u) { return few ? few_us(f.bf, k, dh, u) : step_us(f.bf, 2, 128, k, dh, u); };
+  const int64_t steps = cdiv(a->len_max, keys) + (p->joint ? cdiv(P, keys) : 0);
+  p->splits = splits_for(tiles, (double)steps, steps, 2, cu, us(p->few, keys, cu), part_us(rows_all, dh));
+  p->shared_splits = 0;
+  if (!p->joint) {
+    const int sk = p->shared_few ? f.few_keys : f.tile, su = p->shared_few ? f.few_cu : f.fwd_cu;
+    p->shared_splits = splits_for((p->shared_few ? shared_few_tiles : shared_tiles) * c.kv_heads, (double)cdiv(P, sk), cdiv(P, sk), 2, su,
+                                  us(p->shared_few, sk, su), part_us(rows_all, dh));
+  }
+  if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
+  size_t at = 0;
+  p->o_part = p->o_ml = 0;
+  auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
+  const int parts = p->splits + p->shared_splits;
+  if (parts > 1) {
+    p->o_part = take((size_t)parts * rows_all * dh * 4);
+    p->o_ml = take((size_t)parts * rows_all * 8);
+  }
+  p->bytes = workspace_of(at);
+  return WM_OK;
+}
+
+hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t st) {
+  return typed(&p.w, [&](auto tv, auto dh) {
+    using T = decltype(tv);
+    constexpr int DH = decltype(dh)::value;
+    constexpr int WK = (!IS_BF<T> && DH == 128) ? 2 : 4;
+    hipError_t e = hipSuccess;
+    auto go = [&](const Table& t, int64_t blocks, bool few) {
+      if (blocks == 0 || e != hipSuccess) return;
+      const dim3 grid((unsigned)blocks);
+      if (few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, true>), grid, dim3(256), 0, st, t, a);
+      else hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), grid, dim3(256), 0, st, t, a);
+      e = hipGetLastError();
+    };
+    const int64_t seq_rows = std::min<int64_t>(x->T_max, x->rows) * a.G;
+    const int tile = p.few ? 128 / WK : 128;
+    // by sequences; with their programs' keys in runs of at most MAX_SEGS programs
+    a.part0 = 0;
+    a.splits = p.splits;
+    a.row_tiles = (int)cdiv(seq_rows, tile);
+    const int32_t* const plens = a.plens;
+    if (!p.joint || x->S == 0 || x->prefix_max == 0) {
+      a.plens = nullptr;
+      a.seq0 = 0;
+      a.nseq = x->cache.B;
+      go(Table{}, (int64_t)a.nseq * a.kv_heads * a.row_tiles * a.splits, p.few);
+    } else {
+      for (int s0 = 0; s0 < x->S; s0 += MAX_SEGS) {
+        Table t = {};
+        for (int i = s0; i < std::min(x->S, s0 + MAX_SEGS); ++i) t.seg[t.n++] = {x->seg_off[i], 0, i, 0};
+        a.seq0 = x->seg_off[s0];
+        a.nseq = x->seg_off[s0 + t.n] - a.seq0;
+        go(t, (int64_t)a.nseq * a.kv_heads * a.row_tiles * a.splits, p.few);
+      }
+    }
+    // by programs
+    if (!p.joint) {
+      a.plens = plens;
+      a.part0 = p.splits;
+      a.splits = p.shared_splits;
+      a.row_tiles = 0;
+      for (int s0 = 0; s0 < x->S; s0 += MAX_SEGS) {
+        Table t = {};
+        for (int i = s0; i < std::min(x->S, s0 + MAX_SEGS); ++i) {
+          const int n = x->seg_off[i + 1] - x->seg_off[i];
+          t.seg[t.n] = {x->seg_off[i], n * x->T_max, i, 0};
+          t.off[t.n + 1] = t.off[t.n] + (int32_t)cdiv(cdiv((int64_t)n * x->T_max * a.G, p.shared_few ? 128 / WK : 128) * a.kv_heads * a.splits, XCDS);
+          ++t.n;
+        }
+        go(t, (int64_t)t.off[t.n] * XCDS, p.shared_few);
+      }
+    }
+    if (e != hipSuccess || a.parts == 1) return e;
+    return join<T, DH>(a, x->rows * a.heads, st);
+  });
+}
+
+}  // namespace prefix
+}  // namespace wm
+
+using namespace wm::prefix;
+
+#define WM_PF(K, CALL)                                                                     \
+  do {                                                                                     \
+    timing_begin(K, st);                                                                   \
+    hipError_t e_ = (CALL);                                                                \
+    timing_end(K, st);                                                                     \
+    if (e_ != hipSuccess) return set_error(WM_ERR_DEVICE, std::string("kernel launch: ") + hipGetErrorString(e_)); \
+  } while (0)
+
+extern "C" {
+
+size_t wm_prefix_attention_workspace_bytes(const wm_prefix* a, int32_t grad) {
+  Plan p;
+  return check(a, &p, grad != 0) == WM_OK ? std::max(p.bytes, NO_WORKSPACE) : 0;
+}
+
+wm_status wm_prefix_attention(const wm_prefix* x, void* o, int64_t ld_o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  Plan p;
+  const wm_status s = check(x, &p, false);
+  if (s != WM_OK) return s;
+  const wm_attention* w = &x->shared;
+  if (!rows_ok(w, o, ld_o, p.sh.nq, w->heads)) return bad("o needs 16-byte aligned rows");
+  if (p.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < p.bytes)) return bad("workspace is NULL, not 256-byte aligned or too small");
+  if (p.sh.nq == 0) return clear_error();
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint8_t* w8 = static_cast<uint8_t*>(ws);
+  Args a = base_args(x, p);
+  a.out = o;
+  a.ld_out = ld_o;
+  a.lse = lse;
+  a.splits = a.parts = p.fwd_splits;
+  a.part = reinterpret_cast<float*>(w8 + p.o_part);
+  a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
+  a.part_rows = p.sh.nq * w->heads;
+  WM_PF(TK_PREFIX, forward(w, p, a, st));
+  return clear_error();
+}
+
+wm_status wm_prefix_attention_grad(const wm_prefix* x, const void* o, int64_t ld_o, const float* lse, const void* d_o, int64_t ld_do,
+                                   const wm_prefix_grads* g, void* ws, size_t ws_bytes, void* stream) {
+  Plan p;
+  const wm_status s = check(x, &p, true);
+  if (s != WM_OK) return s;
+  const wm_attention* w = &x->shared;
+  const int64_t nq = p.sh.nq, nk = p.sh.nk;
+  if (!g) return bad("gradient outputs are NULL");
+  if (!rows_ok(w, o, ld_o, nq, w->heads) || !rows_ok(w, d_o, ld_do, nq, w->heads) || !rows_ok(w, g->dq, g->ld_dq, nq, w->heads) ||
+      !rows_ok(w, g->dk, g->ld_dk, nq, w->kv_heads) || !rows_ok(w, g->dv, g->ld_dv, nq, w->kv_heads) ||
+      !rows_ok(w, g->dpk, g->ld_dpk, nk, w->kv_heads) || !rows_ok(w, g->dpv, g->ld_dpv, nk, w->kv_heads))
+    return bad("o, d_o, dq, dk, dv, dpk and dpv need 16-byte aligned rows");
+  if (nq > 0 && !lse) return bad("lse is NULL");
+  if (p.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < p.bytes)) return bad("workspace is NULL, not 256-byte aligned or too small");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint8_t* w8 = static_cast<uint8_t*>(ws);
+  Args a = base_args(x, p);
+  a.o = o; a.ld_o = ld_o;
+  a.d_o = d_o; a.ld_do = ld_do;
+  a.lse = const_cast<float*>(lse);
+  a.stat = reinterpret_cast<float*>(w8 + p.o_stat);
+  a.part = reinterpret_cast<float*>(w8 + p.o_part);
+  if (nq > 0) {
+    a.out = g->dq; a.ld_out = g->ld_dq;
+    a.splits = p.dq_splits;
+    a.part_rows = nq * w->heads;
+    WM_PF(TK_PREFIX, grad_rows(w, p, a, st));
+    a.out = g->dk; a.ld_out = g->ld_dk;
+    a.out2 = g->dv; a.ld_out2 = g->ld_dv;
+    a.splits = p.dkv_splits;
+    a.part_rows = nq * w->kv_heads;
+    WM_PF(TK_PREFIX, grad_own_keys(w, p, a, st));
+  }
+  if (nk > 0) WM_PF(TK_PREFIX, key_grads(w, d_o, ld_do, a.stat, g->dpk, g->ld_dpk, g->dpv, g->ld_dpv, a.part, st));
+  return clear_error();
+}
+
+size_t wm_cached_attention_workspace_bytes(const wm_cached* a) {
+  CachedPlan p;
+  return check(a, &p) == WM_OK ? std::max(p.bytes, NO_WORKSPACE) : 0;
+}
+
+wm_status wm_cached_attention(const wm_cached* x, void* o, int64_t ld_o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  CachedPlan p;
+  const wm_status s = check(x, &p);
+  if (s != WM_OK) return s;
+  if (!rows_ok(&p.w, o, ld_o, x->rows, x->heads)) return bad("o needs 16-byte aligned rows");
+  if (p.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < p.bytes)) return bad("workspace is NULL, not 256-byte aligned or too small");
+  if (x->rows == 0) return clear_error();
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint8_t* w8 = static_cast<uint8_t*>(ws);
+  const wm_cache& c = x->cache;
+  Args a = {};
+  a.q = x->q; a.ld_q = x->ld_q;
+  a.k = c.k; a.v = c.v;
+  a.off = x->off; a.status = x->status; a.rows = x->rows; a.B = c.B; a.T_max = x->T_max;
+  a.scale = x->scale;
+  a.c2 = x->scale * LOG2E;
+  a.heads = x->heads; a.kv_heads = c.kv_heads; a.G = x->heads / c.kv_heads;
+  a.pages = c.pages; a.lens = c.lens; a.ppages = x->prefix_pages; a.plens = x->prefix_lens;
+  a.max_pages = c.max_pages; a.max_ppages = x->prefix_max_pages; a.len_max = x->len_max; a.plen_max = x->prefix_max;
+  a.n_pages = c.n_pages; a.lps = page_bits(c.page);
+  a.out = o;
+  a.ld_out = ld_o;
+  a.lse = lse;
+  a.parts = p.splits + p.shared_splits;
+  a.part = reinterpret_cast<float*>(w8 + p.o_part);
+  a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
+  a.part_rows = x->rows * x->heads;
+  WM_PF(TK_CACHED, cached(x, p, a, st));
+  return clear_error();
+}
+
+}  // extern "C"
