@@ -216,8 +216,8 @@ struct Prob {
 // false: none (a segment's pairs need not divide by the XCDs).  rows_per_tile: of the tiled axis (R, or Lk
 // for keys).
 template <bool KEYS, class Args>
-__device__ __forceinline__ bool problem(const Table& t, const Args& a, int rows_per_tile, Prob& p) {
-  const int x = blockIdx.x % XCDS, i = blockIdx.x / XCDS;
+__device__ __forceinline__ bool problem(const Table& t, const Args& a, int rows_per_tile, Prob& p, int block = blockIdx.x) {
+  const int x = block % XCDS, i = block / XCDS;
   int lo = 0, hi = t.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;

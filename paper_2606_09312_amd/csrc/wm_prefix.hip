@@ -40,6 +40,7 @@ struct Args {
   const int32_t *pages, *lens, *ppages, *plens;
   int max_pages, max_ppages, len_max, plen_max, n_pages, lps;      // lps: log2 of a page's slots
   int seq0, nseq, row_tiles;                // a launch by sequences; 0 row tiles: by programs
+  int32_t* flags;                           // one per workgroup of the launch (null: rows of a tile see the same keys)
 };
 
 // Offsets (and key counts) that do not fit are reported by the launch's threads together, once.
@@ -84,9 +85,11 @@ __device__ __forceinline__ int2 bounds_of(const Args& a, int from, int row, int 
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 __device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// A weight of 0 does not hide a value that is not finite from a product, and in a block of own keys that only some of the
-// rows see, the others' weights are 0.  So where sums come out that are not finite, the workgroup
-// goes through its loop a second time with mm_rows in mm_col's place for own keys.
+// A weight of 0 does not hide a value that is not finite from a product, and in a block of own keys that only some
+// of the rows see, the others' weights are 0.  So every workgroup leaves a flag whether its sums are
+// finite, and where they are not, a launch behind it does its rows (or keys) again, one by one over what they see
+// alone.  (As a second form of the loops in the same kernel it took the first's registers: dk and dv at a width
+// of 128 spilled 115 of them and took 3.6 ms for 1.7.)
 template <int DB>
 __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
   float z = 0.0f;
@@ -96,34 +99,9 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
     for (int r = 0; r < 16; ++r) z = fmaf(acc[b][r], 0.0f, z);
   return z != 0.0f;
 }
-// Tile::mm_col one row after the other, a lane's column taking those of m (bit acc_row(0, r) of its half).
-template <class T, int DH>
-__device__ __forceinline__ void mm_rows(const T* tile, int base, const f32x16& p, uint32_t m, f32x16 (&acc)[DH / 32], int lane) {
-  using TL = Tile<T, DH>;
-  const int h = lane >> 5;
-#pragma unroll 1
-  for (int row = 0; row < 32; ++row) {
-    const int half = (row >> 2) & 1, reg = (row & 3) | ((row >> 3) << 2);
-    float w = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) w = reg == r ? p[r] : w;
-    int use = (m >> acc_row(0, reg)) & 1;
-    const float w2 = __shfl_xor(w, 32);
-    const int use2 = __shfl_xor(use, 32);
-    w = h == half ? w : w2;
-    use = h == half ? use : use2;
-    if constexpr (IS_BF<T>) w = (float)(__bf16)w;
-    typedef T t4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-    for (int b = 0; b < DH / 32; ++b)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int f = 32 * b + acc_row(h, 4 * q);
-        const t4 x = *reinterpret_cast<const t4*>(tile + (base + row) * DH + ((f / TL::E) ^ TL::swz(base + row)) * TL::E + f % TL::E);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[b][4 * q + i] = use ? fmaf(w, (float)x[i], acc[b][4 * q + i]) : acc[b][4 * q + i];
-      }
-  }
+__device__ __forceinline__ void leave_flag(const Args& a, bool bad, int tid) {
+  bad = __syncthreads_or(bad);
+  if (tid == 0) a.flags[blockIdx.x] = bad;
 }
 
 // Page of a table, checked; lanes past the tile's pages have none.
@@ -157,6 +135,71 @@ __device__ __forceinline__ void copy_pages(const Args& a, const void* cache, int
   }
 }
 
+// A workgroup's rows (stacked rows of one key head from packed row q0 on, a tile of them), the program's keys and
+// own keys [o0, o1) that some row of the tile sees.
+struct Work {
+  int64_t q0, p0;                           // p0: dense, the program's first key row
+  int R, hk, tile, split, P, o0, o1;
+  int seq;                                  // dense: the sequence of the tile's first row
+  int before;                               // paged: row i of the sequence sees before + i + 1 own keys
+  const int32_t *own_table, *shared_table;  // paged
+};
+template <bool PAGED>
+__device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block, int blocks, int rows, int lane, Work& w) {
+  w.p0 = w.o0 = w.o1 = w.seq = 0;
+  w.own_table = w.shared_table = nullptr;
+  if constexpr (!PAGED) {
+    Prob p;
+    if (!problem<false>(t, a, rows, p, block)) return false;
+    w.q0 = p.q0; w.p0 = p.k0; w.R = p.R; w.hk = p.hk; w.split = p.split; w.P = p.Lk;
+    w.tile = (w.R + rows - 1) / rows - 1 - p.tile;            // the longest loops first
+    const int first = p.q0 + w.tile * rows / a.G;
+    w.seq = last_start(a.off, 0, a.B - 1, first, lane);
+    w.o0 = min(max(a.off[w.seq], p.q0), first);
+    w.o1 = p.q0 + (min((w.tile + 1) * rows, w.R) - 1) / a.G + 1;
+  } else {
+    int64_t n;
+    int seg = -1, seen = 0;
+    if (a.row_tiles) {
+      int at = xcd_tile(block, blocks);
+      w.split = at % a.splits; at /= a.splits;
+      w.tile = a.row_tiles - 1 - at % a.row_tiles; at /= a.row_tiles;
+      const int s = a.seq0 + at % a.nseq;
+      w.hk = at / a.nseq;
+      const int64_t x = a.off[s], y = a.off[s + 1];
+      w.q0 = min(max(x, (int64_t)0), a.rows);
+      n = min(min(max(y, w.q0), a.rows) - w.q0, (int64_t)a.T_max);
+      int g = 0, gh = t.n - 1;                                // the sequence's program
+      while (g < gh) {
+        const int mid = (g + gh + 1) >> 1;
+        if (t.seg[mid].q0 <= s) g = mid; else gh = mid - 1;
+      }
+      if (t.n > 0) seg = t.seg[g].k0;
+      w.own_table = a.pages + (int64_t)s * a.max_pages;
+      seen = min(max(a.lens[s], 0), a.len_max);
+    } else {
+      Prob p;
+      if (!problem<false>(t, a, rows, p, block)) return false;
+      w.hk = p.hk; w.tile = p.tile; w.split = p.split; seg = p.k0;
+      const int64_t x = a.off[p.q0], y = a.off[p.q0 + p.R / a.G / a.T_max];
+      w.q0 = min(max(x, (int64_t)0), a.rows);
+      n = min(min(max(y, w.q0), a.rows) - w.q0, (int64_t)(p.R / a.G));
+    }
+    w.R = (int)n * a.G;
+    if (w.tile * rows >= w.R) return false;
+    w.before = a.row_tiles ? seen - (int)n : INT32_MIN / 2;
+    w.o1 = max(w.before + (min((w.tile + 1) * rows, w.R) - 1) / a.G + 1, 0);
+    w.P = 0;
+    if (seg >= 0 && a.plens) {
+      const int x = a.plens[seg];
+      w.P = min(max(x, 0), a.plen_max);
+      if (x != w.P && a.status && lane == 0) atomicOr(a.status, ERRBIT_KEYS);
+      w.shared_table = a.ppages + (int64_t)seg * a.max_ppages;
+    }
+  }
+  return true;
+}
+
 // --------------------------------------------------------------------------
 // Forward.  A workgroup of 4 wavefronts takes 128 / WK rows (32 per wavefront); WK wavefronts share
 // rows and take every WK-th block of 32 keys.  Tiles of K and V are staged two deep; softmax online
@@ -178,73 +221,22 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   const int h = lane >> 5, wr = wave % WR, wk = wave / WR;
   if (a.part0 == 0) check_rows(a, tid);
 
-  // The workgroup's rows, the program's keys, own keys [o0, o1) and the interval of them that a lane's row sees.
-  int64_t q0;
-  int R, hk, tile, split, P, o0 = 0, o1 = 0, lo = 0, hi = 0, seg = 0;
-  int64_t p0 = 0;
-  const int32_t *own_table = nullptr, *shared_table = nullptr;
-  if constexpr (!PAGED) {
-    Prob p;
-    if (!problem<false>(t, a, 32 * WR, p)) return;
-    q0 = p.q0; R = p.R; hk = p.hk; split = p.split; P = p.Lk; p0 = p.k0;
-    tile = (R + 32 * WR - 1) / (32 * WR) - 1 - p.tile;        // the longest loops first
-  } else {
-    int64_t n;
-    if (a.row_tiles) {
-      int at = xcd_tile(blockIdx.x, gridDim.x);
-      split = at % a.splits; at /= a.splits;
-      tile = a.row_tiles - 1 - at % a.row_tiles; at /= a.row_tiles;
-      const int s = a.seq0 + at % a.nseq;
-      hk = at / a.nseq;
-      const int64_t x = a.off[s], y = a.off[s + 1];
-      q0 = min(max(x, (int64_t)0), a.rows);
-      n = min(min(max(y, q0), a.rows) - q0, (int64_t)a.T_max);
-      int g = 0, gh = t.n - 1;                                // the sequence's program
-      while (g < gh) {
-        const int mid = (g + gh + 1) >> 1;
-        if (t.seg[mid].q0 <= s) g = mid; else gh = mid - 1;
-      }
-      seg = t.n > 0 ? t.seg[g].k0 : -1;
-      own_table = a.pages + (int64_t)s * a.max_pages;
-      const int L = min(max(a.lens[s], 0), a.len_max);
-      // (hi is formed below; o1 holds what the row before the first sees)
-      o1 = L - (int)n;
-    } else {
-      Prob p;
-      if (!problem<false>(t, a, 32 * WR, p)) return;
-      hk = p.hk; tile = p.tile; split = p.split; seg = p.k0;
-      const int64_t x = a.off[p.q0], y = a.off[p.q0 + p.R / a.G / a.T_max];
-      q0 = min(max(x, (int64_t)0), a.rows);
-      n = min(min(max(y, q0), a.rows) - q0, (int64_t)(p.R / a.G));
-    }
-    R = (int)n * a.G;
-    if (tile * 32 * WR >= R) return;
-    P = 0;
-    if (seg >= 0 && a.plens) {
-      const int x = a.plens[seg];
-      P = min(max(x, 0), a.plen_max);
-      if (x != P && a.status && tid == 0) atomicOr(a.status, ERRBIT_KEYS);
-      shared_table = a.ppages + (int64_t)seg * a.max_ppages;
-    }
-  }
+  Work w;
+  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, lane, w)) return;
+  const int64_t q0 = w.q0, p0 = w.p0;
+  const int R = w.R, hk = w.hk, tile = w.tile, split = w.split, P = w.P, o0 = w.o0, o1 = w.o1;
   const int row = tile * (32 * WR) + wr * 32 + (lane & 31);   // may pass R: computed, not stored
   const int rr = min(row, R - 1), head = hk * a.G + rr % a.G;
   const int64_t qrow = q0 + rr / a.G;
-  const int last = (min((tile + 1) * (32 * WR), R) - 1) / a.G;         // the tile's last query
   typename TL::Op qf;
   TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
   TL::scale_op(qf, a.c2);
+  int lo = 0, hi;                                             // the own keys that the lane's row sees
   if constexpr (!PAGED) {
-    const int first = (int)q0 + tile * (32 * WR) / a.G, end = (int)q0 + R / a.G;
-    const int s = last_start(a.off, 0, a.B - 1, first, lane);
-    const int2 b = bounds_of(a, s, (int)qrow, lane_of((int)qrow, 31), (int)q0, end, lane);
-    lo = b.x;
+    lo = bounds_of(a, w.seq, (int)qrow, lane_of((int)qrow, 31), (int)q0, (int)q0 + R / a.G, lane).x;
     hi = (int)qrow + 1;
-    o0 = min(max(a.off[s], (int)q0), first);
-    o1 = (int)q0 + last + 1;
-  } else if (a.row_tiles) {
-    hi = max(o1 + rr / a.G + 1, 0);
-    o1 = max(o1 + last + 1, 0);
+  } else {
+    hi = max(w.before + rr / a.G + 1, 0);
   }
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
@@ -258,7 +250,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
       const bool own = ti >= nP;
       const int first = (own ? ti - nP : ti) * KB, len = own ? o1 : P;
       const int entry = (first >> a.lps) + lane;
-      pre[0] = page_id(a, own ? own_table : shared_table, entry, lane < max(KB >> a.lps, 1) && ((int64_t)entry << a.lps) < len);
+      pre[0] = page_id(a, own ? w.own_table : w.shared_table, entry, lane < max(KB >> a.lps, 1) && ((int64_t)entry << a.lps) < len);
     } else if (mask && ti < nP) {
 #pragma unroll
       for (int w = 0; w < NV; ++w) {
@@ -293,13 +285,9 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   };
 
   f32x16 acc[DB];
-  float mx, sum;
-  bool careful = false;
-again:
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
-  mx = -INFINITY;
-  sum = 0.0f;
+  float mx = -INFINITY, sum = 0.0f;
   bool started = false;                       // every row has a maximum
   if (t0 < t1) {
     look_ahead(t0);
@@ -380,18 +368,12 @@ again:
       }
       sum += bs;
 #pragma unroll
-      for (int kb = 0; kb < NB; ++kb) {
-        if (careful && own) mm_rows<T, DH>(vt, 32 * (kb * WK + wk), s[kb], seen[kb] >> (4 * h), acc, lane);
-        else TL::mm_col(vt, 32 * (kb * WK + wk), s[kb], acc, lane);
-      }
+      for (int kb = 0; kb < NB; ++kb) TL::mm_col(vt, 32 * (kb * WK + wk), s[kb], acc, lane);
     }
 #pragma unroll
     for (int w = 0; w < NV; ++w) vis[w] = next[w];
   }
-  if (t1 > nP && !careful && __syncthreads_or(not_finite<DB>(acc))) {
-    careful = true;
-    goto again;
-  }
+  if (a.flags) leave_flag(a, t1 > nP && not_finite<DB>(acc), tid);
   sum = pair_sum(sum);
   float m2 = mx == -INFINITY ? -INFINITY : log2_units<T>(mx, a.c2);
   if constexpr (WK > 1) {       // join the wavefronts that share rows
@@ -493,12 +475,11 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
   check_rows(a, tid);
-  Prob p;
-  if (!problem<false>(t, a, 128, p)) return;
-  const int tile = (p.R + 127) / 128 - 1 - p.tile;            // the longest loops first
-  const int row = tile * 128 + wave * 32 + (lane & 31);
-  const int rr = min(row, p.R - 1), head = p.hk * a.G + rr % a.G;
-  const int64_t qrow = (int64_t)p.q0 + rr / a.G, orow = qrow * a.heads + head;
+  Work w;
+  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, lane, w)) return;
+  const int row = w.tile * 128 + wave * 32 + (lane & 31);
+  const int rr = min(row, w.R - 1), head = w.hk * a.G + rr % a.G;
+  const int64_t qrow = w.q0 + rr / a.G, orow = qrow * a.heads + head;
   typename TL::Op qf, gf;
   TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
   TL::scale_op(qf, a.c2);
@@ -512,20 +493,17 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const float lse = a.lse[orow];
   // a row that saw only keys of weight 0 has lse = -inf: its P is 0
   const float l2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
-  const int split = p.split;
-  if (split == 0 && h == 0 && row < p.R) {
+  const int split = w.split;
+  if (split == 0 && h == 0 && row < w.R) {
     a.stat[2 * orow] = l2;
     a.stat[2 * orow + 1] = delta;
   }
-  const int first = p.q0 + tile * 128 / a.G, end = p.q0 + p.R / a.G, last = (min((tile + 1) * 128, p.R) - 1) / a.G;
-  const int s0 = last_start(a.off, 0, a.B - 1, first, lane);
-  const int lo = bounds_of(a, s0, (int)qrow, lane_of((int)qrow, 31), p.q0, end, lane).x, hi = (int)qrow + 1;
-  const int o0 = min(max(a.off[s0], p.q0), first), o1 = p.q0 + last + 1;
+  const int lo = bounds_of(a, w.seq, (int)qrow, lane_of((int)qrow, 31), (int)w.q0, (int)w.q0 + w.R / a.G, lane).x, hi = (int)qrow + 1;
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
-  const int P = p.Lk, nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
+  const int P = w.P, o0 = w.o0, o1 = w.o1, nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
   const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
-  const uint8_t* mask = a.mask ? a.mask + p.k0 : nullptr;
+  const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
   auto mask_byte = [&](int ti) -> int {
     const int key = ti * KB + lane;
     return mask && (KB >= 64 || lane < KB) && key < P ? mask[key] : 0;
@@ -535,18 +513,16 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   };
   auto copy = [&](int ti, uint64_t v) {
     const bool own = ti >= nP;
-    const int64_t at = own ? (int64_t)o0 + (ti - nP) * KB : (int64_t)p.k0 + (int64_t)ti * KB;
+    const int64_t at = own ? (int64_t)o0 + (ti - nP) * KB : w.p0 + (int64_t)ti * KB;
     const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
-    const u32x4 kb = buffer_of(static_cast<const T*>(own ? a.k : a.pk) + at * lk + p.hk * DH, BAD - 1);
-    const u32x4 vb = buffer_of(static_cast<const T*>(own ? a.v : a.pv) + at * lv + p.hk * DH, BAD - 1);
+    const u32x4 kb = buffer_of(static_cast<const T*>(own ? a.k : a.pk) + at * lk + w.hk * DH, BAD - 1);
+    const u32x4 vb = buffer_of(static_cast<const T*>(own ? a.v : a.pv) + at * lv + w.hk * DH, BAD - 1);
     copy_tile<T, DH, KB, 256>(kb, ks + (ti & 1) * KB * DH, tid, [&](int r) { return (v >> r) & 1 ? (uint32_t)(r * lk * sizeof(T)) : BAD; });
     copy_tile<T, DH, KB, 256>(vb, vs + (ti & 1) * KB * DH, tid, [&](int r) { return (v >> r) & 1 ? (uint32_t)(r * lv * sizeof(T)) : BAD; });
   };
   f32x16 acc[DB];
   uint64_t vis = 0, next = 0;
   int mb = 0;
-  bool careful = false;
-again:
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
   if (t0 < t1) {
@@ -587,18 +563,34 @@ again:
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : 0.0f;
       }
-      if (careful && own) mm_rows<T, DH>(kt, 32 * kb, s, seen >> (4 * h), acc, lane);
-      else TL::mm_col(kt, 32 * kb, s, acc, lane);
+      TL::mm_col(kt, 32 * kb, s, acc, lane);
     }
     vis = next;
   }
-  if (t1 > nP && !careful && __syncthreads_or(not_finite<DB>(acc))) {
-    careful = true;
-    goto again;
-  }
-  if (row >= p.R) return;
+  if (a.flags) leave_flag(a, t1 > nP && not_finite<DB>(acc), tid);
+  if (row >= w.R) return;
   if (a.splits > 1) store_cols<float, DB>(a.part + (split * a.part_rows + orow) * DH, acc, a.scale, h);
   else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
+}
+
+// 128 own keys of a segment (of its n from q0 on), and the stacked rows [x0, x1) that see one of them.
+struct KeyWork {
+  int64_t q0;
+  int n, first, hk, split, seq, x0, x1, t0, t1;
+};
+__device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int block, int rows, int lane, KeyWork& w) {
+  Prob p;
+  if (!problem<true>(t, a, 128, p, block)) return false;
+  w.q0 = p.q0; w.n = p.Lk; w.first = p.tile * 128; w.hk = p.hk; w.split = p.split;
+  const int last = min(w.first + 128, w.n) - 1;
+  w.seq = last_start(a.off, 0, a.B - 1, p.q0 + w.first, lane);
+  const int s = last_start(a.off, w.seq, a.B - 1, p.q0 + last, lane);
+  w.x0 = w.first * a.G;
+  w.x1 = (max(min(a.off[s + 1], p.q0 + w.n), p.q0 + last + 1) - p.q0) * a.G;
+  const int tiles = (w.x1 - w.x0 + rows - 1) / rows;
+  w.t0 = (int)((int64_t)tiles * w.split / a.splits);
+  w.t1 = (int)((int64_t)tiles * (w.split + 1) / a.splits);
+  return true;
 }
 
 // dk and dv of 128 own keys (32 per wavefront, in registers as row operands): key j is seen by the rows from its
@@ -613,29 +605,22 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
   T* const gs = lds + 2 * RB * DH;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
-  Prob p;
-  if (!problem<true>(t, a, 128, p)) return;
-  const int key = p.tile * 128 + wave * 32 + (lane & 31), kc = min(key, p.Lk - 1);
-  const int krow = p.q0 + kc;
+  KeyWork w;
+  if (!key_work_of(t, a, blockIdx.x, RB, lane, w)) return;
+  const int key = w.first + wave * 32 + (lane & 31), kc = min(key, w.n - 1);
+  const int q0 = (int)w.q0, krow = q0 + kc, hk = w.hk, split = w.split, x0 = w.x0, x1 = w.x1, t0 = w.t0, t1 = w.t1;
   typename TL::Op kf, vf;
-  TL::load_op(kf, static_cast<const T*>(a.k) + krow * a.ld_k + p.hk * DH, h);
-  TL::load_op(vf, static_cast<const T*>(a.v) + krow * a.ld_v + p.hk * DH, h);
+  TL::load_op(kf, static_cast<const T*>(a.k) + krow * a.ld_k + hk * DH, h);
+  TL::load_op(vf, static_cast<const T*>(a.v) + krow * a.ld_v + hk * DH, h);
   TL::scale_op(kf, a.c2);
-  // stacked rows of the segment that see a lane's key: [lo, hi); of the workgroup's keys: [x0, x1)
-  const int first = p.tile * 128, lastk = min(first + 128, p.Lk) - 1, end = p.q0 + p.Lk;
-  const int s0 = last_start(a.off, 0, a.B - 1, p.q0 + first, lane);
-  const int s1 = last_start(a.off, s0, a.B - 1, p.q0 + lastk, lane);
-  const int2 b = bounds_of(a, s0, krow, lane_of(krow, 31), p.q0, end, lane);
-  const int lo = kc * a.G, hi = (b.y - p.q0) * a.G;
-  const int x0 = first * a.G, x1 = (max(min(a.off[s1 + 1], end), p.q0 + lastk + 1) - p.q0) * a.G;
+  // stacked rows of the segment that see a lane's key: [lo, hi)
+  const int lo = kc * a.G, hi = (bounds_of(a, w.seq, krow, lane_of(krow, 31), q0, q0 + w.n, lane).y - q0) * a.G;
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
-  const int tiles = (x1 - x0 + RB - 1) / RB, split = p.split;
-  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
   auto copy = [&](int ti) {
     const int r0 = x0 + ti * RB, q1 = r0 / a.G;              // the tile's first query
-    const u32x4 qb = buffer_of(static_cast<const T*>(a.q) + ((int64_t)p.q0 + q1) * a.ld_q + p.hk * a.G * DH, BAD - 1);
-    const u32x4 gb = buffer_of(static_cast<const T*>(a.d_o) + ((int64_t)p.q0 + q1) * a.ld_do + p.hk * a.G * DH, BAD - 1);
+    const u32x4 qb = buffer_of(static_cast<const T*>(a.q) + (w.q0 + q1) * a.ld_q + hk * a.G * DH, BAD - 1);
+    const u32x4 gb = buffer_of(static_cast<const T*>(a.d_o) + (w.q0 + q1) * a.ld_do + hk * a.G * DH, BAD - 1);
     auto off = [&](int r, int64_t ld) {
       const int x = r0 + r, qi = x / a.G;
       return x < x1 ? (uint32_t)(((qi - q1) * ld + (x - qi * a.G) * DH) * sizeof(T)) : BAD;
@@ -649,7 +634,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
     const int x = x0 + ti * RB + tid;
     if (tid < RB && x < x1) {
       const int qi = x / a.G;
-      sv = *reinterpret_cast<const float2*>(a.stat + 2 * (((int64_t)p.q0 + qi) * a.heads + p.hk * a.G + x - qi * a.G));
+      sv = *reinterpret_cast<const float2*>(a.stat + 2 * ((w.q0 + qi) * a.heads + hk * a.G + x - qi * a.G));
     }
   };
   auto put_stat = [&](int ti) {
@@ -659,8 +644,6 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
     }
   };
   f32x16 dk[DB], dv[DB];
-  bool careful = false;
-again:
 #pragma unroll
   for (int i = 0; i < DB; ++i) dk[i] = dv[i] = f32x16{};
   if (t0 < t1) {
@@ -689,9 +672,8 @@ again:
         s[r] = weight<T>(s[r], a.c2, l2[r]);
         dp[r] -= de[r];
       }
-      const uint32_t m = (below(hi - r0) & ~below(lo - r0)) >> (4 * h);
       if (lo_z > r0 || hi_a < r0 + 32) {
-        uint32_t see = m;
+        uint32_t see = (below(hi - r0) & ~below(lo - r0)) >> (4 * h);
         asm volatile("" : "+v"(see));             // keeps this a branch
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -699,27 +681,207 @@ again:
           dp[r] = (see >> acc_row(0, r)) & 1 ? dp[r] : 0.0f;
         }
       }
-      if (careful) mm_rows<T, DH>(gt, 32 * rb, s, m, dv, lane);
-      else TL::mm_col(gt, 32 * rb, s, dv, lane);
+      TL::mm_col(gt, 32 * rb, s, dv, lane);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] *= dp[r];
-      if (careful) mm_rows<T, DH>(qt, 32 * rb, s, m, dk, lane);
-      else TL::mm_col(qt, 32 * rb, s, dk, lane);
+      TL::mm_col(qt, 32 * rb, s, dk, lane);
     }
     if (ti + 1 < t1) put_stat(ti + 1);
   }
-  if (!careful && __syncthreads_or(not_finite<DB>(dk) || not_finite<DB>(dv))) {
-    careful = true;
-    goto again;
-  }
-  if (key >= p.Lk) return;
+  if (a.flags) leave_flag(a, not_finite<DB>(dk) || not_finite<DB>(dv), tid);
+  if (key >= w.n) return;
   if (a.splits > 1) {
-    const int64_t prow = (int64_t)krow * a.kv_heads + p.hk;
+    const int64_t prow = (int64_t)krow * a.kv_heads + hk;
     store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
     store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
   } else {
-    store_cols<T, DB>(static_cast<T*>(a.out) + krow * a.ld_out + p.hk * DH, dk, a.scale, h);
-    store_cols<T, DB>(static_cast<T*>(a.out2) + krow * a.ld_out2 + p.hk * DH, dv, 1.0f, h);
+    store_cols<T, DB>(static_cast<T*>(a.out) + krow * a.ld_out + hk * DH, dk, a.scale, h);
+    store_cols<T, DB>(static_cast<T*>(a.out2) + krow * a.ld_out2 + hk * DH, dv, 1.0f, h);
+  }
+}
+
+// --------------------------------------------------------------------------
+// Workgroups whose sums are not finite, again: a wavefront takes every fourth row (key) of the workgroup's and its lanes
+// 64 of the keys (rows) that it sees at a time, then its features.
+__device__ __forceinline__ float wave_max(float v) {
+  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+template <class T>
+__device__ __forceinline__ float dot(const T* x, const T* y, int n) {
+  float d = 0.0f;
+  for (int i = 0; i < n; ++i) d = fmaf((float)x[i], (float)y[i], d);
+  return d;
+}
+// Features lane and lane + 64 of the lanes' rows base + at, weighted by their w, one after the other.
+template <class T, int DH>
+__device__ __forceinline__ void add_rows(float& lower, float& upper, float w, uint64_t used, const T* base, int64_t at, int lane) {
+  for (int i = 0; i < 64; ++i) {
+    if (!((used >> i) & 1)) continue;
+    const float wi = __shfl(w, i);
+    const T* x = base + __shfl(at, i);
+    if (lane < DH) lower = fmaf(wi, (float)x[lane], lower);
+    if (DH > 64) upper = fmaf(wi, (float)x[lane + 64], upper);
+  }
+}
+template <class T, int DH>
+__device__ __forceinline__ void store_lane(T* row, float lower, float upper, int lane) {
+  if (lane < DH) row[lane] = (T)lower;
+  if (DH > 64) row[lane + 64] = (T)upper;
+}
+// Element of key i of a run (its program's, or own) in k or v; -1: its page does not exist, it reads as zero.
+template <int DH, bool PAGED>
+__device__ __forceinline__ int64_t key_at(const Args& a, const Work& w, bool own, int i, bool value) {
+  if constexpr (PAGED) {
+    const int id = (own ? w.own_table : w.shared_table)[i >> a.lps];
+    if (id < 0 || id >= a.n_pages) return -1;
+    return ((((int64_t)id * a.kv_heads + w.hk) << a.lps) + (i & ((1 << a.lps) - 1))) * DH;
+  } else {
+    return (own ? i * (value ? a.ld_v : a.ld_k) : (w.p0 + i) * (value ? a.ld_pv : a.ld_pk)) + w.hk * DH;
+  }
+}
+
+// The part of the loop that a workgroup has, in keys of the program and own keys.
+struct Span {
+  int p_lo, p_hi, o_lo, o_hi;
+};
+__device__ __forceinline__ Span span_of(const Args& a, const Work& w, int KB) {
+  const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.o1 - w.o0 + KB - 1) / KB;
+  const int t0 = (int)((int64_t)tiles * w.split / a.splits), t1 = (int)((int64_t)tiles * (w.split + 1) / a.splits);
+  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, min(w.o0 + max(t1 - nP, 0) * KB, w.o1)};
+}
+// Own keys that a row sees.
+template <bool PAGED>
+__device__ __forceinline__ int2 seen_by(const Args& a, const Work& w, int row, int lane) {
+  if constexpr (PAGED) {
+    return make_int2(0, max(w.before + row / a.G + 1, 0));
+  } else {
+    const int qrow = (int)w.q0 + row / a.G, s = last_start(a.off, w.seq, a.B - 1, qrow, lane);
+    return make_int2(min(max(a.off[s], (int)w.q0), qrow), qrow + 1);
+  }
+}
+
+template <class T, int DH, bool PAGED>
+__global__ __launch_bounds__(256) void forward_again_kernel(const Table t, const Args a, int rows, int KB) {
+  if (!a.flags[blockIdx.x]) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Work w;
+  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, rows, lane, w)) return;
+  const Span sp = span_of(a, w, KB);
+  for (int row = w.tile * rows + wave; row < min((w.tile + 1) * rows, w.R); row += 4) {
+    const int head = w.hk * a.G + row % a.G;
+    const int64_t qrow = w.q0 + row / a.G, orow = qrow * a.heads + head;
+    const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
+    const int2 see = seen_by<PAGED>(a, w, row, lane);
+    float top = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
+    for (int own = 0; own < 2; ++own) {
+      const T* kb = static_cast<const T*>(own || PAGED ? a.k : a.pk);
+      const T* vb = static_cast<const T*>(own || PAGED ? a.v : a.pv);
+      const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
+      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        const bool shown = i < end && (own || PAGED || !a.mask || a.mask[w.p0 + i] != 0);
+        const int64_t at = shown ? key_at<DH, PAGED>(a, w, own, i, false) : -1, vat = shown ? key_at<DH, PAGED>(a, w, own, i, true) : -1;
+        const float s = !shown ? -INFINITY : at < 0 ? 0.0f : dot(q, kb + at, DH) * a.c2;
+        const float m = wave_max(s), f = m > top ? exp2_of(top - m) : 1.0f;
+        top = m > top ? m : top;
+        const float p = shown ? exp2_of(s - (top == -INFINITY ? 0.0f : top)) : 0.0f;
+        sum = sum * f + wave_sum(p);
+        x *= f;
+        y *= f;
+        add_rows<T, DH>(x, y, p, __ballot(vat >= 0), vb, vat, lane);
+      }
+    }
+    if (a.parts > 1) {
+      const int64_t prow = (int64_t)(a.part0 + w.split) * a.part_rows + orow;
+      store_lane<float, DH>(a.part + prow * DH, x, y, lane);
+      if (lane == 0) {
+        a.part_ml[2 * prow] = top;
+        a.part_ml[2 * prow + 1] = sum;
+      }
+    } else {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      store_lane<T, DH>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, x * inv, y * inv, lane);
+      if (a.lse && lane == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+    }
+  }
+}
+
+template <class T, int DH>
+__global__ __launch_bounds__(256) void dq_again_kernel(const Table t, const Args a) {
+  if (!a.flags[blockIdx.x]) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Work w;
+  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, lane, w)) return;
+  const Span sp = span_of(a, w, TILE_ROWS<T, DH>);
+  for (int row = w.tile * 128 + wave; row < min((w.tile + 1) * 128, w.R); row += 4) {
+    const int head = w.hk * a.G + row % a.G;
+    const int64_t qrow = w.q0 + row / a.G, orow = qrow * a.heads + head;
+    const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
+    const T* g = static_cast<const T*>(a.d_o) + qrow * a.ld_do + head * DH;
+    const int2 see = seen_by<false>(a, w, row, lane);
+    const float l2 = a.stat[2 * orow], delta = a.stat[2 * orow + 1];
+    float x = 0.0f, y = 0.0f;
+    for (int own = 0; own < 2; ++own) {
+      const T* kb = static_cast<const T*>(own ? a.k : a.pk);
+      const T* vb = static_cast<const T*>(own ? a.v : a.pv);
+      const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
+      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        const bool shown = i < end && (own || !a.mask || a.mask[w.p0 + i] != 0);
+        const int64_t at = shown ? key_at<DH, false>(a, w, own, i, false) : 0;
+        float ds = 0.0f;
+        if (shown) ds = exp2_of(fmaf(dot(q, kb + at, DH), a.c2, -l2)) * (dot(g, vb + key_at<DH, false>(a, w, own, i, true), DH) - delta);
+        add_rows<T, DH>(x, y, ds, __ballot(shown), kb, at, lane);
+      }
+    }
+    x *= a.scale;
+    y *= a.scale;
+    if (a.splits > 1) store_lane<float, DH>(a.part + (w.split * a.part_rows + orow) * DH, x, y, lane);
+    else store_lane<T, DH>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, x, y, lane);
+  }
+}
+
+template <class T, int DH>
+__global__ __launch_bounds__(256) void dkv_again_kernel(const Table t, const Args a) {
+  if (!a.flags[blockIdx.x]) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  KeyWork w;
+  if (!key_work_of(t, a, blockIdx.x, TILE_ROWS<T, DH>, lane, w)) return;
+  for (int key = w.first + wave; key < min(w.first + 128, w.n); key += 4) {
+    const int64_t krow = w.q0 + key;
+    const T* k = static_cast<const T*>(a.k) + krow * a.ld_k + w.hk * DH;
+    const T* v = static_cast<const T*>(a.v) + krow * a.ld_v + w.hk * DH;
+    const int s = last_start(a.off, w.seq, a.B - 1, (int)krow, lane);
+    const int hi = (max(min(a.off[s + 1], (int)w.q0 + w.n), (int)krow + 1) - (int)w.q0) * a.G;
+    const int end = min(min(w.x0 + w.t1 * TILE_ROWS<T, DH>, w.x1), hi);
+    float kx = 0.0f, ky = 0.0f, vx = 0.0f, vy = 0.0f;
+    for (int x0 = max(w.x0 + w.t0 * TILE_ROWS<T, DH>, key * a.G); x0 < end; x0 += 64) {
+      const int x = min(x0 + lane, end - 1), head = w.hk * a.G + x % a.G;
+      const int64_t qrow = w.q0 + x / a.G, orow = qrow * a.heads + head;
+      const int64_t qat = qrow * a.ld_q + head * DH, gat = qrow * a.ld_do + head * DH;
+      const T* q = static_cast<const T*>(a.q);
+      const T* g = static_cast<const T*>(a.d_o);
+      const float p = exp2_of(fmaf(dot(q + qat, k, DH), a.c2, -a.stat[2 * orow]));
+      const float ds = p * (dot(g + gat, v, DH) - a.stat[2 * orow + 1]);
+      const uint64_t used = __ballot(x0 + lane < end);
+      add_rows<T, DH>(vx, vy, p, used, g, gat, lane);
+      add_rows<T, DH>(kx, ky, ds, used, q, qat, lane);
+    }
+    kx *= a.scale;
+    ky *= a.scale;
+    if (a.splits > 1) {
+      const int64_t prow = krow * a.kv_heads + w.hk;
+      store_lane<float, DH>(a.part + ((2 * w.split) * a.part_rows + prow) * DH, kx, ky, lane);
+      store_lane<float, DH>(a.part + ((2 * w.split + 1) * a.part_rows + prow) * DH, vx, vy, lane);
+    } else {
+      store_lane<T, DH>(static_cast<T*>(a.out) + krow * a.ld_out + w.hk * DH, kx, ky, lane);
+      store_lane<T, DH>(static_cast<T*>(a.out2) + krow * a.ld_out2 + w.hk * DH, vx, vy, lane);
+    }
   }
 }
 
@@ -777,8 +939,11 @@ struct Plan {
   Shared sh;
   bool few;
   int fwd_splits, dq_splits, dkv_splits;
-  size_t o_part, o_ml, o_stat, bytes;
+  size_t o_part, o_ml, o_stat, o_flags, bytes;
 };
+
+// a launch's workgroups: its work, dealt out over the XCDs by segment
+int64_t most_blocks(int64_t work, int S) { return work + XCDS * std::min(S, MAX_SEGS); }
 
 wm_status check(const wm_prefix* a, Plan* p, bool grad) {
   if (!a) return bad("prefix attention arguments are NULL");
@@ -826,14 +991,18 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
                              step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh));
   if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
-  p->o_part = p->o_ml = p->o_stat = 0;
+  p->o_part = p->o_ml = p->o_stat = p->o_flags = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   if (!grad) {
+    if (nq > 0) p->o_flags = take((size_t)most_blocks((p->few ? few_tiles : row_tiles) * w->kv_heads * p->fwd_splits, w->S) * 4);
     if (p->fwd_splits > 1) {
       p->o_part = take((size_t)p->fwd_splits * rows_all * dh * 4);
       p->o_ml = take((size_t)p->fwd_splits * rows_all * 8);
     }
   } else {
+    if (nq > 0)
+      p->o_flags = take((size_t)std::max(most_blocks(row_tiles * w->kv_heads * p->dq_splits, w->S),
+                                         most_blocks(key_tiles * w->kv_heads * p->dkv_splits, w->S)) * 4);
     p->o_stat = take((size_t)rows_all * 8);
     size_t part = p->sh.part_bytes;              // dq's, own keys' and the programs' keys', one after the other on the stream
     if (p->dq_splits > 1) part = std::max(part, (size_t)p->dq_splits * rows_all * dh * 4);
@@ -874,6 +1043,8 @@ hipError_t forward(const wm_attention* w, const Plan& p, const Args& a, hipStrea
                               const dim3 grid(blocks);
                               if (p.few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, false>), grid, dim3(256), 0, st, t, a);
                               else hipLaunchKernelGGL((forward_kernel<T, DH, 1, false>), grid, dim3(256), 0, st, t, a);
+                              hipLaunchKernelGGL((forward_again_kernel<T, DH, false>), grid, dim3(256), 0, st, t, a, rows,
+                                                 p.few ? 32 * WK : TILE_ROWS<T, DH>);
                             });
     if (e != hipSuccess || a.parts == 1) return e;
     return join<T, DH>(a, p.sh.nq * a.heads, st);
@@ -887,6 +1058,7 @@ hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStr
     hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, 128); },
                             [&](const Table& t, int blocks) {
                               hipLaunchKernelGGL((dq_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
+                              hipLaunchKernelGGL((dq_again_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.sh.nq * a.heads;
@@ -905,6 +1077,7 @@ hipError_t grad_own_keys(const wm_attention* w, const Plan& p, const Args& a, hi
     hipError_t e = each_run(&own, true, a.splits, [&](int64_t, int64_t lk) { return cdiv(lk, 128); },
                             [&](const Table& t, int blocks) {
                               hipLaunchKernelGGL((dkv_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
+                              hipLaunchKernelGGL((dkv_again_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.sh.nq * a.kv_heads;
@@ -921,7 +1094,7 @@ struct CachedPlan {
   bool few, shared_few;           // rows of 32 per workgroup, its wavefronts sharing them
   int splits, shared_splits;
   int64_t most_rows;              // stacked rows of a program, at most
-  size_t o_part, o_ml, bytes;
+  size_t o_part, o_ml, o_flags, bytes;
 };
 
 wm_status check(const wm_cached* a, CachedPlan* p) {
@@ -978,9 +1151,10 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   }
   if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
-  p->o_part = p->o_ml = 0;
+  p->o_part = p->o_ml = p->o_flags = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   const int parts = p->splits + p->shared_splits;
+  if (a->T_max > 1 && a->rows > 0) p->o_flags = take((size_t)tiles * p->splits * 4);
   if (parts > 1) {
     p->o_part = take((size_t)parts * rows_all * dh * 4);
     p->o_ml = take((size_t)parts * rows_all * 8);
@@ -1000,6 +1174,8 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
       const dim3 grid((unsigned)blocks);
       if (few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, true>), grid, dim3(256), 0, st, t, a);
       else hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), grid, dim3(256), 0, st, t, a);
+      if (a.flags) hipLaunchKernelGGL((forward_again_kernel<T, DH, true>), grid, dim3(256), 0, st, t, a, few ? 128 / WK : 128,
+                                      few ? 32 * WK : TILE_ROWS<T, DH>);
       e = hipGetLastError();
     };
     const int64_t seq_rows = std::min<int64_t>(x->T_max, x->rows) * a.G;
@@ -1026,6 +1202,7 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
     // by programs
     if (!p.joint) {
       a.plens = plens;
+      a.flags = nullptr;            // all its rows see all its keys
       a.part0 = p.splits;
       a.splits = p.shared_splits;
       a.row_tiles = 0;
@@ -1082,6 +1259,7 @@ wm_status wm_prefix_attention(const wm_prefix* x, void* o, int64_t ld_o, float* 
   a.splits = a.parts = p.fwd_splits;
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
+  a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
   a.part_rows = p.sh.nq * w->heads;
   WM_PF(TK_PREFIX, forward(w, p, a, st));
   return clear_error();
@@ -1109,6 +1287,7 @@ wm_status wm_prefix_attention_grad(const wm_prefix* x, const void* o, int64_t ld
   a.lse = const_cast<float*>(lse);
   a.stat = reinterpret_cast<float*>(w8 + p.o_stat);
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
+  a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
   if (nq > 0) {
     a.out = g->dq; a.ld_out = g->ld_dq;
     a.splits = p.dq_splits;
@@ -1155,6 +1334,8 @@ wm_status wm_cached_attention(const wm_cached* x, void* o, int64_t ld_o, float* 
   a.parts = p.splits + p.shared_splits;
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
+  // one row per sequence: the rows of a tile see the same keys
+  a.flags = x->T_max > 1 ? reinterpret_cast<int32_t*>(w8 + p.o_flags) : nullptr;
   a.part_rows = x->rows * x->heads;
   WM_PF(TK_CACHED, cached(x, p, a, st));
   return clear_error();
