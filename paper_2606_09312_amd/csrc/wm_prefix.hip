@@ -27,7 +27,8 @@ struct Args {
   int64_t rows;
   int B, T_max;
   float c2, scale;                          // scale log2(e), scale
-  int heads, kv_heads, G, splits;
+  int heads, kv_heads, G;
+  int splits, chunk;                        // a loop's shares: `chunk` tiles each, the last what is left
   void *out, *out2;                         // o; dq; dk and dv
   int64_t ld_out, ld_out2;
   float* lse;                               // forward: out (may be null); gradient: in
@@ -40,8 +41,16 @@ struct Args {
   const int32_t *pages, *lens, *ppages, *plens;
   int max_pages, max_ppages, len_max, plen_max, n_pages, lps;      // lps: log2 of a page's slots
   int seq0, nseq, row_tiles;                // a launch by sequences; 0 row tiles: by programs
+  int joint;                                // by sequences: their programs' keys first
+  int more_blocks, more_splits, more_chunk, more_part0;            // the few-row kernel: its first workgroups go by programs
   int32_t* flags;                           // one per workgroup of the launch (null: rows of a tile see the same keys)
 };
+
+// Tiles [x, y) of a loop that a split takes.
+__device__ __forceinline__ int2 share_of(const Args& a, int tiles, int split) {
+  const int64_t x = (int64_t)a.chunk * split;
+  return make_int2((int)min(x, (int64_t)tiles), split == a.splits - 1 ? tiles : (int)min(x + a.chunk, (int64_t)tiles));
+}
 
 // Offsets (and key counts) that do not fit are reported by the launch's threads together, once.
 __device__ __forceinline__ void check_rows(const Args& a, int tid) {
@@ -113,6 +122,23 @@ __device__ __forceinline__ int page_id(const Args& a, const int32_t* table, int 
   return -1;
 }
 
+// Rows of a matrix (stride ld elements) into a tile: the first n of them, others read as zero.  The buffer ends with the last
+// row, so that what a lane adds to its base is the same for every tile; `some`: of the n only those of `vis`.
+template <class T, int DH, int ROWS, int NT, int NV>
+__device__ __forceinline__ void copy_rows(const T* base, int ld, int n, bool some, const uint64_t (&vis)[NV], T* tile, int tid) {
+  using TL = Tile<T, DH>;
+  constexpr int N = ROWS * TL::UPR / NT;
+  n = min(n, ROWS);
+  const u32x4 buf = buffer_of(base, n > 0 ? (uint32_t)(((n - 1) * ld + DH) * sizeof(T)) : 0u);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int row = (i * NT + tid) / TL::UPR, unit = ((i * NT + tid) % TL::UPR) ^ TL::swz(row);
+    uint32_t at = (uint32_t)(row * ld * sizeof(T) + unit * 16);
+    if (some) at = (vis[NV > 1 ? row >> 6 : 0] >> (row & 63)) & 1 ? at : BAD;
+    copy16(buf, tile + (size_t)(i * NT + (tid & ~63)) * TL::E, at);
+  }
+}
+
 // Keys [first, first + ROWS) of a page table, of which the first `len` exist, into a tile.  A page has at least 16
 // slots and a tile starts at a multiple of its length, so the 16 or fewer rows that one
 // instruction copies lie in one page, whose end (or the last key) bounds the buffer: rows past it
@@ -174,7 +200,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
         const int mid = (g + gh + 1) >> 1;
         if (t.seg[mid].q0 <= s) g = mid; else gh = mid - 1;
       }
-      if (t.n > 0) seg = t.seg[g].k0;
+      if (a.joint) seg = t.seg[g].k0;
       w.own_table = a.pages + (int64_t)s * a.max_pages;
       seen = min(max(a.lens[s], 0), a.len_max);
     } else {
@@ -190,7 +216,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
     w.before = a.row_tiles ? seen - (int)n : INT32_MIN / 2;
     w.o1 = max(w.before + (min((w.tile + 1) * rows, w.R) - 1) / a.G + 1, 0);
     w.P = 0;
-    if (seg >= 0 && a.plens) {
+    if (seg >= 0) {
       const int x = a.plens[seg];
       w.P = min(max(x, 0), a.plen_max);
       if (x != w.P && a.status && lane == 0) atomicOr(a.status, ERRBIT_KEYS);
@@ -241,7 +267,8 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
   const int nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
-  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int2 tt = share_of(a, tiles, split);
+  const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = !PAGED && a.mask ? a.mask + p0 : nullptr;
   // What a tile's copy needs from memory, loaded a tile ahead: mask bytes, or page numbers (lane l: page l).
   int pre[NV];
@@ -265,9 +292,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     for (int w = 0; w < NV; ++w)
       v[w] = mask && ti < nP ? __ballot(pre[w] != 0) : in_range(min((ti < nP ? P - ti * KB : o1 - o0 - (ti - nP) * KB) - 64 * w, KB));
   };
-  auto copy = [&](int ti, const uint64_t (&v)[NV]) {
-    T* const kt = ks + (ti & 1) * KB * DH;
-    T* const vt = vs + (ti & 1) * KB * DH;
+  auto copy = [&](int ti, const uint64_t (&v)[NV], T* kt, T* vt) {
     const bool own = ti >= nP;
     if constexpr (PAGED) {
       const int first = (own ? ti - nP : ti) * KB, len = own ? o1 : P;
@@ -275,12 +300,10 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
       copy_pages<T, DH, KB, 256>(a, a.v, hk, vt, first, len, pre[0], tid);
     } else {
       const int64_t first = own ? (int64_t)o0 + (ti - nP) * KB : p0 + (int64_t)ti * KB;
-      const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
-      const u32x4 kb = buffer_of(static_cast<const T*>(own ? a.k : a.pk) + first * lk + hk * DH, BAD - 1);
-      const u32x4 vb = buffer_of(static_cast<const T*>(own ? a.v : a.pv) + first * lv + hk * DH, BAD - 1);
-      auto seen = [&](int r) { return (v[NV > 1 ? r >> 6 : 0] >> (r & 63)) & 1; };
-      copy_tile<T, DH, KB, 256>(kb, kt, tid, [&](int r) { return seen(r) ? (uint32_t)(r * lk * sizeof(T)) : BAD; });
-      copy_tile<T, DH, KB, 256>(vb, vt, tid, [&](int r) { return seen(r) ? (uint32_t)(r * lv * sizeof(T)) : BAD; });
+      const int n = own ? o1 - o0 - (ti - nP) * KB : P - ti * KB;
+      const int lk = (int)(own ? a.ld_k : a.ld_pk), lv = (int)(own ? a.ld_v : a.ld_pv);
+      copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.k : a.pk) + first * lk + hk * DH, lk, n, mask && !own, v, kt, tid);
+      copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.v : a.pv) + first * lv + hk * DH, lv, n, mask && !own, v, vt, tid);
     }
   };
 
@@ -292,19 +315,21 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   if (t0 < t1) {
     look_ahead(t0);
     look(t0, vis);
-    copy(t0, vis);
+    copy(t0, vis, ks, vs);
     if (t0 + 1 < t1) look_ahead(t0 + 1);
   }
-  for (int ti = t0; ti < t1; ++ti) {
+  // a tile; the buffer it is in is known when the kernel is compiled, so that the reads' addresses stay in registers
+  auto step = [&](int ti, auto buffer) {
+    constexpr int BUF = decltype(buffer)::value;
     wait_counts<0, true>();
     raw_barrier();
     if (ti + 1 < t1) {
       look(ti + 1, next);
-      copy(ti + 1, next);
+      copy(ti + 1, next, ks + (BUF ^ 1) * KB * DH, vs + (BUF ^ 1) * KB * DH);
       if (ti + 2 < t1) look_ahead(ti + 2);
     }
-    const T* kt = ks + (ti & 1) * KB * DH;
-    const T* vt = vs + (ti & 1) * KB * DH;
+    const T* kt = ks + BUF * KB * DH;
+    const T* vt = vs + BUF * KB * DH;
     // Keys of the wavefront's blocks that a lane's row sees; own keys are skipped where no row sees any.
     const bool own = ti >= nP;
     const int at = own ? o0 + (ti - nP) * KB : 0;             // the tile's first own key
@@ -372,6 +397,10 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     }
 #pragma unroll
     for (int w = 0; w < NV; ++w) vis[w] = next[w];
+  };
+  for (int ti = t0; ti < t1; ti += 2) {
+    step(ti, std::integral_constant<int, 0>{});
+    if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
   if (a.flags) leave_flag(a, t1 > nP && not_finite<DB>(acc), tid);
   sum = pair_sum(sum);
@@ -417,6 +446,194 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   const int64_t orow = qrow * a.heads + head;
   if (a.parts > 1) {
     const int64_t prow = (int64_t)(a.part0 + split) * a.part_rows + orow;
+    if (sum != 0.0f) store_cols<float, DB>(a.part + prow * DH, acc, 1.0f, h);           // else no part
+    if (h == 0) {
+      a.part_ml[2 * prow] = m2;
+      a.part_ml[2 * prow + 1] = sum;
+    }
+    return;
+  }
+  store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, sum == 0.0f ? 0.0f : 1.0f / sum, h);
+  if (a.lse && h == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : (m2 + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// Single steps: at most 32 rows of a key head, over pages.  Each wavefront takes every fourth block of 32 keys and stages
+// K and V of its own, one block each: the next block's K is under way while the softmax and V's product run, its V
+// while the next scores are formed, and no wavefront waits for another.  What bounds it is reading k and v.
+template <class T, int DH>
+constexpr int FEW_LDS = 8 * 32 * DH * (int)sizeof(T);
+template <class T, int DH>
+constexpr int FEW_PER_CU = FEW_LDS<T, DH> > 80 * 1024 ? 1 : FEW_LDS<T, DH> > 40 * 1024 ? 2 : 4;
+template <class T, int DH>
+__global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Table t, const Args given) {
+  using TL = Tile<T, DH>;
+  constexpr int DB = TL::DB, KB = 128, N = 32 * TL::UPR / 64, RPI = 64 / TL::UPR;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[FEW_LDS<T, DH> + 1024];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  T* const kt = reinterpret_cast<T*>(lds) + wave * 2 * 32 * DH;
+  T* const vt = kt + 32 * DH;
+  Args a = given;
+  const bool by_program = (int)blockIdx.x < given.more_blocks;
+  if (by_program) {
+    a.splits = given.more_splits; a.chunk = given.more_chunk; a.part0 = given.more_part0;
+    a.row_tiles = 0;
+    a.flags = nullptr;
+  }
+  if (given.part0 == 0) check_rows(a, tid);
+  const int block = by_program ? blockIdx.x : blockIdx.x - given.more_blocks;
+  Work w;
+  if (!work_of<true>(t, a, block, by_program ? given.more_blocks : gridDim.x - given.more_blocks, 32, lane, w)) return;
+  const int row = w.tile * 32 + (lane & 31);                  // may pass R: computed, not stored
+  const int rr = min(row, w.R - 1), head = w.hk * a.G + rr % a.G;
+  const int64_t qrow = w.q0 + rr / a.G;
+  const int hi = max(w.before + rr / a.G + 1, 0), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
+  const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.o1 + KB - 1) / KB;
+  const int2 tt = share_of(a, tiles, w.split);
+
+  // a block's first key and how many of its keys exist; its pages (numbers come through scalar loads, which the copies'
+  // count of outstanding loads does not see)
+  struct Block {
+    int first, n, id0, id1;
+  };
+  auto block_of = [&](int ti) {
+    const bool own = ti >= nP;
+    Block b;
+    b.first = __builtin_amdgcn_readfirstlane((own ? ti - nP : ti) * KB + 32 * wave);
+    b.n = __builtin_amdgcn_readfirstlane(ti < tt.y ? min(max((own ? w.o1 : w.P) - b.first, 0), 32) : 0);
+    b.id0 = b.id1 = -1;
+    if (b.n > 0) {
+      const __attribute__((address_space(4))) int32_t* ids =
+          (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(own ? w.own_table : w.shared_table);
+      b.id0 = ids[b.first >> a.lps];
+      b.id1 = ids[(b.first + b.n - 1) >> a.lps];
+      if ((b.id0 < 0 || b.id0 >= a.n_pages || b.id1 < 0 || b.id1 >= a.n_pages) && a.status && lane == 0) atomicOr(a.status, ERRBIT_PAGE);
+    }
+    return b;
+  };
+  auto copy = [&](const void* cache, const Block& b, T* tile) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r0 = i * RPI, at = b.first + r0;              // the instruction's first row
+      const int id = (at >> a.lps) == (b.first >> a.lps) ? b.id0 : b.id1;
+      const bool ok = id >= 0 && id < a.n_pages;
+      const int64_t key = ((int64_t)(ok ? id : 0) * a.kv_heads + w.hk << a.lps) + (at & ((1 << a.lps) - 1));
+      const u32x4 buf = buffer_of(static_cast<const T*>(cache) + key * DH, ok ? (uint32_t)(min(max(b.n - r0, 0), RPI) * DH * sizeof(T)) : 0u);
+      const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(r0 + r);
+      copy16(buf, tile + (size_t)i * 64 * TL::E, (uint32_t)(r * DH * sizeof(T) + unit * 16));
+    }
+  };
+  f32x16 acc[DB];
+#pragma unroll
+  for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
+  float mx = -INFINITY, sum = 0.0f;
+  Block now = block_of(tt.x);
+  if (now.n > 0) {
+    copy(a.k, now, kt);
+    copy(a.v, now, vt);
+  }
+  typename TL::Op qf;
+  TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
+  TL::scale_op(qf, a.c2);
+  int ti = tt.x;
+  bool own = ti >= nP;
+  // A run's blocks of a wavefront end with the first that has no keys; the program's run goes over into the own keys'.
+  auto following = [&](int& tn) {
+    Block b = block_of(++tn);
+    if (b.n == 0 && tn <= nP && nP < tt.y) b = block_of(tn = nP);
+    return b;
+  };
+  if (now.n == 0 && ti < nP && nP < tt.y) {
+    now = block_of(ti = nP);
+    if (now.n > 0) {
+      copy(a.k, now, kt);
+      copy(a.v, now, vt);
+    }
+  }
+  while (now.n > 0) {
+    own = ti >= nP;
+    int tn = ti;
+    const Block next = following(tn);
+    wait_counts<N, true>();                                   // K is there
+    f32x16 s = TL::mm_row(kt, 0, qf, lane);
+    wait_counts<63, true>();
+    if (next.n > 0) copy(a.k, next, kt);
+    const uint32_t seen = own ? below(hi - now.first) & below(now.n) : below(now.n);
+    if (own ? hi_a < now.first + 32 : now.n < 32) {
+      const uint32_t m = seen >> (4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : -INFINITY;
+    }
+    float bm = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) bm = fmaxf(bm, s[r]);
+    bm = pair_max(bm);
+    const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, a.c2)) : 1.0f;
+    mx = bm > mx ? bm : mx;
+    const float mc = mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2);        // only keys of weight 0 so far
+    float bs = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = weight<T>(s[r], a.c2, mc);
+      bs += s[r];
+    }
+    sum = fmaf(sum, f, bs);
+    if (__any(f != 1.0f)) {
+#pragma unroll
+      for (int b = 0; b < DB; ++b) acc[b] *= f;
+    }
+    if (next.n > 0) wait_counts<N, false>(); else wait_counts<0, false>();    // V is there
+    TL::mm_col(vt, 0, s, acc, lane);
+    wait_counts<63, true>();
+    if (next.n > 0) copy(a.v, next, vt);
+    now = next;
+    ti = tn;
+  }
+  if (a.flags) {
+    const bool some = __syncthreads_or(tt.y > nP && not_finite<DB>(acc));
+    if (tid == 0) a.flags[block] = some;
+  }
+  sum = pair_sum(sum);
+  float m2 = mx == -INFINITY ? -INFINITY : log2_units<T>(mx, a.c2);
+  // join the wavefronts
+  constexpr int LW = DH + 4;
+  float* x = reinterpret_cast<float*>(lds);                   // [3][32][LW]
+  float* ml = x + 3 * 32 * LW;                                // [3][32][2]
+  static_assert((3 * 32 * LW + 192) * 4 <= sizeof(lds), "the exchange takes the tiles' place");
+  __syncthreads();
+  if (wave > 0) {
+    store_cols<float, DB>(x + ((wave - 1) * 32 + (lane & 31)) * LW, acc, 1.0f, h);
+    if (h == 0) {
+      ml[((wave - 1) * 32 + lane) * 2] = m2;
+      ml[((wave - 1) * 32 + lane) * 2 + 1] = sum;
+    }
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float top = m2;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) top = fmaxf(top, ml[(32 * k + (lane & 31)) * 2]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float f = exp2_of(m2 - ref);
+  sum *= f;
+#pragma unroll
+  for (int b = 0; b < DB; ++b) acc[b] *= f;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int l = 32 * k + (lane & 31);
+    f = exp2_of(ml[2 * l] - ref);
+    sum = fmaf(ml[2 * l + 1], f, sum);
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+      const f32x16 y = load_acc(x + l * LW + 32 * b, h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] = fmaf(y[r], f, acc[b][r]);
+    }
+  }
+  m2 = top;
+  if (row >= w.R) return;
+  const int64_t orow = qrow * a.heads + head;
+  if (a.parts > 1) {
+    const int64_t prow = (int64_t)(a.part0 + w.split) * a.part_rows + orow;
     if (sum != 0.0f) store_cols<float, DB>(a.part + prow * DH, acc, 1.0f, h);           // else no part
     if (h == 0) {
       a.part_ml[2 * prow] = m2;
@@ -502,7 +719,8 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
   const int P = w.P, o0 = w.o0, o1 = w.o1, nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
-  const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+  const int2 tt = share_of(a, tiles, split);
+  const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
   auto mask_byte = [&](int ti) -> int {
     const int key = ti * KB + lane;
@@ -511,14 +729,14 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   auto look = [&](int ti, int mb) -> uint64_t {
     return mask && ti < nP ? __ballot(mb != 0) : in_range(min(ti < nP ? P - ti * KB : o1 - o0 - (ti - nP) * KB, KB));
   };
-  auto copy = [&](int ti, uint64_t v) {
+  auto copy = [&](int ti, uint64_t vv, T* kt, T* vt) {
+    const uint64_t v[1] = {vv};
     const bool own = ti >= nP;
     const int64_t at = own ? (int64_t)o0 + (ti - nP) * KB : w.p0 + (int64_t)ti * KB;
-    const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
-    const u32x4 kb = buffer_of(static_cast<const T*>(own ? a.k : a.pk) + at * lk + w.hk * DH, BAD - 1);
-    const u32x4 vb = buffer_of(static_cast<const T*>(own ? a.v : a.pv) + at * lv + w.hk * DH, BAD - 1);
-    copy_tile<T, DH, KB, 256>(kb, ks + (ti & 1) * KB * DH, tid, [&](int r) { return (v >> r) & 1 ? (uint32_t)(r * lk * sizeof(T)) : BAD; });
-    copy_tile<T, DH, KB, 256>(vb, vs + (ti & 1) * KB * DH, tid, [&](int r) { return (v >> r) & 1 ? (uint32_t)(r * lv * sizeof(T)) : BAD; });
+    const int n = own ? o1 - o0 - (ti - nP) * KB : P - ti * KB;
+    const int lk = (int)(own ? a.ld_k : a.ld_pk), lv = (int)(own ? a.ld_v : a.ld_pv);
+    copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.k : a.pk) + at * lk + w.hk * DH, lk, n, mask && !own, v, kt, tid);
+    copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.v : a.pv) + at * lv + w.hk * DH, lv, n, mask && !own, v, vt, tid);
   };
   f32x16 acc[DB];
   uint64_t vis = 0, next = 0;
@@ -527,19 +745,20 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
   if (t0 < t1) {
     vis = look(t0, mask_byte(t0));
-    copy(t0, vis);
+    copy(t0, vis, ks, vs);
     if (t0 + 1 < t1) mb = mask_byte(t0 + 1);
   }
-  for (int ti = t0; ti < t1; ++ti) {
+  auto step = [&](int ti, auto buffer) {
+    constexpr int BUF = decltype(buffer)::value;
     wait_counts<0, true>();
     raw_barrier();
     if (ti + 1 < t1) {
       next = look(ti + 1, mb);
-      copy(ti + 1, next);
+      copy(ti + 1, next, ks + (BUF ^ 1) * KB * DH, vs + (BUF ^ 1) * KB * DH);
       if (ti + 2 < t1) mb = mask_byte(ti + 2);
     }
-    const T* kt = ks + (ti & 1) * KB * DH;
-    const T* vt = vs + (ti & 1) * KB * DH;
+    const T* kt = ks + BUF * KB * DH;
+    const T* vt = vs + BUF * KB * DH;
     const bool own = ti >= nP;
     const int at = own ? o0 + (ti - nP) * KB : 0;
 #pragma unroll
@@ -566,6 +785,10 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
       TL::mm_col(kt, 32 * kb, s, acc, lane);
     }
     vis = next;
+  };
+  for (int ti = t0; ti < t1; ti += 2) {
+    step(ti, std::integral_constant<int, 0>{});
+    if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
   if (a.flags) leave_flag(a, t1 > nP && not_finite<DB>(acc), tid);
   if (row >= w.R) return;
@@ -588,8 +811,9 @@ __device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int b
   w.x0 = w.first * a.G;
   w.x1 = (max(min(a.off[s + 1], p.q0 + w.n), p.q0 + last + 1) - p.q0) * a.G;
   const int tiles = (w.x1 - w.x0 + rows - 1) / rows;
-  w.t0 = (int)((int64_t)tiles * w.split / a.splits);
-  w.t1 = (int)((int64_t)tiles * (w.split + 1) / a.splits);
+  const int2 tt = share_of(a, tiles, w.split);
+  w.t0 = tt.x;
+  w.t1 = tt.y;
   return true;
 }
 
@@ -751,7 +975,8 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const Args& a, const Work& w, int KB) {
   const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.o1 - w.o0 + KB - 1) / KB;
-  const int t0 = (int)((int64_t)tiles * w.split / a.splits), t1 = (int)((int64_t)tiles * (w.split + 1) / a.splits);
+  const int2 tt = share_of(a, tiles, w.split);
+  const int t0 = tt.x, t1 = tt.y;
   return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, min(w.o0 + max(t1 - nP, 0) * KB, w.o1)};
 }
 // Own keys that a row sees.
@@ -917,6 +1142,28 @@ double few_us(bool bf, int64_t keys, int dh, int per_cu) {
 }
 double part_us(int64_t values, int dh) { return 2.0 * values * dh * 4 / 4.5e6; }
 
+// How loops are cut into splits of `chunk` tiles (long ones into more): `blocks` loops of `avg` tiles of unit_us each, `longest` at
+// most, on 256 x per_cu places.  The time is that of the fullest place, about half a chunk more than an even
+// share and at least a chunk, plus what a part costs to write and read.  A split of the longest loop keeps `least` tiles.
+struct Cut {
+  int splits, chunk;
+};
+Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_cu, double unit_us, double part_us) {
+  Cut best = {1, (int)std::max<int64_t>(longest, 1)};
+  const double places = 256.0 * per_cu, even = blocks * avg / places;
+  double cost = std::max({std::ceil(blocks / places) * avg, even + 0.5 * avg, (double)longest}) * unit_us;
+  for (int s = 2; s <= 64 && s <= longest / least; ++s) {
+    const int64_t chunk = cdiv(longest, s);
+    const double items = blocks * std::max(1.0, avg / chunk), own = std::min<double>(chunk, avg);
+    const double c = std::max({std::ceil(items / places) * own, even + 0.5 * own, (double)chunk}) * unit_us + (avg / chunk + 0.5) * part_us + 4.0;
+    if (c < 0.98 * cost) {
+      cost = c;
+      best = {(int)cdiv(longest, chunk), (int)chunk};
+    }
+  }
+  return best;
+}
+
 // Rows and keys per tile, workgroups that share a compute unit (registers, LDS).
 struct Shape {
   bool bf;
@@ -938,7 +1185,7 @@ bool too_wide(int64_t rows_all, int dh) { return rows_all > (int64_t)UINT32_MAX 
 struct Plan {
   Shared sh;
   bool few;
-  int fwd_splits, dq_splits, dkv_splits;
+  Cut fwd, dq, dkv;
   size_t o_part, o_ml, o_stat, o_flags, bytes;
 };
 
@@ -980,33 +1227,33 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
   auto avg = [](double steps, int64_t tiles) { return tiles ? steps / tiles : 0.0; };
   p->few = p->sh.max_r <= f.few_rows;
   if (p->few)
-    p->fwd_splits = splits_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu,
+    p->fwd = cut_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu,
                                few_us(f.bf, f.few_keys, dh, f.few_cu), part_us(rows_all, dh));
   else
-    p->fwd_splits = splits_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.fwd_cu,
+    p->fwd = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.fwd_cu,
                                step_us(f.bf, 2, 128, f.tile, dh, f.fwd_cu), part_us(rows_all, dh));
-  p->dq_splits = splits_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.dq_cu,
+  p->dq = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.dq_cu,
                             step_us(f.bf, 3, 128, f.tile, dh, f.dq_cu), part_us(rows_all, dh));
-  p->dkv_splits = splits_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu,
+  p->dkv = cut_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu,
                              step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh));
   if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
   p->o_part = p->o_ml = p->o_stat = p->o_flags = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   if (!grad) {
-    if (nq > 0) p->o_flags = take((size_t)most_blocks((p->few ? few_tiles : row_tiles) * w->kv_heads * p->fwd_splits, w->S) * 4);
-    if (p->fwd_splits > 1) {
-      p->o_part = take((size_t)p->fwd_splits * rows_all * dh * 4);
-      p->o_ml = take((size_t)p->fwd_splits * rows_all * 8);
+    if (nq > 0) p->o_flags = take((size_t)most_blocks((p->few ? few_tiles : row_tiles) * w->kv_heads * p->fwd.splits, w->S) * 4);
+    if (p->fwd.splits > 1) {
+      p->o_part = take((size_t)p->fwd.splits * rows_all * dh * 4);
+      p->o_ml = take((size_t)p->fwd.splits * rows_all * 8);
     }
   } else {
     if (nq > 0)
-      p->o_flags = take((size_t)std::max(most_blocks(row_tiles * w->kv_heads * p->dq_splits, w->S),
-                                         most_blocks(key_tiles * w->kv_heads * p->dkv_splits, w->S)) * 4);
+      p->o_flags = take((size_t)std::max(most_blocks(row_tiles * w->kv_heads * p->dq.splits, w->S),
+                                         most_blocks(key_tiles * w->kv_heads * p->dkv.splits, w->S)) * 4);
     p->o_stat = take((size_t)rows_all * 8);
     size_t part = p->sh.part_bytes;              // dq's, own keys' and the programs' keys', one after the other on the stream
-    if (p->dq_splits > 1) part = std::max(part, (size_t)p->dq_splits * rows_all * dh * 4);
-    if (p->dkv_splits > 1) part = std::max(part, (size_t)p->dkv_splits * 2 * kv_all * dh * 4);
+    if (p->dq.splits > 1) part = std::max(part, (size_t)p->dq.splits * rows_all * dh * 4);
+    if (p->dkv.splits > 1) part = std::max(part, (size_t)p->dkv.splits * 2 * kv_all * dh * 4);
     if (part) p->o_part = take(part);
   }
   p->bytes = workspace_of(at);
@@ -1092,7 +1339,7 @@ struct CachedPlan {
   wm_attention w;                 // types and widths
   bool joint;                     // one launch by sequences (their program's keys among them), no launch by programs
   bool few, shared_few;           // rows of 32 per workgroup, its wavefronts sharing them
-  int splits, shared_splits;
+  Cut own, shared;                // of the launch by sequences, by programs
   int64_t most_rows;              // stacked rows of a program, at most
   size_t o_part, o_ml, o_flags, bytes;
 };
@@ -1118,6 +1365,8 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   const int64_t seq_rows = std::min<int64_t>(a->T_max, std::max<int64_t>(a->rows, 1)) * G;
   int64_t most_seqs = 0, shared_tiles = 0, shared_few_tiles = 0;
   const Shape f = shape_of(c.dtype, dh);
+  constexpr int FEW_ROWS = 32, FEW_KEYS = 128;
+  const int few_cu = c.dtype == WM_BF16 ? (dh == 128 ? 2 : 4) : (dh == 128 ? 1 : dh == 64 ? 2 : 4);
   if (a->S > 0) {
     if (!a->seg_off || a->seg_off[0] != 0 || a->seg_off[a->S] != c.B) return bad("seg_off must run from 0 to B");
     for (int i = 0; i < a->S; ++i) {
@@ -1125,36 +1374,35 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
       if (n < 0) return bad("seg_off must not decrease");
       most_seqs = std::max(most_seqs, n);
       shared_tiles += cdiv(n * a->T_max * G, 128);
-      shared_few_tiles += cdiv(n * a->T_max * G, f.few_rows);
+      shared_few_tiles += cdiv(n * a->T_max * G, FEW_ROWS);
     }
     if (a->prefix_max < 0 || a->prefix_max > (int64_t)a->prefix_max_pages * c.page) return bad("prefix_max must be in [0, prefix_max_pages page]");
     if (!a->prefix_lens || (a->prefix_max_pages > 0 && !a->prefix_pages)) return bad("prefix_lens/prefix_pages is NULL");
   }
   if (most_seqs * a->T_max * G > INT32_MAX) return set_error(WM_ERR_UNSUPPORTED, "a program has more than 2^31 rows of one key head");
   const int P = a->S > 0 ? a->prefix_max : 0;
-  p->few = seq_rows <= f.few_rows;
+  p->few = seq_rows <= FEW_ROWS;
   p->most_rows = most_seqs * a->T_max * G;
-  p->shared_few = p->most_rows <= f.few_rows;
+  p->shared_few = p->most_rows <= FEW_ROWS;
   // Sequences of many rows fill a tile by themselves and read the program's keys along with their own.
   p->joint = P == 0 || most_seqs <= 1 || seq_rows >= 64;
-  const int rows = p->few ? f.few_rows : 128, keys = p->few ? f.few_keys : f.tile, cu = p->few ? f.few_cu : f.fwd_cu;
-  const int64_t tiles = c.B * cdiv(seq_rows, rows) * c.kv_heads, rows_all = a->rows * a->heads;
+  const int64_t tiles = c.B * cdiv(seq_rows, p->few ? FEW_ROWS : 128) * c.kv_heads, rows_all = a->rows * a->heads;
   if (tiles > MOST_TILES || shared_few_tiles * c.kv_heads > MOST_TILES) return set_error(WM_ERR_UNSUPPORTED, "too many row tiles");
-  auto us = [&](bool few, int k, int u) { return few ? few_us(f.bf, k, dh, u) : step_us(f.bf, 2, 128, k, dh, u); };
-  const int64_t steps = cdiv(a->len_max, keys) + (p->joint ? cdiv(P, keys) : 0);
-  p->splits = splits_for(tiles, (double)steps, steps, 2, cu, us(p->few, keys, cu), part_us(rows_all, dh));
-  p->shared_splits = 0;
-  if (!p->joint) {
-    const int sk = p->shared_few ? f.few_keys : f.tile, su = p->shared_few ? f.few_cu : f.fwd_cu;
-    p->shared_splits = splits_for((p->shared_few ? shared_few_tiles : shared_tiles) * c.kv_heads, (double)cdiv(P, sk), cdiv(P, sk), 2, su,
-                                  us(p->shared_few, sk, su), part_us(rows_all, dh));
-  }
+  // lengths are known to the device alone: loops of 0.6 of the longest on average
+  auto cut = [&](bool few, int64_t blocks, int64_t longest) {
+    const int keys = few ? FEW_KEYS : f.tile, cu = few ? few_cu : f.fwd_cu;
+    const int64_t steps = cdiv(longest, keys);
+    return cut_for(blocks, 0.6 * steps, steps, 2, cu, few ? few_us(f.bf, keys, dh, cu) : step_us(f.bf, 2, 128, keys, dh, cu), part_us(rows_all, dh));
+  };
+  p->own = cut(p->few, tiles, (int64_t)a->len_max + (p->joint ? P : 0));
+  p->shared = {0, 0};
+  if (!p->joint) p->shared = cut(p->shared_few, (p->shared_few ? shared_few_tiles : shared_tiles) * c.kv_heads, P);
   if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
   p->o_part = p->o_ml = p->o_flags = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
-  const int parts = p->splits + p->shared_splits;
-  if (a->T_max > 1 && a->rows > 0) p->o_flags = take((size_t)tiles * p->splits * 4);
+  const int parts = p->own.splits + p->shared.splits;
+  if (a->T_max > 1 && a->rows > 0) p->o_flags = take((size_t)tiles * p->own.splits * 4);
   if (parts > 1) {
     p->o_part = take((size_t)parts * rows_all * dh * 4);
     p->o_ml = take((size_t)parts * rows_all * 8);
@@ -1167,55 +1415,51 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
   return typed(&p.w, [&](auto tv, auto dh) {
     using T = decltype(tv);
     constexpr int DH = decltype(dh)::value;
-    constexpr int WK = (!IS_BF<T> && DH == 128) ? 2 : 4;
     hipError_t e = hipSuccess;
-    auto go = [&](const Table& t, int64_t blocks, bool few) {
-      if (blocks == 0 || e != hipSuccess) return;
-      const dim3 grid((unsigned)blocks);
-      if (few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, true>), grid, dim3(256), 0, st, t, a);
-      else hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), grid, dim3(256), 0, st, t, a);
-      if (a.flags) hipLaunchKernelGGL((forward_again_kernel<T, DH, true>), grid, dim3(256), 0, st, t, a, few ? 128 / WK : 128,
-                                      few ? 32 * WK : TILE_ROWS<T, DH>);
+    const int tile = p.few ? 32 : 128, shared_tile = p.shared_few ? 32 : 128;
+    a.row_tiles = (int)cdiv(std::min<int64_t>(x->T_max, x->rows) * a.G, tile);
+    a.splits = p.own.splits;
+    a.chunk = p.own.chunk;
+    a.joint = p.joint && x->S > 0 && x->prefix_max > 0;
+    a.more_splits = p.shared.splits;
+    a.more_chunk = p.shared.chunk;
+    a.more_part0 = p.own.splits;
+    // a launch by sequences, its first workgroups by programs
+    auto by_sequences = [&](const Table& t) {
+      const int64_t own = (int64_t)a.nseq * a.kv_heads * a.row_tiles * a.splits;
+      if (own + a.more_blocks == 0 || e != hipSuccess) return;
+      if (p.few) hipLaunchKernelGGL((few_kernel<T, DH>), dim3((unsigned)(own + a.more_blocks)), dim3(256), 0, st, t, a);
+      else hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), dim3((unsigned)own), dim3(256), 0, st, t, a);
+      if (a.flags && own)
+        hipLaunchKernelGGL((forward_again_kernel<T, DH, true>), dim3((unsigned)own), dim3(256), 0, st, t, a, tile, p.few ? 128 : TILE_ROWS<T, DH>);
       e = hipGetLastError();
     };
-    const int64_t seq_rows = std::min<int64_t>(x->T_max, x->rows) * a.G;
-    const int tile = p.few ? 128 / WK : 128;
-    // by sequences; with their programs' keys in runs of at most MAX_SEGS programs
-    a.part0 = 0;
-    a.splits = p.splits;
-    a.row_tiles = (int)cdiv(seq_rows, tile);
-    const int32_t* const plens = a.plens;
-    if (!p.joint || x->S == 0 || x->prefix_max == 0) {
-      a.plens = nullptr;
-      a.seq0 = 0;
+    const bool programs = x->S > 0 && x->prefix_max > 0;
+    if (!programs) {
       a.nseq = x->cache.B;
-      go(Table{}, (int64_t)a.nseq * a.kv_heads * a.row_tiles * a.splits, p.few);
-    } else {
-      for (int s0 = 0; s0 < x->S; s0 += MAX_SEGS) {
-        Table t = {};
-        for (int i = s0; i < std::min(x->S, s0 + MAX_SEGS); ++i) t.seg[t.n++] = {x->seg_off[i], 0, i, 0};
-        a.seq0 = x->seg_off[s0];
-        a.nseq = x->seg_off[s0 + t.n] - a.seq0;
-        go(t, (int64_t)a.nseq * a.kv_heads * a.row_tiles * a.splits, p.few);
-      }
+      by_sequences(Table{});
     }
-    // by programs
-    if (!p.joint) {
-      a.plens = plens;
-      a.flags = nullptr;            // all its rows see all its keys
-      a.part0 = p.splits;
-      a.splits = p.shared_splits;
-      a.row_tiles = 0;
-      for (int s0 = 0; s0 < x->S; s0 += MAX_SEGS) {
-        Table t = {};
-        for (int i = s0; i < std::min(x->S, s0 + MAX_SEGS); ++i) {
-          const int n = x->seg_off[i + 1] - x->seg_off[i];
-          t.seg[t.n] = {x->seg_off[i], n * x->T_max, i, 0};
-          t.off[t.n + 1] = t.off[t.n] + (int32_t)cdiv(cdiv((int64_t)n * x->T_max * a.G, p.shared_few ? 128 / WK : 128) * a.kv_heads * a.splits, XCDS);
-          ++t.n;
-        }
-        go(t, (int64_t)t.off[t.n] * XCDS, p.shared_few);
+    for (int s0 = 0; programs && s0 < x->S; s0 += MAX_SEGS) {
+      Table t = {};
+      for (int i = s0; i < std::min(x->S, s0 + MAX_SEGS); ++i) {
+        const int n = x->seg_off[i + 1] - x->seg_off[i];
+        t.seg[t.n] = {x->seg_off[i], n * x->T_max, i, 0};
+        t.off[t.n + 1] = t.off[t.n] + (int32_t)cdiv(cdiv((int64_t)n * x->T_max * a.G, shared_tile) * a.kv_heads * p.shared.splits, XCDS);
+        ++t.n;
       }
+      a.seq0 = x->seg_off[s0];
+      a.nseq = x->seg_off[s0 + t.n] - a.seq0;
+      a.more_blocks = p.shared_few && p.few ? t.off[t.n] * XCDS : 0;
+      by_sequences(t);
+      if (p.joint || a.more_blocks || t.off[t.n] == 0 || e != hipSuccess) continue;
+      Args b = a;                   // by programs: all their rows see all their keys
+      b.row_tiles = 0;
+      b.flags = nullptr;
+      b.part0 = a.more_part0;
+      b.splits = a.more_splits;
+      b.chunk = a.more_chunk;
+      hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), dim3((unsigned)t.off[t.n] * XCDS), dim3(256), 0, st, t, b);
+      e = hipGetLastError();
     }
     if (e != hipSuccess || a.parts == 1) return e;
     return join<T, DH>(a, x->rows * a.heads, st);
@@ -1256,7 +1500,8 @@ wm_status wm_prefix_attention(const wm_prefix* x, void* o, int64_t ld_o, float* 
   a.out = o;
   a.ld_out = ld_o;
   a.lse = lse;
-  a.splits = a.parts = p.fwd_splits;
+  a.splits = a.parts = p.fwd.splits;
+  a.chunk = p.fwd.chunk;
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
   a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
@@ -1290,12 +1535,14 @@ wm_status wm_prefix_attention_grad(const wm_prefix* x, const void* o, int64_t ld
   a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
   if (nq > 0) {
     a.out = g->dq; a.ld_out = g->ld_dq;
-    a.splits = p.dq_splits;
+    a.splits = p.dq.splits;
+    a.chunk = p.dq.chunk;
     a.part_rows = nq * w->heads;
     WM_PF(TK_PREFIX, grad_rows(w, p, a, st));
     a.out = g->dk; a.ld_out = g->ld_dk;
     a.out2 = g->dv; a.ld_out2 = g->ld_dv;
-    a.splits = p.dkv_splits;
+    a.splits = p.dkv.splits;
+    a.chunk = p.dkv.chunk;
     a.part_rows = nq * w->kv_heads;
     WM_PF(TK_PREFIX, grad_own_keys(w, p, a, st));
   }
@@ -1331,7 +1578,7 @@ wm_status wm_cached_attention(const wm_cached* x, void* o, int64_t ld_o, float* 
   a.out = o;
   a.ld_out = ld_o;
   a.lse = lse;
-  a.parts = p.splits + p.shared_splits;
+  a.parts = p.own.splits + p.shared.splits;
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
   // one row per sequence: the rows of a tile see the same keys
