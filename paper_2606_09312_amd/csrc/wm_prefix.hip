@@ -161,18 +161,80 @@ __device__ __forceinline__ void copy_pages(const Args& a, const void* cache, int
   }
 }
 
+// A wavefront's own block of 32 keys (or rows): from key `first` of a run on, n of them exist.  Paged: its one or two pages;
+// their numbers come through scalar loads, which the copies' count of outstanding loads does not see.
+struct Block {
+  int first, n, id0, id1;
+};
+__device__ __forceinline__ Block paged_block(const Args& a, const int32_t* table, int first, int n, int lane) {
+  Block b = {__builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(min(max(n, 0), 32)), -1, -1};
+  if (b.n > 0) {
+    const __attribute__((address_space(4))) int32_t* ids = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
+    b.id0 = ids[b.first >> a.lps];
+    b.id1 = ids[(b.first + b.n - 1) >> a.lps];
+    if ((b.id0 < 0 || b.id0 >= a.n_pages || b.id1 < 0 || b.id1 >= a.n_pages) && a.status && lane == 0) atomicOr(a.status, ERRBIT_PAGE);
+  }
+  return b;
+}
+template <class T, int DH>
+__device__ __forceinline__ void copy_block(const Args& a, const void* cache, int hk, const Block& b, T* tile, int lane) {
+  using TL = Tile<T, DH>;
+  constexpr int N = 32 * TL::UPR / 64, RPI = 64 / TL::UPR;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r0 = i * RPI, at = b.first + r0;                // the instruction's first row
+    const int id = (at >> a.lps) == (b.first >> a.lps) ? b.id0 : b.id1;
+    const bool ok = id >= 0 && id < a.n_pages;
+    const int64_t key = ((((int64_t)(ok ? id : 0) * a.kv_heads + hk) << a.lps) + (at & ((1 << a.lps) - 1))) * DH;
+    const u32x4 buf = buffer_of(static_cast<const T*>(cache) + key, ok ? (uint32_t)(min(max(b.n - r0, 0), RPI) * DH * sizeof(T)) : 0u);
+    const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(r0 + r);
+    copy16(buf, tile + (size_t)i * 64 * TL::E, (uint32_t)(r * DH * sizeof(T) + unit * 16));
+  }
+}
+
+// Scores of 32 keys to weights against the running maximum of a lane's row, with its sum and accumulators brought along.
+template <class T, int DB>
+__device__ __forceinline__ void weigh(f32x16& s, float& mx, float& sum, f32x16 (&acc)[DB], float c2) {
+  float bm = s[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) bm = fmaxf(bm, s[r]);
+  bm = pair_max(bm);
+  const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, c2)) : 1.0f;
+  mx = bm > mx ? bm : mx;
+  const float mc = mx == -INFINITY ? 0.0f : log2_units<T>(mx, c2);            // only keys of weight 0 so far
+  float bs = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    s[r] = weight<T>(s[r], c2, mc);
+    bs += s[r];
+  }
+  sum = fmaf(sum, f, bs);
+  if (__any(f != 1.0f)) {
+#pragma unroll
+    for (int b = 0; b < DB; ++b) acc[b] *= f;
+  }
+}
+// Values of a lane's column where bit acc_row(0, r) of its half of `seen` is set, `other` elsewhere.
+__device__ __forceinline__ void only(f32x16& s, uint32_t seen, float other, int h) {
+  const uint32_t m = seen >> (4 * h);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : other;
+}
+
 // A workgroup's rows (stacked rows of one key head from packed row q0 on, a tile of them), the program's keys and
-// own keys [o0, o1) that some row of the tile sees.
+// own keys [o0, o1) that some row of the tile sees.  Those before `rest` come in whole tiles of KB, which the rows of the tile's
+// first sequence see (the paged forms' only one); of those from there on, about as many as the tile has queries, every
+// wavefront takes what its own rows see.
 struct Work {
   int64_t q0, p0;                           // p0: dense, the program's first key row
-  int R, hk, tile, split, P, o0, o1;
+  int R, hk, tile, split, P, o0, rest, o1;
   int seq;                                  // dense: the sequence of the tile's first row
   int before;                               // paged: row i of the sequence sees before + i + 1 own keys
   const int32_t *own_table, *shared_table;  // paged
 };
 template <bool PAGED>
-__device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block, int blocks, int rows, int lane, Work& w) {
-  w.p0 = w.o0 = w.o1 = w.seq = 0;
+__device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block, int blocks, int rows, int KB, int lane, Work& w) {
+  w.p0 = w.o0 = w.rest = w.o1 = w.seq = 0;
   w.own_table = w.shared_table = nullptr;
   if constexpr (!PAGED) {
     Prob p;
@@ -182,6 +244,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
     const int first = p.q0 + w.tile * rows / a.G;
     w.seq = last_start(a.off, 0, a.B - 1, first, lane);
     w.o0 = min(max(a.off[w.seq], p.q0), first);
+    w.rest = w.o0 + (first + 1 - w.o0) / KB * KB;
     w.o1 = p.q0 + (min((w.tile + 1) * rows, w.R) - 1) / a.G + 1;
   } else {
     int64_t n;
@@ -215,6 +278,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
     if (w.tile * rows >= w.R) return false;
     w.before = a.row_tiles ? seen - (int)n : INT32_MIN / 2;
     w.o1 = max(w.before + (min((w.tile + 1) * rows, w.R) - 1) / a.G + 1, 0);
+    w.rest = max(w.before + w.tile * rows / a.G + 1, 0) / KB * KB;
     w.P = 0;
     if (seg >= 0) {
       const int x = a.plens[seg];
@@ -248,9 +312,9 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   if (a.part0 == 0) check_rows(a, tid);
 
   Work w;
-  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, lane, w)) return;
+  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB, lane, w)) return;
   const int64_t q0 = w.q0, p0 = w.p0;
-  const int R = w.R, hk = w.hk, tile = w.tile, split = w.split, P = w.P, o0 = w.o0, o1 = w.o1;
+  const int R = w.R, hk = w.hk, tile = w.tile, split = w.split, P = w.P, o0 = w.o0, rest = w.rest, o1 = w.o1;
   const int row = tile * (32 * WR) + wr * 32 + (lane & 31);   // may pass R: computed, not stored
   const int rr = min(row, R - 1), head = hk * a.G + rr % a.G;
   const int64_t qrow = q0 + rr / a.G;
@@ -266,7 +330,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   }
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
-  const int nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
+  const int nP = (P + KB - 1) / KB, tiles = nP + (rest - o0) / KB;
   const int2 tt = share_of(a, tiles, split);
   const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = !PAGED && a.mask ? a.mask + p0 : nullptr;
@@ -275,7 +339,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   auto look_ahead = [&](int ti) {
     if constexpr (PAGED) {
       const bool own = ti >= nP;
-      const int first = (own ? ti - nP : ti) * KB, len = own ? o1 : P;
+      const int first = (own ? ti - nP : ti) * KB, len = own ? rest : P;
       const int entry = (first >> a.lps) + lane;
       pre[0] = page_id(a, own ? w.own_table : w.shared_table, entry, lane < max(KB >> a.lps, 1) && ((int64_t)entry << a.lps) < len);
     } else if (mask && ti < nP) {
@@ -290,17 +354,17 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   auto look = [&](int ti, uint64_t (&v)[NV]) {
 #pragma unroll
     for (int w = 0; w < NV; ++w)
-      v[w] = mask && ti < nP ? __ballot(pre[w] != 0) : in_range(min((ti < nP ? P - ti * KB : o1 - o0 - (ti - nP) * KB) - 64 * w, KB));
+      v[w] = mask && ti < nP ? __ballot(pre[w] != 0) : in_range(min((ti < nP ? P - ti * KB : KB) - 64 * w, KB));
   };
   auto copy = [&](int ti, const uint64_t (&v)[NV], T* kt, T* vt) {
     const bool own = ti >= nP;
     if constexpr (PAGED) {
-      const int first = (own ? ti - nP : ti) * KB, len = own ? o1 : P;
+      const int first = (own ? ti - nP : ti) * KB, len = own ? rest : P;
       copy_pages<T, DH, KB, 256>(a, a.k, hk, kt, first, len, pre[0], tid);
       copy_pages<T, DH, KB, 256>(a, a.v, hk, vt, first, len, pre[0], tid);
     } else {
       const int64_t first = own ? (int64_t)o0 + (ti - nP) * KB : p0 + (int64_t)ti * KB;
-      const int n = own ? o1 - o0 - (ti - nP) * KB : P - ti * KB;
+      const int n = own ? KB : P - ti * KB;
       const int lk = (int)(own ? a.ld_k : a.ld_pk), lv = (int)(own ? a.ld_v : a.ld_pv);
       copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.k : a.pk) + first * lk + hk * DH, lk, n, mask && !own, v, kt, tid);
       copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.v : a.pv) + first * lv + hk * DH, lv, n, mask && !own, v, vt, tid);
@@ -402,7 +466,53 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     step(ti, std::integral_constant<int, 0>{});
     if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
-  if (a.flags) leave_flag(a, t1 > nP && not_finite<DB>(acc), tid);
+  if (split == a.splits - 1 && rest < o1) {
+    // What is left of the own keys, without barriers: K and V of 32 keys per wavefront (one buffer for both in turn
+    // where a tile has 32 rows).
+    constexpr bool TWO = KB >= 64;
+    constexpr int N = 32 * TL::UPR / 64;
+    __syncthreads();
+    T* const kt = lds + wave * KB * DH;
+    T* const vt = TWO ? kt + 32 * DH : kt;
+    const int end = min(hi_z, o1);
+    const uint64_t every[1] = {~0ull};
+    auto block_of = [&](int first) -> Block {
+      if constexpr (PAGED) return paged_block(a, w.own_table, first, end - first, lane);
+      else return {first, min(max(end - first, 0), 32), 0, 0};
+    };
+    auto copy_k = [&](const Block& b) {
+      if constexpr (PAGED) copy_block<T, DH>(a, a.k, hk, b, kt, lane);
+      else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.k) + b.first * a.ld_k + hk * DH, (int)a.ld_k, b.n, false, every, kt, lane);
+    };
+    auto copy_v = [&](const Block& b) {
+      if constexpr (PAGED) copy_block<T, DH>(a, a.v, hk, b, vt, lane);
+      else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.v) + b.first * a.ld_v + hk * DH, (int)a.ld_v, b.n, false, every, vt, lane);
+    };
+    Block now = block_of(max(lo_a, rest) + 32 * wk);
+    if (now.n > 0) {
+      copy_k(now);
+      if (TWO) copy_v(now);
+    }
+    while (now.n > 0) {
+      const Block after = block_of(now.first + 32 * WK);
+      wait_counts<TWO ? N : 0, true>();                       // K is there
+      f32x16 s = TL::mm_row(kt, 0, qf, lane);
+      wait_counts<63, true>();
+      if (!TWO) copy_v(now);
+      else if (after.n > 0) copy_k(after);
+      if (lo_z > now.first || hi_a < now.first + 32) only(s, below(hi - now.first) & ~below(lo - now.first), -INFINITY, h);
+      weigh<T, DB>(s, mx, sum, acc, a.c2);
+      if (TWO && after.n > 0) wait_counts<N, false>(); else wait_counts<0, false>();      // V is there
+      TL::mm_col(vt, 0, s, acc, lane);
+      wait_counts<63, true>();
+      if (after.n > 0) {
+        if (TWO) copy_v(after);
+        else copy_k(after);
+      }
+      now = after;
+    }
+  }
+  if (a.flags) leave_flag(a, not_finite<DB>(acc), tid);
   sum = pair_sum(sum);
   float m2 = mx == -INFINITY ? -INFINITY : log2_units<T>(mx, a.c2);
   if constexpr (WK > 1) {       // join the wavefronts that share rows
@@ -467,7 +577,7 @@ constexpr int FEW_PER_CU = FEW_LDS<T, DH> > 80 * 1024 ? 1 : FEW_LDS<T, DH> > 40 
 template <class T, int DH>
 __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Table t, const Args given) {
   using TL = Tile<T, DH>;
-  constexpr int DB = TL::DB, KB = 128, N = 32 * TL::UPR / 64, RPI = 64 / TL::UPR;
+  constexpr int DB = TL::DB, KB = 128, N = 32 * TL::UPR / 64;
   __shared__ __attribute__((aligned(16))) uint8_t lds[FEW_LDS<T, DH> + 1024];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   T* const kt = reinterpret_cast<T*>(lds) + wave * 2 * 32 * DH;
@@ -482,7 +592,7 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
   if (given.part0 == 0) check_rows(a, tid);
   const int block = by_program ? blockIdx.x : blockIdx.x - given.more_blocks;
   Work w;
-  if (!work_of<true>(t, a, block, by_program ? given.more_blocks : gridDim.x - given.more_blocks, 32, lane, w)) return;
+  if (!work_of<true>(t, a, block, by_program ? given.more_blocks : gridDim.x - given.more_blocks, 32, KB, lane, w)) return;
   const int row = w.tile * 32 + (lane & 31);                  // may pass R: computed, not stored
   const int rr = min(row, w.R - 1), head = w.hk * a.G + rr % a.G;
   const int64_t qrow = w.q0 + rr / a.G;
@@ -490,38 +600,12 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
   const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.o1 + KB - 1) / KB;
   const int2 tt = share_of(a, tiles, w.split);
 
-  // a block's first key and how many of its keys exist; its pages (numbers come through scalar loads, which the copies'
-  // count of outstanding loads does not see)
-  struct Block {
-    int first, n, id0, id1;
-  };
   auto block_of = [&](int ti) {
     const bool own = ti >= nP;
-    Block b;
-    b.first = __builtin_amdgcn_readfirstlane((own ? ti - nP : ti) * KB + 32 * wave);
-    b.n = __builtin_amdgcn_readfirstlane(ti < tt.y ? min(max((own ? w.o1 : w.P) - b.first, 0), 32) : 0);
-    b.id0 = b.id1 = -1;
-    if (b.n > 0) {
-      const __attribute__((address_space(4))) int32_t* ids =
-          (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(own ? w.own_table : w.shared_table);
-      b.id0 = ids[b.first >> a.lps];
-      b.id1 = ids[(b.first + b.n - 1) >> a.lps];
-      if ((b.id0 < 0 || b.id0 >= a.n_pages || b.id1 < 0 || b.id1 >= a.n_pages) && a.status && lane == 0) atomicOr(a.status, ERRBIT_PAGE);
-    }
-    return b;
+    const int first = (own ? ti - nP : ti) * KB + 32 * wave;
+    return paged_block(a, own ? w.own_table : w.shared_table, first, ti < tt.y ? (own ? w.o1 : w.P) - first : 0, lane);
   };
-  auto copy = [&](const void* cache, const Block& b, T* tile) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r0 = i * RPI, at = b.first + r0;              // the instruction's first row
-      const int id = (at >> a.lps) == (b.first >> a.lps) ? b.id0 : b.id1;
-      const bool ok = id >= 0 && id < a.n_pages;
-      const int64_t key = ((int64_t)(ok ? id : 0) * a.kv_heads + w.hk << a.lps) + (at & ((1 << a.lps) - 1));
-      const u32x4 buf = buffer_of(static_cast<const T*>(cache) + key * DH, ok ? (uint32_t)(min(max(b.n - r0, 0), RPI) * DH * sizeof(T)) : 0u);
-      const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(r0 + r);
-      copy16(buf, tile + (size_t)i * 64 * TL::E, (uint32_t)(r * DH * sizeof(T) + unit * 16));
-    }
-  };
+  auto copy = [&](const void* cache, const Block& b, T* tile) { copy_block<T, DH>(a, cache, w.hk, b, tile, lane); };
   f32x16 acc[DB];
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
@@ -557,30 +641,8 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
     f32x16 s = TL::mm_row(kt, 0, qf, lane);
     wait_counts<63, true>();
     if (next.n > 0) copy(a.k, next, kt);
-    const uint32_t seen = own ? below(hi - now.first) & below(now.n) : below(now.n);
-    if (own ? hi_a < now.first + 32 : now.n < 32) {
-      const uint32_t m = seen >> (4 * h);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : -INFINITY;
-    }
-    float bm = s[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) bm = fmaxf(bm, s[r]);
-    bm = pair_max(bm);
-    const float f = bm > mx ? exp2_of(log2_units<T>(mx - bm, a.c2)) : 1.0f;
-    mx = bm > mx ? bm : mx;
-    const float mc = mx == -INFINITY ? 0.0f : log2_units<T>(mx, a.c2);        // only keys of weight 0 so far
-    float bs = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = weight<T>(s[r], a.c2, mc);
-      bs += s[r];
-    }
-    sum = fmaf(sum, f, bs);
-    if (__any(f != 1.0f)) {
-#pragma unroll
-      for (int b = 0; b < DB; ++b) acc[b] *= f;
-    }
+    if (own ? hi_a < now.first + 32 : now.n < 32) only(s, own ? below(hi - now.first) & below(now.n) : below(now.n), -INFINITY, h);
+    weigh<T, DB>(s, mx, sum, acc, a.c2);
     if (next.n > 0) wait_counts<N, false>(); else wait_counts<0, false>();    // V is there
     TL::mm_col(vt, 0, s, acc, lane);
     wait_counts<63, true>();
@@ -693,7 +755,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const int h = lane >> 5;
   check_rows(a, tid);
   Work w;
-  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, lane, w)) return;
+  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, KB, lane, w)) return;
   const int row = w.tile * 128 + wave * 32 + (lane & 31);
   const int rr = min(row, w.R - 1), head = w.hk * a.G + rr % a.G;
   const int64_t qrow = w.q0 + rr / a.G, orow = qrow * a.heads + head;
@@ -718,7 +780,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const int lo = bounds_of(a, w.seq, (int)qrow, lane_of((int)qrow, 31), (int)w.q0, (int)w.q0 + w.R / a.G, lane).x, hi = (int)qrow + 1;
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
-  const int P = w.P, o0 = w.o0, o1 = w.o1, nP = (P + KB - 1) / KB, tiles = nP + (o1 - o0 + KB - 1) / KB;
+  const int P = w.P, o0 = w.o0, rest = w.rest, o1 = w.o1, nP = (P + KB - 1) / KB, tiles = nP + (rest - o0) / KB;
   const int2 tt = share_of(a, tiles, split);
   const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
@@ -727,13 +789,13 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
     return mask && (KB >= 64 || lane < KB) && key < P ? mask[key] : 0;
   };
   auto look = [&](int ti, int mb) -> uint64_t {
-    return mask && ti < nP ? __ballot(mb != 0) : in_range(min(ti < nP ? P - ti * KB : o1 - o0 - (ti - nP) * KB, KB));
+    return mask && ti < nP ? __ballot(mb != 0) : in_range(min(ti < nP ? P - ti * KB : KB, KB));
   };
   auto copy = [&](int ti, uint64_t vv, T* kt, T* vt) {
     const uint64_t v[1] = {vv};
     const bool own = ti >= nP;
     const int64_t at = own ? (int64_t)o0 + (ti - nP) * KB : w.p0 + (int64_t)ti * KB;
-    const int n = own ? o1 - o0 - (ti - nP) * KB : P - ti * KB;
+    const int n = own ? KB : P - ti * KB;
     const int lk = (int)(own ? a.ld_k : a.ld_pk), lv = (int)(own ? a.ld_v : a.ld_pv);
     copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.k : a.pk) + at * lk + w.hk * DH, lk, n, mask && !own, v, kt, tid);
     copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.v : a.pv) + at * lv + w.hk * DH, lv, n, mask && !own, v, vt, tid);
@@ -790,7 +852,39 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
     step(ti, std::integral_constant<int, 0>{});
     if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
-  if (a.flags) leave_flag(a, t1 > nP && not_finite<DB>(acc), tid);
+  if (split == a.splits - 1 && rest < o1) {                    // as in the forward kernel
+    constexpr bool TWO = KB >= 64;
+    __syncthreads();
+    T* const kt = lds + wave * KB * DH;
+    T* const vt = TWO ? kt + 32 * DH : kt;
+    const int end = min(hi_z, o1);
+    const uint64_t every[1] = {~0ull};
+    auto copy_of = [&](const void* x, int64_t ld, int first, T* tile) {
+      copy_rows<T, DH, 32, 64>(static_cast<const T*>(x) + first * ld + w.hk * DH, (int)ld, end - first, false, every, tile, lane);
+    };
+    int first = max(lo_a, rest);
+    if (first < end) copy_of(a.v, a.ld_v, first, vt);
+    if (TWO && first < end) copy_of(a.k, a.ld_k, first, kt);
+    for (; first < end; first += 32) {
+      const bool more = first + 32 < end;
+      wait_counts<0, true>();
+      const f32x16 dp = TL::mm_row(vt, 0, gf, lane);
+      wait_counts<63, true>();
+      if (!TWO) {
+        copy_of(a.k, a.ld_k, first, kt);
+        wait_counts<0, true>();
+      }
+      f32x16 s = TL::mm_row(kt, 0, qf, lane);
+      if (TWO && more) copy_of(a.v, a.ld_v, first + 32, vt);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * (dp[r] - delta);
+      if (lo_z > first || hi_a < first + 32) only(s, below(hi - first) & ~below(lo - first), 0.0f, h);
+      TL::mm_col(kt, 0, s, acc, lane);
+      wait_counts<63, true>();
+      if (more) copy_of(TWO ? a.k : a.v, TWO ? a.ld_k : a.ld_v, first + 32, TWO ? kt : vt);
+    }
+  }
+  if (a.flags) leave_flag(a, not_finite<DB>(acc), tid);
   if (row >= w.R) return;
   if (a.splits > 1) store_cols<float, DB>(a.part + (split * a.part_rows + orow) * DH, acc, a.scale, h);
   else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
@@ -974,10 +1068,10 @@ struct Span {
   int p_lo, p_hi, o_lo, o_hi;
 };
 __device__ __forceinline__ Span span_of(const Args& a, const Work& w, int KB) {
-  const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.o1 - w.o0 + KB - 1) / KB;
+  const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.rest - w.o0) / KB;
   const int2 tt = share_of(a, tiles, w.split);
   const int t0 = tt.x, t1 = tt.y;
-  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, min(w.o0 + max(t1 - nP, 0) * KB, w.o1)};
+  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, w.split == a.splits - 1 ? w.o1 : w.o0 + max(t1 - nP, 0) * KB};
 }
 // Own keys that a row sees.
 template <bool PAGED>
@@ -995,7 +1089,8 @@ __global__ __launch_bounds__(256) void forward_again_kernel(const Table t, const
   if (!a.flags[blockIdx.x]) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Work w;
-  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, rows, lane, w)) return;
+  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, rows, KB, lane, w)) return;
+  if (rows == 32 && PAGED) w.rest = (w.o1 + KB - 1) / KB * KB;         // the few-row kernel's: all keys in tiles
   const Span sp = span_of(a, w, KB);
   for (int row = w.tile * rows + wave; row < min((w.tile + 1) * rows, w.R); row += 4) {
     const int head = w.hk * a.G + row % a.G;
@@ -1041,7 +1136,7 @@ __global__ __launch_bounds__(256) void dq_again_kernel(const Table t, const Args
   if (!a.flags[blockIdx.x]) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Work w;
-  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, lane, w)) return;
+  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, TILE_ROWS<T, DH>, lane, w)) return;
   const Span sp = span_of(a, w, TILE_ROWS<T, DH>);
   for (int row = w.tile * 128 + wave; row < min((w.tile + 1) * 128, w.R); row += 4) {
     const int head = w.hk * a.G + row % a.G;
