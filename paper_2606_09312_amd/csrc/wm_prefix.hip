@@ -139,25 +139,73 @@ __device__ __forceinline__ void copy_rows(const T* base, int ld, int n, bool som
   }
 }
 
+// Two matrices' rows tile after tile: where the next tile begins, bytes from one to the next and of a whole one, and what a
+// lane adds to a tile's beginning.  A whole tile costs four scalar additions beside its copies (with everything
+// formed anew a tile took 169 scalar instructions, as long as its products).
+template <class T, int DH, int ROWS>
+struct Stream {
+  using TL = Tile<T, DH>;
+  static constexpr int N = ROWS * TL::UPR / 256;
+  uint64_t x, y;
+  uint32_t step_x, step_y, whole_x, whole_y;
+  uint32_t at_x[N], at_y[N];
+  __device__ __forceinline__ void start(const T* px, int64_t ldx, const T* py, int64_t ldy, int tid) {
+    x = (uint64_t)px;
+    y = (uint64_t)py;
+    const uint32_t bx = (uint32_t)ldx * sizeof(T), by = (uint32_t)ldy * sizeof(T);
+    step_x = ROWS * bx;
+    step_y = ROWS * by;
+    whole_x = (ROWS - 1) * bx + DH * sizeof(T);
+    whole_y = (ROWS - 1) * by + DH * sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = (i * 256 + tid) / TL::UPR, unit = ((i * 256 + tid) % TL::UPR) ^ TL::swz(row);
+      at_x[i] = row * bx + unit * 16;
+      at_y[i] = row * by + unit * 16;
+    }
+  }
+  // the next tile, its first n rows, of them those of `vis` (where `some`)
+  template <int NV>
+  __device__ __forceinline__ void copy(T* tx, T* ty, int n, bool some, const uint64_t (&vis)[NV], int wave, int tid) {
+    const bool whole = n >= ROWS && !some;
+    const u32x4 bx = buffer_of((const void*)x, whole ? whole_x : whole_x - (uint32_t)(ROWS - n) * (step_x / ROWS));
+    const u32x4 by = buffer_of((const void*)y, whole ? whole_y : whole_y - (uint32_t)(ROWS - n) * (step_y / ROWS));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t ax = at_x[i], ay = at_y[i];
+      if (some) {
+        const int row = (i * 256 + tid) / TL::UPR;
+        const bool see = (vis[NV > 1 ? row >> 6 : 0] >> (row & 63)) & 1;
+        ax = see ? ax : BAD;
+        ay = see ? ay : BAD;
+      }
+      copy16(bx, tx + (i * 256 + wave * 64) * TL::E, ax);
+      copy16(by, ty + (i * 256 + wave * 64) * TL::E, ay);
+    }
+    x += step_x;
+    y += step_y;
+  }
+};
+
 // Keys [first, first + ROWS) of a page table, of which the first `len` exist, into a tile.  A page has at least 16
 // slots and a tile starts at a multiple of its length, so the 16 or fewer rows that one
 // instruction copies lie in one page, whose end (or the last key) bounds the buffer: rows past it
 // read as zero.  ids: lane l has the tile's l-th page.
-template <class T, int DH, int ROWS, int NT>
-__device__ __forceinline__ void copy_pages(const Args& a, const void* cache, int hk, T* tile, int first, int len, int ids, int tid) {
+template <class T, int DH, int ROWS>
+__device__ __forceinline__ void copy_pages(const Args& a, int hk, T* kt, T* vt, int first, int len, int ids, int wave, int lane) {
   using TL = Tile<T, DH>;
-  constexpr int N = ROWS * TL::UPR / NT, RPI = 64 / TL::UPR;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int N = ROWS * TL::UPR / 256, RPI = 64 / TL::UPR;
   const int slots = 1 << a.lps;
+  const uint32_t unit_of = (uint32_t)(lane / TL::UPR * DH * sizeof(T));
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int r0 = (i * NT + wave * 64) / TL::UPR;                   // the instruction's first row
+    const int r0 = (i * 256 + wave * 64) / TL::UPR;                  // the instruction's first row
     const int id = lane_of(ids, r0 >> a.lps);
     const int n = id < 0 ? 0 : min(max(len - first - r0, 0), RPI);
-    const int64_t at = ((int64_t)max(id, 0) * a.kv_heads + hk) * slots + ((first + r0) & (slots - 1));
-    const u32x4 buf = buffer_of(static_cast<const T*>(cache) + at * DH, (uint32_t)(n * DH * sizeof(T)));
-    const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(r0 + r);
-    copy16(buf, tile + (size_t)(i * NT + wave * 64) * TL::E, (uint32_t)(r * DH * sizeof(T) + unit * 16));
+    const uint64_t at = ((((uint64_t)(uint32_t)max(id, 0) * a.kv_heads + hk) << a.lps) + ((first + r0) & (slots - 1))) * (DH * sizeof(T));
+    const uint32_t vo = unit_of + ((lane % TL::UPR) ^ TL::swz(r0 + lane / TL::UPR)) * 16;
+    copy16(buffer_of(static_cast<const uint8_t*>(a.k) + at, n * DH * sizeof(T)), kt + (i * 256 + wave * 64) * TL::E, vo);
+    copy16(buffer_of(static_cast<const uint8_t*>(a.v) + at, n * DH * sizeof(T)), vt + (i * 256 + wave * 64) * TL::E, vo);
   }
 }
 
@@ -350,24 +398,26 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
       }
     }
   };
-  uint64_t vis[NV], next[NV];                                 // keys of the program that exist and are shown
-  auto look = [&](int ti, uint64_t (&v)[NV]) {
+  uint64_t vis[NV], next[NV];                                 // with a mask: the tile's keys that are shown
 #pragma unroll
-    for (int w = 0; w < NV; ++w)
-      v[w] = mask && ti < nP ? __ballot(pre[w] != 0) : in_range(min((ti < nP ? P - ti * KB : KB) - 64 * w, KB));
-  };
-  auto copy = [&](int ti, const uint64_t (&v)[NV], T* kt, T* vt) {
+  for (int w = 0; w < NV; ++w) vis[w] = next[w] = 0;
+  Stream<T, DH, KB> rows;
+  auto copy = [&](int ti, uint64_t (&v)[NV], T* kt, T* vt) {
     const bool own = ti >= nP;
     if constexpr (PAGED) {
-      const int first = (own ? ti - nP : ti) * KB, len = own ? rest : P;
-      copy_pages<T, DH, KB, 256>(a, a.k, hk, kt, first, len, pre[0], tid);
-      copy_pages<T, DH, KB, 256>(a, a.v, hk, vt, first, len, pre[0], tid);
+      copy_pages<T, DH, KB>(a, hk, kt, vt, (own ? ti - nP : ti) * KB, own ? rest : P, pre[0], wave, lane);
     } else {
-      const int64_t first = own ? (int64_t)o0 + (ti - nP) * KB : p0 + (int64_t)ti * KB;
-      const int n = own ? KB : P - ti * KB;
-      const int lk = (int)(own ? a.ld_k : a.ld_pk), lv = (int)(own ? a.ld_v : a.ld_pv);
-      copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.k : a.pk) + first * lk + hk * DH, lk, n, mask && !own, v, kt, tid);
-      copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.v : a.pv) + first * lv + hk * DH, lv, n, mask && !own, v, vt, tid);
+      if (ti == nP || ti == t0) {
+        const int64_t first = own ? (int64_t)o0 + (int64_t)(ti - nP) * KB : p0 + (int64_t)ti * KB;
+        const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
+        rows.start(static_cast<const T*>(own ? a.k : a.pk) + first * lk + hk * DH, lk,
+                   static_cast<const T*>(own ? a.v : a.pv) + first * lv + hk * DH, lv, tid);
+      }
+      if (mask && !own) {
+#pragma unroll
+        for (int w = 0; w < NV; ++w) v[w] = __ballot(pre[w] != 0);
+      }
+      rows.copy(kt, vt, own ? KB : min(P - ti * KB, KB), mask && !own, v, wave, tid);
     }
   };
 
@@ -378,7 +428,6 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   bool started = false;                       // every row has a maximum
   if (t0 < t1) {
     look_ahead(t0);
-    look(t0, vis);
     copy(t0, vis, ks, vs);
     if (t0 + 1 < t1) look_ahead(t0 + 1);
   }
@@ -388,30 +437,16 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     wait_counts<0, true>();
     raw_barrier();
     if (ti + 1 < t1) {
-      look(ti + 1, next);
       copy(ti + 1, next, ks + (BUF ^ 1) * KB * DH, vs + (BUF ^ 1) * KB * DH);
       if (ti + 2 < t1) look_ahead(ti + 2);
     }
     const T* kt = ks + BUF * KB * DH;
     const T* vt = vs + BUF * KB * DH;
-    // Keys of the wavefront's blocks that a lane's row sees; own keys are skipped where no row sees any.
+    // All rows see all keys of the program that are shown, and an own tile is seen whole by the rows of the tile's
+    // first sequence and not at all by the others.
     const bool own = ti >= nP;
-    const int at = own ? o0 + (ti - nP) * KB : 0;             // the tile's first own key
-    uint32_t seen[NB];
-    bool all = true, none = true;
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) {
-      const int base = 32 * (kb * WK + wk);
-      if (own) {
-        seen[kb] = below(hi - at - base) & ~below(lo - at - base);
-        all = all && lo_z <= at + base && hi_a >= at + base + 32;
-        none = none && (lo_a >= at + base + 32 || hi_z <= at + base);
-      } else {
-        seen[kb] = (uint32_t)(vis[NV > 1 ? base >> 6 : 0] >> (base & 63));
-        all = all && seen[kb] == ~0u;
-        none = none && seen[kb] == 0u;
-      }
-    }
+    const int at = own ? o0 + (ti - nP) * KB : ti * KB;
+    const bool all = own ? lo_z <= at : !mask && at + KB <= P, none = own && lo_a > at;
     if (!none) {
       f32x16 s[NB];
       float bs;
@@ -423,7 +458,9 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
         if (!all) {
 #pragma unroll
           for (int kb = 0; kb < NB; ++kb) {
-            uint32_t m = seen[kb] >> (4 * h);
+            const int base = 32 * (kb * WK + wk);
+            const uint32_t seen = own ? (lo <= at ? ~0u : 0u) : mask ? (uint32_t)(vis[NV > 1 ? base >> 6 : 0] >> (base & 63)) : below(P - at - base);
+            uint32_t m = seen >> (4 * h);
             asm volatile("" : "+v"(m));               // keeps this a branch: seldom taken, 48 instructions
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kb][r] = (m >> acc_row(0, r)) & 1 ? s[kb][r] : -INFINITY;
@@ -459,8 +496,10 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb) TL::mm_col(vt, 32 * (kb * WK + wk), s[kb], acc, lane);
     }
+    if (mask) {
 #pragma unroll
-    for (int w = 0; w < NV; ++w) vis[w] = next[w];
+      for (int w = 0; w < NV; ++w) vis[w] = next[w];
+    }
   };
   for (int ti = t0; ti < t1; ti += 2) {
     step(ti, std::integral_constant<int, 0>{});
@@ -784,29 +823,29 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   const int2 tt = share_of(a, tiles, split);
   const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
+  uint64_t vis[1] = {0}, next[1] = {0};
+  int mb = 0;
   auto mask_byte = [&](int ti) -> int {
     const int key = ti * KB + lane;
     return mask && (KB >= 64 || lane < KB) && key < P ? mask[key] : 0;
   };
-  auto look = [&](int ti, int mb) -> uint64_t {
-    return mask && ti < nP ? __ballot(mb != 0) : in_range(min(ti < nP ? P - ti * KB : KB, KB));
-  };
-  auto copy = [&](int ti, uint64_t vv, T* kt, T* vt) {
-    const uint64_t v[1] = {vv};
+  Stream<T, DH, KB> rows;
+  auto copy = [&](int ti, uint64_t (&v)[1], T* kt, T* vt) {
     const bool own = ti >= nP;
-    const int64_t at = own ? (int64_t)o0 + (ti - nP) * KB : w.p0 + (int64_t)ti * KB;
-    const int n = own ? KB : P - ti * KB;
-    const int lk = (int)(own ? a.ld_k : a.ld_pk), lv = (int)(own ? a.ld_v : a.ld_pv);
-    copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.k : a.pk) + at * lk + w.hk * DH, lk, n, mask && !own, v, kt, tid);
-    copy_rows<T, DH, KB, 256>(static_cast<const T*>(own ? a.v : a.pv) + at * lv + w.hk * DH, lv, n, mask && !own, v, vt, tid);
+    if (ti == nP || ti == t0) {
+      const int64_t first = own ? (int64_t)o0 + (int64_t)(ti - nP) * KB : w.p0 + (int64_t)ti * KB;
+      const int64_t lk = own ? a.ld_k : a.ld_pk, lv = own ? a.ld_v : a.ld_pv;
+      rows.start(static_cast<const T*>(own ? a.k : a.pk) + first * lk + w.hk * DH, lk,
+                 static_cast<const T*>(own ? a.v : a.pv) + first * lv + w.hk * DH, lv, tid);
+    }
+    if (mask && !own) v[0] = __ballot(mb != 0);
+    rows.copy(kt, vt, own ? KB : min(P - ti * KB, KB), mask && !own, v, wave, tid);
   };
   f32x16 acc[DB];
-  uint64_t vis = 0, next = 0;
-  int mb = 0;
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
   if (t0 < t1) {
-    vis = look(t0, mask_byte(t0));
+    mb = mask_byte(t0);
     copy(t0, vis, ks, vs);
     if (t0 + 1 < t1) mb = mask_byte(t0 + 1);
   }
@@ -815,30 +854,23 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
     wait_counts<0, true>();
     raw_barrier();
     if (ti + 1 < t1) {
-      next = look(ti + 1, mb);
       copy(ti + 1, next, ks + (BUF ^ 1) * KB * DH, vs + (BUF ^ 1) * KB * DH);
       if (ti + 2 < t1) mb = mask_byte(ti + 2);
     }
     const T* kt = ks + BUF * KB * DH;
     const T* vt = vs + BUF * KB * DH;
     const bool own = ti >= nP;
-    const int at = own ? o0 + (ti - nP) * KB : 0;
+    const int at = own ? o0 + (ti - nP) * KB : ti * KB;
+    const bool all = own ? lo_z <= at : !mask && at + KB <= P, none = own && lo_a > at;
 #pragma unroll
     for (int kb = 0; kb < KB / 32; ++kb) {
-      uint32_t seen = (uint32_t)(vis >> (32 * kb));
-      bool all = seen == ~0u, none = seen == 0u;
-      if (own) {
-        const int k0 = at + 32 * kb;
-        seen = below(hi - k0) & ~below(lo - k0);
-        all = lo_z <= k0 && hi_a >= k0 + 32;
-        none = lo_a >= k0 + 32 || hi_z <= k0;
-      }
-      if (none) continue;
+      if (none) break;
       f32x16 s = TL::mm_row(kt, 32 * kb, qf, lane);
       const f32x16 dp = TL::mm_row(vt, 32 * kb, gf, lane);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * (dp[r] - delta);
       if (!all) {
+        const uint32_t seen = own ? (lo <= at ? ~0u : 0u) : mask ? (uint32_t)(vis[0] >> (32 * kb)) : below(P - at - 32 * kb);
         uint32_t m = seen >> (4 * h);
         asm volatile("" : "+v"(m));             // keeps this a branch: seldom taken, 48 instructions
 #pragma unroll
@@ -846,7 +878,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
       }
       TL::mm_col(kt, 32 * kb, s, acc, lane);
     }
-    vis = next;
+    vis[0] = next[0];
   };
   for (int ti = t0; ti < t1; ti += 2) {
     step(ti, std::integral_constant<int, 0>{});
