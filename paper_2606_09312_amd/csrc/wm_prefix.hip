@@ -170,17 +170,20 @@ struct Stream {
     const bool whole = n >= ROWS && !some;
     const u32x4 bx = buffer_of((const void*)x, whole ? whole_x : whole_x - (uint32_t)(ROWS - n) * (step_x / ROWS));
     const u32x4 by = buffer_of((const void*)y, whole ? whole_y : whole_y - (uint32_t)(ROWS - n) * (step_y / ROWS));
+    if (!some) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint32_t ax = at_x[i], ay = at_y[i];
-      if (some) {
+      for (int i = 0; i < N; ++i) {
+        copy16(bx, tx + (i * 256 + wave * 64) * TL::E, at_x[i]);
+        copy16(by, ty + (i * 256 + wave * 64) * TL::E, at_y[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
         const int row = (i * 256 + tid) / TL::UPR;
         const bool see = (vis[NV > 1 ? row >> 6 : 0] >> (row & 63)) & 1;
-        ax = see ? ax : BAD;
-        ay = see ? ay : BAD;
+        copy16(bx, tx + (i * 256 + wave * 64) * TL::E, see ? at_x[i] : BAD);
+        copy16(by, ty + (i * 256 + wave * 64) * TL::E, see ? at_y[i] : BAD);
       }
-      copy16(bx, tx + (i * 256 + wave * 64) * TL::E, ax);
-      copy16(by, ty + (i * 256 + wave * 64) * TL::E, ay);
     }
     x += step_x;
     y += step_y;
@@ -344,7 +347,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
 // (wm_attend.hip).  PAGED: the launch goes by programs (the rows of all its sequences, the program's keys
 // only) or by sequences (row_tiles > 0: its own keys, after the program's if it has any).
 template <class T, int DH, int WK>
-constexpr int FWD_PER_CU = 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
+constexpr int FWD_PER_CU = IS_BF<T> && DH == 64 && WK == 1 ? 4 : 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 template <class T, int DH, int WK, bool PAGED>
 __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
