@@ -321,12 +321,8 @@ auto typed(const wm_attention* a, F f) {
 // wm_attention's checks, and what a call that does more needs of its plan.
 struct Shared {
   int64_t nq, nk, max_lk, max_r;
-  size_t part_bytes;              // of key_grads' partial sums
 };
 wm_status check_shared(const wm_attention* w, Shared* sh);
-// dk and dv of w's keys alone, from the statistics of the rows (lse log2 e and do . o, [rows heads][2]).
-hipError_t key_grads(const wm_attention* w, const void* d_o, int64_t ld_do, float* stat, void* dk, int64_t ld_dk, void* dv,
-                     int64_t ld_dv, float* part, hipStream_t st);
 
 }  // namespace attend
 }  // namespace wm

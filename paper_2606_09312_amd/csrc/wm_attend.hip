@@ -648,23 +648,7 @@ wm_status check_shared(const wm_attention* w, Shared* sh) {
   sh->nk = p.nk;
   sh->max_r = p.max_r;
   sh->max_lk = p.max_lk;
-  sh->part_bytes = p.dkv_splits > 1 ? (size_t)p.dkv_splits * 2 * p.nk * w->kv_heads * w->head_dim * 4 : 0;
   return WM_OK;
-}
-
-hipError_t key_grads(const wm_attention* w, const void* d_o, int64_t ld_do, float* stat, void* dk, int64_t ld_dk, void* dv,
-                     int64_t ld_dv, float* part, hipStream_t st) {
-  Plan p;
-  if (check(w, &p, true) != WM_OK) return hipErrorInvalidValue;
-  Args a = base_args(w);
-  a.d_o = d_o; a.ld_do = ld_do;
-  a.stat = stat;
-  a.part = part;
-  a.out = dk; a.ld_out = ld_dk;
-  a.out2 = dv; a.ld_out2 = ld_dv;
-  a.splits = p.dkv_splits;
-  a.part_rows = p.nk * w->kv_heads;
-  return grad_keys(w, p, a, st);
 }
 
 }  // namespace attend

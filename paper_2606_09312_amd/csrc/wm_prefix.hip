@@ -139,54 +139,107 @@ __device__ __forceinline__ void copy_rows(const T* base, int ld, int n, bool som
   }
 }
 
-// Two matrices' rows tile after tile: where the next tile begins, bytes from one to the next and of a whole one, and what a
-// lane adds to a tile's beginning.  A whole tile costs four scalar additions beside its copies (with everything
-// formed anew a tile took 169 scalar instructions, as long as its products).
+// Two matrices' rows tile after tile: where the next tile begins, bytes from one to the next and of a whole one, what a lane
+// adds to a tile's beginning and what each further copy of a tile adds to that.  A whole tile costs four scalar additions
+// beside its copies (with everything formed anew a tile took 169 scalar instructions, as long as its
+// products).  `stacked`: a tile's rows are G heads of each of ROWS / G rows of the matrix (G divides the 256 threads' rows).
 template <class T, int DH, int ROWS>
 struct Stream {
   using TL = Tile<T, DH>;
-  static constexpr int N = ROWS * TL::UPR / 256;
+  static constexpr int N = ROWS * TL::UPR / 256, STEP = 256 / TL::UPR;
+  static constexpr int K = STEP >= 16 ? 1 : 2;        // the swizzle goes by a row's last 4 bits
+  static_assert(STEP >= 8, "at most two patterns");
   uint64_t x, y;
-  uint32_t step_x, step_y, whole_x, whole_y;
-  uint32_t at_x[N], at_y[N];
-  __device__ __forceinline__ void start(const T* px, int64_t ldx, const T* py, int64_t ldy, int tid) {
+  uint32_t next_x, next_y, step_x, step_y, last_x, last_y;
+  uint32_t at_x[K], at_y[K];
+  __device__ __forceinline__ void start(const T* px, int64_t ldx, const T* py, int64_t ldy, int tid, int G = 1) {
     x = (uint64_t)px;
     y = (uint64_t)py;
     const uint32_t bx = (uint32_t)ldx * sizeof(T), by = (uint32_t)ldy * sizeof(T);
-    step_x = ROWS * bx;
-    step_y = ROWS * by;
-    whole_x = (ROWS - 1) * bx + DH * sizeof(T);
-    whole_y = (ROWS - 1) * by + DH * sizeof(T);
+    next_x = ROWS / G * bx;
+    next_y = ROWS / G * by;
+    step_x = STEP / G * bx;
+    step_y = STEP / G * by;
+    const int row = tid / TL::UPR;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int row = (i * 256 + tid) / TL::UPR, unit = ((i * 256 + tid) % TL::UPR) ^ TL::swz(row);
-      at_x[i] = row * bx + unit * 16;
-      at_y[i] = row * by + unit * 16;
+    for (int k = 0; k < K; ++k) {
+      const uint32_t in_row = row % G * (uint32_t)(DH * sizeof(T)) + ((tid % TL::UPR) ^ TL::swz(row + k * STEP)) * 16;
+      at_x[k] = row / G * bx + in_row;
+      at_y[k] = row / G * by + in_row;
     }
+    last_x = bx;                                      // bytes of n rows: (n / G - 1) last + G rows' widths
+    last_y = by;
   }
-  // the next tile, its first n rows, of them those of `vis` (where `some`)
+  // the next tile, its first n > 0 rows (a multiple of G), of them those of `vis` (where `some`)
   template <int NV>
-  __device__ __forceinline__ void copy(T* tx, T* ty, int n, bool some, const uint64_t (&vis)[NV], int wave, int tid) {
-    const bool whole = n >= ROWS && !some;
-    const u32x4 bx = buffer_of((const void*)x, whole ? whole_x : whole_x - (uint32_t)(ROWS - n) * (step_x / ROWS));
-    const u32x4 by = buffer_of((const void*)y, whole ? whole_y : whole_y - (uint32_t)(ROWS - n) * (step_y / ROWS));
+  __device__ __forceinline__ void copy(T* tx, T* ty, int n, bool some, const uint64_t (&vis)[NV], int wave, int tid, int G = 1) {
+    const uint32_t rows = (n < ROWS ? n : ROWS) / G - 1, width = G * (uint32_t)(DH * sizeof(T));
+    const u32x4 bx = buffer_of((const void*)x, rows * last_x + width), by = buffer_of((const void*)y, rows * last_y + width);
     if (!some) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        copy16(bx, tx + (i * 256 + wave * 64) * TL::E, at_x[i]);
-        copy16(by, ty + (i * 256 + wave * 64) * TL::E, at_y[i]);
+        copy16(bx, tx + (i * 256 + wave * 64) * TL::E, at_x[i % K], i * step_x);
+        copy16(by, ty + (i * 256 + wave * 64) * TL::E, at_y[i % K], i * step_y);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = (i * 256 + tid) / TL::UPR;
         const bool see = (vis[NV > 1 ? row >> 6 : 0] >> (row & 63)) & 1;
-        copy16(bx, tx + (i * 256 + wave * 64) * TL::E, see ? at_x[i] : BAD);
-        copy16(by, ty + (i * 256 + wave * 64) * TL::E, see ? at_y[i] : BAD);
+        copy16(bx, tx + (i * 256 + wave * 64) * TL::E, see ? at_x[i % K] : BAD, i * step_x);
+        copy16(by, ty + (i * 256 + wave * 64) * TL::E, see ? at_y[i % K] : BAD, i * step_y);
       }
     }
-    x += step_x;
-    y += step_y;
+    x += next_x;
+    y += next_y;
+  }
+};
+
+// Where a lane reads in the tiles of a workgroup (LDS bytes).  In bf16 the units of a row differ in their place by
+// exclusive ors of constants, so two addresses and an instruction per read serve in place of one register each.
+template <class T, int DH>
+struct Reads {
+  using TL = Tile<T, DH>;
+  typedef __attribute__((address_space(3))) const u32x4 lds_unit;
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  uint32_t row, col;
+  __device__ __forceinline__ void start(const T* lds, int lane) {
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)const_cast<T*>(lds);
+    const int h = lane >> 5, r = lane & 31, c = 4 * h + ((lane >> 2) & 3);
+    row = base + r * DH * 2 + ((h ^ TL::swz(r)) * 16);
+    col = base + c * DH * 2 + (((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ TL::swz(c)) * 16) + 8 * (lane & 1);
+  }
+  // Tile::mm_row and mm_col of the block at byte OFF (a multiple of 32 rows) of the workgroup's tiles
+  template <int OFF>
+  __device__ __forceinline__ f32x16 mm_row(const typename TL::Op& op) const {
+    f32x16 acc = {};
+#pragma unroll
+    for (int i = 0; i < TL::NR; ++i) {
+      const u32x4 u = *(lds_unit*)(uintptr_t)((row ^ (i * 32)) + OFF);
+      acc = TL::mm_one(u, op[i], acc);
+    }
+    return acc;
+  }
+  template <int OFF>
+  __device__ __forceinline__ void mm_col(const f32x16& p, f32x16 (&acc)[TL::DB]) const {
+    constexpr int TURN = DH == 64 ? 16 : 32;          // row + 8: swz of its fourth bit
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      bf16x8 pf;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pf[j] = (__bf16)p[8 * f + j];
+#pragma unroll
+      for (int b = 0; b < TL::DB; ++b) {
+        s16x4 half[2];
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj)
+          half[jj] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((col ^ (b * 64 ^ jj * TURN)) + (16 * f + 8 * jj) * DH * 2 + OFF));
+        const s16x8 x = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf, acc[b], 0, 0, 0);
+      }
+    }
   }
 };
 
@@ -787,7 +840,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
 // program's keys take the cross attention's.
 
 template <class T, int DH>
-__global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel(const Table t, const Args a) {
+__global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
   constexpr int DB = TL::DB, KB = TILE_ROWS<T, DH>;
   __shared__ __attribute__((aligned(16))) T lds[4 * KB * DH];
@@ -925,31 +978,36 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dq_kernel
   else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
 }
 
-// 128 own keys of a segment (of its n from q0 on), and the stacked rows [x0, x1) that see one of them.
+// 128 keys of a segment (of its n from row k0 on), and the stacked rows [x0, x1) from row q0 on that see one of them: OWN, its
+// own keys (each seen by the rows from its own to its sequence's last), or the program's.
 struct KeyWork {
-  int64_t q0;
+  int64_t q0, k0;
   int n, first, hk, split, seq, x0, x1, t0, t1;
 };
+template <bool OWN>
 __device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int block, int rows, int lane, KeyWork& w) {
   Prob p;
   if (!problem<true>(t, a, 128, p, block)) return false;
-  w.q0 = p.q0; w.n = p.Lk; w.first = p.tile * 128; w.hk = p.hk; w.split = p.split;
-  const int last = min(w.first + 128, w.n) - 1;
-  w.seq = last_start(a.off, 0, a.B - 1, p.q0 + w.first, lane);
-  const int s = last_start(a.off, w.seq, a.B - 1, p.q0 + last, lane);
-  w.x0 = w.first * a.G;
-  w.x1 = (max(min(a.off[s + 1], p.q0 + w.n), p.q0 + last + 1) - p.q0) * a.G;
-  const int tiles = (w.x1 - w.x0 + rows - 1) / rows;
-  const int2 tt = share_of(a, tiles, w.split);
+  w.q0 = p.q0; w.k0 = p.k0; w.n = p.Lk; w.first = p.tile * 128; w.hk = p.hk; w.split = p.split;
+  w.x0 = w.seq = 0;
+  w.x1 = p.R;
+  if constexpr (OWN) {
+    const int last = min(w.first + 128, w.n) - 1;
+    w.seq = last_start(a.off, 0, a.B - 1, p.q0 + w.first, lane);
+    const int s = last_start(a.off, w.seq, a.B - 1, p.q0 + last, lane);
+    w.x0 = w.first * a.G;
+    w.x1 = (max(min(a.off[s + 1], p.q0 + w.n), p.q0 + last + 1) - p.q0) * a.G;
+  }
+  const int2 tt = share_of(a, (w.x1 - w.x0 + rows - 1) / rows, w.split);
   w.t0 = tt.x;
   w.t1 = tt.y;
   return true;
 }
 
-// dk and dv of 128 own keys (32 per wavefront, in registers as row operands): key j is seen by the rows from its
-// own to its sequence's last.
-template <class T, int DH>
-__global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kernel(const Table t, const Args a) {
+// dk and dv of 128 keys (32 per wavefront, in registers as row operands).  EVEN: the heads of a key head divide the rows of
+// a copy, so that a tile of stacked rows is the same pattern everywhere.
+template <class T, int DH, bool OWN, bool EVEN>
+__global__ __launch_bounds__(256, (IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void dkv_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
   constexpr int DB = TL::DB, RB = TILE_ROWS<T, DH>;
   __shared__ __attribute__((aligned(16))) T lds[4 * RB * DH];
@@ -959,27 +1017,40 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
   KeyWork w;
-  if (!key_work_of(t, a, blockIdx.x, RB, lane, w)) return;
+  if (!key_work_of<OWN>(t, a, blockIdx.x, RB, lane, w)) return;
   const int key = w.first + wave * 32 + (lane & 31), kc = min(key, w.n - 1);
-  const int q0 = (int)w.q0, krow = q0 + kc, hk = w.hk, split = w.split, x0 = w.x0, x1 = w.x1, t0 = w.t0, t1 = w.t1;
+  const int hk = w.hk, split = w.split, x0 = w.x0, x1 = w.x1, t0 = w.t0, t1 = w.t1;
+  const int64_t krow = w.k0 + kc;
   typename TL::Op kf, vf;
   TL::load_op(kf, static_cast<const T*>(a.k) + krow * a.ld_k + hk * DH, h);
   TL::load_op(vf, static_cast<const T*>(a.v) + krow * a.ld_v + hk * DH, h);
   TL::scale_op(kf, a.c2);
   // stacked rows of the segment that see a lane's key: [lo, hi)
-  const int lo = kc * a.G, hi = (bounds_of(a, w.seq, krow, lane_of(krow, 31), q0, q0 + w.n, lane).y - q0) * a.G;
+  int lo = 0, hi = x1;
+  if constexpr (OWN) {
+    lo = kc * a.G;
+    hi = (bounds_of(a, w.seq, (int)krow, lane_of((int)krow, 31), (int)w.q0, (int)w.q0 + w.n, lane).y - (int)w.q0) * a.G;
+  }
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
-  auto copy = [&](int ti) {
+  Stream<T, DH, RB> rows;
+  auto copy = [&](int ti, T* qt, T* gt) {
     const int r0 = x0 + ti * RB, q1 = r0 / a.G;              // the tile's first query
-    const u32x4 qb = buffer_of(static_cast<const T*>(a.q) + (w.q0 + q1) * a.ld_q + hk * a.G * DH, BAD - 1);
-    const u32x4 gb = buffer_of(static_cast<const T*>(a.d_o) + (w.q0 + q1) * a.ld_do + hk * a.G * DH, BAD - 1);
-    auto off = [&](int r, int64_t ld) {
-      const int x = r0 + r, qi = x / a.G;
-      return x < x1 ? (uint32_t)(((qi - q1) * ld + (x - qi * a.G) * DH) * sizeof(T)) : BAD;
-    };
-    copy_tile<T, DH, RB, 256>(qb, qs + (ti & 1) * RB * DH, tid, [&](int r) { return off(r, a.ld_q); });
-    copy_tile<T, DH, RB, 256>(gb, gs + (ti & 1) * RB * DH, tid, [&](int r) { return off(r, a.ld_do); });
+    const T* const q = static_cast<const T*>(a.q) + (w.q0 + q1) * a.ld_q + hk * a.G * DH;
+    const T* const g = static_cast<const T*>(a.d_o) + (w.q0 + q1) * a.ld_do + hk * a.G * DH;
+    if constexpr (EVEN) {
+      const uint64_t every[1] = {~0ull};
+      if (ti == t0) rows.start(q, a.ld_q, g, a.ld_do, tid, a.G);
+      rows.copy(qt, gt, min(x1 - r0, RB), false, every, wave, tid, a.G);
+    } else {
+      const u32x4 qb = buffer_of(q, BAD - 1), gb = buffer_of(g, BAD - 1);
+      auto off = [&](int r, int64_t ld) {
+        const int x = r0 + r, qi = x / a.G;
+        return x < x1 ? (uint32_t)(((qi - q1) * ld + (x - qi * a.G) * DH) * sizeof(T)) : BAD;
+      };
+      copy_tile<T, DH, RB, 256>(qb, qt, tid, [&](int r) { return off(r, a.ld_q); });
+      copy_tile<T, DH, RB, 256>(gb, gt, tid, [&](int r) { return off(r, a.ld_do); });
+    }
   };
   float2 sv = make_float2(INFINITY, 0.0f);
   auto load_stat = [&](int ti) {
@@ -990,42 +1061,54 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
       sv = *reinterpret_cast<const float2*>(a.stat + 2 * ((w.q0 + qi) * a.heads + hk * a.G + x - qi * a.G));
     }
   };
-  auto put_stat = [&](int ti) {
+  auto put_stat = [&](int buffer) {
     if (tid < RB) {
-      st[ti & 1][0][tid] = sv.x;
-      st[ti & 1][1][tid] = sv.y;
+      st[buffer][0][tid] = sv.x;
+      st[buffer][1][tid] = sv.y;
     }
   };
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) dk[i] = dv[i] = f32x16{};
   if (t0 < t1) {
-    copy(t0);
+    copy(t0, qs, gs);
     load_stat(t0);
-    put_stat(t0);
+    put_stat(0);
   }
-  for (int ti = t0; ti < t1; ++ti) {
+  Reads<T, DH> at;
+  at.start(lds, lane);
+  auto step = [&](int ti, auto buffer) {
+    constexpr int BUF = decltype(buffer)::value;
     wait_counts<0, true>();
     raw_barrier();
     if (ti + 1 < t1) {
-      copy(ti + 1);
+      copy(ti + 1, qs + (BUF ^ 1) * RB * DH, gs + (BUF ^ 1) * RB * DH);
       load_stat(ti + 1);
     }
-    const T* qt = qs + (ti & 1) * RB * DH;
-    const T* gt = gs + (ti & 1) * RB * DH;
-#pragma unroll
-    for (int rb = 0; rb < RB / 32; ++rb) {
-      const int r0 = x0 + ti * RB + 32 * rb;
-      if (lo_a >= r0 + 32 || hi_z <= r0) continue;           // no key is seen by these rows
-      f32x16 s = TL::mm_row(qt, 32 * rb, kf, lane);
-      f32x16 dp = TL::mm_row(gt, 32 * rb, vf, lane);
-      const f32x16 l2 = load_acc(&st[ti & 1][0][32 * rb], h), de = load_acc(&st[ti & 1][1][32 * rb], h);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = weight<T>(s[r], a.c2, l2[r]);
-        dp[r] -= de[r];
+    if constexpr (IS_BF<T> && DH == 128) asm volatile("" : "+v"(at.row), "+v"(at.col));        // not a register per read
+    auto block = [&](auto which) {
+      constexpr int RBK = decltype(which)::value, QOFF = (BUF * RB + 32 * RBK) * DH * (int)sizeof(T), GOFF = QOFF + 2 * RB * DH * (int)sizeof(T);
+      const int r0 = x0 + ti * RB + 32 * RBK;
+      if (OWN ? lo_a >= r0 + 32 || hi_z <= r0 : r0 >= x1) return;          // no key is seen by these rows
+      f32x16 s, dp;
+      if constexpr (IS_BF<T>) {
+        s = at.template mm_row<QOFF>(kf);
+        dp = at.template mm_row<GOFF>(vf);
+      } else {
+        s = TL::mm_row(qs + BUF * RB * DH, 32 * RBK, kf, lane);
+        dp = TL::mm_row(gs + BUF * RB * DH, 32 * RBK, vf, lane);
       }
-      if (lo_z > r0 || hi_a < r0 + 32) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 l2 = *reinterpret_cast<const f32x4*>(&st[BUF][0][32 * RBK + acc_row(h, 4 * q)]);
+        const f32x4 de = *reinterpret_cast<const f32x4*>(&st[BUF][1][32 * RBK + acc_row(h, 4 * q)]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[4 * q + i] = weight<T>(s[4 * q + i], a.c2, l2[i]);
+          dp[4 * q + i] -= de[i];
+        }
+      }
+      if (OWN && (lo_z > r0 || hi_a < r0 + 32)) {
         uint32_t see = (below(hi - r0) & ~below(lo - r0)) >> (4 * h);
         asm volatile("" : "+v"(see));             // keeps this a branch
 #pragma unroll
@@ -1034,17 +1117,29 @@ __global__ __launch_bounds__(256, (IS_BF<T> && DH <= 64) ? 2 : 1) void dkv_kerne
           dp[r] = (see >> acc_row(0, r)) & 1 ? dp[r] : 0.0f;
         }
       }
-      TL::mm_col(gt, 32 * rb, s, dv, lane);
+      if constexpr (IS_BF<T>) at.template mm_col<GOFF>(s, dv);
+      else TL::mm_col(gs + BUF * RB * DH, 32 * RBK, s, dv, lane);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] *= dp[r];
-      TL::mm_col(qt, 32 * rb, s, dk, lane);
-    }
-    if (ti + 1 < t1) put_stat(ti + 1);
+      if constexpr (IS_BF<T>) at.template mm_col<QOFF>(s, dk);
+      else TL::mm_col(qs + BUF * RB * DH, 32 * RBK, s, dk, lane);
+    };
+    block(std::integral_constant<int, 0>{});
+    if constexpr (RB > 32) block(std::integral_constant<int, 1>{});
+    if (ti + 1 < t1) put_stat(BUF ^ 1);
+  };
+  for (int ti = t0; ti < t1; ti += 2) {
+    step(ti, std::integral_constant<int, 0>{});
+    if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
-  if (a.flags) leave_flag(a, not_finite<DB>(dk) || not_finite<DB>(dv), tid);
+  if (OWN) leave_flag(a, not_finite<DB>(dk) || not_finite<DB>(dv), tid);
   if (key >= w.n) return;
+  if (!OWN && a.mask && a.mask[krow] == 0) {                 // also where such a key holds NaN
+#pragma unroll
+    for (int b = 0; b < DB; ++b) dk[b] = dv[b] = f32x16{};
+  }
   if (a.splits > 1) {
-    const int64_t prow = (int64_t)krow * a.kv_heads + hk;
+    const int64_t prow = krow * a.kv_heads + hk;
     store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
     store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
   } else {
@@ -1206,7 +1301,7 @@ __global__ __launch_bounds__(256) void dkv_again_kernel(const Table t, const Arg
   if (!a.flags[blockIdx.x]) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   KeyWork w;
-  if (!key_work_of(t, a, blockIdx.x, TILE_ROWS<T, DH>, lane, w)) return;
+  if (!key_work_of<true>(t, a, blockIdx.x, TILE_ROWS<T, DH>, lane, w)) return;
   for (int key = w.first + wave; key < min(w.first + 128, w.n); key += 4) {
     const int64_t krow = w.q0 + key;
     const T* k = static_cast<const T*>(a.k) + krow * a.ld_k + w.hk * DH;
@@ -1302,8 +1397,8 @@ struct Shape {
 Shape shape_of(int dtype, int dh) {
   const bool bf = dtype == WM_BF16, wide32 = !bf && dh == 128;
   const int wi = dh == 32 ? 0 : dh == 64 ? 1 : 2;
-  static const int few[2][3] = {{2, 1, 1}, {4, 2, 1}}, fwd[2][3] = {{3, 2, 2}, {4, 3, 2}};
-  static const int dq[2][3] = {{2, 2, 1}, {4, 3, 1}}, dkv[2][3] = {{2, 1, 1}, {3, 2, 1}};
+  static const int few[2][3] = {{2, 1, 1}, {4, 2, 1}}, fwd[2][3] = {{3, 2, 2}, {4, 4, 2}};
+  static const int dq[2][3] = {{2, 2, 1}, {4, 3, 2}}, dkv[2][3] = {{2, 1, 1}, {3, 2, 2}};
   return {bf, wide32 ? 64 : 32, wide32 ? 64 : 128, wide32 ? 32 : 64, few[bf][wi], fwd[bf][wi], dq[bf][wi], dkv[bf][wi]};
 }
 
@@ -1315,7 +1410,7 @@ bool too_wide(int64_t rows_all, int dh) { return rows_all > (int64_t)UINT32_MAX 
 struct Plan {
   Shared sh;
   bool few;
-  Cut fwd, dq, dkv;
+  Cut fwd, dq, dkv, dpkv;
   size_t o_part, o_ml, o_stat, o_flags, bytes;
 };
 
@@ -1334,10 +1429,12 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
     return bad("k and v need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
   const Shape f = shape_of(w->dtype, w->head_dim);
   const int G = w->heads / w->kv_heads, dh = w->head_dim;
-  int64_t row_tiles = 0, few_tiles = 0, key_tiles = 0, longest = 0, longest_rows = 0;
-  double row_steps = 0, few_steps = 0, key_steps = 0;
+  int64_t row_tiles = 0, few_tiles = 0, key_tiles = 0, shared_tiles = 0, longest = 0, longest_rows = 0;
+  double row_steps = 0, few_steps = 0, key_steps = 0, shared_steps = 0;
   for (int i = 0; i < w->S; ++i) {
     const int64_t lq = (int64_t)w->q_off[i + 1] - w->q_off[i], P = (int64_t)w->k_off[i + 1] - w->k_off[i];
+    shared_tiles += cdiv(P, 128);
+    shared_steps += (double)cdiv(P, 128) * cdiv(lq * G, f.tile);
     if (lq == 0) continue;
     // own keys of a tile's rows: their own and those before them, half a sequence on average
     const int64_t T = std::min<int64_t>(a->T_max, lq), own = std::min(lq, 128 / G + T / 2 + 1), few_own = std::min(lq, f.few_rows / G + T / 2 + 1);
@@ -1366,7 +1463,9 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
                             step_us(f.bf, 3, 128, f.tile, dh, f.dq_cu), part_us(rows_all, dh));
   p->dkv = cut_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu,
                              step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh));
-  if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
+  p->dpkv = cut_for(shared_tiles * w->kv_heads, avg(shared_steps, shared_tiles), cdiv(p->sh.max_r, f.tile), 2, f.dkv_cu,
+                    step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * p->sh.nk * w->kv_heads, dh));
+  if (too_wide(rows_all, dh) || too_wide(p->sh.nk * w->kv_heads, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
   p->o_part = p->o_ml = p->o_stat = p->o_flags = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
@@ -1381,9 +1480,10 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
       p->o_flags = take((size_t)std::max(most_blocks(row_tiles * w->kv_heads * p->dq.splits, w->S),
                                          most_blocks(key_tiles * w->kv_heads * p->dkv.splits, w->S)) * 4);
     p->o_stat = take((size_t)rows_all * 8);
-    size_t part = p->sh.part_bytes;              // dq's, own keys' and the programs' keys', one after the other on the stream
+    size_t part = 0;                             // dq's, own keys' and the programs' keys', one after the other on the stream
     if (p->dq.splits > 1) part = std::max(part, (size_t)p->dq.splits * rows_all * dh * 4);
     if (p->dkv.splits > 1) part = std::max(part, (size_t)p->dkv.splits * 2 * kv_all * dh * 4);
+    if (p->dpkv.splits > 1) part = std::max(part, (size_t)p->dpkv.splits * 2 * p->sh.nk * w->kv_heads * dh * 4);
     if (part) p->o_part = take(part);
   }
   p->bytes = workspace_of(at);
@@ -1445,19 +1545,23 @@ hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStr
   });
 }
 
-hipError_t grad_own_keys(const wm_attention* w, const Plan& p, const Args& a, hipStream_t st) {
-  wm_attention own = *w;          // its keys are the rows themselves
-  own.k_off = w->q_off;
+// dk and dv of own keys (OWN: they are the rows themselves) or of the programs' keys.
+template <bool OWN>
+hipError_t grad_keys(const wm_attention* w, int64_t keys, const Args& a, hipStream_t st) {
+  wm_attention own = *w;
+  own.k_off = OWN ? w->q_off : w->k_off;
   return typed(w, [&](auto tv, auto dh) {
     using T = decltype(tv);
     constexpr int DH = decltype(dh)::value;
+    const bool even = Stream<T, DH, TILE_ROWS<T, DH>>::STEP % a.G == 0;
     hipError_t e = each_run(&own, true, a.splits, [&](int64_t, int64_t lk) { return cdiv(lk, 128); },
                             [&](const Table& t, int blocks) {
-                              hipLaunchKernelGGL((dkv_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
-                              hipLaunchKernelGGL((dkv_again_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
+                              if (even) hipLaunchKernelGGL((dkv_kernel<T, DH, OWN, true>), dim3(blocks), dim3(256), 0, st, t, a);
+                              else hipLaunchKernelGGL((dkv_kernel<T, DH, OWN, false>), dim3(blocks), dim3(256), 0, st, t, a);
+                              if (OWN) hipLaunchKernelGGL((dkv_again_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t n = p.sh.nq * a.kv_heads;
+    const int64_t n = keys * a.kv_heads;
     hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 2), dim3(256), 0, st, a.part, n,
                        a.splits, 2, a.kv_heads, a.out, a.ld_out, a.out2, a.ld_out2);
     return hipGetLastError();
@@ -1674,9 +1778,18 @@ wm_status wm_prefix_attention_grad(const wm_prefix* x, const void* o, int64_t ld
     a.splits = p.dkv.splits;
     a.chunk = p.dkv.chunk;
     a.part_rows = nq * w->kv_heads;
-    WM_PF(TK_PREFIX, grad_own_keys(w, p, a, st));
+    WM_PF(TK_PREFIX, grad_keys<true>(w, nq, a, st));
   }
-  if (nk > 0) WM_PF(TK_PREFIX, key_grads(w, d_o, ld_do, a.stat, g->dpk, g->ld_dpk, g->dpv, g->ld_dpv, a.part, st));
+  if (nk > 0) {
+    a.k = w->k; a.ld_k = w->ld_k;
+    a.v = w->v; a.ld_v = w->ld_v;
+    a.out = g->dpk; a.ld_out = g->ld_dpk;
+    a.out2 = g->dpv; a.ld_out2 = g->ld_dpv;
+    a.splits = p.dpkv.splits;
+    a.chunk = p.dpkv.chunk;
+    a.part_rows = nk * w->kv_heads;
+    WM_PF(TK_PREFIX, grad_keys<false>(w, nk, a, st));
+  }
   return clear_error();
 }
 
