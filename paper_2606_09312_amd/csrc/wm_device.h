@@ -322,6 +322,12 @@ __device__ __forceinline__ void copy16(u32x4 r, void* d, uint32_t vo, uint32_t s
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :: "s"(l), "v"(vo), "s"(r), "s"(__builtin_amdgcn_readfirstlane(so)) : "memory", "m0");
 }
+// 4 bytes per lane, a wavefront's 256 side by side.
+__device__ __forceinline__ void copy4(u32x4 r, void* d, uint32_t vo) {
+  const uint32_t l = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)d);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :: "s"(l), "v"(vo), "s"(r) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 // Wait until at most VM vector-memory operations are outstanding, and (LGKM)
 // for every LDS read.

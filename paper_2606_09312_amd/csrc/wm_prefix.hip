@@ -44,9 +44,11 @@ struct Args {
   int joint;                                // by sequences: their programs' keys first
   int more_blocks, more_splits, more_chunk, more_part0;            // the few-row kernel: its first workgroups go by programs
   int32_t* flags;                           // one per workgroup of the launch (null: rows of a tile see the same keys)
+  int32_t* counts;                          // gradient: how many parts a row (a key) of a head has
 };
 
-// Tiles [x, y) of a loop that a split takes.
+// Into how many shares a loop is cut, and the tiles [x, y) of a split's.
+__device__ __forceinline__ int shares_of(const Args& a, int tiles) { return min(max((tiles - 1) / a.chunk + 1, 1), a.splits); }
 __device__ __forceinline__ int2 share_of(const Args& a, int tiles, int split) {
   const int64_t x = (int64_t)a.chunk * split;
   return make_int2((int)min(x, (int64_t)tiles), split == a.splits - 1 ? tiles : (int)min(x + a.chunk, (int64_t)tiles));
@@ -142,7 +144,8 @@ __device__ __forceinline__ void copy_rows(const T* base, int ld, int n, bool som
 // Two matrices' rows tile after tile: where the next tile begins, bytes from one to the next and of a whole one, what a lane
 // adds to a tile's beginning and what each further copy of a tile adds to that.  A whole tile costs four scalar additions
 // beside its copies (with everything formed anew a tile took 169 scalar instructions, as long as its
-// products).  `stacked`: a tile's rows are G heads of each of ROWS / G rows of the matrix (G divides the 256 threads' rows).
+// products).  With lg > 0 a tile's
+// rows are 2^lg heads of each row of the matrix (which divide the rows of a copy).
 template <class T, int DH, int ROWS>
 struct Stream {
   using TL = Tile<T, DH>;
@@ -152,28 +155,28 @@ struct Stream {
   uint64_t x, y;
   uint32_t next_x, next_y, step_x, step_y, last_x, last_y;
   uint32_t at_x[K], at_y[K];
-  __device__ __forceinline__ void start(const T* px, int64_t ldx, const T* py, int64_t ldy, int tid, int G = 1) {
+  __device__ __forceinline__ void start(const T* px, int64_t ldx, const T* py, int64_t ldy, int tid, int lg = 0) {
     x = (uint64_t)px;
     y = (uint64_t)py;
     const uint32_t bx = (uint32_t)ldx * sizeof(T), by = (uint32_t)ldy * sizeof(T);
-    next_x = ROWS / G * bx;
-    next_y = ROWS / G * by;
-    step_x = STEP / G * bx;
-    step_y = STEP / G * by;
+    next_x = (ROWS >> lg) * bx;
+    next_y = (ROWS >> lg) * by;
+    step_x = (STEP >> lg) * bx;
+    step_y = (STEP >> lg) * by;
     const int row = tid / TL::UPR;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const uint32_t in_row = row % G * (uint32_t)(DH * sizeof(T)) + ((tid % TL::UPR) ^ TL::swz(row + k * STEP)) * 16;
-      at_x[k] = row / G * bx + in_row;
-      at_y[k] = row / G * by + in_row;
+      const uint32_t in_row = (row & ((1 << lg) - 1)) * (uint32_t)(DH * sizeof(T)) + ((tid % TL::UPR) ^ TL::swz(row + k * STEP)) * 16;
+      at_x[k] = (row >> lg) * bx + in_row;
+      at_y[k] = (row >> lg) * by + in_row;
     }
     last_x = bx;                                      // bytes of n rows: (n / G - 1) last + G rows' widths
     last_y = by;
   }
-  // the next tile, its first n > 0 rows (a multiple of G), of them those of `vis` (where `some`)
+  // the next tile, its first n > 0 rows (whole rows of the matrix), of them those of `vis` (where `some`)
   template <int NV>
-  __device__ __forceinline__ void copy(T* tx, T* ty, int n, bool some, const uint64_t (&vis)[NV], int wave, int tid, int G = 1) {
-    const uint32_t rows = (n < ROWS ? n : ROWS) / G - 1, width = G * (uint32_t)(DH * sizeof(T));
+  __device__ __forceinline__ void copy(T* tx, T* ty, int n, bool some, const uint64_t (&vis)[NV], int wave, int tid, int lg = 0) {
+    const uint32_t rows = ((n < ROWS ? n : ROWS) >> lg) - 1, width = (uint32_t)(DH * sizeof(T)) << lg;
     const u32x4 bx = buffer_of((const void*)x, rows * last_x + width), by = buffer_of((const void*)y, rows * last_y + width);
     if (!some) {
 #pragma unroll
@@ -212,13 +215,13 @@ struct Reads {
     col = base + c * DH * 2 + (((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ TL::swz(c)) * 16) + 8 * (lane & 1);
   }
   // Tile::mm_row and mm_col of the block at byte OFF (a multiple of 32 rows) of the workgroup's tiles
-  template <int OFF>
-  __device__ __forceinline__ f32x16 mm_row(const typename TL::Op& op) const {
-    f32x16 acc = {};
+  // (op: its registers, the last of which may be kept in LDS)
+  template <int OFF, class Op>
+  __device__ __forceinline__ f32x16 mm_row(Op op, f32x16 acc = f32x16{}) const {
 #pragma unroll
     for (int i = 0; i < TL::NR; ++i) {
       const u32x4 u = *(lds_unit*)(uintptr_t)((row ^ (i * 32)) + OFF);
-      acc = TL::mm_one(u, op[i], acc);
+      acc = TL::mm_one(u, op(i), acc);
     }
     return acc;
   }
@@ -320,7 +323,8 @@ __device__ __forceinline__ void weigh(f32x16& s, float& mx, float& sum, f32x16 (
 }
 // Values of a lane's column where bit acc_row(0, r) of its half of `seen` is set, `other` elsewhere.
 __device__ __forceinline__ void only(f32x16& s, uint32_t seen, float other, int h) {
-  const uint32_t m = seen >> (4 * h);
+  uint32_t m = seen >> (4 * h);
+  asm volatile("" : "+v"(m));                 // where this is under a condition it stays a branch: 48 instructions
 #pragma unroll
   for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : other;
 }
@@ -811,19 +815,36 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
   const int64_t r = i / Q;
   if (r / a.heads >= a.off[a.B]) return;                      // behind the last sequence
   const int d = (int)(i % Q) * 4;
-  float top = -INFINITY;
-  for (int s = 0; s < a.parts; ++s) top = fmaxf(top, a.part_ml[2 * (s * a.part_rows + r)]);
-  float sum = 0.0f;
+  float top = -INFINITY, sum = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < a.parts; ++s) {
-    const int64_t p = s * a.part_rows + r;
-    const float l = a.part_ml[2 * p + 1];
-    if (l == 0.0f) continue;
-    const float f = exp2_of(a.part_ml[2 * p] - top);
-    sum = fmaf(l, f, sum);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + p * DH + d);
+  constexpr int AHEAD = 8;                                    // parts whose loads are under way together
+  for (int s0 = 0; s0 < a.parts; s0 += AHEAD) {
+    float2 ml[AHEAD];
+    f32x4 x[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = fmaf(x[j], f, acc[j]);
+    for (int i = 0; i < AHEAD; ++i) {
+      const int64_t p = min(s0 + i, a.parts - 1) * a.part_rows + r;
+      ml[i] = *reinterpret_cast<const float2*>(a.part_ml + 2 * p);
+      if (s0 + i >= a.parts) ml[i].y = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (ml[i].y != 0.0f) x[i] = *reinterpret_cast<const f32x4*>(a.part + ((s0 + i) * a.part_rows + r) * DH + d);
+    float m = top;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) m = ml[i].y != 0.0f ? fmaxf(m, ml[i].x) : m;
+    const float f0 = top == m ? 1.0f : exp2_of(top - m);
+    top = m;
+    sum *= f0;
+    acc *= f0;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (ml[i].y == 0.0f) continue;
+      const float f = exp2_of(ml[i].x - top);
+      sum = fmaf(ml[i].y, f, sum);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = fmaf(x[i][j], f, acc[j]);
+    }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   typedef T t4 __attribute__((ext_vector_type(4)));
@@ -877,6 +898,12 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
 
   const int P = w.P, o0 = w.o0, rest = w.rest, o1 = w.o1, nP = (P + KB - 1) / KB, tiles = nP + (rest - o0) / KB;
   const int2 tt = share_of(a, tiles, split);
+  const int shares = shares_of(a, tiles);
+  if (split >= shares) {
+    if (tid == 0) a.flags[blockIdx.x] = 0;
+    return;
+  }
+  if (split == 0 && h == 0 && row < w.R) a.counts[orow] = shares;
   const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
   uint64_t vis[1] = {0}, next[1] = {0};
@@ -940,7 +967,7 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
     step(ti, std::integral_constant<int, 0>{});
     if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
-  if (split == a.splits - 1 && rest < o1) {                    // as in the forward kernel
+  if (split == shares - 1 && rest < o1) {                      // as in the forward kernel
     constexpr bool TWO = KB >= 64;
     __syncthreads();
     T* const kt = lds + wave * KB * DH;
@@ -972,7 +999,7 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
       if (more) copy_of(TWO ? a.k : a.v, TWO ? a.ld_k : a.ld_v, first + 32, TWO ? kt : vt);
     }
   }
-  if (a.flags) leave_flag(a, not_finite<DB>(acc), tid);
+  leave_flag(a, not_finite<DB>(acc), tid);
   if (row >= w.R) return;
   if (a.splits > 1) store_cols<float, DB>(a.part + (split * a.part_rows + orow) * DH, acc, a.scale, h);
   else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
@@ -1007,42 +1034,69 @@ __device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int b
 // dk and dv of 128 keys (32 per wavefront, in registers as row operands).  EVEN: the heads of a key head divide the rows of
 // a copy, so that a tile of stacked rows is the same pattern everywhere.
 template <class T, int DH, bool OWN, bool EVEN>
-__global__ __launch_bounds__(256, (IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void dkv_kernel(const Table t, const Args a) {
+__global__ __launch_bounds__(256, (IS_BF<T> && EVEN && DH == 64 ? 3 : IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void dkv_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
   constexpr int DB = TL::DB, RB = TILE_ROWS<T, DH>;
   __shared__ __attribute__((aligned(16))) T lds[4 * RB * DH];
-  __shared__ __attribute__((aligned(16))) float st[2][2][RB];      // [buffer][lse log2 e, delta][row]
+  __shared__ __attribute__((aligned(16))) float st[2][2 * RB];     // [buffer][row][lse log2 e, delta]
+  // The sums and operands leave too few of 256 registers (168 at a width of 64): some of the operands' stay in LDS.  (Where the
+  // compiler spilled three, every reload waited for the copies under way, 1.53 ms for 1.25.)
+  constexpr int KEPT_K = IS_BF<T> && EVEN && (DH == 128 || (DH == 64 && OWN)) ? 1 : 0, KEPT_V = DH == 128 ? 2 * KEPT_K : 0;
+  __shared__ __attribute__((aligned(16))) u32x4 kept[KEPT_K ? (KEPT_K + KEPT_V) * 256 : 1];
   T* const qs = lds;
   T* const gs = lds + 2 * RB * DH;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
   KeyWork w;
   if (!key_work_of<OWN>(t, a, blockIdx.x, RB, lane, w)) return;
-  const int key = w.first + wave * 32 + (lane & 31), kc = min(key, w.n - 1);
+  const int shares = shares_of(a, (w.x1 - w.x0 + RB - 1) / RB);
+  if (w.split >= shares) {
+    if (OWN && tid == 0) a.flags[blockIdx.x] = 0;
+    return;
+  }
+  const int kc = min(w.first + wave * 32 + (lane & 31), w.n - 1);
   const int hk = w.hk, split = w.split, x0 = w.x0, x1 = w.x1, t0 = w.t0, t1 = w.t1;
-  const int64_t krow = w.k0 + kc;
+  const int64_t kclamped = w.k0 + kc;
   typename TL::Op kf, vf;
-  TL::load_op(kf, static_cast<const T*>(a.k) + krow * a.ld_k + hk * DH, h);
-  TL::load_op(vf, static_cast<const T*>(a.v) + krow * a.ld_v + hk * DH, h);
+  TL::load_op(kf, static_cast<const T*>(a.k) + kclamped * a.ld_k + hk * DH, h);
+  TL::load_op(vf, static_cast<const T*>(a.v) + kclamped * a.ld_v + hk * DH, h);
   TL::scale_op(kf, a.c2);
+  if constexpr (KEPT_K > 0) {                                // a thread reads back its own: no barrier
+    kept[tid] = kf[TL::NR - 1];
+#pragma unroll
+    for (int i = 1; i <= KEPT_V; ++i) kept[256 * i + tid] = vf[TL::NR - i];
+  }
+  auto k_op = [&](int i) -> u32x4 { return i < TL::NR - KEPT_K ? kf[i] : kept[tid]; };
+  auto v_op = [&](int i) -> u32x4 { return i < TL::NR - KEPT_V ? vf[i] : kept[256 * (TL::NR - i) + tid]; };
   // stacked rows of the segment that see a lane's key: [lo, hi)
   int lo = 0, hi = x1;
   if constexpr (OWN) {
     lo = kc * a.G;
-    hi = (bounds_of(a, w.seq, (int)krow, lane_of((int)krow, 31), (int)w.q0, (int)w.q0 + w.n, lane).y - (int)w.q0) * a.G;
+    hi = (bounds_of(a, w.seq, (int)kclamped, lane_of((int)kclamped, 31), (int)w.q0, (int)w.q0 + w.n, lane).y - (int)w.q0) * a.G;
   }
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
+  __shared__ int2 seen_by[OWN ? 128 : 1];                    // out of the registers' way; written and read by the same wavefront
+  const int mine = 32 * wave + (lane & 31);
+  if constexpr (OWN) seen_by[mine] = make_int2(lo, hi);
 
   Stream<T, DH, RB> rows;
+  const float* stats;
+  const int lg = EVEN ? 31 - __builtin_clz(a.G) : 0;
+  auto start = [&]() {
+    const int64_t q1 = w.q0 + ((x0 + t0 * RB) >> lg);        // the first tile's first query
+    rows.start(static_cast<const T*>(a.q) + q1 * a.ld_q + hk * a.G * DH, a.ld_q, static_cast<const T*>(a.d_o) + q1 * a.ld_do + hk * a.G * DH,
+               a.ld_do, tid, lg);
+    stats = a.stat + 2 * (q1 * a.heads + hk * a.G);
+  };
   auto copy = [&](int ti, T* qt, T* gt) {
-    const int r0 = x0 + ti * RB, q1 = r0 / a.G;              // the tile's first query
-    const T* const q = static_cast<const T*>(a.q) + (w.q0 + q1) * a.ld_q + hk * a.G * DH;
-    const T* const g = static_cast<const T*>(a.d_o) + (w.q0 + q1) * a.ld_do + hk * a.G * DH;
+    const int r0 = x0 + ti * RB;
     if constexpr (EVEN) {
       const uint64_t every[1] = {~0ull};
-      if (ti == t0) rows.start(q, a.ld_q, g, a.ld_do, tid, a.G);
-      rows.copy(qt, gt, min(x1 - r0, RB), false, every, wave, tid, a.G);
+      rows.copy(qt, gt, x1 - r0, false, every, wave, tid, lg);
     } else {
+      const int q1 = r0 / a.G;                               // the tile's first query
+      const T* const q = static_cast<const T*>(a.q) + (w.q0 + q1) * a.ld_q + hk * a.G * DH;
+      const T* const g = static_cast<const T*>(a.d_o) + (w.q0 + q1) * a.ld_do + hk * a.G * DH;
       const u32x4 qb = buffer_of(q, BAD - 1), gb = buffer_of(g, BAD - 1);
       auto off = [&](int r, int64_t ld) {
         const int x = r0 + r, qi = x / a.G;
@@ -1052,28 +1106,26 @@ __global__ __launch_bounds__(256, (IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void
       copy_tile<T, DH, RB, 256>(gb, gt, tid, [&](int r) { return off(r, a.ld_do); });
     }
   };
-  float2 sv = make_float2(INFINITY, 0.0f);
-  auto load_stat = [&](int ti) {
-    sv = make_float2(INFINITY, 0.0f);                        // rows past the end: P = 0
-    const int x = x0 + ti * RB + tid;
-    if (tid < RB && x < x1) {
-      const int qi = x / a.G;
-      sv = *reinterpret_cast<const float2*>(a.stat + 2 * ((w.q0 + qi) * a.heads + hk * a.G + x - qi * a.G));
-    }
-  };
-  auto put_stat = [&](int buffer) {
-    if (tid < RB) {
-      st[buffer][0][tid] = sv.x;
-      st[buffer][1][tid] = sv.y;
+  // (lse log2 e, delta) of a tile's rows; rows past the end read as zero like q and do, and add nothing
+  auto copy_stat = [&](int ti, int buffer) {
+    if (wave >= RB / 32) return;
+    const int r0 = x0 + ti * RB, r = 32 * wave + (lane >> 1);
+    if constexpr (EVEN) {
+      const int n = min(x1 - r0, RB) >> lg;
+      copy4(buffer_of(stats, ((n - 1) * a.heads + a.G) * 8), &st[buffer][64 * wave], ((r >> lg) * a.heads + (r & (a.G - 1))) * 8 + (lane & 1) * 4);
+      stats += 2 * (RB >> lg) * a.heads;
+    } else {
+      const int q1 = r0 / a.G, qi = (r0 + r) / a.G;
+      copy4(buffer_of(a.stat + 2 * ((w.q0 + q1) * a.heads + hk * a.G), BAD - 1), &st[buffer][64 * wave], r0 + r < x1 ? ((qi - q1) * a.heads + r0 + r - qi * a.G) * 8 + (lane & 1) * 4 : BAD);
     }
   };
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) dk[i] = dv[i] = f32x16{};
   if (t0 < t1) {
+    if constexpr (EVEN) start();
     copy(t0, qs, gs);
-    load_stat(t0);
-    put_stat(0);
+    copy_stat(t0, 0);
   }
   Reads<T, DH> at;
   at.start(lds, lane);
@@ -1083,38 +1135,38 @@ __global__ __launch_bounds__(256, (IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void
     raw_barrier();
     if (ti + 1 < t1) {
       copy(ti + 1, qs + (BUF ^ 1) * RB * DH, gs + (BUF ^ 1) * RB * DH);
-      load_stat(ti + 1);
+      copy_stat(ti + 1, BUF ^ 1);
     }
     if constexpr (IS_BF<T> && DH == 128) asm volatile("" : "+v"(at.row), "+v"(at.col));        // not a register per read
     auto block = [&](auto which) {
       constexpr int RBK = decltype(which)::value, QOFF = (BUF * RB + 32 * RBK) * DH * (int)sizeof(T), GOFF = QOFF + 2 * RB * DH * (int)sizeof(T);
       const int r0 = x0 + ti * RB + 32 * RBK;
       if (OWN ? lo_a >= r0 + 32 || hi_z <= r0 : r0 >= x1) return;          // no key is seen by these rows
-      f32x16 s, dp;
+      // Where not every key sees every row, scores start from -infinity in the others' place: weights of 0 there, at no
+      // register's cost.
+      f32x16 s = {}, dp;
+      if (OWN && (lo_z > r0 || hi_a < r0 + 32)) {
+        const int2 by = seen_by[mine];
+        only(s, below(by.y - r0) & ~below(by.x - r0), -INFINITY, h);
+      }
       if constexpr (IS_BF<T>) {
-        s = at.template mm_row<QOFF>(kf);
-        dp = at.template mm_row<GOFF>(vf);
+        s = at.template mm_row<QOFF>(k_op, s);
+        dp = at.template mm_row<GOFF>(v_op);
       } else {
-        s = TL::mm_row(qs + BUF * RB * DH, 32 * RBK, kf, lane);
+        const f32x16 x = TL::mm_row(qs + BUF * RB * DH, 32 * RBK, kf, lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] += x[r];
         dp = TL::mm_row(gs + BUF * RB * DH, 32 * RBK, vf, lane);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const f32x4 l2 = *reinterpret_cast<const f32x4*>(&st[BUF][0][32 * RBK + acc_row(h, 4 * q)]);
-        const f32x4 de = *reinterpret_cast<const f32x4*>(&st[BUF][1][32 * RBK + acc_row(h, 4 * q)]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[4 * q + i] = weight<T>(s[4 * q + i], a.c2, l2[i]);
-          dp[4 * q + i] -= de[i];
-        }
-      }
-      if (OWN && (lo_z > r0 || hi_a < r0 + 32)) {
-        uint32_t see = (below(hi - r0) & ~below(lo - r0)) >> (4 * h);
-        asm volatile("" : "+v"(see));             // keeps this a branch
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[r] = (see >> acc_row(0, r)) & 1 ? s[r] : 0.0f;
-          dp[r] = (see >> acc_row(0, r)) & 1 ? dp[r] : 0.0f;
+        for (int i = 0; i < 4; i += 2) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(&st[BUF][2 * (32 * RBK + acc_row(h, 4 * q) + i)]);
+          s[4 * q + i] = weight<T>(s[4 * q + i], a.c2, x[0]);
+          s[4 * q + i + 1] = weight<T>(s[4 * q + i + 1], a.c2, x[2]);
+          dp[4 * q + i] -= x[1];
+          dp[4 * q + i + 1] -= x[3];
         }
       }
       if constexpr (IS_BF<T>) at.template mm_col<GOFF>(s, dv);
@@ -1126,13 +1178,16 @@ __global__ __launch_bounds__(256, (IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void
     };
     block(std::integral_constant<int, 0>{});
     if constexpr (RB > 32) block(std::integral_constant<int, 1>{});
-    if (ti + 1 < t1) put_stat(BUF ^ 1);
   };
   for (int ti = t0; ti < t1; ti += 2) {
     step(ti, std::integral_constant<int, 0>{});
     if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
   if (OWN) leave_flag(a, not_finite<DB>(dk) || not_finite<DB>(dv), tid);
+  int kl = threadIdx.x & 31;                                 // formed again, as above
+  asm volatile("" : "+v"(kl));
+  const int key = w.first + wave * 32 + kl;
+  const int64_t krow = w.k0 + key;
   if (key >= w.n) return;
   if (!OWN && a.mask && a.mask[krow] == 0) {                 // also where such a key holds NaN
 #pragma unroll
@@ -1140,6 +1195,7 @@ __global__ __launch_bounds__(256, (IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void
   }
   if (a.splits > 1) {
     const int64_t prow = krow * a.kv_heads + hk;
+    if (split == 0 && h == 0) a.counts[prow] = shares;
     store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
     store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
   } else {
@@ -1200,8 +1256,8 @@ struct Span {
 __device__ __forceinline__ Span span_of(const Args& a, const Work& w, int KB) {
   const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.rest - w.o0) / KB;
   const int2 tt = share_of(a, tiles, w.split);
-  const int t0 = tt.x, t1 = tt.y;
-  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, w.split == a.splits - 1 ? w.o1 : w.o0 + max(t1 - nP, 0) * KB};
+  const int t0 = tt.x, t1 = tt.y, last = a.counts ? shares_of(a, tiles) - 1 : a.splits - 1;
+  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, w.split == last ? w.o1 : w.o0 + max(t1 - nP, 0) * KB};
 }
 // Own keys that a row sees.
 template <bool PAGED>
@@ -1335,9 +1391,9 @@ __global__ __launch_bounds__(256) void dkv_again_kernel(const Table t, const Arg
   }
 }
 
-// out[row] = sum of the splits' rows, in order; blockIdx.y picks dk or dv.
+// out[row] = sum of its parts' rows, in order; blockIdx.y picks dk or dv.
 template <class T, int DH>
-__global__ __launch_bounds__(256) void add_kernel(const float* part, int64_t rows, int splits, int sets, int heads,
+__global__ __launch_bounds__(256) void add_kernel(const float* part, const int32_t* counts, int64_t rows, int sets, int heads,
                                                   void* out0, int64_t ld0, void* out1, int64_t ld1) {
   constexpr int Q = DH / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -1346,7 +1402,8 @@ __global__ __launch_bounds__(256) void add_kernel(const float* part, int64_t row
   const int64_t r = i / Q, ld = set ? ld1 : ld0;
   const int d = (int)(i % Q) * 4;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < splits; ++s) acc += *reinterpret_cast<const f32x4*>(part + (((int64_t)s * sets + set) * rows + r) * DH + d);
+  const int n = counts[r];
+  for (int s = 0; s < n; ++s) acc += *reinterpret_cast<const f32x4*>(part + (((int64_t)s * sets + set) * rows + r) * DH + d);
   typedef T t4 __attribute__((ext_vector_type(4)));
   t4 y;
 #pragma unroll
@@ -1365,25 +1422,30 @@ double step_us(bool bf, int products, int64_t rows, int64_t keys, int dh, int pe
 double few_us(bool bf, int64_t keys, int dh, int per_cu) {
   return std::max(1.0, 2.0 * keys * dh * (bf ? 2 : 4) * 256 * per_cu / 4.5e6);
 }
+// A tile's time beside few others, of that where a compute unit's places are taken: products hardly gain, reading does.
+double alone_of(bool few, int per_cu) { return few ? 0.3 + 0.7 / per_cu : 0.7 + 0.3 / per_cu; }
 double part_us(int64_t values, int dh) { return 2.0 * values * dh * 4 / 4.5e6; }
 
-// How loops are cut into splits of `chunk` tiles (long ones into more): `blocks` loops of `avg` tiles of unit_us each, `longest` at
-// most, on 256 x per_cu places.  The time is that of the fullest place, about half a chunk more than an even
-// share and at least a chunk, plus what a part costs to write and read.  A split of the longest loop keeps `least` tiles.
+// How loops are cut into splits of `chunk` tiles (long ones into more): `blocks` loops of `avg` tiles on average and `longest` at
+// most, on 256 x per_cu places.  A tile takes unit_us where all places are taken, and `alone` of that where few are.  More shares than
+// places take an even part of the work and half a share on top, fewer as long as the longest share; parts have to be
+// written and read.  A split of the longest loop keeps `least` tiles.  (Measured at 256 loops of 64 to 256 tiles on 512 places, a
+// step over long programs: 9 splits 284 us, 3 splits 375.)
 struct Cut {
   int splits, chunk;
 };
-Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_cu, double unit_us, double part_us) {
+Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_cu, double alone, double unit_us, double part_us) {
   Cut best = {1, (int)std::max<int64_t>(longest, 1)};
   const double places = 256.0 * per_cu, even = blocks * avg / places;
-  double cost = std::max({std::ceil(blocks / places) * avg, even + 0.5 * avg, (double)longest}) * unit_us;
-  for (int s = 2; s <= 64 && s <= longest / least; ++s) {
-    const int64_t chunk = cdiv(longest, s);
-    const double items = blocks * std::max(1.0, avg / chunk), own = std::min<double>(chunk, avg);
-    const double c = std::max({std::ceil(items / places) * own, even + 0.5 * own, (double)chunk}) * unit_us + (avg / chunk + 0.5) * part_us + 4.0;
-    if (c < 0.98 * cost) {
+  double cost = 0.0;
+  for (int s = 1; s <= 64 && (s == 1 || s <= longest / least); ++s) {
+    const int64_t chunk = std::max<int64_t>(cdiv(longest, s), 1);
+    const double shares = s > 1 ? avg / chunk + 0.5 : 1.0, fill = blocks * shares / places;
+    const double tiles = std::max(fill <= 1.0 ? even : even + 0.5 * std::min<double>(chunk, avg), chunk * alone);
+    const double c = tiles * unit_us + (s > 1 ? shares * part_us + 4.0 : 0.0);
+    if (s == 1 || c < 0.98 * cost) {
       cost = c;
-      best = {(int)cdiv(longest, chunk), (int)chunk};
+      best = {(int)std::max<int64_t>(cdiv(longest, chunk), 1), (int)chunk};
     }
   }
   return best;
@@ -1398,7 +1460,7 @@ Shape shape_of(int dtype, int dh) {
   const bool bf = dtype == WM_BF16, wide32 = !bf && dh == 128;
   const int wi = dh == 32 ? 0 : dh == 64 ? 1 : 2;
   static const int few[2][3] = {{2, 1, 1}, {4, 2, 1}}, fwd[2][3] = {{3, 2, 2}, {4, 4, 2}};
-  static const int dq[2][3] = {{2, 2, 1}, {4, 3, 2}}, dkv[2][3] = {{2, 1, 1}, {3, 2, 2}};
+  static const int dq[2][3] = {{2, 2, 1}, {4, 3, 2}}, dkv[2][3] = {{2, 1, 1}, {4, 3, 2}};
   return {bf, wide32 ? 64 : 32, wide32 ? 64 : 128, wide32 ? 32 : 64, few[bf][wi], fwd[bf][wi], dq[bf][wi], dkv[bf][wi]};
 }
 
@@ -1411,7 +1473,7 @@ struct Plan {
   Shared sh;
   bool few;
   Cut fwd, dq, dkv, dpkv;
-  size_t o_part, o_ml, o_stat, o_flags, bytes;
+  size_t o_part, o_ml, o_stat, o_flags, o_counts, bytes;
 };
 
 // a launch's workgroups: its work, dealt out over the XCDs by segment
@@ -1454,20 +1516,20 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
   auto avg = [](double steps, int64_t tiles) { return tiles ? steps / tiles : 0.0; };
   p->few = p->sh.max_r <= f.few_rows;
   if (p->few)
-    p->fwd = cut_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu,
+    p->fwd = cut_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu, alone_of(true, f.few_cu),
                                few_us(f.bf, f.few_keys, dh, f.few_cu), part_us(rows_all, dh));
   else
-    p->fwd = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.fwd_cu,
+    p->fwd = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.fwd_cu, alone_of(false, f.fwd_cu),
                                step_us(f.bf, 2, 128, f.tile, dh, f.fwd_cu), part_us(rows_all, dh));
-  p->dq = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.dq_cu,
+  p->dq = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.dq_cu, alone_of(false, f.dq_cu),
                             step_us(f.bf, 3, 128, f.tile, dh, f.dq_cu), part_us(rows_all, dh));
-  p->dkv = cut_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu,
+  p->dkv = cut_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu, alone_of(false, f.dkv_cu),
                              step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh));
-  p->dpkv = cut_for(shared_tiles * w->kv_heads, avg(shared_steps, shared_tiles), cdiv(p->sh.max_r, f.tile), 2, f.dkv_cu,
+  p->dpkv = cut_for(shared_tiles * w->kv_heads, avg(shared_steps, shared_tiles), cdiv(p->sh.max_r, f.tile), 2, f.dkv_cu, alone_of(false, f.dkv_cu),
                     step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * p->sh.nk * w->kv_heads, dh));
   if (too_wide(rows_all, dh) || too_wide(p->sh.nk * w->kv_heads, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
-  p->o_part = p->o_ml = p->o_stat = p->o_flags = 0;
+  p->o_part = p->o_ml = p->o_stat = p->o_flags = p->o_counts = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   if (!grad) {
     if (nq > 0) p->o_flags = take((size_t)most_blocks((p->few ? few_tiles : row_tiles) * w->kv_heads * p->fwd.splits, w->S) * 4);
@@ -1485,6 +1547,7 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
     if (p->dkv.splits > 1) part = std::max(part, (size_t)p->dkv.splits * 2 * kv_all * dh * 4);
     if (p->dpkv.splits > 1) part = std::max(part, (size_t)p->dpkv.splits * 2 * p->sh.nk * w->kv_heads * dh * 4);
     if (part) p->o_part = take(part);
+    p->o_counts = take((size_t)std::max({rows_all, kv_all, p->sh.nk * w->kv_heads}) * 4);
   }
   p->bytes = workspace_of(at);
   return WM_OK;
@@ -1539,8 +1602,8 @@ hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStr
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.sh.nq * a.heads;
-    hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 1), dim3(256), 0, st, a.part, n,
-                       a.splits, 1, a.heads, a.out, a.ld_out, nullptr, (int64_t)0);
+    hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 1), dim3(256), 0, st, a.part, a.counts, n,
+                       1, a.heads, a.out, a.ld_out, nullptr, (int64_t)0);
     return hipGetLastError();
   });
 }
@@ -1562,8 +1625,8 @@ hipError_t grad_keys(const wm_attention* w, int64_t keys, const Args& a, hipStre
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = keys * a.kv_heads;
-    hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 2), dim3(256), 0, st, a.part, n,
-                       a.splits, 2, a.kv_heads, a.out, a.ld_out, a.out2, a.ld_out2);
+    hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 2), dim3(256), 0, st, a.part, a.counts, n,
+                       2, a.kv_heads, a.out, a.ld_out, a.out2, a.ld_out2);
     return hipGetLastError();
   });
 }
@@ -1626,7 +1689,7 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   auto cut = [&](bool few, int64_t blocks, int64_t longest) {
     const int keys = few ? FEW_KEYS : f.tile, cu = few ? few_cu : f.fwd_cu;
     const int64_t steps = cdiv(longest, keys);
-    return cut_for(blocks, 0.6 * steps, steps, 2, cu, few ? few_us(f.bf, keys, dh, cu) : step_us(f.bf, 2, 128, keys, dh, cu), part_us(rows_all, dh));
+    return cut_for(blocks, 0.6 * steps, steps, 2, cu, alone_of(few, cu), few ? few_us(f.bf, keys, dh, cu) : step_us(f.bf, 2, 128, keys, dh, cu), part_us(rows_all, dh));
   };
   p->own = cut(p->few, tiles, (int64_t)a->len_max + (p->joint ? P : 0));
   p->shared = {0, 0};
@@ -1767,6 +1830,7 @@ wm_status wm_prefix_attention_grad(const wm_prefix* x, const void* o, int64_t ld
   a.stat = reinterpret_cast<float*>(w8 + p.o_stat);
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
+  a.counts = reinterpret_cast<int32_t*>(w8 + p.o_counts);
   if (nq > 0) {
     a.out = g->dq; a.ld_out = g->ld_dq;
     a.splits = p.dq.splits;
