@@ -272,7 +272,7 @@ wm_status wm_rotate(const wm_rotation* x, void* y, int64_t ld_y, void* stream) {
   const int64_t width = (int64_t)x->heads * x->head_dim;
   if (!rows_ok(x->dtype, x->x, x->ld_x, x->rows, width) || !rows_ok(x->dtype, y, ld_y, x->rows, width))
     return bad("x and y need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
-  if (x->x == y && x->ld_x != ld_y) return bad("y may be x with the same row stride only");
+  if (x->rows > 0 && x->x == y && x->ld_x != ld_y) return bad("y may be x with the same row stride only");
   if (x->rows == 0) return clear_error();
   hipStream_t st = static_cast<hipStream_t>(stream);
   Args a = {};
@@ -298,7 +298,7 @@ wm_status wm_cache_append(const wm_append* x, void* q_out, int64_t ld_q_out, voi
     return bad("k and v need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
   if (x->q && (!rows_ok(c.dtype, x->q, x->ld_q, x->rows, qw) || !rows_ok(c.dtype, q_out, ld_q_out, x->rows, qw)))
     return bad("q and q_out need 16-byte aligned rows: pointer, stride at least the row's width, at most 2^22 elements");
-  if (x->q && x->q == q_out && x->ld_q != ld_q_out) return bad("q_out may be q with the same row stride only");
+  if (x->rows > 0 && x->q && x->q == q_out && x->ld_q != ld_q_out) return bad("q_out may be q with the same row stride only");
   if (x->rows == 0) return clear_error();
   hipStream_t st = static_cast<hipStream_t>(stream);
   Args a = {};
