@@ -145,3 +145,20 @@ def prefix_grad(do, q, k, v, pk, pv, off, q_off, p_off, scale, mask=None, o=None
         dk[rows, g] += gk[n:]
         dv[rows, g] += gv[n:]
     return dq, dk, dv, dpk, dpv
+
+
+def grad_spread(do, q, k, v, pk, pv, off, q_off, p_off, scale, mask, o):
+    """How far dq, dk, dv, dpk, dpv can be from prefix_grad's when any of the rows take the mean of their score gradients, do . o, from
+    the exact o instead of this one: bounds element by element."""
+    do, q, k, v, pk, pv, o = (np.asarray(t, np.float64) for t in (do, q, k, v, pk, pv, o))
+    exact = prefix(q, k, v, pk, pv, off, q_off, p_off, scale, mask)[0]
+    dq, dk, dv, dpk, dpv = (np.zeros(t.shape) for t in (q, k, v, pk, pv))
+    for rows, shown, h, g, seen in _parts(q, k, v, pk, pv, off, q_off, p_off, mask):
+        keys = np.concatenate([pk[shown, g], k[rows, g]])
+        w, _ = _softmax(q[rows, h], keys, scale, seen)
+        change = np.abs((do[rows, h] * (o - exact)[rows, h]).sum(1, keepdims=True)) * scale
+        dq[rows, h] = np.abs(w @ keys) * change
+        gk, n = (w * change).T @ np.abs(q[rows, h]), len(shown)
+        dpk[shown, g] += gk[:n]
+        dk[rows, g] += gk[n:]
+    return dq, dk, dv, dpk, dpv

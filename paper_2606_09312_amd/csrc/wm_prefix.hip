@@ -889,10 +889,6 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
   // a row that saw only keys of weight 0 has lse = -inf: its P is 0
   const float l2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
   const int split = w.split;
-  if (split == 0 && h == 0 && row < w.R) {
-    a.stat[2 * orow] = l2;
-    a.stat[2 * orow + 1] = delta;
-  }
   const int lo = bounds_of(a, w.seq, (int)qrow, lane_of((int)qrow, 31), (int)w.q0, (int)w.q0 + w.R / a.G, lane).x, hi = (int)qrow + 1;
   const int lo_a = lane_of(lo, 0), lo_z = lane_of(lo, 31), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
 
@@ -978,6 +974,27 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
       copy_rows<T, DH, 32, 64>(static_cast<const T*>(x) + first * ld + w.hk * DH, (int)ld, end - first, false, every, tile, lane);
     };
     int first = max(lo_a, rest);
+    // Rows without shared tiles see so few keys that the rounding of o in do . o would be the largest of their errors (16 bits,
+    // sequences of 3 rows: dq and dk 2.0 roundings off instead of 1.4; of 128 rows, 1.5): theirs is the sum of P (do . v).
+    if (tiles == 0 && first < end) {
+      float sum = 0.0f;
+      for (int at = first; at < end; at += 32) {
+        copy_of(a.v, a.ld_v, at, vt);
+        wait_counts<0, true>();
+        const f32x16 dp = TL::mm_row(vt, 0, gf, lane);
+        wait_counts<63, true>();
+        copy_of(a.k, a.ld_k, at, kt);
+        wait_counts<0, true>();
+        f32x16 s = TL::mm_row(kt, 0, qf, lane);
+        wait_counts<63, true>();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * dp[r];
+        only(s, below(hi - at) & ~below(lo - at), 0.0f, h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += s[r];
+      }
+      delta = pair_sum(sum);
+    }
     if (first < end) copy_of(a.v, a.ld_v, first, vt);
     if (TWO && first < end) copy_of(a.k, a.ld_k, first, kt);
     for (; first < end; first += 32) {
@@ -1001,6 +1018,10 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
   }
   leave_flag(a, not_finite<DB>(acc), tid);
   if (row >= w.R) return;
+  if (split == 0 && h == 0) {
+    a.stat[2 * orow] = l2;
+    a.stat[2 * orow + 1] = delta;
+  }
   if (a.splits > 1) store_cols<float, DB>(a.part + (split * a.part_rows + orow) * DH, acc, a.scale, h);
   else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
 }

@@ -26,7 +26,8 @@ def host(t):
     return t.detach().double().cpu().numpy()
 
 
-def close(name, got, want, tol):
+def close(name, got, want, tol, spread=None):
+    """spread: what a result may be off besides, element by element."""
     g, o = host(got), np.asarray(want, np.float64)
     assert g.shape == o.shape, name
     fin = np.isfinite(o)
@@ -34,6 +35,8 @@ def close(name, got, want, tol):
     inf = np.isinf(o)
     assert (g[inf] == o[inf]).all() and np.isfinite(g[fin]).all(), f"{name}: values that are not finite"
     d = np.abs(g[fin] - o[fin])
+    if spread is not None:
+        d = np.maximum(d - spread[fin], 0.0)
     norm = np.linalg.norm(o[fin])
     if norm == 0.0:
         assert d.max(initial=0.0) <= tol, f"{name}: {d.max()} for 0"

@@ -105,6 +105,22 @@ def test_training_through_the_rotation(wm, dtype):
         close(name, got, Q.rotate(want, pos, host(m.freq), inverse=True), ATTN[dtype] + TURN[dtype])
 
 
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("T", [2, 3, 4])
+def test_gradients_of_few_keys(wm, T, G):
+    """Where a row sees few keys, a gradient formed with the stored bfloat16 o would be wrong by its rounding more than by anything
+    else (1.4 times what is asked here, for sequences of 3).  What remains are two roundings to bfloat16, of the score gradients and
+    of the results: each is spread evenly over at most half a step of 2^-8, relative to values spread over a binade 0.42 x 2^-8
+    in the 2-norm; both together 0.59 x 2^-8, and a quarter more for the spread of that: 0.75 x 2^-8."""
+    n = 120
+    c = make_prefix("bf16", [n], [T] * n, [0], 2 * G, 2, 64, seed=T)
+    got = run_prefix(wm, c)
+    x = [host(c[m]) for m in ("q", "k", "v", "pk", "pv")]
+    want = Q.prefix_grad(host(c["do"]), *x, c["off"], c["q_off"], c["p_off"], 64 ** -0.5)
+    for name, w in zip(("dq", "dk", "dv"), want):
+        close(name, got[name], w, 0.75 * 2.0 ** -8)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_captured_steps(wm, dtype):
     """A rollout's step captured once (append, then attention, lengths raised on the device) and replayed for every action, with
