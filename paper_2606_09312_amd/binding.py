@@ -898,25 +898,48 @@ def selective_scan_grad(dy, u, delta, A, Bm, Cm, off, checkpoints, *, T_max, D=N
 
 
 # ---- attention over a shared prefix ------------------------------------------------
-def _i32(dev, shape, **tensors):
-    """Checks that tensors (None allowed) are dense int32 of `shape` on `dev`."""
+# A step of a program is a few microseconds of kernels: the checks look at each tensor once (on the host, 9 us for an append, 14 before).
+def _dense(name, t, dtype, gpu, shape):
+    """Address of a dense tensor (None allowed) of `shape` on device `gpu`."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name} must be dense {tuple(shape)} {dtype} on the GPU of the other tensors")
+    return t.data_ptr()
+
+
+def _rows3(name, t, dtype, gpu, shape):
+    """Address and row stride of [rows][heads][head_dim] whose rows are dense."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != gpu:
+        raise ValueError(f"{name} must be {tuple(shape)} {dtype} on the GPU of the other tensors, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    rows, heads, dim = shape
+    s = t.stride()
+    if (s[2] != 1 and dim > 1) or (s[1] != dim and heads > 1):
+        raise ValueError(f"{name}: only the row stride may differ from a dense tensor's")
+    return t.data_ptr(), s[0] if rows > 1 else heads * dim
+
+
+def _status(name, t, gpu):
+    if t is None:
+        return None
+    if t.numel() < 64:
+        raise ValueError(f"{name} must be dense int32 [64] on the tensors' device")
     import torch
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.int32 or t.shape != shape or t.device != dev or not t.is_contiguous()):
-            raise ValueError(f"{name} must be dense int32 {tuple(shape)} on {dev}")
+    return _dense(name, t, torch.int32, gpu, t.shape)
 
 
-def _heads(**tensors):
-    for name, t in tensors.items():
-        if t.dim() != 3:
-            raise ValueError(f"{name} is [rows][heads][head_dim]")
+def _shape3(name, t):
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError(f"{name} is [rows][heads][head_dim]")
+    return shape
 
 
-def _frequencies(freq, dev):
-    if freq.dim() != 1:
-        raise ValueError("freq is [rot / 2]")
-    _f32(dev, freq.shape, freq=freq)
-    return 2 * freq.shape[0]
+def _length1(name, t):
+    shape = t.shape
+    if len(shape) != 1 or shape[0] < 1:
+        raise ValueError(f"{name} has one axis, not empty")
+    return shape[0]
 
 
 @_on_stream
@@ -930,37 +953,33 @@ def rotate(x, off, freq, *, T_max, first=None, interleaved=False, inverse=False,
     y (given: may be x).  status: zeroed int32 [64] for device_status.
     """
     import torch
-    _heads(x=x)
-    dtype = _dtype(x)
-    B = _offsets_ok(off, x.device)
-    _i32(x.device, (B,), first=first)
-    rot = _frequencies(freq, x.device)
+    shape, dtype, gpu = _shape3("x", x), x.dtype, x.get_device()
+    kind, B, pairs = _dtype(x), _length1("off", off) - 1, _length1("freq", freq)
     _on_gpu(x)
-    if status is not None:
-        _status_ok(status, x.device)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
-    _same(x, x.shape, y=y)
+    xp, ld_x = _rows3("x", x, dtype, gpu, shape)
+    y = torch.empty(shape, dtype=dtype, device=x.device) if y is None else y
+    yp, ld_y = _rows3("y", y, dtype, gpu, shape)
     # in the order of Rotation's fields
-    a = Rotation(dtype, B, T_max, x.shape[1], x.shape[2], rot, 1 if interleaved else 0, 1 if inverse else 0, x.shape[0], off.data_ptr(),
-                 _addr(first), freq.data_ptr(), x.data_ptr(), _rows("x", x), _addr(status))
-    _launch(load_library().wm_rotate, x.device, a, y.data_ptr(), _rows("y", y))
+    a = Rotation(kind, B, T_max, shape[1], shape[2], 2 * pairs, 1 if interleaved else 0, 1 if inverse else 0, shape[0],
+                 _dense("off", off, torch.int32, gpu, (B + 1,)), _dense("first", first, torch.int32, gpu, (B,)),
+                 _dense("freq", freq, torch.float32, gpu, (pairs,)), xp, ld_x, _status("status", status, gpu))
+    _launch(load_library().wm_rotate, x.device, a, yp, ld_y)
     return {"y": y}
 
 
 def _cache(k_cache, v_cache, pages, lens):
-    if k_cache.dim() != 4 or pages.dim() != 2:
+    shape, table, kind = k_cache.shape, pages.shape, _dtype(k_cache)
+    if len(shape) != 4 or len(table) != 2:
         raise ValueError("caches are [n_pages][kv_heads][page][head_dim], pages [B][max_pages]")
-    dtype, dev = _dtype(k_cache), k_cache.device
-    _same(k_cache, k_cache.shape, v_cache=v_cache)
-    if not k_cache.is_contiguous() or not v_cache.is_contiguous():
-        raise ValueError("k_cache and v_cache must be dense")
-    B = pages.shape[0]
-    _i32(dev, pages.shape, pages=pages)
-    _i32(dev, (B,), lens=lens)
-    n, heads, page, dim = k_cache.shape
     _on_gpu(k_cache)
+    import torch
+    dtype, gpu = k_cache.dtype, k_cache.get_device()
+    n, heads, page, dim = shape
+    B, width = table
     # in the order of Cache's fields
-    return Cache(dtype, heads, dim, page, n, B, pages.shape[1], k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), lens.data_ptr())
+    return Cache(kind, heads, dim, page, n, B, width, _dense("k_cache", k_cache, dtype, gpu, shape),
+                 _dense("v_cache", v_cache, dtype, gpu, shape), _dense("pages", pages, torch.int32, gpu, table),
+                 _dense("lens", lens, torch.int32, gpu, (B,)))
 
 
 @_on_stream
@@ -975,30 +994,26 @@ def cache_append(k, v, k_cache, v_cache, pages, lens, off, *, T_max, first=None,
     q_out may be q), k_cache and v_cache.  status: zeroed int32 [64] for device_status.
     """
     import torch
-    _heads(k=k)
     c = _cache(k_cache, v_cache, pages, lens)
-    dev = k_cache.device
-    shape = (k.shape[0], c.kv_heads, c.head_dim)
-    _same(k_cache, shape, k=k, v=v)
-    if _offsets_ok(off, dev) != c.B:
-        raise ValueError("off needs an entry more than pages has rows")
-    _i32(dev, (c.B,), first=first)
-    rot = 0 if freq is None else _frequencies(freq, dev)
-    if status is not None:
-        _status_ok(status, dev)
-    heads = 0
+    dtype, dev, gpu, int32, B = k_cache.dtype, k_cache.device, k_cache.get_device(), torch.int32, c.B
+    rows = _shape3("k", k)[0]
+    (kp, ld_k), (vp, ld_v) = (_rows3(n, t, dtype, gpu, (rows, c.kv_heads, c.head_dim)) for n, t in (("k", k), ("v", v)))
+    pairs = 0 if freq is None else _length1("freq", freq)
+    heads = ld_q = ld_out = 0
+    qp = out = None
     if q is not None:
-        _heads(q=q)
-        heads = q.shape[1]
-        shape = (k.shape[0], heads, c.head_dim)
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q_out is None else q_out
-        _same(k_cache, shape, q=q, q_out=q_out)
+        heads = _shape3("q", q)[1]
+        shape = (rows, heads, c.head_dim)
+        qp, ld_q = _rows3("q", q, dtype, gpu, shape)
+        q_out = torch.empty(shape, dtype=dtype, device=dev) if q_out is None else q_out
+        out, ld_out = _rows3("q_out", q_out, dtype, gpu, shape)
     elif q_out is not None:
         raise ValueError("q_out without q")
     # in the order of Append's fields
-    a = Append(c, T_max, heads, rot, 1 if interleaved else 0, k.shape[0], off.data_ptr(), _addr(first), _addr(freq), k.data_ptr(), v.data_ptr(),
-               _addr(q), _rows("k", k), _rows("v", v), _rows("q", q) if heads else 0, _addr(status))
-    _launch(load_library().wm_cache_append, dev, a, _addr(q_out), _rows("q_out", q_out) if heads else 0)
+    a = Append(c, T_max, heads, 2 * pairs, 1 if interleaved else 0, rows, _dense("off", off, int32, gpu, (B + 1,)),
+               _dense("first", first, int32, gpu, (B,)), _dense("freq", freq, torch.float32, gpu, (pairs,)), kp, vp, qp, ld_k, ld_v, ld_q,
+               _status("status", status, gpu))
+    _launch(load_library().wm_cache_append, dev, a, out, ld_out)
     return {"q": q_out, "k_cache": k_cache, "v_cache": v_cache}
 
 
@@ -1016,15 +1031,15 @@ def cached_attention(q, k_cache, v_cache, pages, lens, off, *, T_max, len_max=No
     [64] for device_status.
     """
     import torch
-    _heads(q=q)
     c = _cache(k_cache, v_cache, pages, lens)
-    dev = k_cache.device
-    _same(k_cache, (q.shape[0], q.shape[1], c.head_dim), q=q)
-    if _offsets_ok(off, dev) != c.B:
-        raise ValueError("off needs an entry more than pages has rows")
+    dtype, dev, gpu, int32, B = k_cache.dtype, k_cache.device, k_cache.get_device(), torch.int32, c.B
+    rows, heads, dim = shape = _shape3("q", q)
+    if dim != c.head_dim:
+        raise ValueError("q and the caches differ in head_dim")
+    qp, ld_q = _rows3("q", q, dtype, gpu, shape)
     len_max = c.max_pages * c.page if len_max is None else len_max
     S = shared_pages = 0
-    seg = segp = None
+    seg = segp = table = shared_lens = None
     if seg_off is None:
         if prefix_pages is not None or prefix_lens is not None:
             raise ValueError("prefix_pages and prefix_lens need seg_off")
@@ -1033,30 +1048,28 @@ def cached_attention(q, k_cache, v_cache, pages, lens, off, *, T_max, len_max=No
             raise ValueError("seg_off needs prefix_pages [S][...] and prefix_lens [S]")
         seg = np.ascontiguousarray(seg_off, dtype=np.int32)
         S = len(seg) - 1
-        if seg.ndim != 1 or S < 1 or seg[-1] != c.B:
+        if seg.ndim != 1 or S < 1 or seg[-1] != B:
             raise ValueError("seg_off must end at the number of sequences")
         segp, shared_pages = seg.ctypes.data, prefix_pages.shape[1]
-        _i32(dev, (S, shared_pages), prefix_pages=prefix_pages)
-        _i32(dev, (S,), prefix_lens=prefix_lens)
+        table = _dense("prefix_pages", prefix_pages, int32, gpu, (S, shared_pages))
+        shared_lens = _dense("prefix_lens", prefix_lens, int32, gpu, (S,))
     prefix_max = shared_pages * c.page if prefix_max is None else prefix_max
-    if status is not None:
-        _status_ok(status, dev)
-    o = torch.empty(q.shape, dtype=q.dtype, device=dev) if o is None else o
-    _same(q, q.shape, o=o)
+    o = torch.empty(shape, dtype=dtype, device=dev) if o is None else o
+    op, ld_o = _rows3("o", o, dtype, gpu, shape)
     if lse is None and need_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
-    _f32(dev, q.shape[:2], lse=lse)
+        lse = torch.empty((rows, heads), dtype=torch.float32, device=dev)
     # in the order of Cached's fields
-    a = Cached(c, T_max, len_max, q.shape[1], S, shared_pages, prefix_max, q.shape[0], off.data_ptr(), segp, _addr(prefix_pages),
-               _addr(prefix_lens), q.data_ptr(), _rows("q", q), q.shape[2] ** -0.5 if scale is None else scale, _addr(status))
+    a = Cached(c, T_max, len_max, heads, S, shared_pages, prefix_max, rows, _dense("off", off, int32, gpu, (B + 1,)), segp, table, shared_lens,
+               qp, ld_q, dim ** -0.5 if scale is None else scale, _status("status", status, gpu))
     lib = load_library()
     ws, n = _workspace(lib.wm_cached_attention_workspace_bytes(a), ws, dev)
-    _launch(lib.wm_cached_attention, dev, a, o.data_ptr(), _rows("o", o), _addr(lse), _addr(ws), n)
+    _launch(lib.wm_cached_attention, dev, a, op, ld_o, _dense("lse", lse, torch.float32, gpu, (rows, heads)), _addr(ws), n)
     return {"o": o, "lse": lse, "ws": ws}
 
 
 def _prefix(q, k, v, pk, pv, off, q_off, p_off, T_max, kv_mask, scale, status):
-    _heads(k=k, pk=pk)
+    _shape3("k", k)
+    _shape3("pk", pk)
     a = _attention(q, pk, pv, q_off, p_off, kv_mask, scale)
     _same(q, (q.shape[0],) + tuple(pk.shape[1:]), k=k, v=v)
     B = _offsets_ok(off, q.device)

@@ -62,8 +62,8 @@ def append(**kw):
 
 def cached(seg_off=(0, 2), **kw):
     keep, p = host((0, 2) if seg_off is None else seg_off)
-    a = B.Cached(cache=cache(), T_max=5, len_max=48, heads=4, S=len(keep) - 1, prefix_max_pages=4, prefix_max=64, rows=8, off=FAKE, seg_off=None if seg_off is None else p,
-                 prefix_pages=FAKE, prefix_lens=FAKE, q=FAKE, ld_q=256, scale=0.125)
+    a = B.Cached(cache=cache(), T_max=5, len_max=48, heads=4, S=len(keep) - 1, prefix_max_pages=4, prefix_max=64, rows=8, off=FAKE,
+                 seg_off=None if seg_off is None else p, prefix_pages=FAKE, prefix_lens=FAKE, q=FAKE, ld_q=256, scale=0.125)
     a.keep = keep
     return put(a, kw)
 
