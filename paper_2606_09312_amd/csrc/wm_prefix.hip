@@ -1701,7 +1701,11 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   const int P = a->S > 0 ? a->prefix_max : 0;
   p->few = seq_rows <= FEW_ROWS;
   p->most_rows = most_seqs * a->T_max * G;
-  p->shared_few = p->most_rows <= FEW_ROWS;
+  // Tiles of 32 rows of a program in the launch by sequences, or of 128 in a launch of their own.  The former read the keys as often
+  // as there are tiles, from L2; they win while that is little.  16-bit, width 64, of 120 rows, 16 programs: of 300 keys 47 us (53
+  // in two launches), of 4096 106 (104), of 48 rows 71 (81); width 128, 16 of 4096: 48 rows 95 (122), 96 rows 150 (130).
+  const int64_t few_tiles = cdiv(p->most_rows, FEW_ROWS);
+  p->shared_few = p->few && (few_tiles <= 2 || (few_tiles <= 8 && few_tiles * P <= 4096));
   // Sequences of many rows fill a tile by themselves and read the program's keys along with their own.
   p->joint = P == 0 || most_seqs <= 1 || seq_rows >= 64;
   const int64_t tiles = c.B * cdiv(seq_rows, p->few ? FEW_ROWS : 128) * c.kv_heads, rows_all = a->rows * a->heads;

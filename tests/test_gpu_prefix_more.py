@@ -351,3 +351,13 @@ def test_nothing_to_do(wm):
     p = torch.randn((5, 2, 32), device="cuda")
     g = wm.prefix_attention_grad(x, x, x, x, p, p, o["o"], o["lse"], e, [0, 0], [0, 5], T_max=0)
     assert (g["dpk"] == 0).all() and (g["dpv"] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per,G,P", [([11, 3], 4, [70, 5]), ([16, 0, 4], 4, [700, 3, 0]), ([50], 5, [513]), ([9, 30], 8, [17, 90])])
+def test_single_steps_of_wide_beams(wm, dtype, per, G, P):
+    """Programs of more rows than a tile of the single steps' kernel, on both sides of the rule that chooses their kernel."""
+    lens = [1 + (7 * i) % 40 for i in range(sum(per))]
+    for dh in (32, 64, 128):
+        pool = Pool(dtype, 16, 2, dh, lens, P, seed=dh)
+        check_cached(wm, dtype, pool, list(range(sum(per) + 1)), per, 2 * G, 2, dh)
