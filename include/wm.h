@@ -539,7 +539,7 @@ wm_status wm_scan_grad(const wm_scan_args* a, const void* checkpoints, const voi
  * Other features stay.  Angles are reduced in 64 bits: they are right to 2e-7 at every int32 position. */
 
 /* x [rows][heads][head_dim], head_dim a multiple of 8 up to 512, rot even, 2 <= rot <= head_dim.  Row
- * off[s] + i is at position first[s] + i (first: device int32 [B], NULL = 0).  inverse != 0 turns
+ * off[s] + i is at position first[s] + i (first: device int32 [B], NULL = 0); at most 2^26 - 4 rows.  inverse != 0 turns
  * back, which is the gradient: dx = wm_rotate(dy) with the other sign. */
 typedef struct wm_rotation {
   int32_t dtype, B, T_max, heads, head_dim, rot, interleaved, inverse;
@@ -569,7 +569,7 @@ typedef struct wm_cache {
 /* Appends rows [rows][kv_heads][head_dim] of k and v: row i of the n of sequence s goes to slot
  * lens[s] - n + i, at position first[s] + slot.  Keys are rotated on the way (freq NULL: as they are, rot
  * and interleaved without meaning), values are copied.  q [rows][heads][head_dim] (may be NULL, heads 0) is rotated alike
- * to q_out.  Slots that the rows do not name stay.  Two rows of a call must not name the same
+ * to q_out.  At most 2^26 - 4 rows.  Slots that the rows do not name stay.  Two rows of a call must not name the same
  * slot of one page. */
 typedef struct wm_append {
   wm_cache cache;
@@ -634,7 +634,8 @@ typedef struct wm_prefix_grads {
   int64_t ld_dq, ld_dk, ld_dv, ld_dpk, ld_dpv;
 } wm_prefix_grads;
 
-/* Gradients given d_o = dL/do, with o and lse of the forward call. */
+/* Gradients given d_o = dL/do, with o and lse of the forward call.  (Rows that see few keys take the mean of their score
+ * gradients from the keys instead of d_o . o, which o's rounding would spoil.) */
 wm_status wm_prefix_attention_grad(const wm_prefix* a, const void* o, int64_t ld_o, const float* lse, const void* d_o, int64_t ld_do,
                                    const wm_prefix_grads* grads, void* ws, size_t ws_bytes, void* stream);
 

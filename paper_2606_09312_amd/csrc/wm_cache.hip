@@ -198,16 +198,19 @@ bool rows_ok(int32_t dtype, const void* p, int64_t ld, int64_t rows, int64_t wid
   return rows == 0 || (p && (uintptr_t)p % 16 == 0 && ld >= width && ld * e % 16 == 0 && ld <= (1 << 22));
 }
 
+// Four rows per workgroup, so that a thread has several items, or one where that leaves compute units without work (rotation in bf16,
+// four and one: 4095 rows of 12 heads of 64 4.8 and 6.6 us, 2048 4.0 and 4.3, 64 rows of 64 heads of 128 6.5 and 3.9, 2048 13.5 and 12.6).
+constexpr int64_t MANY_ROWS = 2048;
+constexpr int64_t MOST_ROWS = 4 * (((int64_t)1 << 32) / 256 - 1);          // a launch has fewer than 2^32 threads
+
 wm_status check_rows(int32_t B, int32_t T_max, int64_t rows, const int32_t* off) {
   if (rows < 0 || rows > INT32_MAX) return bad("rows must be in [0, 2^31)");
+  if (rows > MOST_ROWS) return set_error(WM_ERR_UNSUPPORTED, "more than 2^26 - 4 rows");
   if (B < 0 || T_max < 0) return bad("B and T_max must not be negative");
   if (rows > 0 && (B < 1 || T_max < 1)) return bad("rows need sequences: B and T_max at least 1");
   if (B > 0 && !off) return bad("off is NULL");
   return WM_OK;
 }
-
-// Four rows per workgroup where there are enough for all compute units, so that a thread has several items.
-constexpr int64_t MANY_ROWS = 4096;
 
 template <bool APPEND>
 hipError_t launch(const Args& a, int32_t dtype, hipStream_t st) {
