@@ -695,7 +695,7 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
   const int row = w.tile * 32 + (lane & 31);                  // may pass R: computed, not stored
   const int rr = min(row, w.R - 1), head = w.hk * a.G + rr % a.G;
   const int64_t qrow = w.q0 + rr / a.G;
-  const int hi = max(w.before + rr / a.G + 1, 0), hi_a = lane_of(hi, 0), hi_z = lane_of(hi, 31);
+  const int hi = max(w.before + rr / a.G + 1, 0), hi_a = lane_of(hi, 0);
   const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.o1 + KB - 1) / KB;
   const int2 tt = share_of(a, tiles, w.split);
 
@@ -1454,9 +1454,10 @@ double part_us(int64_t values, int dh) { return 2.0 * values * dh * 4 / 4.5e6; }
 // step over long programs: 9 splits 284 us, 3 splits 375.)
 struct Cut {
   int splits, chunk;
+  double us;                      // what the loops and their parts take, by this
 };
 Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_cu, double alone, double unit_us, double part_us) {
-  Cut best = {1, (int)std::max<int64_t>(longest, 1)};
+  Cut best = {1, (int)std::max<int64_t>(longest, 1), 0.0};
   const double places = 256.0 * per_cu, even = blocks * avg / places;
   double cost = 0.0;
   for (int s = 1; s <= 64 && (s == 1 || s <= longest / least); ++s) {
@@ -1466,7 +1467,7 @@ Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_
     const double c = tiles * unit_us + (s > 1 ? shares * part_us + 4.0 : 0.0);
     if (s == 1 || c < 0.98 * cost) {
       cost = c;
-      best = {(int)std::max<int64_t>(cdiv(longest, chunk), 1), (int)chunk};
+      best = {(int)std::max<int64_t>(cdiv(longest, chunk), 1), (int)chunk, c};
     }
   }
   return best;
@@ -1681,7 +1682,7 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   if (a->S < 0 || a->S > WM_MAX_SEGMENTS) return bad("S must be in [0, WM_MAX_SEGMENTS]");
   const int G = a->heads / c.kv_heads, dh = c.head_dim;
   const int64_t seq_rows = std::min<int64_t>(a->T_max, std::max<int64_t>(a->rows, 1)) * G;
-  int64_t most_seqs = 0, shared_tiles = 0, shared_few_tiles = 0;
+  int64_t most_seqs = 0, shared_few_tiles = 0;
   const Shape f = shape_of(c.dtype, dh);
   constexpr int FEW_ROWS = 32, FEW_KEYS = 128;
   const int few_cu = c.dtype == WM_BF16 ? (dh == 128 ? 2 : 4) : (dh == 128 ? 1 : dh == 64 ? 2 : 4);
@@ -1691,7 +1692,6 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
       const int64_t n = (int64_t)a->seg_off[i + 1] - a->seg_off[i];
       if (n < 0) return bad("seg_off must not decrease");
       most_seqs = std::max(most_seqs, n);
-      shared_tiles += cdiv(n * a->T_max * G, 128);
       shared_few_tiles += cdiv(n * a->T_max * G, FEW_ROWS);
     }
     if (a->prefix_max < 0 || a->prefix_max > (int64_t)a->prefix_max_pages * c.page) return bad("prefix_max must be in [0, prefix_max_pages page]");
@@ -1706,8 +1706,6 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   // in two launches), of 4096 106 (104), of 48 rows 71 (81); width 128, 16 of 4096: 48 rows 95 (122), 96 rows 150 (130).
   const int64_t few_tiles = cdiv(p->most_rows, FEW_ROWS);
   p->shared_few = p->few && (few_tiles <= 2 || (few_tiles <= 8 && few_tiles * P <= 4096));
-  // Sequences of many rows fill a tile by themselves and read the program's keys along with their own.
-  p->joint = P == 0 || most_seqs <= 1 || seq_rows >= 64;
   const int64_t tiles = c.B * cdiv(seq_rows, p->few ? FEW_ROWS : 128) * c.kv_heads, rows_all = a->rows * a->heads;
   if (tiles > MOST_TILES || shared_few_tiles * c.kv_heads > MOST_TILES) return set_error(WM_ERR_UNSUPPORTED, "too many row tiles");
   // lengths are known to the device alone: loops of 0.6 of the longest on average
@@ -1716,9 +1714,23 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
     const int64_t steps = cdiv(longest, keys);
     return cut_for(blocks, 0.6 * steps, steps, 2, cu, alone_of(few, cu), few ? few_us(f.bf, keys, dh, cu) : step_us(f.bf, 2, 128, keys, dh, cu), part_us(rows_all, dh));
   };
-  p->own = cut(p->few, tiles, (int64_t)a->len_max + (p->joint ? P : 0));
-  p->shared = {0, 0};
-  if (!p->joint) p->shared = cut(p->shared_few, (p->shared_few ? shared_few_tiles : shared_tiles) * c.kv_heads, P);
+  // Sequences of many rows may read the program's keys along with their own, in tiles that the last rows of each do not fill, or leave
+  // them to a launch by programs, whose tiles are full; the latter's parts have to be written and read, and where the estimates are close
+  // it is the slower.  (16-bit, width 64, 64 sequences of two programs of up to 2048 keys, in one and in two launches: 32 to 64 rows
+  // each 90 and 69 us, 64 to 128 rows 75 and 89; float32, four key heads: 188 and 102, 145 and 132.)
+  const int64_t avg_rows = cdiv(a->rows, std::max(c.B, 1)) * G, program_rows = a->S > 0 ? cdiv(a->rows, a->S) * G : 0;
+  const int64_t own_tiles = c.B * cdiv(avg_rows, p->few ? FEW_ROWS : 128) * c.kv_heads;
+  p->own = cut(p->few, own_tiles, (int64_t)a->len_max + P);
+  p->shared = {0, 0, 0.0};
+  p->joint = true;
+  if (P > 0 && most_seqs > 1) {
+    const Cut own = cut(p->few, own_tiles, a->len_max), shared = cut(p->shared_few, a->S * cdiv(program_rows, p->shared_few ? FEW_ROWS : 128) * c.kv_heads, P);
+    p->joint = !p->few && own.us + shared.us + 8.0 >= 0.8 * p->own.us;
+    if (!p->joint) {
+      p->own = own;
+      p->shared = shared;
+    }
+  }
   if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
   p->o_part = p->o_ml = p->o_flags = 0;

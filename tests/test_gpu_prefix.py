@@ -52,7 +52,7 @@ def test_rotate(wm, dtype, interleaved, H, dh, rot):
 
 
 def test_rotate_many_rows(wm):
-    """Past 4096 rows a workgroup takes four."""
+    """Enough rows that a workgroup takes four."""
     lens = list(np.random.default_rng(1).integers(0, 60, 200))
     off = offsets(lens)
     x = torch.randn((off[-1], 2, 64), device="cuda")

@@ -361,3 +361,15 @@ def test_single_steps_of_wide_beams(wm, dtype, per, G, P):
     for dh in (32, 64, 128):
         pool = Pool(dtype, 16, 2, dh, lens, P, seed=dh)
         check_cached(wm, dtype, pool, list(range(sum(per) + 1)), per, 2 * G, 2, dh)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per,T,P,Hq,Hk", [([9, 12], 40, [900, 700], 2, 2), ([3, 2], 70, [90, 17], 2, 1), ([5, 0, 6], 130, [400, 9, 0], 3, 3)])
+def test_chunks_of_many_rows(wm, dtype, per, T, P, Hq, Hk):
+    """Sequences of more rows than the single steps' kernel takes, on both sides of the rule whether they read their program's keys
+    themselves."""
+    n = [T - (11 * i) % 37 for i in range(sum(per))]
+    L = [x + (13 * i) % 50 for i, x in enumerate(n)]
+    for dh in (32, 64, 128):
+        pool = Pool(dtype, 32, Hk, dh, L, P, seed=dh)
+        check_cached(wm, dtype, pool, offsets(n), per, Hq, Hk, dh)
