@@ -671,8 +671,9 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
 // while the next scores are formed, and no wavefront waits for another.  What bounds it is reading k and v.
 template <class T, int DH>
 constexpr int FEW_LDS = 8 * 32 * DH * (int)sizeof(T);
+// (three at 64, 16 bits: with four, 24 bytes of spilled registers made every reload wait for the copies, 16 streams of 8000 keys 70 us for 67)
 template <class T, int DH>
-constexpr int FEW_PER_CU = FEW_LDS<T, DH> > 80 * 1024 ? 1 : FEW_LDS<T, DH> > 40 * 1024 ? 2 : 4;
+constexpr int FEW_PER_CU = FEW_LDS<T, DH> > 80 * 1024 ? 1 : FEW_LDS<T, DH> > 40 * 1024 ? 2 : DH == 64 ? 3 : 4;
 template <class T, int DH>
 __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Table t, const Args given) {
   using TL = Tile<T, DH>;
@@ -1685,7 +1686,7 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   int64_t most_seqs = 0, shared_few_tiles = 0;
   const Shape f = shape_of(c.dtype, dh);
   constexpr int FEW_ROWS = 32, FEW_KEYS = 128;
-  const int few_cu = c.dtype == WM_BF16 ? (dh == 128 ? 2 : 4) : (dh == 128 ? 1 : dh == 64 ? 2 : 4);
+  const int few_cu = c.dtype == WM_BF16 ? (dh == 128 ? 2 : dh == 64 ? 3 : 4) : (dh == 128 ? 1 : dh == 64 ? 2 : 4);
   if (a->S > 0) {
     if (!a->seg_off || a->seg_off[0] != 0 || a->seg_off[a->S] != c.B) return bad("seg_off must run from 0 to B");
     for (int i = 0; i < a->S; ++i) {
