@@ -254,17 +254,21 @@ template <class T, int DH, int ROWS>
 __device__ __forceinline__ void copy_pages(const Args& a, int hk, T* kt, T* vt, int first, int len, int ids, int wave, int lane) {
   using TL = Tile<T, DH>;
   constexpr int N = ROWS * TL::UPR / 256, RPI = 64 / TL::UPR;
+  constexpr uint32_t ROW = DH * sizeof(T);
   const int slots = 1 << a.lps;
-  const uint32_t unit_of = (uint32_t)(lane / TL::UPR * DH * sizeof(T));
+  auto place = [&](int id, int row) {
+    return ((((uint64_t)(uint32_t)max(id, 0) * (uint32_t)a.kv_heads + (uint32_t)hk) << a.lps) + ((first + row) & (slots - 1))) * ROW;
+  };
+  const uint32_t unit_of = (uint32_t)(lane / TL::UPR) * ROW;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int r0 = (i * 256 + wave * 64) / TL::UPR;                  // the instruction's first row
     const int id = lane_of(ids, r0 >> a.lps);
-    const int n = id < 0 ? 0 : min(max(len - first - r0, 0), RPI);
-    const uint64_t at = ((((uint64_t)(uint32_t)max(id, 0) * a.kv_heads + hk) << a.lps) + ((first + r0) & (slots - 1))) * (DH * sizeof(T));
+    const uint32_t size = id < 0 ? 0 : min(max(len - first - r0, 0), RPI) * ROW;
+    const uint64_t at = place(id, r0);
     const uint32_t vo = unit_of + ((lane % TL::UPR) ^ TL::swz(r0 + lane / TL::UPR)) * 16;
-    copy16(buffer_of(static_cast<const uint8_t*>(a.k) + at, n * DH * sizeof(T)), kt + (i * 256 + wave * 64) * TL::E, vo);
-    copy16(buffer_of(static_cast<const uint8_t*>(a.v) + at, n * DH * sizeof(T)), vt + (i * 256 + wave * 64) * TL::E, vo);
+    copy16(buffer_of(static_cast<const uint8_t*>(a.k) + at, size), kt + (i * 256 + wave * 64) * TL::E, vo);
+    copy16(buffer_of(static_cast<const uint8_t*>(a.v) + at, size), vt + (i * 256 + wave * 64) * TL::E, vo);
   }
 }
 
@@ -283,19 +287,38 @@ __device__ __forceinline__ Block paged_block(const Args& a, const int32_t* table
   }
   return b;
 }
+// Where the block's halves of 16 keys lie in the caches, each in one page (a block starts at a multiple of 32), and their bytes.
+struct Place {
+  uint64_t at[2];
+  uint32_t size[2];
+};
 template <class T, int DH>
-__device__ __forceinline__ void copy_block(const Args& a, const void* cache, int hk, const Block& b, T* tile, int lane) {
+__device__ __forceinline__ Place place_of(const Args& a, int hk, const Block& b) {
+  constexpr uint32_t ROW = DH * sizeof(T);
+  Place p;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int id = half ? b.id1 : b.id0;
+    const bool ok = id >= 0 && id < a.n_pages;
+    p.at[half] = ((((uint64_t)(uint32_t)(ok ? id : 0) * (uint32_t)a.kv_heads + (uint32_t)hk) << a.lps) + ((b.first + 16 * half) & ((1 << a.lps) - 1))) * ROW;
+    p.size[half] = ok ? min(max(b.n - 16 * half, 0), 16) * ROW : 0;
+  }
+  return p;
+}
+template <class T, int DH>
+__device__ __forceinline__ void copy_block(const void* cache, const Place& p, T* tile, int lane) {
   using TL = Tile<T, DH>;
   constexpr int N = 32 * TL::UPR / 64, RPI = 64 / TL::UPR;
+  constexpr uint32_t ROW = DH * sizeof(T);
+  static_assert(RPI <= 16, "an instruction's rows lie in one half");
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int r0 = i * RPI, at = b.first + r0;                // the instruction's first row
-    const int id = (at >> a.lps) == (b.first >> a.lps) ? b.id0 : b.id1;
-    const bool ok = id >= 0 && id < a.n_pages;
-    const int64_t key = ((((int64_t)(ok ? id : 0) * a.kv_heads + hk) << a.lps) + (at & ((1 << a.lps) - 1))) * DH;
-    const u32x4 buf = buffer_of(static_cast<const T*>(cache) + key, ok ? (uint32_t)(min(max(b.n - r0, 0), RPI) * DH * sizeof(T)) : 0u);
-    const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(r0 + r);
-    copy16(buf, tile + (size_t)i * 64 * TL::E, (uint32_t)(r * DH * sizeof(T) + unit * 16));
+  for (int half = 0; half < 2; ++half) {
+    const u32x4 buf = buffer_of(static_cast<const uint8_t*>(cache) + p.at[half], p.size[half]);
+#pragma unroll
+    for (int i = half * N / 2; i < (half + 1) * N / 2; ++i) {
+      const int r = lane / TL::UPR, unit = (lane % TL::UPR) ^ TL::swz(i * RPI + r);
+      copy16(buf, tile + (size_t)i * 64 * TL::E, (uint32_t)(r * ROW + unit * 16), (uint32_t)(i * RPI % 16) * ROW);
+    }
   }
 }
 
@@ -579,12 +602,16 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
       if constexpr (PAGED) return paged_block(a, w.own_table, first, end - first, lane);
       else return {first, min(max(end - first, 0), 32), 0, 0};
     };
+    Place place;
     auto copy_k = [&](const Block& b) {
-      if constexpr (PAGED) copy_block<T, DH>(a, a.k, hk, b, kt, lane);
+      if constexpr (PAGED) {
+        place = place_of<T, DH>(a, hk, b);
+        copy_block<T, DH>(a.k, place, kt, lane);
+      }
       else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.k) + b.first * a.ld_k + hk * DH, (int)a.ld_k, b.n, false, every, kt, lane);
     };
     auto copy_v = [&](const Block& b) {
-      if constexpr (PAGED) copy_block<T, DH>(a, a.v, hk, b, vt, lane);
+      if constexpr (PAGED) copy_block<T, DH>(a.v, place, vt, lane);        // K's block
       else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.v) + b.first * a.ld_v + hk * DH, (int)a.ld_v, b.n, false, every, vt, lane);
     };
     Block now = block_of(max(lo_a, rest) + 32 * wk);
@@ -671,9 +698,8 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
 // while the next scores are formed, and no wavefront waits for another.  What bounds it is reading k and v.
 template <class T, int DH>
 constexpr int FEW_LDS = 8 * 32 * DH * (int)sizeof(T);
-// (three at 64, 16 bits: with four, 24 bytes of spilled registers made every reload wait for the copies, 16 streams of 8000 keys 70 us for 67)
 template <class T, int DH>
-constexpr int FEW_PER_CU = FEW_LDS<T, DH> > 80 * 1024 ? 1 : FEW_LDS<T, DH> > 40 * 1024 ? 2 : DH == 64 ? 3 : 4;
+constexpr int FEW_PER_CU = FEW_LDS<T, DH> > 80 * 1024 ? 1 : FEW_LDS<T, DH> > 40 * 1024 ? 2 : 4;
 template <class T, int DH>
 __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Table t, const Args given) {
   using TL = Tile<T, DH>;
@@ -705,16 +731,18 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
     const int first = (own ? ti - nP : ti) * KB + 32 * wave;
     return paged_block(a, own ? w.own_table : w.shared_table, first, ti < tt.y ? (own ? w.o1 : w.P) - first : 0, lane);
   };
-  auto copy = [&](const void* cache, const Block& b, T* tile) { copy_block<T, DH>(a, cache, w.hk, b, tile, lane); };
+  Place place;
   f32x16 acc[DB];
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = f32x16{};
   float mx = -INFINITY, sum = 0.0f;
   Block now = block_of(tt.x);
-  if (now.n > 0) {
-    copy(a.k, now, kt);
-    copy(a.v, now, vt);
-  }
+  auto copy_both = [&]() {
+    place = place_of<T, DH>(a, w.hk, now);
+    copy_block<T, DH>(a.k, place, kt, lane);
+    copy_block<T, DH>(a.v, place, vt, lane);
+  };
+  if (now.n > 0) copy_both();
   typename TL::Op qf;
   TL::load_op(qf, static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH, h);
   TL::scale_op(qf, a.c2);
@@ -728,10 +756,7 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
   };
   if (now.n == 0 && ti < nP && nP < tt.y) {
     now = block_of(ti = nP);
-    if (now.n > 0) {
-      copy(a.k, now, kt);
-      copy(a.v, now, vt);
-    }
+    if (now.n > 0) copy_both();
   }
   while (now.n > 0) {
     own = ti >= nP;
@@ -740,13 +765,16 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
     wait_counts<N, true>();                                   // K is there
     f32x16 s = TL::mm_row(kt, 0, qf, lane);
     wait_counts<63, true>();
-    if (next.n > 0) copy(a.k, next, kt);
+    if (next.n > 0) {
+      place = place_of<T, DH>(a, w.hk, next);
+      copy_block<T, DH>(a.k, place, kt, lane);
+    }
     if (own ? hi_a < now.first + 32 : now.n < 32) only(s, own ? below(hi - now.first) & below(now.n) : below(now.n), -INFINITY, h);
     weigh<T, DB>(s, mx, sum, acc, a.c2);
     if (next.n > 0) wait_counts<N, false>(); else wait_counts<0, false>();    // V is there
     TL::mm_col(vt, 0, s, acc, lane);
     wait_counts<63, true>();
-    if (next.n > 0) copy(a.v, next, vt);
+    if (next.n > 0) copy_block<T, DH>(a.v, place, vt, lane);
     now = next;
     ti = tn;
   }
@@ -1686,7 +1714,7 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   int64_t most_seqs = 0, shared_few_tiles = 0;
   const Shape f = shape_of(c.dtype, dh);
   constexpr int FEW_ROWS = 32, FEW_KEYS = 128;
-  const int few_cu = c.dtype == WM_BF16 ? (dh == 128 ? 2 : dh == 64 ? 3 : 4) : (dh == 128 ? 1 : dh == 64 ? 2 : 4);
+  const int few_cu = c.dtype == WM_BF16 ? (dh == 128 ? 2 : 4) : (dh == 128 ? 1 : dh == 64 ? 2 : 4);
   if (a->S > 0) {
     if (!a->seg_off || a->seg_off[0] != 0 || a->seg_off[a->S] != c.B) return bad("seg_off must run from 0 to B");
     for (int i = 0; i < a->S; ++i) {
