@@ -238,7 +238,8 @@ struct Reads {
         s16x4 half[2];
 #pragma unroll
         for (int jj = 0; jj < 2; ++jj)
-          half[jj] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((col ^ (b * 64 ^ jj * TURN)) + (16 * f + 8 * jj) * DH * 2 + OFF));
+          half[jj] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_s16x4*)(uintptr_t)((col ^ (b * 64 ^ jj * TURN)) + (16 * f + 8 * jj) * DH * 2 + OFF));
         const s16x8 x = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
         acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf, acc[b], 0, 0, 0);
       }
@@ -300,7 +301,8 @@ __device__ __forceinline__ Place place_of(const Args& a, int hk, const Block& b)
   for (int half = 0; half < 2; ++half) {
     const int id = half ? b.id1 : b.id0;
     const bool ok = id >= 0 && id < a.n_pages;
-    p.at[half] = ((((uint64_t)(uint32_t)(ok ? id : 0) * (uint32_t)a.kv_heads + (uint32_t)hk) << a.lps) + ((b.first + 16 * half) & ((1 << a.lps) - 1))) * ROW;
+    const uint64_t page = (uint64_t)(uint32_t)(ok ? id : 0) * (uint32_t)a.kv_heads + (uint32_t)hk;
+    p.at[half] = ((page << a.lps) + ((b.first + 16 * half) & ((1 << a.lps) - 1))) * ROW;
     p.size[half] = ok ? min(max(b.n - 16 * half, 0), 16) * ROW : 0;
   }
   return p;
@@ -422,10 +424,12 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
 }
 
 // --------------------------------------------------------------------------
-// Forward.  A workgroup of 4 wavefronts takes 128 / WK rows (32 per wavefront); WK wavefronts share
-// rows and take every WK-th block of 32 keys.  Tiles of K and V are staged two deep; softmax online
-// (wm_attend.hip).  PAGED: the launch goes by programs (the rows of all its sequences, the program's keys
+// Forward: o = sum P v / sum P, P = exp(S - m), S = scale q k, m the running maximum.  A workgroup of 4 wavefronts takes 128 / WK
+// rows (32 per wavefront); WK wavefronts share rows and take every WK-th block of 32 keys.  Tiles of K and V are staged two deep;
+// softmax online (wm_attend.hip).  PAGED: the launch goes by programs (the rows of all its sequences, the program's keys
 // only) or by sequences (row_tiles > 0: its own keys, after the program's if it has any).
+// What bounds it is the vector unit, 64% busy at a width of 64 beside matrix cores at 34% (16 bits; 33324 rows on 256 to 2048 keys
+// 174 us, 628 TFLOP/s; 183 with three wavefronts per SIMD for four); at 128 both, 39 and 42% (850 TFLOP/s causal).
 template <class T, int DH, int WK>
 constexpr int FWD_PER_CU = IS_BF<T> && DH == 64 && WK == 1 ? 4 : 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 template <class T, int DH, int WK, bool PAGED>
@@ -695,7 +699,8 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
 
 // Single steps: at most 32 rows of a key head, over pages.  Each wavefront takes every fourth block of 32 keys and stages
 // K and V of its own, one block each: the next block's K is under way while the softmax and V's product run, its V
-// while the next scores are formed, and no wavefront waits for another.  What bounds it is reading k and v.
+// while the next scores are formed, and no wavefront waits for another.  What bounds it is reading k and v: 16 streams over 4k to
+// 16k keys, 8 key heads of 128, 16 bits, 119 us, 4.9 TB/s.
 template <class T, int DH>
 constexpr int FEW_LDS = 8 * 32 * DH * (int)sizeof(T);
 template <class T, int DH>
@@ -835,7 +840,8 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
   if (a.lse && h == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : (m2 + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
-// Joins the parts of every row that some sequence has: 16-byte quads of a row's features, one per thread.
+// Joins the parts of every row that some sequence has, o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) s_i in their order: 16-byte quads
+// of a row's features, one per thread.  Reading the parts bounds it (32768 rows of 128 in up to 9 parts 27 us); eight are under way together.
 template <class T, int DH>
 __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
   constexpr int Q = DH / 4;
@@ -886,8 +892,9 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
 
 // --------------------------------------------------------------------------
 // Gradients, as in wm_attend.hip: P = exp(S - lse) is formed again; delta = do . o; dS = P (do . v - delta).
-// One kernel owns rows (dq; it also writes every row's statistics), one owns own keys, and the
-// program's keys take the cross attention's.
+// One kernel owns rows (dq; it also writes every row's statistics) and one keys, own ones or the programs': seven products where
+// five are counted, no atomics.  dq: matrix cores 43% and vector unit 53% busy at a width of 64 (31129 rows on 1k to 2k keys 253 us,
+// 16 bits), 50 and 33% at 128.
 
 template <class T, int DH>
 __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t, const Args a) {
@@ -1082,9 +1089,13 @@ __device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int b
 }
 
 // dk and dv of 128 keys (32 per wavefront, in registers as row operands).  EVEN: the heads of a key head divide the rows of
-// a copy, so that a tile of stacked rows is the same pattern everywhere.
+// a copy, so that a tile of stacked rows is the same pattern everywhere (with the other form everywhere: training at a width of 64
+// 879 us for 817, causal at 128 3224 for 2280).  The programs' keys at 64: matrix cores 54%, vector unit 48% busy (280 us); own keys
+// at 128: 41 and 29% (1270 us, 570 TFLOP/s), where LDS is read as long as the products take.
+template <class T, int DH, bool EVEN>
+constexpr int KEYS_PER_CU = IS_BF<T> && EVEN && DH == 64 ? 3 : IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1;
 template <class T, int DH, bool OWN, bool EVEN>
-__global__ __launch_bounds__(256, (IS_BF<T> && EVEN && DH == 64 ? 3 : IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1)) void dkv_kernel(const Table t, const Args a) {
+__global__ __launch_bounds__(256, (KEYS_PER_CU<T, DH, EVEN>)) void dkv_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
   constexpr int DB = TL::DB, RB = TILE_ROWS<T, DH>;
   __shared__ __attribute__((aligned(16))) T lds[4 * RB * DH];
@@ -1166,7 +1177,8 @@ __global__ __launch_bounds__(256, (IS_BF<T> && EVEN && DH == 64 ? 3 : IS_BF<T> &
       stats += 2 * (RB >> lg) * a.heads;
     } else {
       const int q1 = r0 / a.G, qi = (r0 + r) / a.G;
-      copy4(buffer_of(a.stat + 2 * ((w.q0 + q1) * a.heads + hk * a.G), BAD - 1), &st[buffer][64 * wave], r0 + r < x1 ? ((qi - q1) * a.heads + r0 + r - qi * a.G) * 8 + (lane & 1) * 4 : BAD);
+      copy4(buffer_of(a.stat + 2 * ((w.q0 + q1) * a.heads + hk * a.G), BAD - 1), &st[buffer][64 * wave],
+            r0 + r < x1 ? ((qi - q1) * a.heads + r0 + r - qi * a.G) * 8 + (lane & 1) * 4 : BAD);
     }
   };
   f32x16 dk[DB], dv[DB];
@@ -1565,7 +1577,10 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
     return set_error(WM_ERR_UNSUPPORTED, "too many row or key tiles");
   const int64_t rows_all = nq * w->heads, kv_all = nq * w->kv_heads;
   auto avg = [](double steps, int64_t tiles) { return tiles ? steps / tiles : 0.0; };
-  p->few = p->sh.max_r <= f.few_rows;
+  // Few rows: a program's keys by four wavefronts (two), not by one after the other.  16-bit, width 64, 32 rows over 500, 8000 keys: 13 us
+  // (22 in tiles of 128 rows), 42 (56); float32, width 128, 35 (48), 128 (205).  16-bit at 128 one workgroup fits a compute unit, and
+  // tiles are no slower: 18.0 (18.5), 70 us (83) with 64 programs of 2000.
+  p->few = !(f.bf && dh == 128) && p->sh.max_r <= f.few_rows;
   if (p->few)
     p->fwd = cut_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu, alone_of(true, f.few_cu),
                                few_us(f.bf, f.few_keys, dh, f.few_cu), part_us(rows_all, dh));
@@ -1632,8 +1647,10 @@ hipError_t forward(const wm_attention* w, const Plan& p, const Args& a, hipStrea
     hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, rows); },
                             [&](const Table& t, int blocks) {
                               const dim3 grid(blocks);
-                              if (p.few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, false>), grid, dim3(256), 0, st, t, a);
-                              else hipLaunchKernelGGL((forward_kernel<T, DH, 1, false>), grid, dim3(256), 0, st, t, a);
+                              if constexpr (!IS_BF<T> || DH < 128) {
+                                if (p.few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, false>), grid, dim3(256), 0, st, t, a);
+                              }
+                              if (!p.few) hipLaunchKernelGGL((forward_kernel<T, DH, 1, false>), grid, dim3(256), 0, st, t, a);
                               hipLaunchKernelGGL((forward_again_kernel<T, DH, false>), grid, dim3(256), 0, st, t, a, rows,
                                                  p.few ? 32 * WK : TILE_ROWS<T, DH>);
                             });
@@ -1741,7 +1758,8 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   auto cut = [&](bool few, int64_t blocks, int64_t longest) {
     const int keys = few ? FEW_KEYS : f.tile, cu = few ? few_cu : f.fwd_cu;
     const int64_t steps = cdiv(longest, keys);
-    return cut_for(blocks, 0.6 * steps, steps, 2, cu, alone_of(few, cu), few ? few_us(f.bf, keys, dh, cu) : step_us(f.bf, 2, 128, keys, dh, cu), part_us(rows_all, dh));
+    const double unit_us = few ? few_us(f.bf, keys, dh, cu) : step_us(f.bf, 2, 128, keys, dh, cu);
+    return cut_for(blocks, 0.6 * steps, steps, 2, cu, alone_of(few, cu), unit_us, part_us(rows_all, dh));
   };
   // Sequences of many rows may read the program's keys along with their own, in tiles that the last rows of each do not fill, or leave
   // them to a launch by programs, whose tiles are full; the latter's parts have to be written and read, and where the estimates are close
@@ -1753,7 +1771,8 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   p->shared = {0, 0, 0.0};
   p->joint = true;
   if (P > 0 && most_seqs > 1) {
-    const Cut own = cut(p->few, own_tiles, a->len_max), shared = cut(p->shared_few, a->S * cdiv(program_rows, p->shared_few ? FEW_ROWS : 128) * c.kv_heads, P);
+    const int64_t program_tiles = a->S * cdiv(program_rows, p->shared_few ? FEW_ROWS : 128) * c.kv_heads;
+    const Cut own = cut(p->few, own_tiles, a->len_max), shared = cut(p->shared_few, program_tiles, P);
     p->joint = !p->few && own.us + shared.us + 8.0 >= 0.8 * p->own.us;
     if (!p->joint) {
       p->own = own;

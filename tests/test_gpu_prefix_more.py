@@ -175,7 +175,8 @@ def test_captured_training(wm):
 
     def go(x):
         f = wm.prefix_attention(x["q"], x["k"], x["v"], x["pk"], x["pv"], off, c["q_off"], c["p_off"], T_max=c["T_max"], need_lse=True)
-        b = wm.prefix_attention_grad(x["do"], x["q"], x["k"], x["v"], x["pk"], x["pv"], f["o"], f["lse"], off, c["q_off"], c["p_off"], T_max=c["T_max"])
+        b = wm.prefix_attention_grad(x["do"], x["q"], x["k"], x["v"], x["pk"], x["pv"], f["o"], f["lse"], off, c["q_off"], c["p_off"],
+                                     T_max=c["T_max"])
         return {"o": f["o"], "lse": f["lse"], **{n: b[n] for n in ("dq", "dk", "dv", "dpk", "dpv")}}
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
@@ -285,7 +286,8 @@ def test_the_device_reports(wm):
             elif name == "cached":
                 wm.cached_attention(q, kc, vc, pages, lens, off, T_max=2, status=st)
             else:
-                wm.cached_attention(q, kc, vc, pages, lens, off, T_max=2, status=st, seg_off=[0, 2], prefix_pages=i32(pool.prefix_pages), prefix_lens=i32([9]))
+                wm.cached_attention(q, kc, vc, pages, lens, off, T_max=2, status=st, seg_off=[0, 2], prefix_pages=i32(pool.prefix_pages),
+                                    prefix_lens=i32([9]))
             if not what:
                 wm.device_status(st)
                 continue

@@ -33,7 +33,8 @@ def rotation(**kw):
     (dict(dtype=2), INVALID), (dict(heads=0), INVALID), (dict(heads=1025), INVALID), (dict(head_dim=60), UNSUPPORTED),
     (dict(head_dim=520, ld_x=4096), UNSUPPORTED), (dict(rot=0), INVALID), (dict(rot=3), INVALID), (dict(rot=66), INVALID),
     (dict(freq=None), INVALID), (dict(off=None), INVALID), (dict(B=0), INVALID), (dict(T_max=0), INVALID), (dict(B=-1), INVALID),
-    (dict(rows=-1), INVALID), (dict(rows=1 << 31), INVALID), (dict(rows=(1 << 26) - 3), UNSUPPORTED), (dict(x=None), INVALID), (dict(x=FAKE + 8), INVALID),
+    (dict(rows=-1), INVALID), (dict(rows=1 << 31), INVALID), (dict(rows=(1 << 26) - 3), UNSUPPORTED), (dict(x=None), INVALID),
+    (dict(x=FAKE + 8), INVALID),
     (dict(ld_x=248), INVALID), (dict(ld_x=260), INVALID), (dict(ld_x=1 << 23), INVALID),
 ])
 def test_rotate_refuses(kw, want):
@@ -80,7 +81,8 @@ CACHE = [
 
 @pytest.mark.parametrize("kw,want", CACHE + [
     (dict(rot=0), INVALID), (dict(rot=65), INVALID), (dict(rot=128), INVALID), (dict(heads=0), INVALID), (dict(q=None), INVALID),
-    (dict(rows=1 << 27), UNSUPPORTED), (dict(heads=-1), INVALID), (dict(k=None), INVALID), (dict(v=FAKE + 4), INVALID), (dict(ld_k=120), INVALID), (dict(ld_v=132), INVALID),
+    (dict(rows=1 << 27), UNSUPPORTED), (dict(heads=-1), INVALID), (dict(k=None), INVALID),
+    (dict(v=FAKE + 4), INVALID), (dict(ld_k=120), INVALID), (dict(ld_v=132), INVALID),
 ])
 def test_append_refuses(kw, want):
     lib = wm.load_library()
