@@ -613,7 +613,8 @@ wm_status wm_cached_attention(const wm_cached* a, void* o, int64_t ld_o, float* 
 /* The same on packed rows.  `shared`: q, the programs' rows q_off and their keys k, v at k_off, with kv_mask
  * over them, as in wm_cross_attention; k and v here: own keys, one for every query row, [rows][kv_heads][head_dim].
  * A row sees its program's (shown) keys and own keys from its sequence's first row to itself.  off as above with B
- * sequences (a sequence that crosses the border of two programs is cut there). */
+ * sequences (a sequence that crosses the border of two programs is cut there).  Rows behind the last sequence stay, their
+ * gradients too, and add nothing to others'. */
 typedef struct wm_prefix {
   wm_attention shared;
   const void *k, *v;

@@ -93,6 +93,11 @@ __device__ __forceinline__ int2 bounds_of(const Args& a, int from, int row, int 
   return make_int2(min(max(a.off[lo], first), row), max(min(a.off[lo + 1], end), row + 1));
 }
 
+// Of n rows from q0 on those that some sequence has; rows behind the last one stay as they are and add nothing.
+__device__ __forceinline__ int rows_before_end(const Args& a, int64_t q0, int n) {
+  return (int)min(max((int64_t)a.off[a.B] - q0, (int64_t)0), (int64_t)n);
+}
+
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 __device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
@@ -372,8 +377,10 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
   if constexpr (!PAGED) {
     Prob p;
     if (!problem<false>(t, a, rows, p, block)) return false;
-    w.q0 = p.q0; w.p0 = p.k0; w.R = p.R; w.hk = p.hk; w.split = p.split; w.P = p.Lk;
-    w.tile = (w.R + rows - 1) / rows - 1 - p.tile;            // the longest loops first
+    w.q0 = p.q0; w.p0 = p.k0; w.hk = p.hk; w.split = p.split; w.P = p.Lk;
+    w.tile = (p.R + rows - 1) / rows - 1 - p.tile;            // the longest loops first
+    w.R = rows_before_end(a, p.q0, p.R / a.G) * a.G;
+    if (w.tile * rows >= w.R) return false;
     const int first = p.q0 + w.tile * rows / a.G;
     w.seq = last_start(a.off, 0, a.B - 1, first, lane);
     w.o0 = min(max(a.off[w.seq], p.q0), first);
@@ -848,7 +855,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= rows * Q) return;
   const int64_t r = i / Q;
-  if (r / a.heads >= a.off[a.B]) return;                      // behind the last sequence
+  if (r / a.heads >= a.off[a.B]) return;
   const int d = (int)(i % Q) * 4;
   float top = -INFINITY, sum = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1074,8 +1081,10 @@ __device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int b
   if (!problem<true>(t, a, 128, p, block)) return false;
   w.q0 = p.q0; w.k0 = p.k0; w.n = p.Lk; w.first = p.tile * 128; w.hk = p.hk; w.split = p.split;
   w.x0 = w.seq = 0;
-  w.x1 = p.R;
+  w.x1 = p.R > 0 ? rows_before_end(a, p.q0, p.R / a.G) * a.G : 0;
   if constexpr (OWN) {
+    w.n = rows_before_end(a, p.q0, w.n);
+    if (w.first >= w.n) return false;
     const int last = min(w.first + 128, w.n) - 1;
     w.seq = last_start(a.off, 0, a.B - 1, p.q0 + w.first, lane);
     const int s = last_start(a.off, w.seq, a.B - 1, p.q0 + last, lane);
@@ -1453,15 +1462,16 @@ __global__ __launch_bounds__(256) void dkv_again_kernel(const Table t, const Arg
   }
 }
 
-// out[row] = sum of its parts' rows, in order; blockIdx.y picks dk or dv.
+// out[row] = sum of its parts' rows, in order; blockIdx.y picks dk or dv.  end (may be null): rows before it have parts.
 template <class T, int DH>
-__global__ __launch_bounds__(256) void add_kernel(const float* part, const int32_t* counts, int64_t rows, int sets, int heads,
+__global__ __launch_bounds__(256) void add_kernel(const float* part, const int32_t* counts, int64_t rows, int sets, int heads, const int32_t* end,
                                                   void* out0, int64_t ld0, void* out1, int64_t ld1) {
   constexpr int Q = DH / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= rows * Q) return;
   const int set = blockIdx.y;
   const int64_t r = i / Q, ld = set ? ld1 : ld0;
+  if (end && r / heads >= *end) return;
   const int d = (int)(i % Q) * 4;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   const int n = counts[r];
@@ -1671,7 +1681,7 @@ hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStr
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.sh.nq * a.heads;
     hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 1), dim3(256), 0, st, a.part, a.counts, n,
-                       1, a.heads, a.out, a.ld_out, nullptr, (int64_t)0);
+                       1, a.heads, a.off + a.B, a.out, a.ld_out, nullptr, (int64_t)0);
     return hipGetLastError();
   });
 }
@@ -1694,7 +1704,7 @@ hipError_t grad_keys(const wm_attention* w, int64_t keys, const Args& a, hipStre
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = keys * a.kv_heads;
     hipLaunchKernelGGL((add_kernel<T, DH>), dim3((unsigned)cdiv(n * (DH / 4), 256), 2), dim3(256), 0, st, a.part, a.counts, n,
-                       2, a.kv_heads, a.out, a.ld_out, a.out2, a.ld_out2);
+                       2, a.kv_heads, OWN ? a.off + a.B : nullptr, a.out, a.ld_out, a.out2, a.ld_out2);
     return hipGetLastError();
   });
 }

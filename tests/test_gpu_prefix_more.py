@@ -375,3 +375,28 @@ def test_chunks_of_many_rows(wm, dtype, per, T, P, Hq, Hk):
     for dh in (32, 64, 128):
         pool = Pool(dtype, 32, Hk, dh, L, P, seed=dh)
         check_cached(wm, dtype, pool, offsets(n), per, Hq, Hk, dh)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per,T,P,extra", [([3, 2], [30, 70, 33, 129, 1], [65, 40], 150), ([1, 1], [3, 2], [2000, 90], 2), ([1], [700], [0], 40), ([1], [0], [70], 9)])
+def test_rows_behind_the_last_sequence(wm, dtype, per, T, P, extra):
+    """Padding of packed rows, here NaN: its results stay, and others' results and gradients are those without it."""
+    c = make_prefix(dtype, per, T, P, 4, 2, 64, seed=5)
+    n = c["off"][-1]
+    x = {}
+    for m in ("q", "k", "v", "do"):
+        x[m] = torch.full((n + extra, *c[m].shape[1:]), float("nan"), dtype=c[m].dtype, device="cuda")
+        x[m][:n] = c[m]
+    rows = [x["q"], x["k"], x["v"], c["pk"], c["pv"]]
+    where = (i32(c["off"]), c["q_off"][:-1] + [n + extra], c["p_off"])
+    o = torch.full((n + extra, 4, 64), 7.0, dtype=x["q"].dtype, device="cuda")
+    lse = torch.full((n + extra, 4), 7.0, device="cuda")
+    kw = dict(T_max=max(T) + extra)
+    wm.prefix_attention(*rows, *where, o=o, lse=lse, **kw)
+    assert (o[n:] == 7.0).all() and (lse[n:] == 7.0).all()
+    g = wm.prefix_attention_grad(x["do"], *rows, o, lse, *where, **kw)
+    clean = [host(c[m]) for m in ("q", "k", "v", "pk", "pv")] + [c["off"], c["q_off"], c["p_off"], 0.125]
+    close("o", o[:n], Q.prefix(*clean)[0], ATTN[dtype])
+    spread = Q.grad_spread(host(c["do"]), *clean, None, host(o[:n]))
+    for m, want, s in zip(("dq", "dk", "dv", "dpk", "dpv"), Q.prefix_grad(host(c["do"]), *clean, o=host(o[:n])), spread):
+        close(m, g[m][:n] if m in ("dq", "dk", "dv") else g[m], want, ATTN[dtype], s)
