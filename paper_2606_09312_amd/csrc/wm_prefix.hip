@@ -43,7 +43,7 @@ struct Args {
   int seq0, nseq, row_tiles;                // a launch by sequences; 0 row tiles: by programs
   int joint;                                // by sequences: their programs' keys first
   int more_blocks, more_splits, more_chunk, more_part0;            // the few-row kernel: its first workgroups go by programs
-  int32_t* flags;                           // one per workgroup of the launch (null: rows of a tile see the same keys)
+  int again;                                // rows of a tile see different keys: sums that are not finite are formed again
   int32_t* counts;                          // gradient: how many parts a row (a key) of a head has
 };
 
@@ -102,10 +102,10 @@ __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0
 __device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
 // A weight of 0 does not hide a value that is not finite from a product, and in a block of own keys that only some
-// of the rows see, the others' weights are 0.  So every workgroup leaves a flag whether its sums are
-// finite, and where they are not, a launch behind it does its rows (or keys) again, one by one over what they see
-// alone.  (As a second form of the loops in the same kernel it took the first's registers: dk and dv at a width
-// of 128 spilled 115 of them and took 3.6 ms for 1.7.)
+// of the rows see, the others' weights are 0.  So a workgroup whose sums are not finite does its rows (or keys) again, one by
+// one over what they see alone.  It starts from its block's number, so that nothing is kept for it meanwhile.  (As a second form
+// of the loops it took the first's registers: dk and dv at a width of 128 spilled 115 of them and took 3.6 ms for 1.7.  Launches behind
+// the kernels', with a flag per workgroup, took 4.6 us each.)
 template <int DB>
 __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
   float z = 0.0f;
@@ -115,9 +115,9 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
     for (int r = 0; r < 16; ++r) z = fmaf(acc[b][r], 0.0f, z);
   return z != 0.0f;
 }
-__device__ __forceinline__ void leave_flag(const Args& a, bool bad, int tid) {
-  bad = __syncthreads_or(bad);
-  if (tid == 0) a.flags[blockIdx.x] = bad;
+__device__ __forceinline__ int formed_anew(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
 }
 
 // Page of a table, checked; lanes past the tile's pages have none.
@@ -430,6 +430,218 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
   return true;
 }
 
+// 128 keys of a segment (of its n from row k0 on), and the stacked rows [x0, x1) from row q0 on that see one of them: OWN, its
+// own keys (each seen by the rows from its own to its sequence's last), or the program's.
+struct KeyWork {
+  int64_t q0, k0;
+  int n, first, hk, split, seq, x0, x1, t0, t1;
+};
+template <bool OWN>
+__device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int block, int rows, int lane, KeyWork& w) {
+  Prob p;
+  if (!problem<true>(t, a, 128, p, block)) return false;
+  w.q0 = p.q0; w.k0 = p.k0; w.n = p.Lk; w.first = p.tile * 128; w.hk = p.hk; w.split = p.split;
+  w.x0 = w.seq = 0;
+  w.x1 = p.R > 0 ? rows_before_end(a, p.q0, p.R / a.G) * a.G : 0;
+  if constexpr (OWN) {
+    w.n = rows_before_end(a, p.q0, w.n);
+    if (w.first >= w.n) return false;
+    const int last = min(w.first + 128, w.n) - 1;
+    w.seq = last_start(a.off, 0, a.B - 1, p.q0 + w.first, lane);
+    const int s = last_start(a.off, w.seq, a.B - 1, p.q0 + last, lane);
+    w.x0 = w.first * a.G;
+    w.x1 = (max(min(a.off[s + 1], p.q0 + w.n), p.q0 + last + 1) - p.q0) * a.G;
+  }
+  const int2 tt = share_of(a, (w.x1 - w.x0 + rows - 1) / rows, w.split);
+  w.t0 = tt.x;
+  w.t1 = tt.y;
+  return true;
+}
+
+// --------------------------------------------------------------------------
+// Workgroups whose sums are not finite, again: a wavefront takes every fourth row (key) of the workgroup's and its lanes
+// 64 of the keys (rows) that it sees at a time, then its features.
+__device__ __forceinline__ float wave_max(float v) {
+  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+template <class T>
+__device__ __forceinline__ float dot(const T* x, const T* y, int n) {
+  float d = 0.0f;
+  for (int i = 0; i < n; ++i) d = fmaf((float)x[i], (float)y[i], d);
+  return d;
+}
+// Features lane and lane + 64 of the lanes' rows base + at, weighted by their w, one after the other.
+template <class T, int DH>
+__device__ __forceinline__ void add_rows(float& lower, float& upper, float w, uint64_t used, const T* base, int64_t at, int lane) {
+  for (int i = 0; i < 64; ++i) {
+    if (!((used >> i) & 1)) continue;
+    const float wi = __shfl(w, i);
+    const T* x = base + __shfl(at, i);
+    if (lane < DH) lower = fmaf(wi, (float)x[lane], lower);
+    if (DH > 64) upper = fmaf(wi, (float)x[lane + 64], upper);
+  }
+}
+template <class T, int DH>
+__device__ __forceinline__ void store_lane(T* row, float lower, float upper, int lane) {
+  if (lane < DH) row[lane] = (T)lower;
+  if (DH > 64) row[lane + 64] = (T)upper;
+}
+// Element of key i of a run (its program's, or own) in k or v; -1: its page does not exist, it reads as zero.
+template <int DH, bool PAGED>
+__device__ __forceinline__ int64_t key_at(const Args& a, const Work& w, bool own, int i, bool value) {
+  if constexpr (PAGED) {
+    const int id = (own ? w.own_table : w.shared_table)[i >> a.lps];
+    if (id < 0 || id >= a.n_pages) return -1;
+    return ((((int64_t)id * a.kv_heads + w.hk) << a.lps) + (i & ((1 << a.lps) - 1))) * DH;
+  } else {
+    return (own ? i * (value ? a.ld_v : a.ld_k) : (w.p0 + i) * (value ? a.ld_pv : a.ld_pk)) + w.hk * DH;
+  }
+}
+
+// The part of the loop that a workgroup has, in keys of the program and own keys.
+struct Span {
+  int p_lo, p_hi, o_lo, o_hi;
+};
+__device__ __forceinline__ Span span_of(const Args& a, const Work& w, int KB) {
+  const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.rest - w.o0) / KB;
+  const int2 tt = share_of(a, tiles, w.split);
+  const int t0 = tt.x, t1 = tt.y, last = a.counts ? shares_of(a, tiles) - 1 : a.splits - 1;
+  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, w.split == last ? w.o1 : w.o0 + max(t1 - nP, 0) * KB};
+}
+// Own keys that a row sees.
+template <bool PAGED>
+__device__ __forceinline__ int2 seen_by(const Args& a, const Work& w, int row, int lane) {
+  if constexpr (PAGED) {
+    return make_int2(0, max(w.before + row / a.G + 1, 0));
+  } else {
+    const int qrow = (int)w.q0 + row / a.G, s = last_start(a.off, w.seq, a.B - 1, qrow, lane);
+    return make_int2(min(max(a.off[s], (int)w.q0), qrow), qrow + 1);
+  }
+}
+
+template <class T, int DH, bool PAGED>
+__device__ __forceinline__ void forward_again(const Table& t, const Args& a, int block, int blocks, int rows, int KB) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Work w;
+  if (!work_of<PAGED>(t, a, formed_anew(block), blocks, rows, KB, lane, w)) return;
+  if (rows == 32 && PAGED) w.rest = (w.o1 + KB - 1) / KB * KB;         // the few-row kernel's: all keys in tiles
+  const Span sp = span_of(a, w, KB);
+  for (int row = w.tile * rows + wave; row < min((w.tile + 1) * rows, w.R); row += 4) {
+    const int head = w.hk * a.G + row % a.G;
+    const int64_t qrow = w.q0 + row / a.G, orow = qrow * a.heads + head;
+    const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
+    const int2 see = seen_by<PAGED>(a, w, row, lane);
+    float top = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
+    for (int own = 0; own < 2; ++own) {
+      const T* kb = static_cast<const T*>(own || PAGED ? a.k : a.pk);
+      const T* vb = static_cast<const T*>(own || PAGED ? a.v : a.pv);
+      const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
+      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        const bool shown = i < end && (own || PAGED || !a.mask || a.mask[w.p0 + i] != 0);
+        const int64_t at = shown ? key_at<DH, PAGED>(a, w, own, i, false) : -1, vat = shown ? key_at<DH, PAGED>(a, w, own, i, true) : -1;
+        const float s = !shown ? -INFINITY : at < 0 ? 0.0f : dot(q, kb + at, DH) * a.c2;
+        const float m = wave_max(s), f = m > top ? exp2_of(top - m) : 1.0f;
+        top = m > top ? m : top;
+        const float p = shown ? exp2_of(s - (top == -INFINITY ? 0.0f : top)) : 0.0f;
+        sum = sum * f + wave_sum(p);
+        x *= f;
+        y *= f;
+        add_rows<T, DH>(x, y, p, __ballot(vat >= 0), vb, vat, lane);
+      }
+    }
+    if (a.parts > 1) {
+      const int64_t prow = (int64_t)(a.part0 + w.split) * a.part_rows + orow;
+      store_lane<float, DH>(a.part + prow * DH, x, y, lane);
+      if (lane == 0) {
+        a.part_ml[2 * prow] = top;
+        a.part_ml[2 * prow + 1] = sum;
+      }
+    } else {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      store_lane<T, DH>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, x * inv, y * inv, lane);
+      if (a.lse && lane == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+    }
+  }
+}
+
+template <class T, int DH>
+__device__ __forceinline__ void dq_again(const Table& t, const Args& a, const float2* stat) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Work w;
+  if (!work_of<false>(t, a, formed_anew(blockIdx.x), gridDim.x, 128, TILE_ROWS<T, DH>, lane, w)) return;
+  const Span sp = span_of(a, w, TILE_ROWS<T, DH>);
+  for (int row = w.tile * 128 + wave; row < min((w.tile + 1) * 128, w.R); row += 4) {
+    const int head = w.hk * a.G + row % a.G;
+    const int64_t qrow = w.q0 + row / a.G, orow = qrow * a.heads + head;
+    const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
+    const T* g = static_cast<const T*>(a.d_o) + qrow * a.ld_do + head * DH;
+    const int2 see = seen_by<false>(a, w, row, lane);
+    const float l2 = stat[row - 128 * w.tile].x, delta = stat[row - 128 * w.tile].y;
+    float x = 0.0f, y = 0.0f;
+    for (int own = 0; own < 2; ++own) {
+      const T* kb = static_cast<const T*>(own ? a.k : a.pk);
+      const T* vb = static_cast<const T*>(own ? a.v : a.pv);
+      const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
+      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        const bool shown = i < end && (own || !a.mask || a.mask[w.p0 + i] != 0);
+        const int64_t at = shown ? key_at<DH, false>(a, w, own, i, false) : 0;
+        float ds = 0.0f;
+        if (shown) ds = exp2_of(fmaf(dot(q, kb + at, DH), a.c2, -l2)) * (dot(g, vb + key_at<DH, false>(a, w, own, i, true), DH) - delta);
+        add_rows<T, DH>(x, y, ds, __ballot(shown), kb, at, lane);
+      }
+    }
+    x *= a.scale;
+    y *= a.scale;
+    if (a.splits > 1) store_lane<float, DH>(a.part + (w.split * a.part_rows + orow) * DH, x, y, lane);
+    else store_lane<T, DH>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, x, y, lane);
+  }
+}
+
+template <class T, int DH>
+__device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  KeyWork w;
+  if (!key_work_of<true>(t, a, formed_anew(blockIdx.x), TILE_ROWS<T, DH>, lane, w)) return;
+  for (int key = w.first + wave; key < min(w.first + 128, w.n); key += 4) {
+    const int64_t krow = w.q0 + key;
+    const T* k = static_cast<const T*>(a.k) + krow * a.ld_k + w.hk * DH;
+    const T* v = static_cast<const T*>(a.v) + krow * a.ld_v + w.hk * DH;
+    const int s = last_start(a.off, w.seq, a.B - 1, (int)krow, lane);
+    const int hi = (max(min(a.off[s + 1], (int)w.q0 + w.n), (int)krow + 1) - (int)w.q0) * a.G;
+    const int end = min(min(w.x0 + w.t1 * TILE_ROWS<T, DH>, w.x1), hi);
+    float kx = 0.0f, ky = 0.0f, vx = 0.0f, vy = 0.0f;
+    for (int x0 = max(w.x0 + w.t0 * TILE_ROWS<T, DH>, key * a.G); x0 < end; x0 += 64) {
+      const int x = min(x0 + lane, end - 1), head = w.hk * a.G + x % a.G;
+      const int64_t qrow = w.q0 + x / a.G, orow = qrow * a.heads + head;
+      const int64_t qat = qrow * a.ld_q + head * DH, gat = qrow * a.ld_do + head * DH;
+      const T* q = static_cast<const T*>(a.q);
+      const T* g = static_cast<const T*>(a.d_o);
+      const float p = exp2_of(fmaf(dot(q + qat, k, DH), a.c2, -a.stat[2 * orow]));
+      const float ds = p * (dot(g + gat, v, DH) - a.stat[2 * orow + 1]);
+      const uint64_t used = __ballot(x0 + lane < end);
+      add_rows<T, DH>(vx, vy, p, used, g, gat, lane);
+      add_rows<T, DH>(kx, ky, ds, used, q, qat, lane);
+    }
+    kx *= a.scale;
+    ky *= a.scale;
+    if (a.splits > 1) {
+      const int64_t prow = krow * a.kv_heads + w.hk;
+      store_lane<float, DH>(a.part + ((2 * w.split) * a.part_rows + prow) * DH, kx, ky, lane);
+      store_lane<float, DH>(a.part + ((2 * w.split + 1) * a.part_rows + prow) * DH, vx, vy, lane);
+    } else {
+      store_lane<T, DH>(static_cast<T*>(a.out) + krow * a.ld_out + w.hk * DH, kx, ky, lane);
+      store_lane<T, DH>(static_cast<T*>(a.out2) + krow * a.ld_out2 + w.hk * DH, vx, vy, lane);
+    }
+  }
+}
+
 // --------------------------------------------------------------------------
 // Forward: o = sum P v / sum P, P = exp(S - m), S = scale q k, m the running maximum.  A workgroup of 4 wavefronts takes 128 / WK
 // rows (32 per wavefront); WK wavefronts share rows and take every WK-th block of 32 keys.  Tiles of K and V are staged two deep;
@@ -649,7 +861,10 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
       now = after;
     }
   }
-  if (a.flags) leave_flag(a, not_finite<DB>(acc), tid);
+  if (a.again && __syncthreads_or(not_finite<DB>(acc))) {
+    forward_again<T, DH, PAGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB);
+    return;
+  }
   sum = pair_sum(sum);
   float m2 = mx == -INFINITY ? -INFINITY : log2_units<T>(mx, a.c2);
   if constexpr (WK > 1) {       // join the wavefronts that share rows
@@ -725,7 +940,7 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
   if (by_program) {
     a.splits = given.more_splits; a.chunk = given.more_chunk; a.part0 = given.more_part0;
     a.row_tiles = 0;
-    a.flags = nullptr;
+    a.again = 0;
   }
   if (given.part0 == 0) check_rows(a, tid);
   const int block = by_program ? blockIdx.x : blockIdx.x - given.more_blocks;
@@ -790,9 +1005,9 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
     now = next;
     ti = tn;
   }
-  if (a.flags) {
-    const bool some = __syncthreads_or(tt.y > nP && not_finite<DB>(acc));
-    if (tid == 0) a.flags[block] = some;
+  if (a.again && __syncthreads_or(tt.y > nP && not_finite<DB>(acc))) {
+    forward_again<T, DH, true>(t, a, block, gridDim.x - given.more_blocks, 32, KB);
+    return;
   }
   sum = pair_sum(sum);
   float m2 = mx == -INFINITY ? -INFINITY : log2_units<T>(mx, a.c2);
@@ -904,7 +1119,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a, int64_t rows) {
 // 16 bits), 50 and 33% at 128.
 
 template <class T, int DH>
-__global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t, const Args a) {
+__global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
   constexpr int DB = TL::DB, KB = TILE_ROWS<T, DH>;
   __shared__ __attribute__((aligned(16))) T lds[4 * KB * DH];
@@ -938,10 +1153,7 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
   const int P = w.P, o0 = w.o0, rest = w.rest, o1 = w.o1, nP = (P + KB - 1) / KB, tiles = nP + (rest - o0) / KB;
   const int2 tt = share_of(a, tiles, split);
   const int shares = shares_of(a, tiles);
-  if (split >= shares) {
-    if (tid == 0) a.flags[blockIdx.x] = 0;
-    return;
-  }
+  if (split >= shares) return;
   if (split == 0 && h == 0 && row < w.R) a.counts[orow] = shares;
   const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
@@ -1059,42 +1271,20 @@ __global__ __launch_bounds__(256, IS_BF<T> ? 2 : 1) void dq_kernel(const Table t
       if (more) copy_of(TWO ? a.k : a.v, TWO ? a.ld_k : a.ld_v, first + 32, TWO ? kt : vt);
     }
   }
-  leave_flag(a, not_finite<DB>(acc), tid);
-  if (row >= w.R) return;
-  if (split == 0 && h == 0) {
+  if (split == 0 && h == 0 && row < w.R) {
     a.stat[2 * orow] = l2;
     a.stat[2 * orow + 1] = delta;
   }
+  if (__syncthreads_or(not_finite<DB>(acc))) {
+    float2* const stat = reinterpret_cast<float2*>(lds);     // the tile's rows'
+    if (h == 0) stat[32 * wave + lane] = make_float2(l2, delta);
+    __syncthreads();
+    dq_again<T, DH>(t, a, stat);
+    return;
+  }
+  if (row >= w.R) return;
   if (a.splits > 1) store_cols<float, DB>(a.part + (split * a.part_rows + orow) * DH, acc, a.scale, h);
   else store_cols<T, DB>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, acc, a.scale, h);
-}
-
-// 128 keys of a segment (of its n from row k0 on), and the stacked rows [x0, x1) from row q0 on that see one of them: OWN, its
-// own keys (each seen by the rows from its own to its sequence's last), or the program's.
-struct KeyWork {
-  int64_t q0, k0;
-  int n, first, hk, split, seq, x0, x1, t0, t1;
-};
-template <bool OWN>
-__device__ __forceinline__ bool key_work_of(const Table& t, const Args& a, int block, int rows, int lane, KeyWork& w) {
-  Prob p;
-  if (!problem<true>(t, a, 128, p, block)) return false;
-  w.q0 = p.q0; w.k0 = p.k0; w.n = p.Lk; w.first = p.tile * 128; w.hk = p.hk; w.split = p.split;
-  w.x0 = w.seq = 0;
-  w.x1 = p.R > 0 ? rows_before_end(a, p.q0, p.R / a.G) * a.G : 0;
-  if constexpr (OWN) {
-    w.n = rows_before_end(a, p.q0, w.n);
-    if (w.first >= w.n) return false;
-    const int last = min(w.first + 128, w.n) - 1;
-    w.seq = last_start(a.off, 0, a.B - 1, p.q0 + w.first, lane);
-    const int s = last_start(a.off, w.seq, a.B - 1, p.q0 + last, lane);
-    w.x0 = w.first * a.G;
-    w.x1 = (max(min(a.off[s + 1], p.q0 + w.n), p.q0 + last + 1) - p.q0) * a.G;
-  }
-  const int2 tt = share_of(a, (w.x1 - w.x0 + rows - 1) / rows, w.split);
-  w.t0 = tt.x;
-  w.t1 = tt.y;
-  return true;
 }
 
 // dk and dv of 128 keys (32 per wavefront, in registers as row operands).  EVEN: the heads of a key head divide the rows of
@@ -1120,10 +1310,7 @@ __global__ __launch_bounds__(256, (KEYS_PER_CU<T, DH, EVEN>)) void dkv_kernel(co
   KeyWork w;
   if (!key_work_of<OWN>(t, a, blockIdx.x, RB, lane, w)) return;
   const int shares = shares_of(a, (w.x1 - w.x0 + RB - 1) / RB);
-  if (w.split >= shares) {
-    if (OWN && tid == 0) a.flags[blockIdx.x] = 0;
-    return;
-  }
+  if (w.split >= shares) return;
   const int kc = min(w.first + wave * 32 + (lane & 31), w.n - 1);
   const int hk = w.hk, split = w.split, x0 = w.x0, x1 = w.x1, t0 = w.t0, t1 = w.t1;
   const int64_t kclamped = w.k0 + kc;
@@ -1254,7 +1441,13 @@ __global__ __launch_bounds__(256, (KEYS_PER_CU<T, DH, EVEN>)) void dkv_kernel(co
     step(ti, std::integral_constant<int, 0>{});
     if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
-  if (OWN) leave_flag(a, not_finite<DB>(dk) || not_finite<DB>(dv), tid);
+  if constexpr (OWN) {
+    if (split == 0 && h == 0 && a.splits > 1 && w.first + mine < w.n) a.counts[(w.k0 + w.first + mine) * a.kv_heads + hk] = shares;
+    if (__syncthreads_or(not_finite<DB>(dk) || not_finite<DB>(dv))) {
+      dkv_again<T, DH>(t, a);
+      return;
+    }
+  }
   int kl = threadIdx.x & 31;                                 // formed again, as above
   asm volatile("" : "+v"(kl));
   const int key = w.first + wave * 32 + kl;
@@ -1266,199 +1459,12 @@ __global__ __launch_bounds__(256, (KEYS_PER_CU<T, DH, EVEN>)) void dkv_kernel(co
   }
   if (a.splits > 1) {
     const int64_t prow = krow * a.kv_heads + hk;
-    if (split == 0 && h == 0) a.counts[prow] = shares;
+    if (!OWN && split == 0 && h == 0) a.counts[prow] = shares;
     store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
     store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
   } else {
     store_cols<T, DB>(static_cast<T*>(a.out) + krow * a.ld_out + hk * DH, dk, a.scale, h);
     store_cols<T, DB>(static_cast<T*>(a.out2) + krow * a.ld_out2 + hk * DH, dv, 1.0f, h);
-  }
-}
-
-// --------------------------------------------------------------------------
-// Workgroups whose sums are not finite, again: a wavefront takes every fourth row (key) of the workgroup's and its lanes
-// 64 of the keys (rows) that it sees at a time, then its features.
-__device__ __forceinline__ float wave_max(float v) {
-  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
-template <class T>
-__device__ __forceinline__ float dot(const T* x, const T* y, int n) {
-  float d = 0.0f;
-  for (int i = 0; i < n; ++i) d = fmaf((float)x[i], (float)y[i], d);
-  return d;
-}
-// Features lane and lane + 64 of the lanes' rows base + at, weighted by their w, one after the other.
-template <class T, int DH>
-__device__ __forceinline__ void add_rows(float& lower, float& upper, float w, uint64_t used, const T* base, int64_t at, int lane) {
-  for (int i = 0; i < 64; ++i) {
-    if (!((used >> i) & 1)) continue;
-    const float wi = __shfl(w, i);
-    const T* x = base + __shfl(at, i);
-    if (lane < DH) lower = fmaf(wi, (float)x[lane], lower);
-    if (DH > 64) upper = fmaf(wi, (float)x[lane + 64], upper);
-  }
-}
-template <class T, int DH>
-__device__ __forceinline__ void store_lane(T* row, float lower, float upper, int lane) {
-  if (lane < DH) row[lane] = (T)lower;
-  if (DH > 64) row[lane + 64] = (T)upper;
-}
-// Element of key i of a run (its program's, or own) in k or v; -1: its page does not exist, it reads as zero.
-template <int DH, bool PAGED>
-__device__ __forceinline__ int64_t key_at(const Args& a, const Work& w, bool own, int i, bool value) {
-  if constexpr (PAGED) {
-    const int id = (own ? w.own_table : w.shared_table)[i >> a.lps];
-    if (id < 0 || id >= a.n_pages) return -1;
-    return ((((int64_t)id * a.kv_heads + w.hk) << a.lps) + (i & ((1 << a.lps) - 1))) * DH;
-  } else {
-    return (own ? i * (value ? a.ld_v : a.ld_k) : (w.p0 + i) * (value ? a.ld_pv : a.ld_pk)) + w.hk * DH;
-  }
-}
-
-// The part of the loop that a workgroup has, in keys of the program and own keys.
-struct Span {
-  int p_lo, p_hi, o_lo, o_hi;
-};
-__device__ __forceinline__ Span span_of(const Args& a, const Work& w, int KB) {
-  const int nP = (w.P + KB - 1) / KB, tiles = nP + (w.rest - w.o0) / KB;
-  const int2 tt = share_of(a, tiles, w.split);
-  const int t0 = tt.x, t1 = tt.y, last = a.counts ? shares_of(a, tiles) - 1 : a.splits - 1;
-  return {min(t0, nP) * KB, min(min(t1, nP) * KB, w.P), w.o0 + max(t0 - nP, 0) * KB, w.split == last ? w.o1 : w.o0 + max(t1 - nP, 0) * KB};
-}
-// Own keys that a row sees.
-template <bool PAGED>
-__device__ __forceinline__ int2 seen_by(const Args& a, const Work& w, int row, int lane) {
-  if constexpr (PAGED) {
-    return make_int2(0, max(w.before + row / a.G + 1, 0));
-  } else {
-    const int qrow = (int)w.q0 + row / a.G, s = last_start(a.off, w.seq, a.B - 1, qrow, lane);
-    return make_int2(min(max(a.off[s], (int)w.q0), qrow), qrow + 1);
-  }
-}
-
-template <class T, int DH, bool PAGED>
-__global__ __launch_bounds__(256) void forward_again_kernel(const Table t, const Args a, int rows, int KB) {
-  if (!a.flags[blockIdx.x]) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Work w;
-  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, rows, KB, lane, w)) return;
-  if (rows == 32 && PAGED) w.rest = (w.o1 + KB - 1) / KB * KB;         // the few-row kernel's: all keys in tiles
-  const Span sp = span_of(a, w, KB);
-  for (int row = w.tile * rows + wave; row < min((w.tile + 1) * rows, w.R); row += 4) {
-    const int head = w.hk * a.G + row % a.G;
-    const int64_t qrow = w.q0 + row / a.G, orow = qrow * a.heads + head;
-    const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
-    const int2 see = seen_by<PAGED>(a, w, row, lane);
-    float top = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
-    for (int own = 0; own < 2; ++own) {
-      const T* kb = static_cast<const T*>(own || PAGED ? a.k : a.pk);
-      const T* vb = static_cast<const T*>(own || PAGED ? a.v : a.pv);
-      const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
-      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const bool shown = i < end && (own || PAGED || !a.mask || a.mask[w.p0 + i] != 0);
-        const int64_t at = shown ? key_at<DH, PAGED>(a, w, own, i, false) : -1, vat = shown ? key_at<DH, PAGED>(a, w, own, i, true) : -1;
-        const float s = !shown ? -INFINITY : at < 0 ? 0.0f : dot(q, kb + at, DH) * a.c2;
-        const float m = wave_max(s), f = m > top ? exp2_of(top - m) : 1.0f;
-        top = m > top ? m : top;
-        const float p = shown ? exp2_of(s - (top == -INFINITY ? 0.0f : top)) : 0.0f;
-        sum = sum * f + wave_sum(p);
-        x *= f;
-        y *= f;
-        add_rows<T, DH>(x, y, p, __ballot(vat >= 0), vb, vat, lane);
-      }
-    }
-    if (a.parts > 1) {
-      const int64_t prow = (int64_t)(a.part0 + w.split) * a.part_rows + orow;
-      store_lane<float, DH>(a.part + prow * DH, x, y, lane);
-      if (lane == 0) {
-        a.part_ml[2 * prow] = top;
-        a.part_ml[2 * prow + 1] = sum;
-      }
-    } else {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      store_lane<T, DH>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, x * inv, y * inv, lane);
-      if (a.lse && lane == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
-    }
-  }
-}
-
-template <class T, int DH>
-__global__ __launch_bounds__(256) void dq_again_kernel(const Table t, const Args a) {
-  if (!a.flags[blockIdx.x]) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Work w;
-  if (!work_of<false>(t, a, blockIdx.x, gridDim.x, 128, TILE_ROWS<T, DH>, lane, w)) return;
-  const Span sp = span_of(a, w, TILE_ROWS<T, DH>);
-  for (int row = w.tile * 128 + wave; row < min((w.tile + 1) * 128, w.R); row += 4) {
-    const int head = w.hk * a.G + row % a.G;
-    const int64_t qrow = w.q0 + row / a.G, orow = qrow * a.heads + head;
-    const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
-    const T* g = static_cast<const T*>(a.d_o) + qrow * a.ld_do + head * DH;
-    const int2 see = seen_by<false>(a, w, row, lane);
-    const float l2 = a.stat[2 * orow], delta = a.stat[2 * orow + 1];
-    float x = 0.0f, y = 0.0f;
-    for (int own = 0; own < 2; ++own) {
-      const T* kb = static_cast<const T*>(own ? a.k : a.pk);
-      const T* vb = static_cast<const T*>(own ? a.v : a.pv);
-      const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
-      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const bool shown = i < end && (own || !a.mask || a.mask[w.p0 + i] != 0);
-        const int64_t at = shown ? key_at<DH, false>(a, w, own, i, false) : 0;
-        float ds = 0.0f;
-        if (shown) ds = exp2_of(fmaf(dot(q, kb + at, DH), a.c2, -l2)) * (dot(g, vb + key_at<DH, false>(a, w, own, i, true), DH) - delta);
-        add_rows<T, DH>(x, y, ds, __ballot(shown), kb, at, lane);
-      }
-    }
-    x *= a.scale;
-    y *= a.scale;
-    if (a.splits > 1) store_lane<float, DH>(a.part + (w.split * a.part_rows + orow) * DH, x, y, lane);
-    else store_lane<T, DH>(static_cast<T*>(a.out) + qrow * a.ld_out + head * DH, x, y, lane);
-  }
-}
-
-template <class T, int DH>
-__global__ __launch_bounds__(256) void dkv_again_kernel(const Table t, const Args a) {
-  if (!a.flags[blockIdx.x]) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  KeyWork w;
-  if (!key_work_of<true>(t, a, blockIdx.x, TILE_ROWS<T, DH>, lane, w)) return;
-  for (int key = w.first + wave; key < min(w.first + 128, w.n); key += 4) {
-    const int64_t krow = w.q0 + key;
-    const T* k = static_cast<const T*>(a.k) + krow * a.ld_k + w.hk * DH;
-    const T* v = static_cast<const T*>(a.v) + krow * a.ld_v + w.hk * DH;
-    const int s = last_start(a.off, w.seq, a.B - 1, (int)krow, lane);
-    const int hi = (max(min(a.off[s + 1], (int)w.q0 + w.n), (int)krow + 1) - (int)w.q0) * a.G;
-    const int end = min(min(w.x0 + w.t1 * TILE_ROWS<T, DH>, w.x1), hi);
-    float kx = 0.0f, ky = 0.0f, vx = 0.0f, vy = 0.0f;
-    for (int x0 = max(w.x0 + w.t0 * TILE_ROWS<T, DH>, key * a.G); x0 < end; x0 += 64) {
-      const int x = min(x0 + lane, end - 1), head = w.hk * a.G + x % a.G;
-      const int64_t qrow = w.q0 + x / a.G, orow = qrow * a.heads + head;
-      const int64_t qat = qrow * a.ld_q + head * DH, gat = qrow * a.ld_do + head * DH;
-      const T* q = static_cast<const T*>(a.q);
-      const T* g = static_cast<const T*>(a.d_o);
-      const float p = exp2_of(fmaf(dot(q + qat, k, DH), a.c2, -a.stat[2 * orow]));
-      const float ds = p * (dot(g + gat, v, DH) - a.stat[2 * orow + 1]);
-      const uint64_t used = __ballot(x0 + lane < end);
-      add_rows<T, DH>(vx, vy, p, used, g, gat, lane);
-      add_rows<T, DH>(kx, ky, ds, used, q, qat, lane);
-    }
-    kx *= a.scale;
-    ky *= a.scale;
-    if (a.splits > 1) {
-      const int64_t prow = krow * a.kv_heads + w.hk;
-      store_lane<float, DH>(a.part + ((2 * w.split) * a.part_rows + prow) * DH, kx, ky, lane);
-      store_lane<float, DH>(a.part + ((2 * w.split + 1) * a.part_rows + prow) * DH, vx, vy, lane);
-    } else {
-      store_lane<T, DH>(static_cast<T*>(a.out) + krow * a.ld_out + w.hk * DH, kx, ky, lane);
-      store_lane<T, DH>(static_cast<T*>(a.out2) + krow * a.ld_out2 + w.hk * DH, vx, vy, lane);
-    }
   }
 }
 
@@ -1546,11 +1552,8 @@ struct Plan {
   Shared sh;
   bool few;
   Cut fwd, dq, dkv, dpkv;
-  size_t o_part, o_ml, o_stat, o_flags, o_counts, bytes;
+  size_t o_part, o_ml, o_stat, o_counts, bytes;
 };
-
-// a launch's workgroups: its work, dealt out over the XCDs by segment
-int64_t most_blocks(int64_t work, int S) { return work + XCDS * std::min(S, MAX_SEGS); }
 
 wm_status check(const wm_prefix* a, Plan* p, bool grad) {
   if (!a) return bad("prefix attention arguments are NULL");
@@ -1605,18 +1608,14 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
                     step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * p->sh.nk * w->kv_heads, dh));
   if (too_wide(rows_all, dh) || too_wide(p->sh.nk * w->kv_heads, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
-  p->o_part = p->o_ml = p->o_stat = p->o_flags = p->o_counts = 0;
+  p->o_part = p->o_ml = p->o_stat = p->o_counts = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   if (!grad) {
-    if (nq > 0) p->o_flags = take((size_t)most_blocks((p->few ? few_tiles : row_tiles) * w->kv_heads * p->fwd.splits, w->S) * 4);
     if (p->fwd.splits > 1) {
       p->o_part = take((size_t)p->fwd.splits * rows_all * dh * 4);
       p->o_ml = take((size_t)p->fwd.splits * rows_all * 8);
     }
   } else {
-    if (nq > 0)
-      p->o_flags = take((size_t)std::max(most_blocks(row_tiles * w->kv_heads * p->dq.splits, w->S),
-                                         most_blocks(key_tiles * w->kv_heads * p->dkv.splits, w->S)) * 4);
     p->o_stat = take((size_t)rows_all * 8);
     size_t part = 0;                             // dq's, own keys' and the programs' keys', one after the other on the stream
     if (p->dq.splits > 1) part = std::max(part, (size_t)p->dq.splits * rows_all * dh * 4);
@@ -1661,8 +1660,6 @@ hipError_t forward(const wm_attention* w, const Plan& p, const Args& a, hipStrea
                                 if (p.few) hipLaunchKernelGGL((forward_kernel<T, DH, WK, false>), grid, dim3(256), 0, st, t, a);
                               }
                               if (!p.few) hipLaunchKernelGGL((forward_kernel<T, DH, 1, false>), grid, dim3(256), 0, st, t, a);
-                              hipLaunchKernelGGL((forward_again_kernel<T, DH, false>), grid, dim3(256), 0, st, t, a, rows,
-                                                 p.few ? 32 * WK : TILE_ROWS<T, DH>);
                             });
     if (e != hipSuccess || a.parts == 1) return e;
     return join<T, DH>(a, p.sh.nq * a.heads, st);
@@ -1676,7 +1673,6 @@ hipError_t grad_rows(const wm_attention* w, const Plan& p, const Args& a, hipStr
     hipError_t e = each_run(w, false, a.splits, [&](int64_t lq, int64_t) { return cdiv(lq * a.G, 128); },
                             [&](const Table& t, int blocks) {
                               hipLaunchKernelGGL((dq_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
-                              hipLaunchKernelGGL((dq_again_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = p.sh.nq * a.heads;
@@ -1699,7 +1695,6 @@ hipError_t grad_keys(const wm_attention* w, int64_t keys, const Args& a, hipStre
                             [&](const Table& t, int blocks) {
                               if (even) hipLaunchKernelGGL((dkv_kernel<T, DH, OWN, true>), dim3(blocks), dim3(256), 0, st, t, a);
                               else hipLaunchKernelGGL((dkv_kernel<T, DH, OWN, false>), dim3(blocks), dim3(256), 0, st, t, a);
-                              if (OWN) hipLaunchKernelGGL((dkv_again_kernel<T, DH>), dim3(blocks), dim3(256), 0, st, t, a);
                             });
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t n = keys * a.kv_heads;
@@ -1716,7 +1711,7 @@ struct CachedPlan {
   bool few, shared_few;           // rows of 32 per workgroup, its wavefronts sharing them
   Cut own, shared;                // of the launch by sequences, by programs
   int64_t most_rows;              // stacked rows of a program, at most
-  size_t o_part, o_ml, o_flags, bytes;
+  size_t o_part, o_ml, bytes;
 };
 
 wm_status check(const wm_cached* a, CachedPlan* p) {
@@ -1791,10 +1786,9 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   }
   if (too_wide(rows_all, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
-  p->o_part = p->o_ml = p->o_flags = 0;
+  p->o_part = p->o_ml = 0;
   auto take = [&](size_t n) { const size_t o = at; at = al256(at + n); return o; };
   const int parts = p->own.splits + p->shared.splits;
-  if (a->T_max > 1 && a->rows > 0) p->o_flags = take((size_t)tiles * p->own.splits * 4);
   if (parts > 1) {
     p->o_part = take((size_t)parts * rows_all * dh * 4);
     p->o_ml = take((size_t)parts * rows_all * 8);
@@ -1822,8 +1816,6 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
       if (own + a.more_blocks == 0 || e != hipSuccess) return;
       if (p.few) hipLaunchKernelGGL((few_kernel<T, DH>), dim3((unsigned)(own + a.more_blocks)), dim3(256), 0, st, t, a);
       else hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), dim3((unsigned)own), dim3(256), 0, st, t, a);
-      if (a.flags && own)
-        hipLaunchKernelGGL((forward_again_kernel<T, DH, true>), dim3((unsigned)own), dim3(256), 0, st, t, a, tile, p.few ? 128 : TILE_ROWS<T, DH>);
       e = hipGetLastError();
     };
     const bool programs = x->S > 0 && x->prefix_max > 0;
@@ -1846,7 +1838,7 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
       if (p.joint || a.more_blocks || t.off[t.n] == 0 || e != hipSuccess) continue;
       Args b = a;                   // by programs: all their rows see all their keys
       b.row_tiles = 0;
-      b.flags = nullptr;
+      b.again = 0;
       b.part0 = a.more_part0;
       b.splits = a.more_splits;
       b.chunk = a.more_chunk;
@@ -1896,7 +1888,7 @@ wm_status wm_prefix_attention(const wm_prefix* x, void* o, int64_t ld_o, float* 
   a.chunk = p.fwd.chunk;
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
-  a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
+  a.again = 1;
   a.part_rows = p.sh.nq * w->heads;
   WM_PF(TK_PREFIX, forward(w, p, a, st));
   return clear_error();
@@ -1924,7 +1916,6 @@ wm_status wm_prefix_attention_grad(const wm_prefix* x, const void* o, int64_t ld
   a.lse = const_cast<float*>(lse);
   a.stat = reinterpret_cast<float*>(w8 + p.o_stat);
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
-  a.flags = reinterpret_cast<int32_t*>(w8 + p.o_flags);
   a.counts = reinterpret_cast<int32_t*>(w8 + p.o_counts);
   if (nq > 0) {
     a.out = g->dq; a.ld_out = g->ld_dq;
@@ -1984,7 +1975,7 @@ wm_status wm_cached_attention(const wm_cached* x, void* o, int64_t ld_o, float* 
   a.part = reinterpret_cast<float*>(w8 + p.o_part);
   a.part_ml = reinterpret_cast<float*>(w8 + p.o_ml);
   // one row per sequence: the rows of a tile see the same keys
-  a.flags = x->T_max > 1 ? reinterpret_cast<int32_t*>(w8 + p.o_flags) : nullptr;
+  a.again = x->T_max > 1;
   a.part_rows = x->rows * x->heads;
   WM_PF(TK_CACHED, cached(x, p, a, st));
   return clear_error();
