@@ -1506,21 +1506,22 @@ double part_us(int64_t values, int dh) { return 2.0 * values * dh * 4 / 4.5e6; }
 
 // How loops are cut into splits of `chunk` tiles (long ones into more): `blocks` loops of `avg` tiles on average and `longest` at
 // most, on 256 x per_cu places.  A tile takes unit_us where all places are taken, and `alone` of that where few are.  More shares than
-// places take an even part of the work and half a share on top, fewer as long as the longest share; parts have to be
+// places take an even part of the work and `tail` of a share on top, fewer as long as the longest share; parts have to be
 // written and read.  A split of the longest loop keeps `least` tiles.  (Measured at 256 loops of 64 to 256 tiles on 512 places, a
 // step over long programs: 9 splits 284 us, 3 splits 375.)
 struct Cut {
   int splits, chunk;
   double us;                      // what the loops and their parts take, by this
 };
-Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_cu, double alone, double unit_us, double part_us) {
+Cut cut_for(int64_t blocks, double avg, int64_t longest, int64_t least, int per_cu, double alone, double unit_us, double part_us,
+            double tail = 0.5) {
   Cut best = {1, (int)std::max<int64_t>(longest, 1), 0.0};
   const double places = 256.0 * per_cu, even = blocks * avg / places;
   double cost = 0.0;
   for (int s = 1; s <= 64 && (s == 1 || s <= longest / least); ++s) {
     const int64_t chunk = std::max<int64_t>(cdiv(longest, s), 1);
     const double shares = s > 1 ? avg / chunk + 0.5 : 1.0, fill = blocks * shares / places;
-    const double tiles = std::max(fill <= 1.0 ? even : even + 0.5 * std::min<double>(chunk, avg), chunk * alone);
+    const double tiles = std::max(fill <= 1.0 ? even : even + tail * std::min<double>(chunk, avg), chunk * alone);
     const double c = tiles * unit_us + (s > 1 ? shares * part_us + 4.0 : 0.0);
     if (s == 1 || c < 0.98 * cost) {
       cost = c;
@@ -1590,22 +1591,28 @@ wm_status check(const wm_prefix* a, Plan* p, bool grad) {
     return set_error(WM_ERR_UNSUPPORTED, "too many row or key tiles");
   const int64_t rows_all = nq * w->heads, kv_all = nq * w->kv_heads;
   auto avg = [](double steps, int64_t tiles) { return tiles ? steps / tiles : 0.0; };
+  // Where loops differ (causal ones), shares do too, and the last ones leave more places empty: up to a whole share (training of four
+  // causal sequences of 2583 to 3990 rows, 32 heads on 8 of 128: 1911 us, with half a share 2258).
+  auto tail = [&](int64_t longest, double steps, int64_t tiles) { return 0.5 * std::min(2.0, longest / std::max(avg(steps, tiles), 1.0)); };
   // Few rows: a program's keys by four wavefronts (two), not by one after the other.  16-bit, width 64, 32 rows over 500, 8000 keys: 13 us
   // (22 in tiles of 128 rows), 42 (56); float32, width 128, 35 (48), 128 (205).  16-bit at 128 one workgroup fits a compute unit, and
   // tiles are no slower: 18.0 (18.5), 70 us (83) with 64 programs of 2000.
   p->few = !(f.bf && dh == 128) && p->sh.max_r <= f.few_rows;
+  const int64_t few_loop = cdiv(longest, f.few_keys), loop = cdiv(longest, f.tile), key_loop = cdiv(longest_rows, f.tile),
+                shared_loop = cdiv(p->sh.max_r, f.tile);
   if (p->few)
-    p->fwd = cut_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), cdiv(longest, f.few_keys), 2, f.few_cu, alone_of(true, f.few_cu),
-                               few_us(f.bf, f.few_keys, dh, f.few_cu), part_us(rows_all, dh));
+    p->fwd = cut_for(few_tiles * w->kv_heads, avg(few_steps, few_tiles), few_loop, 2, f.few_cu, alone_of(true, f.few_cu),
+                     few_us(f.bf, f.few_keys, dh, f.few_cu), part_us(rows_all, dh), tail(few_loop, few_steps, few_tiles));
   else
-    p->fwd = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.fwd_cu, alone_of(false, f.fwd_cu),
-                               step_us(f.bf, 2, 128, f.tile, dh, f.fwd_cu), part_us(rows_all, dh));
-  p->dq = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), cdiv(longest, f.tile), 2, f.dq_cu, alone_of(false, f.dq_cu),
-                            step_us(f.bf, 3, 128, f.tile, dh, f.dq_cu), part_us(rows_all, dh));
-  p->dkv = cut_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), cdiv(longest_rows, f.tile), 2, f.dkv_cu, alone_of(false, f.dkv_cu),
-                             step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh));
-  p->dpkv = cut_for(shared_tiles * w->kv_heads, avg(shared_steps, shared_tiles), cdiv(p->sh.max_r, f.tile), 2, f.dkv_cu, alone_of(false, f.dkv_cu),
-                    step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * p->sh.nk * w->kv_heads, dh));
+    p->fwd = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), loop, 2, f.fwd_cu, alone_of(false, f.fwd_cu),
+                     step_us(f.bf, 2, 128, f.tile, dh, f.fwd_cu), part_us(rows_all, dh), tail(loop, row_steps, row_tiles));
+  p->dq = cut_for(row_tiles * w->kv_heads, avg(row_steps, row_tiles), loop, 2, f.dq_cu, alone_of(false, f.dq_cu),
+                  step_us(f.bf, 3, 128, f.tile, dh, f.dq_cu), part_us(rows_all, dh), tail(loop, row_steps, row_tiles));
+  p->dkv = cut_for(key_tiles * w->kv_heads, avg(key_steps, key_tiles), key_loop, 2, f.dkv_cu, alone_of(false, f.dkv_cu),
+                   step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * kv_all, dh), tail(key_loop, key_steps, key_tiles));
+  p->dpkv = cut_for(shared_tiles * w->kv_heads, avg(shared_steps, shared_tiles), shared_loop, 2, f.dkv_cu, alone_of(false, f.dkv_cu),
+                    step_us(f.bf, 4, 128, f.tile, dh, f.dkv_cu), part_us(2 * p->sh.nk * w->kv_heads, dh),
+                    tail(shared_loop, shared_steps, shared_tiles));
   if (too_wide(rows_all, dh) || too_wide(p->sh.nk * w->kv_heads, dh)) return set_error(WM_ERR_UNSUPPORTED, "rows x heads x head_dim is too large");
   size_t at = 0;
   p->o_part = p->o_ml = p->o_stat = p->o_counts = 0;
