@@ -648,7 +648,7 @@ __device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
 // softmax online (wm_attend.hip).  PAGED: the launch goes by programs (the rows of all its sequences, the program's keys
 // only) or by sequences (row_tiles > 0: its own keys, after the program's if it has any).
 // What bounds it is the vector unit, 64% busy at a width of 64 beside matrix cores at 34% (16 bits; 33324 rows on 256 to 2048 keys
-// 174 us, 628 TFLOP/s; 183 with three wavefronts per SIMD for four); at 128 both, 39 and 42% (850 TFLOP/s causal).
+// 174 us, 628 TFLOP/s; 183 with three wavefronts per SIMD for four); at 128 both, 38 and 41% (830 TFLOP/s causal).
 template <class T, int DH, int WK>
 constexpr int FWD_PER_CU = IS_BF<T> && DH == 64 && WK == 1 ? 4 : 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 template <class T, int DH, int WK, bool PAGED>
@@ -1289,8 +1289,8 @@ __global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kerne
 
 // dk and dv of 128 keys (32 per wavefront, in registers as row operands).  EVEN: the heads of a key head divide the rows of
 // a copy, so that a tile of stacked rows is the same pattern everywhere (with the other form everywhere: training at a width of 64
-// 879 us for 817, causal at 128 3224 for 2280).  The programs' keys at 64: matrix cores 54%, vector unit 48% busy (280 us); own keys
-// at 128: 41 and 29% (1270 us, 570 TFLOP/s), where LDS is read as long as the products take.
+// 879 us for 817, causal at 128 3224 for 2280).  The programs' keys at 64: matrix cores 47%, vector unit 42% busy at two wavefronts per
+// SIMD (320 us); own keys at 128: 44 and 32% (820 us, 890 TFLOP/s), where LDS is read as long as the products take.
 template <class T, int DH, bool EVEN>
 constexpr int KEYS_PER_CU = IS_BF<T> && EVEN && DH == 64 ? 3 : IS_BF<T> && (EVEN || DH <= 64) ? 2 : 1;
 template <class T, int DH, bool OWN, bool EVEN>
