@@ -167,7 +167,8 @@ def test_prefix_refuses(kw, want):
 
 def test_prefix_refuses_outputs_and_workspace():
     lib = wm.load_library()
-    a = prefix()
+    assert lib.wm_prefix_attention_workspace_bytes(prefix(), 0) == 256              # a loop in one part needs none
+    a = prefix(p_off=(0, 60000))
     n, m = (lib.wm_prefix_attention_workspace_bytes(a, g) for g in (0, 1))
     assert n > 256 and m > 256
     for args in ((None, 256, None, FAKE, n), (FAKE, 200, None, FAKE, n), (FAKE, 256, None, None, n), (FAKE, 256, None, FAKE, n - 1)):
