@@ -536,7 +536,8 @@ wm_status wm_scan_grad(const wm_scan_args* a, const void* checkpoints, const voi
  * i + rot / 2, or 2 i and 2 i + 1 where interleaved != 0) is turned by the angle
  * position x freq[i], freq [rot / 2] float32:
  *   (a, b) -> (a cos - b sin, a sin + b cos)
- * Other features stay.  Angles are reduced in 64 bits: they are right to 2e-7 at every int32 position. */
+ * Other features stay.  Whole turns are taken off before anything is rounded: sine and cosine are right to 2e-7 at every
+ * int32 position and frequency of up to 2^32. */
 
 /* x [rows][heads][head_dim], head_dim a multiple of 8 up to 512, rot even, 2 <= rot <= head_dim.  Row
  * off[s] + i is at position first[s] + i (first: device int32 [B], NULL = 0); at most 2^26 - 4 rows.  inverse != 0 turns

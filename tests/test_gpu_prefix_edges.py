@@ -1,0 +1,64 @@
+"""The operators over a shared prefix where their statements are tightest: far positions."""
+import numpy as np
+import pytest
+
+from prefix_util import host, i32
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def wm():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2606_09312_amd as wm
+    wm.load_library()
+    return wm
+
+
+# ---- far positions -------------------------------------------------------------------
+PI_DIGITS = 314159265358979323846264338327950288419716939937510582097494459230781640628620899
+
+
+def sines(position, freq):
+    """sin and cos of position x freq: whole turns are taken off in integers, from pi to 80 digits."""
+    bits = 200
+    per_turn = (10 ** 80 << bits) // (2 * PI_DIGITS)                   # 2^200 / (2 pi)
+    out = np.zeros((len(position), len(freq), 2))
+    for j, f in enumerate(np.asarray(freq, np.float32)):
+        num, den = float(f).as_integer_ratio()
+        for i, p in enumerate(position):
+            turns = int(p) * num * per_turn % (den << bits)
+            angle = 2.0 * np.pi * (turns * (1 << 60) // (den << bits)) / 2.0 ** 60
+            out[i, j] = np.sin(angle), np.cos(angle)
+    return out
+
+
+FAR = [2 ** 31 - 1, 2 ** 31 - 54321, 2 ** 30 + 7, -2 ** 31, -2 ** 31 + 99, 2 ** 24 + 1, 0, 1, -1]
+
+
+@pytest.mark.parametrize("op", ["rotate", "append"])
+def test_angles_of_far_positions(wm, op):
+    """A pair (1, 0) turns to (cos, sin), which float32 products leave as they are: the angle's error and the sums' of sine and cosine,
+    2e-7 together at every int32 position, frequencies above 1 among them."""
+    r = np.random.default_rng(3)
+    at = FAR + r.integers(2 ** 30, 2 ** 31, 60).tolist() + r.integers(-2 ** 31, -2 ** 30, 30).tolist()
+    n, dh = len(at), 128
+    freq = np.concatenate([10000.0 ** (-np.arange(32) / 32.0), 1.0 + r.random(16), 2.0 ** r.uniform(0, 20, 16)]).astype(np.float32)
+    f = torch.tensor(freq, device="cuda")
+    x = torch.zeros((n, 1, dh), device="cuda")
+    x[..., :dh // 2] = 1.0
+    off = i32(range(n + 1))
+    if op == "rotate":
+        y = wm.rotate(x, off, f, T_max=1, first=i32(at))["y"]
+    else:
+        kc, vc = (torch.zeros((n, 1, 16, dh), device="cuda") for _ in range(2))
+        first = [min(p, 2 ** 31 - 1) - 2 if p > -2 ** 31 + 2 else p for p in at]         # slot 2
+        at = [p + 2 for p in first]
+        wm.cache_append(x, x, kc, vc, i32(np.arange(n)[:, None]), i32([3] * n), off, T_max=1, first=i32(first), freq=f)
+        y = kc[:, :, 2]
+    got, want = host(y)[:, 0], sines(at, freq)
+    worst = max(np.abs(got[:, :dh // 2] - want[..., 1]).max(), np.abs(got[:, dh // 2:] - want[..., 0]).max())
+    assert worst <= 2e-7, worst
