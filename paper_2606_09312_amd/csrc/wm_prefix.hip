@@ -39,6 +39,7 @@ struct Args {
   int part0, parts;                         // this launch's first part (cached), all parts (join)
   // cached
   const int32_t *pages, *lens, *ppages, *plens;
+  int programs;                             // lengths in plens
   int max_pages, max_ppages, len_max, plen_max, n_pages, lps;      // lps: log2 of a page's slots
   int seq0, nseq, row_tiles;                // a launch by sequences; 0 row tiles: by programs
   int joint;                                // by sequences: their programs' keys first
@@ -66,6 +67,9 @@ __device__ __forceinline__ void check_rows(const Args& a, int tid) {
       if (a.lens && (a.lens[s] < 0 || a.lens[s] > a.len_max)) atomicOr(a.status, ERRBIT_KEYS);
     }
   }
+  // here and not where a workgroup reads a program: a program without sequences, or all of them where prefix_max is 0, is read by none
+  for (int64_t s = (int64_t)blockIdx.x * 256 + tid; s < a.programs; s += (int64_t)gridDim.x * 256)
+    if (a.plens[s] < 0 || a.plens[s] > a.plen_max) atomicOr(a.status, ERRBIT_KEYS);
 }
 
 // The last sequence of [lo, hi] that starts at `row` or before, looked for by a wavefront's lanes together (the
@@ -421,9 +425,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
     w.rest = max(w.before + w.tile * rows / a.G + 1, 0) / KB * KB;
     w.P = 0;
     if (seg >= 0) {
-      const int x = a.plens[seg];
-      w.P = min(max(x, 0), a.plen_max);
-      if (x != w.P && a.status && lane == 0) atomicOr(a.status, ERRBIT_KEYS);
+      w.P = min(max(a.plens[seg], 0), a.plen_max);
       w.shared_table = a.ppages + (int64_t)seg * a.max_ppages;
     }
   }
@@ -1973,6 +1975,7 @@ wm_status wm_cached_attention(const wm_cached* x, void* o, int64_t ld_o, float* 
   a.c2 = x->scale * LOG2E;
   a.heads = x->heads; a.kv_heads = c.kv_heads; a.G = x->heads / c.kv_heads;
   a.pages = c.pages; a.lens = c.lens; a.ppages = x->prefix_pages; a.plens = x->prefix_lens;
+  a.programs = x->S;
   a.max_pages = c.max_pages; a.max_ppages = x->prefix_max_pages; a.len_max = x->len_max; a.plen_max = x->prefix_max;
   a.n_pages = c.n_pages; a.lps = page_bits(c.page);
   a.out = o;

@@ -1,8 +1,10 @@
-"""The operators over a shared prefix where their statements are tightest: far positions."""
+"""The operators over a shared prefix where their statements are tightest: far positions, and lengths of programs that no
+sequence reads."""
 import numpy as np
 import pytest
 
-from prefix_util import host, i32
+from prefix_util import host, i32, offsets
+from test_gpu_prefix import status
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +64,27 @@ def test_angles_of_far_positions(wm, op):
     got, want = host(y)[:, 0], sines(at, freq)
     worst = max(np.abs(got[:, :dh // 2] - want[..., 1]).max(), np.abs(got[:, dh // 2:] - want[..., 0]).max())
     assert worst <= 2e-7, worst
+
+
+# ---- lengths of programs -------------------------------------------------------------
+@pytest.mark.parametrize("n,T_max", [([1, 1, 1], 1), ([40, 1, 3], 40)])
+@pytest.mark.parametrize("lens,pages,most", [([0, 5], 1, 0), ([0, -1], 1, 0), ([3, 0], 0, 0), ([0, 17], 1, 16), ([9, 5], 1, 8)])
+def test_lengths_of_programs_are_reported(wm, n, T_max, lens, pages, most):
+    """A program's length that is negative or passes prefix_max, also where that is 0, where the table has no pages, and where the
+    program has no sequences."""
+    off, own = offsets(n), [50, 9, 5]
+    kc = torch.randn((16, 1, 16, 32), device="cuda")
+    q = torch.randn((off[-1], 2, 32), device="cuda")
+    table = i32(np.arange(12).reshape(3, 4))
+    for seg_off in ([0, 2, 3], [0, 3, 3], [0, 0, 3]):
+        for good in (True, False):
+            st = status()
+            wm.cached_attention(q, kc, kc, table, i32(own), i32(off), T_max=T_max, len_max=64, seg_off=seg_off,
+                                prefix_pages=i32(12 + np.arange(2 * pages).reshape(2, pages)), prefix_lens=i32([min(max(x, 0), most) if good else x for x in lens]),
+                                prefix_max=most, status=st)
+            if good:
+                wm.device_status(st)
+                continue
+            with pytest.raises(wm.WMError) as e:
+                wm.device_status(st)
+            assert e.value.status == 5 and "keys" in str(e.value), seg_off
