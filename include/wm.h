@@ -636,8 +636,8 @@ typedef struct wm_prefix_grads {
   int64_t ld_dq, ld_dk, ld_dv, ld_dpk, ld_dpv;
 } wm_prefix_grads;
 
-/* Gradients given d_o = dL/do, with o and lse of the forward call.  (Rows that see few keys take the mean of their score
- * gradients from the keys instead of d_o . o, which o's rounding would spoil.) */
+/* Gradients given d_o = dL/do, with o and lse of the forward call.  (Rows that see at most 64 keys, their program's hidden ones
+ * counted, take the mean of their score gradients from the keys instead of d_o . o, which o's rounding would spoil.) */
 wm_status wm_prefix_attention_grad(const wm_prefix* a, const void* o, int64_t ld_o, const float* lse, const void* d_o, int64_t ld_do,
                                    const wm_prefix_grads* grads, void* ws, size_t ws_bytes, void* stream);
 

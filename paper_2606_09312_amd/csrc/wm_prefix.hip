@@ -1159,6 +1159,50 @@ __global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kerne
   if (split == 0 && h == 0 && row < w.R) a.counts[orow] = shares;
   const int t0 = tt.x, t1 = tt.y;
   const uint8_t* mask = a.mask ? a.mask + w.p0 : nullptr;
+  // Where a row sees few keys, the rounding of o in do . o would be the largest of its errors: its delta is the sum of P (do . v) instead.
+  // (16 bits, width 64, dq's 2-norm in 2^-8 of it: sequences of 3 rows 0.57, with do . o 0.8; with a program of 16 keys 0.61 and 0.67;
+  // of 64 keys, where do . o is taken, 0.63.)  The row alone decides, by its own keys and its program's, so that it does not matter what
+  // shares its tile.
+  constexpr int FEW = 64;
+  if (P < FEW) {
+    constexpr bool TWO = KB >= 64;
+    T* const kt = lds + wave * KB * DH;
+    T* const vt = TWO ? kt + 32 * DH : kt;
+    const uint64_t every[1] = {~0ull};
+    const bool few = P + hi - lo <= FEW;
+    const uint64_t which = __ballot(few);
+    float sum = 0.0f;
+    auto block = [&](const T* k, int64_t ldk, const T* v, int64_t ldv, int n, uint32_t seen) {
+      copy_rows<T, DH, 32, 64>(v, (int)ldv, n, false, every, vt, lane);
+      wait_counts<0, true>();
+      const f32x16 dp = TL::mm_row(vt, 0, gf, lane);
+      wait_counts<63, true>();
+      copy_rows<T, DH, 32, 64>(k, (int)ldk, n, false, every, kt, lane);
+      wait_counts<0, true>();
+      f32x16 s = TL::mm_row(kt, 0, qf, lane);
+      wait_counts<63, true>();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * dp[r];
+      only(s, seen, 0.0f, h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum += s[r];
+    };
+    if (which) {
+      for (int at = 0; at < P; at += 32) {
+        const uint32_t seen = (uint32_t)__ballot(lane < 32 && at + lane < P && (!mask || mask[at + lane] != 0));
+        block(static_cast<const T*>(a.pk) + (w.p0 + at) * a.ld_pk + w.hk * DH, a.ld_pk,
+              static_cast<const T*>(a.pv) + (w.p0 + at) * a.ld_pv + w.hk * DH, a.ld_pv, P - at, seen);
+      }
+      // rows ascend: from the first such row's keys to the last one's
+      const int end = lane_of(hi, 63 - __builtin_clzll(which));
+      for (int at = lane_of(lo, __builtin_ctzll(which)); at < end; at += 32)
+        block(static_cast<const T*>(a.k) + at * a.ld_k + w.hk * DH, a.ld_k, static_cast<const T*>(a.v) + at * a.ld_v + w.hk * DH, a.ld_v,
+              end - at, below(hi - at) & ~below(lo - at));
+      const float d = pair_sum(sum);
+      delta = few ? d : delta;
+    }
+    __syncthreads();
+  }
   uint64_t vis[1] = {0}, next[1] = {0};
   int mb = 0;
   auto mask_byte = [&](int ti) -> int {
@@ -1231,27 +1275,6 @@ __global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kerne
       copy_rows<T, DH, 32, 64>(static_cast<const T*>(x) + first * ld + w.hk * DH, (int)ld, end - first, false, every, tile, lane);
     };
     int first = max(lo_a, rest);
-    // Rows without shared tiles see so few keys that the rounding of o in do . o would be the largest of their errors (16 bits,
-    // sequences of 3 rows: dq and dk 2.0 roundings off instead of 1.4; of 128 rows, 1.5): theirs is the sum of P (do . v).
-    if (tiles == 0 && first < end) {
-      float sum = 0.0f;
-      for (int at = first; at < end; at += 32) {
-        copy_of(a.v, a.ld_v, at, vt);
-        wait_counts<0, true>();
-        const f32x16 dp = TL::mm_row(vt, 0, gf, lane);
-        wait_counts<63, true>();
-        copy_of(a.k, a.ld_k, at, kt);
-        wait_counts<0, true>();
-        f32x16 s = TL::mm_row(kt, 0, qf, lane);
-        wait_counts<63, true>();
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = weight<T>(s[r], a.c2, l2) * dp[r];
-        only(s, below(hi - at) & ~below(lo - at), 0.0f, h);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum += s[r];
-      }
-      delta = pair_sum(sum);
-    }
     if (first < end) copy_of(a.v, a.ld_v, first, vt);
     if (TWO && first < end) copy_of(a.k, a.ld_k, first, kt);
     for (; first < end; first += 32) {

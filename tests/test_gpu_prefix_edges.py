@@ -1,10 +1,11 @@
-"""The operators over a shared prefix where their statements are tightest: far positions, and lengths of programs that no
-sequence reads."""
+"""The operators over a shared prefix where their statements are tightest: far positions, lengths of programs that no sequence
+reads, gradients of rows that see few keys."""
 import numpy as np
 import pytest
 
-from prefix_util import host, i32, offsets
-from test_gpu_prefix import status
+from oracle import prefix as Q
+from prefix_util import close, host, i32, offsets
+from test_gpu_prefix import make_prefix, run_prefix, status
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +89,44 @@ def test_lengths_of_programs_are_reported(wm, n, T_max, lens, pages, most):
             with pytest.raises(wm.WMError) as e:
                 wm.device_status(st)
             assert e.value.status == 5 and "keys" in str(e.value), seg_off
+
+
+# ---- gradients of rows that see few keys -----------------------------------------------
+# Two roundings to bfloat16 remain, of the score gradients and of the results: each is spread evenly over at most half a step of
+# 2^-8, relative to values spread over a binade 0.42 x 2^-8 in the 2-norm; both together 0.59 x 2^-8, and a quarter more for the
+# spread of that.  The stored o's rounding would add as much again.
+FEW = 0.75 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_gradients_of_few_keys_beside_many(wm, dh, G):
+    """Short sequences that share a workgroup's rows with the end of a long one."""
+    T = ([200] + [3] * 25) * 8
+    c = make_prefix("bf16", [len(T)], T, [0], 2 * G, 2, dh, seed=dh + G)
+    got = run_prefix(wm, c)
+    want = Q.prefix_grad(host(c["do"]), *[host(c[m]) for m in ("q", "k", "v", "pk", "pv")], c["off"], c["q_off"], c["p_off"], dh ** -0.5)
+    short = np.repeat(np.array(T) == 3, T)
+    for name, w in zip(("dq", "dk", "dv"), want):
+        close(name, got[name][torch.tensor(short, device="cuda")], w[short], FEW)
+
+
+@pytest.mark.parametrize("hidden", [False, True])
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("P", [1, 2, 3, 4])
+def test_gradients_of_few_keys_with_a_program(wm, P, G, hidden):
+    """Programs of few keys, some of them hidden (and NaN)."""
+    S, n = 12, 10
+    T = [2 + i % 3 for i in range(S * n)]
+    c = make_prefix("bf16", [n] * S, T, [P] * S, 2 * G, 2, 64, seed=P)
+    clean = [host(c[m]) for m in ("q", "k", "v", "pk", "pv")]
+    if hidden:
+        c["mask"] = torch.ones(S * P, dtype=torch.uint8, device="cuda")
+        c["mask"][::3] = 0
+        for m in ("pk", "pv"):
+            c[m] = c[m].clone()
+            c[m][::3] = float("nan")
+    got = run_prefix(wm, c)
+    want = Q.prefix_grad(host(c["do"]), *clean, c["off"], c["q_off"], c["p_off"], 0.125, None if c["mask"] is None else c["mask"].cpu().numpy())
+    for name, w in zip(("dq", "dk", "dv", "dpk", "dpv"), want):
+        close(name, got[name], w, FEW)
