@@ -41,7 +41,8 @@ struct Args {
   const int32_t *pages, *lens, *ppages, *plens;
   int programs;                             // lengths in plens
   int max_pages, max_ppages, len_max, plen_max, n_pages, lps;      // lps: log2 of a page's slots
-  int seq0, nseq, row_tiles;                // a launch by sequences; 0 row tiles: by programs
+  int seq0, nseq, row_tiles;                // a launch by sequences, tiles of each at most; 0 row tiles: by programs
+  int slots;                                // RAGGED: workgroups of a key head and split, in place of nseq row_tiles
   int joint;                                // by sequences: their programs' keys first
   int more_blocks, more_splits, more_chunk, more_part0;            // the few-row kernel: its first workgroups go by programs
   int again;                                // rows of a tile see different keys: sums that are not finite are formed again
@@ -363,6 +364,26 @@ __device__ __forceinline__ void only(f32x16& s, uint32_t seen, float other, int 
   for (int r = 0; r < 16; ++r) s[r] = (m >> acc_row(0, r)) & 1 ? s[r] : other;
 }
 
+// RAGGED: sequences that differ so much that as many tiles for each as for the longest would be more than their rows' and one for each
+// (1024 single steps with a chunk of 300 rows, 12 heads of 64: 352 us with the longest's for each, 133 so; of 4000 rows 2227 and 618).
+// Sequence i of the launch has the slots from floor((off[i] - off[0]) G / rows) + i on, of which there are always enough for its tiles
+// before the next one's.  (A form of its own: in the common one it cost single steps and chunks 1%.)  `sequence_of_slot`: the last
+// sequence that begins at the slot or before.
+__device__ __forceinline__ int first_slot(const Args& a, int rows, int i) {
+  const int64_t x = (int64_t)a.off[a.seq0 + i] - a.off[a.seq0];
+  return (int)min(max(x * a.G / rows, (int64_t)0), (int64_t)a.slots) + i;
+}
+__device__ __forceinline__ int sequence_of_slot(const Args& a, int rows, int slot, int lane) {
+  int lo = 0, hi = a.nseq - 1;
+  while (lo < hi) {
+    const int step = (hi - lo + 63) >> 6, at = lo + step * (lane + 1);
+    const int n = __popcll(__ballot(at <= hi && first_slot(a, rows, min(at, hi)) <= slot));
+    lo += step * n;
+    hi = min(hi, lo + step - 1);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
 // A workgroup's rows (stacked rows of one key head from packed row q0 on, a tile of them), the program's keys and
 // own keys [o0, o1) that some row of the tile sees.  Those before `rest` come in whole tiles of KB, which the rows of the tile's
 // first sequence see (the paged forms' only one); of those from there on, about as many as the tile has queries, every
@@ -374,7 +395,7 @@ struct Work {
   int before;                               // paged: row i of the sequence sees before + i + 1 own keys
   const int32_t *own_table, *shared_table;  // paged
 };
-template <bool PAGED>
+template <bool PAGED, bool RAGGED = false>
 __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block, int blocks, int rows, int KB, int lane, Work& w) {
   w.p0 = w.o0 = w.rest = w.o1 = w.seq = 0;
   w.own_table = w.shared_table = nullptr;
@@ -396,12 +417,24 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
     if (a.row_tiles) {
       int at = xcd_tile(block, blocks);
       w.split = at % a.splits; at /= a.splits;
-      w.tile = a.row_tiles - 1 - at % a.row_tiles; at /= a.row_tiles;
-      const int s = a.seq0 + at % a.nseq;
-      w.hk = at / a.nseq;
+      int s;
+      if constexpr (RAGGED) {
+        w.hk = at / a.slots; at -= w.hk * a.slots;
+        s = sequence_of_slot(a, rows, at, lane);
+        at -= first_slot(a, rows, s);
+        s += a.seq0;
+      } else {
+        w.tile = a.row_tiles - 1 - at % a.row_tiles; at /= a.row_tiles;
+        s = a.seq0 + at % a.nseq;
+        w.hk = at / a.nseq;
+      }
       const int64_t x = a.off[s], y = a.off[s + 1];
       w.q0 = min(max(x, (int64_t)0), a.rows);
       n = min(min(max(y, w.q0), a.rows) - w.q0, (int64_t)a.T_max);
+      if constexpr (RAGGED) {
+        w.tile = (int)((n * a.G + rows - 1) / rows) - 1 - at;                 // the longest loops first
+        if (w.tile < 0) return false;
+      }
       int g = 0, gh = t.n - 1;                                // the sequence's program
       while (g < gh) {
         const int mid = (g + gh + 1) >> 1;
@@ -414,7 +447,7 @@ __device__ __forceinline__ bool work_of(const Table& t, const Args& a, int block
       Prob p;
       if (!problem<false>(t, a, rows, p, block)) return false;
       w.hk = p.hk; w.tile = p.tile; w.split = p.split; seg = p.k0;
-      const int64_t x = a.off[p.q0], y = a.off[p.q0 + p.R / a.G / a.T_max];
+      const int64_t x = a.off[p.q0], y = a.off[p.q0 + p.Lk];
       w.q0 = min(max(x, (int64_t)0), a.rows);
       n = min(min(max(y, w.q0), a.rows) - w.q0, (int64_t)(p.R / a.G));
     }
@@ -526,11 +559,11 @@ __device__ __forceinline__ int2 seen_by(const Args& a, const Work& w, int row, i
   }
 }
 
-template <class T, int DH, bool PAGED>
+template <class T, int DH, bool PAGED, bool RAGGED>
 __device__ __forceinline__ void forward_again(const Table& t, const Args& a, int block, int blocks, int rows, int KB) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Work w;
-  if (!work_of<PAGED>(t, a, formed_anew(block), blocks, rows, KB, lane, w)) return;
+  if (!work_of<PAGED, RAGGED>(t, a, formed_anew(block), blocks, rows, KB, lane, w)) return;
   if (rows == 32 && PAGED) w.rest = (w.o1 + KB - 1) / KB * KB;         // the few-row kernel's: all keys in tiles
   const Span sp = span_of(a, w, KB);
   for (int row = w.tile * rows + wave; row < min((w.tile + 1) * rows, w.R); row += 4) {
@@ -653,7 +686,7 @@ __device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
 // 174 us, 628 TFLOP/s; 183 with three wavefronts per SIMD for four); at 128 both, 38 and 41% (830 TFLOP/s causal).
 template <class T, int DH, int WK>
 constexpr int FWD_PER_CU = IS_BF<T> && DH == 64 && WK == 1 ? 4 : 4 * (WK > 1 ? 32 * WK : TILE_ROWS<T, DH>) * DH * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
-template <class T, int DH, int WK, bool PAGED>
+template <class T, int DH, int WK, bool PAGED, bool RAGGED = false>
 __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(const Table t, const Args a) {
   using TL = Tile<T, DH>;
   constexpr int WR = 4 / WK, DB = TL::DB;
@@ -668,7 +701,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
   if (a.part0 == 0) check_rows(a, tid);
 
   Work w;
-  if (!work_of<PAGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB, lane, w)) return;
+  if (!work_of<PAGED, RAGGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB, lane, w)) return;
   const int64_t q0 = w.q0, p0 = w.p0;
   const int R = w.R, hk = w.hk, tile = w.tile, split = w.split, P = w.P, o0 = w.o0, rest = w.rest, o1 = w.o1;
   const int row = tile * (32 * WR) + wr * 32 + (lane & 31);   // may pass R: computed, not stored
@@ -864,7 +897,7 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     }
   }
   if (a.again && __syncthreads_or(not_finite<DB>(acc))) {
-    forward_again<T, DH, PAGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB);
+    forward_again<T, DH, PAGED, RAGGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB);
     return;
   }
   sum = pair_sum(sum);
@@ -1008,7 +1041,7 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
     ti = tn;
   }
   if (a.again && __syncthreads_or(tt.y > nP && not_finite<DB>(acc))) {
-    forward_again<T, DH, true>(t, a, block, gridDim.x - given.more_blocks, 32, KB);
+    forward_again<T, DH, true, false>(t, a, block, gridDim.x - given.more_blocks, 32, KB);
     return;
   }
   sum = pair_sum(sum);
@@ -1746,6 +1779,15 @@ struct CachedPlan {
   size_t o_part, o_ml, bytes;
 };
 
+// Workgroups of a key head and split for the tiles of `seqs` sequences: as many for each as the longest needs, or, where that is more,
+// their rows' and one for each (first_slot).
+int64_t tiles_of_longest(const wm_cached* a, int G, int tile) { return cdiv(std::min<int64_t>(a->T_max, a->rows) * G, tile); }
+int64_t slots_of(const wm_cached* a, int64_t seqs, int G, int tile) {
+  return std::min(seqs * tiles_of_longest(a, G, tile), a->rows * G / tile + seqs);
+}
+// Rows of n sequences of one program, at most.
+int64_t rows_of(const wm_cached* a, int64_t n) { return std::min(n * a->T_max, a->rows); }
+
 wm_status check(const wm_cached* a, CachedPlan* p) {
   if (!a) return bad("cached attention arguments are NULL");
   const wm_status s = check_cache(&a->cache);
@@ -1775,22 +1817,24 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
       const int64_t n = (int64_t)a->seg_off[i + 1] - a->seg_off[i];
       if (n < 0) return bad("seg_off must not decrease");
       most_seqs = std::max(most_seqs, n);
-      shared_few_tiles += cdiv(n * a->T_max * G, FEW_ROWS);
+      shared_few_tiles += cdiv(rows_of(a, n) * G, FEW_ROWS);
     }
     if (a->prefix_max < 0 || a->prefix_max > (int64_t)a->prefix_max_pages * c.page) return bad("prefix_max must be in [0, prefix_max_pages page]");
     if (!a->prefix_lens || (a->prefix_max_pages > 0 && !a->prefix_pages)) return bad("prefix_lens/prefix_pages is NULL");
   }
-  if (most_seqs * a->T_max * G > INT32_MAX) return set_error(WM_ERR_UNSUPPORTED, "a program has more than 2^31 rows of one key head");
+  if (rows_of(a, most_seqs) * G > INT32_MAX) return set_error(WM_ERR_UNSUPPORTED, "a program has more than 2^31 rows of one key head");
   const int P = a->S > 0 ? a->prefix_max : 0;
   p->few = seq_rows <= FEW_ROWS;
-  p->most_rows = most_seqs * a->T_max * G;
+  p->most_rows = rows_of(a, most_seqs) * G;
   // Tiles of 32 rows of a program in the launch by sequences, or of 128 in a launch of their own.  The former read the keys as often
   // as there are tiles, from L2; they win while that is little.  16-bit, width 64, of 120 rows, 16 programs: of 300 keys 47 us (53
   // in two launches), of 4096 106 (104), of 48 rows 71 (81); width 128, 16 of 4096: 48 rows 95 (122), 96 rows 150 (130).
   const int64_t few_tiles = cdiv(p->most_rows, FEW_ROWS);
   p->shared_few = p->few && (few_tiles <= 2 || (few_tiles <= 8 && few_tiles * P <= 4096));
-  const int64_t tiles = c.B * cdiv(seq_rows, p->few ? FEW_ROWS : 128) * c.kv_heads, rows_all = a->rows * a->heads;
-  if (tiles > MOST_TILES || shared_few_tiles * c.kv_heads > MOST_TILES) return set_error(WM_ERR_UNSUPPORTED, "too many row tiles");
+  const int64_t rows_all = a->rows * a->heads;
+  const bool full = shared_few_tiles * c.kv_heads > MOST_TILES;            // no launch by programs
+  if (slots_of(a, c.B, G, p->few ? FEW_ROWS : 128) * c.kv_heads > MOST_TILES || (full && p->few))
+    return set_error(WM_ERR_UNSUPPORTED, "too many row tiles");
   // lengths are known to the device alone: loops of 0.6 of the longest on average
   auto cut = [&](bool few, int64_t blocks, int64_t longest) {
     const int keys = few ? FEW_KEYS : f.tile, cu = few ? few_cu : f.fwd_cu;
@@ -1810,7 +1854,7 @@ wm_status check(const wm_cached* a, CachedPlan* p) {
   if (P > 0 && most_seqs > 1) {
     const int64_t program_tiles = a->S * cdiv(program_rows, p->shared_few ? FEW_ROWS : 128) * c.kv_heads;
     const Cut own = cut(p->few, own_tiles, a->len_max), shared = cut(p->shared_few, program_tiles, P);
-    p->joint = !p->few && own.us + shared.us + 8.0 >= 0.8 * p->own.us;
+    p->joint = !p->few && (full || own.us + shared.us + 8.0 >= 0.8 * p->own.us);
     if (!p->joint) {
       p->own = own;
       p->shared = shared;
@@ -1835,7 +1879,7 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
     constexpr int DH = decltype(dh)::value;
     hipError_t e = hipSuccess;
     const int tile = p.few ? 32 : 128, shared_tile = p.shared_few ? 32 : 128;
-    a.row_tiles = (int)cdiv(std::min<int64_t>(x->T_max, x->rows) * a.G, tile);
+    a.row_tiles = (int)tiles_of_longest(x, a.G, tile);
     a.splits = p.own.splits;
     a.chunk = p.own.chunk;
     a.joint = p.joint && x->S > 0 && x->prefix_max > 0;
@@ -1844,9 +1888,11 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
     a.more_part0 = p.own.splits;
     // a launch by sequences, its first workgroups by programs
     auto by_sequences = [&](const Table& t) {
-      const int64_t own = (int64_t)a.nseq * a.kv_heads * a.row_tiles * a.splits;
+      a.slots = (int)slots_of(x, a.nseq, a.G, tile);
+      const int64_t own = (int64_t)a.slots * a.kv_heads * a.splits;
       if (own + a.more_blocks == 0 || e != hipSuccess) return;
       if (p.few) hipLaunchKernelGGL((few_kernel<T, DH>), dim3((unsigned)(own + a.more_blocks)), dim3(256), 0, st, t, a);
+      else if (a.slots < (int64_t)a.nseq * a.row_tiles) hipLaunchKernelGGL((forward_kernel<T, DH, 1, true, true>), dim3((unsigned)own), dim3(256), 0, st, t, a);
       else hipLaunchKernelGGL((forward_kernel<T, DH, 1, true>), dim3((unsigned)own), dim3(256), 0, st, t, a);
       e = hipGetLastError();
     };
@@ -1859,8 +1905,9 @@ hipError_t cached(const wm_cached* x, const CachedPlan& p, Args a, hipStream_t s
       Table t = {};
       for (int i = s0; i < std::min(x->S, s0 + MAX_SEGS); ++i) {
         const int n = x->seg_off[i + 1] - x->seg_off[i];
-        t.seg[t.n] = {x->seg_off[i], n * x->T_max, i, 0};
-        t.off[t.n + 1] = t.off[t.n] + (int32_t)cdiv(cdiv((int64_t)n * x->T_max * a.G, shared_tile) * a.kv_heads * p.shared.splits, XCDS);
+        const int64_t rows = rows_of(x, n);
+        t.seg[t.n] = {x->seg_off[i], (int32_t)rows, i, n};
+        t.off[t.n + 1] = t.off[t.n] + (int32_t)cdiv(cdiv(rows * a.G, shared_tile) * a.kv_heads * p.shared.splits, XCDS);
         ++t.n;
       }
       a.seq0 = x->seg_off[s0];

@@ -1,11 +1,11 @@
 """The operators over a shared prefix where their statements are tightest: far positions, lengths of programs that no sequence
-reads, gradients of rows that see few keys."""
+reads, gradients of rows that see few keys, batches of sequences that differ widely."""
 import numpy as np
 import pytest
 
 from oracle import prefix as Q
-from prefix_util import close, host, i32, offsets
-from test_gpu_prefix import make_prefix, run_prefix, status
+from prefix_util import ATTN, Pool, close, host, i32, offsets
+from test_gpu_prefix import check_cached, make_prefix, run_prefix, status
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,45 @@ def test_gradients_of_few_keys_with_a_program(wm, P, G, hidden):
     want = Q.prefix_grad(host(c["do"]), *clean, c["off"], c["q_off"], c["p_off"], 0.125, None if c["mask"] is None else c["mask"].cpu().numpy())
     for name, w in zip(("dq", "dk", "dv", "dpk", "dpv"), want):
         close(name, got[name], w, FEW)
+
+
+# ---- sequences that differ widely ------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,G,Hk", [(32, 1, 2), (64, 4, 1), (128, 3, 2)])
+@pytest.mark.parametrize("T,per,shared", [
+    ([300] + [1] * 20 + [0, 7, 130], None, []),                            # tiles dealt out by rows
+    ([1] * 30 + [0] * 40 + [257] + [2] * 9, [10, 0, 70], [90, 5, 40]),     # programs beside them, one without sequences
+    ([0] * 70 + [513, 0, 0] + [1] * 200 + [0] * 3, [100, 176], [700, 0]),  # empty ones first and last
+])
+def test_chunks_among_single_steps(wm, dtype, dh, G, Hk, T, per, shared):
+    own = [t + (5 * i) % 23 for i, t in enumerate(T)]
+    pool = Pool(dtype, 16, Hk, dh, own, shared, seed=dh, wide=1)
+    check_cached(wm, dtype, pool, offsets(T), per, G * Hk, Hk, dh, extra=3)
+
+
+@pytest.mark.parametrize("S", [1, 200])
+def test_many_sequences_and_one_long(wm, S):
+    """More workgroups than the library takes if every sequence had the longest one's; the longest comes first, in the middle and last, and
+    T_max is larger than any."""
+    B, n = 20000, 900
+    for at in (0, B // 2, B - 1):
+        T = np.ones(B, int)
+        T[at] = n
+        off = offsets(T)
+        r = np.random.default_rng(at)
+        k = torch.randn((64, 2, 16, 32), device="cuda").bfloat16()
+        v = torch.randn((64, 2, 16, 32), device="cuda").bfloat16()
+        pages, lens = r.integers(0, 64, (B, 60)), np.where(T > 1, T + 3, 2 + np.arange(B) % 9)
+        q = torch.randn((off[-1], 32, 32), device="cuda").bfloat16()
+        seg, table, plens = np.linspace(0, B, S + 1).astype(int), r.integers(0, 64, (S, 2)), np.arange(S) % 30
+        st = status()
+        o = wm.cached_attention(q, k, v, i32(pages), i32(lens), i32(off), T_max=40000, len_max=960, seg_off=seg, prefix_pages=i32(table),
+                                prefix_lens=i32(plens), status=st)["o"]
+        wm.device_status(st)
+        for s in (0, 1, at - 1, at, at + 1, B - 2, B - 1):
+            if not 0 <= s < B:
+                continue
+            p = int(np.searchsorted(seg, s, side="right")) - 1
+            want = Q.cached(host(q[off[s]:off[s + 1], :4]), host(k[:, :1]), host(v[:, :1]), pages[s:s + 1], lens[s:s + 1], [0, int(T[s])], 32 ** -0.5,
+                            [0, 1], table[p:p + 1], plens[p:p + 1])[0]
+            close(f"o of {s}", o[off[s]:off[s + 1], :4], want, ATTN["bf16"])
