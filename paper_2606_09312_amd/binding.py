@@ -950,7 +950,7 @@ def rotate(x, off, freq, *, T_max, first=None, interleaved=False, inverse=False,
     rows; freq [rot / 2] float32 turns the first rot features of a head: features i and i + rot / 2, or 2 i and
     2 i + 1 (interleaved).  Row i of sequence s is at position first[s] + i (first: device int32 [B], None = 0).
     inverse turns back: the gradient of a rotation is the rotation of its gradient with the other sign.  Returns
-    y (given: may be x).  status: zeroed int32 [64] for device_status.
+    y (given: may be x; rows behind the last sequence stay).  status: zeroed int32 [64] for device_status.
     """
     import torch
     shape, dtype, gpu = _shape3("x", x), x.dtype, x.get_device()
@@ -1027,8 +1027,8 @@ def cached_attention(q, k_cache, v_cache, pages, lens, off, *, T_max, len_max=No
     sequence's keys 0 .. lens[s] - n + i.  With seg_off (HOST [S + 1], from 0 to B), the sequences of program p also see
     its prefix_lens[p] keys (device int32 [S]) in the pages prefix_pages[p] (device int32 [S][...]) of the same pool.  len_max and
     prefix_max: no length is greater (default: what the tables hold; closer bounds divide the work better).  scale
-    defaults to head_dim ** -0.5.  Returns o, lse [rows][heads] (with need_lse or when given) and ws.  status: zeroed int32
-    [64] for device_status.
+    defaults to head_dim ** -0.5.  Returns o, lse [rows][heads] (with need_lse or when given; rows behind the last sequence
+    stay) and ws.  status: zeroed int32 [64] for device_status.
     """
     import torch
     c = _cache(k_cache, v_cache, pages, lens)
@@ -1090,7 +1090,8 @@ def prefix_attention(q, k, v, pk, pv, off, q_off, p_off, *, T_max, kv_mask=None,
     [program rows][kv_heads][head_dim], float32 or bfloat16; row strides may be larger than dense.  off: device int32
     [B + 1], the sequences' rows (at most T_max each); q_off, p_off: HOST [S + 1], the programs' query rows and keys.  A
     row sees its program's keys (those with kv_mask != 0) and own keys from its sequence's first row to itself.  Returns o, lse
-    [rows][heads] (with need_lse or when given; the gradient needs it) and ws.  status: zeroed int32 [64] for device_status.
+    [rows][heads] (with need_lse or when given; the gradient needs it) and ws.  Rows behind the last sequence stay.  status: zeroed
+    int32 [64] for device_status.
     """
     import torch
     a = _prefix(q, k, v, pk, pv, off, q_off, p_off, T_max, kv_mask, scale, status)
@@ -1106,14 +1107,22 @@ def prefix_attention(q, k, v, pk, pv, off, q_off, p_off, *, T_max, kv_mask=None,
 
 
 @_on_stream
-def prefix_attention_grad(do, q, k, v, pk, pv, o, lse, off, q_off, p_off, *, T_max, kv_mask=None, scale=None, status=None, ws=None):
-    """Gradients dq, dk, dv, dpk and dpv of prefix_attention given do = dL/do (wm_prefix_attention_grad)."""
+def prefix_attention_grad(do, q, k, v, pk, pv, o, lse, off, q_off, p_off, *, T_max, kv_mask=None, scale=None, dq=None, dk=None, dv=None,
+                          dpk=None, dpv=None, status=None, ws=None):
+    """Gradients dq, dk, dv, dpk and dpv of prefix_attention given do = dL/do (wm_prefix_attention_grad).
+
+    Each may be given, with a row stride larger than dense.  Rows behind the last sequence stay: in a gradient that is not
+    given they hold what its memory held.
+    """
     import torch
     a = _prefix(q, k, v, pk, pv, off, q_off, p_off, T_max, kv_mask, scale, status)
     dev = q.device
-    _same(q, q.shape, o=o, do=do)
+    _same(q, q.shape, o=o, do=do, dq=dq)
+    _same(q, k.shape, dk=dk, dv=dv)
+    _same(q, pk.shape, dpk=dpk, dpv=dpv)
     _f32(dev, q.shape[:2], lse=lse)
-    r = {"d" + n: torch.empty(t.shape, dtype=t.dtype, device=dev) for n, t in (("q", q), ("k", k), ("v", v), ("pk", pk), ("pv", pv))}
+    r = {n: torch.empty(t.shape, dtype=t.dtype, device=dev) if g is None else g
+         for n, t, g in (("dq", q, dq), ("dk", k, dk), ("dv", v, dv), ("dpk", pk, dpk), ("dpv", pv, dpv))}
     g = PrefixGrads(*[_addr(t) for t in r.values()], *[_rows(n, t) for n, t in r.items()])
     lib = load_library()
     ws, n = _workspace(lib.wm_prefix_attention_workspace_bytes(a, 1), ws, dev)

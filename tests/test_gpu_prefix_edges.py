@@ -1,10 +1,11 @@
 """The operators over a shared prefix where their statements are tightest: far positions, lengths of programs that no sequence
-reads, gradients of rows that see few keys, batches of sequences that differ widely."""
+reads, gradients of rows that see few keys, batches of sequences that differ widely,
+outputs that a program gives."""
 import numpy as np
 import pytest
 
 from oracle import prefix as Q
-from prefix_util import ATTN, Pool, close, host, i32, offsets
+from prefix_util import ATTN, Pool, close, dt, host, i32, offsets, same_bits
 from test_gpu_prefix import check_cached, make_prefix, run_prefix, status
 
 pytestmark = pytest.mark.gpu
@@ -172,3 +173,27 @@ def test_many_sequences_and_one_long(wm, S):
             want = Q.cached(host(q[off[s]:off[s + 1], :4]), host(k[:, :1]), host(v[:, :1]), pages[s:s + 1], lens[s:s + 1], [0, int(T[s])], 32 ** -0.5,
                             [0, 1], table[p:p + 1], plens[p:p + 1])[0]
             close(f"o of {s}", o[off[s]:off[s + 1], :4], want, ATTN["bf16"])
+
+
+# ---- outputs that a program gives ------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradient_outputs_of_the_caller(wm, dtype):
+    """Gradients into given tensors, strided ones among them: rows behind the last sequence stay."""
+    c = make_prefix(dtype, [2, 2], [30, 5, 70, 9], [40, 90], 4, 2, 64, seed=9)
+    n, extra = c["off"][-1], 7
+    x = {}
+    for m in ("q", "k", "v", "do"):
+        x[m] = torch.full((n + extra, *c[m].shape[1:]), float("nan"), dtype=c[m].dtype, device="cuda")
+        x[m][:n] = c[m]
+    where = (i32(c["off"]), c["q_off"][:-1] + [n + extra], c["p_off"])
+    o, lse = torch.zeros_like(x["q"]), torch.zeros((n + extra, 4), device="cuda")
+    rows = (x["q"], x["k"], x["v"], c["pk"], c["pv"])
+    wm.prefix_attention(*rows, *where, T_max=70, o=o, lse=lse)
+    want = wm.prefix_attention_grad(x["do"], *rows, o, lse, *where, T_max=70)
+    dqkv = torch.full((n + extra, 8, 64), 7.0, dtype=dt(dtype), device="cuda")
+    dpkv = torch.full((130, 2, 2, 64), 7.0, dtype=dt(dtype), device="cuda")
+    out = dict(dq=dqkv[:, :4], dk=dqkv[:, 4:6], dv=dqkv[:, 6:], dpk=dpkv[:, 0], dpv=dpkv[:, 1])
+    r = wm.prefix_attention_grad(x["do"], *rows, o, lse, *where, T_max=70, **out)
+    assert (dqkv[n:] == 7.0).all()
+    for m, t in out.items():
+        assert r[m] is t and same_bits(*(y[:n] if m in ("dq", "dk", "dv") else y for y in (t, want[m]))), m
