@@ -107,10 +107,13 @@ __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0
 __device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
 // A weight of 0 does not hide a value that is not finite from a product, and in a block of own keys that only some
-// of the rows see, the others' weights are 0.  So a workgroup whose sums are not finite does its rows (or keys) again, one by
-// one over what they see alone.  It starts from its block's number, so that nothing is kept for it meanwhile.  (As a second form
+// of the rows see, the others' weights are 0.  So a workgroup whose sums are not finite, and some of whose rows (or keys) do not see
+// values that can have made them so, does its rows (or keys) again, one by one over what they see alone, as long as that is not NaN
+// anyway.  It starts from its block's number, so that nothing is kept for it meanwhile.  (As a second form
 // of the loops it took the first's registers: dk and dv at a width of 128 spilled 115 of them and took 3.6 ms for 1.7.  Launches behind
-// the kernels', with a flag per workgroup, took 4.6 us each.)
+// the kernels', with a flag per workgroup, took 4.6 us each.  A training step of four sequences of 1500 rows, 32 heads on 8 of 128,
+// whose values are all NaN takes 5.9 ms for 0.6, with one row of v that is NaN 9.8; each doing again whatever is not finite, to its
+// last key, 82 and 37.)
 template <int DB>
 __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
   float z = 0.0f;
@@ -526,6 +529,32 @@ __device__ __forceinline__ void store_lane(T* row, float lower, float upper, int
   if (lane < DH) row[lane] = (T)lower;
   if (DH > 64) row[lane + 64] = (T)upper;
 }
+// A NaN stays one, whatever is added: a loop whose sums are all NaN can end.
+template <int DH>
+__device__ __forceinline__ bool all_nan(float lower, float upper, int lane) {
+  return __all((lane >= DH || lower != lower) && (DH <= 64 || upper != upper));
+}
+// Whether one of the rows [first, end), `row` gives their addresses (null: none), holds a value that is not below `limit` (as NaN is not).
+template <class T, int DH, class Row>
+__device__ __forceinline__ bool any_beyond(int first, int end, float limit, int lane, Row row) {
+  using TL = Tile<T, DH>;
+  typedef T unit __attribute__((ext_vector_type(TL::E)));
+  constexpr int RPI = 64 / TL::UPR, AHEAD = 4;
+  bool beyond = false;
+  for (int at = first; at < end && !__any(beyond); at += AHEAD * RPI) {
+    unit x[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const T* p = row(min(at + i * RPI + lane / TL::UPR, end - 1));
+      x[i] = p ? *reinterpret_cast<const unit*>(p + (lane % TL::UPR) * TL::E) : unit{};
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+      for (int e = 0; e < TL::E; ++e) beyond |= !(fabsf((float)x[i][e]) < limit);
+  }
+  return __any(beyond);
+}
 // Element of key i of a run (its program's, or own) in k or v; -1: its page does not exist, it reads as zero.
 template <int DH, bool PAGED>
 __device__ __forceinline__ int64_t key_at(const Args& a, const Work& w, bool own, int i, bool value) {
@@ -572,7 +601,7 @@ __device__ __forceinline__ void forward_again(const Table& t, const Args& a, int
     const T* q = static_cast<const T*>(a.q) + qrow * a.ld_q + head * DH;
     const int2 see = seen_by<PAGED>(a, w, row, lane);
     float top = -INFINITY, sum = 0.0f, x = 0.0f, y = 0.0f;
-    for (int own = 0; own < 2; ++own) {
+    for (int own = 0; own < 2 && sum == sum; ++own) {
       const T* kb = static_cast<const T*>(own || PAGED ? a.k : a.pk);
       const T* vb = static_cast<const T*>(own || PAGED ? a.v : a.pv);
       const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
@@ -587,7 +616,8 @@ __device__ __forceinline__ void forward_again(const Table& t, const Args& a, int
         sum = sum * f + wave_sum(p);
         x *= f;
         y *= f;
-        add_rows<T, DH>(x, y, p, __ballot(vat >= 0), vb, vat, lane);
+        if (sum != sum) break;
+        if (!all_nan<DH>(x, y, lane)) add_rows<T, DH>(x, y, p, __ballot(vat >= 0), vb, vat, lane);
       }
     }
     if (a.parts > 1) {
@@ -623,7 +653,7 @@ __device__ __forceinline__ void dq_again(const Table& t, const Args& a, const fl
       const T* kb = static_cast<const T*>(own ? a.k : a.pk);
       const T* vb = static_cast<const T*>(own ? a.v : a.pv);
       const int end = own ? min(sp.o_hi, see.y) : sp.p_hi;
-      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end; i0 += 64) {
+      for (int i0 = own ? max(sp.o_lo, see.x) : sp.p_lo; i0 < end && !all_nan<DH>(x, y, lane); i0 += 64) {
         const int i = i0 + lane;
         const bool shown = i < end && (own || !a.mask || a.mask[w.p0 + i] != 0);
         const int64_t at = shown ? key_at<DH, false>(a, w, own, i, false) : 0;
@@ -639,8 +669,32 @@ __device__ __forceinline__ void dq_again(const Table& t, const Args& a, const fl
   }
 }
 
+// Whether rows that only some of a wavefront's keys see, in the blocks that it took, can have spoilt its sums: values that are not
+// finite, and such that a score that starts from -infinity may overflow the other way.
 template <class T, int DH>
-__device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
+__device__ __forceinline__ bool dkv_spoilt(const Args& a, const KeyWork& w, int lo_a, int lo_z, int hi_a, int hi_z, int wave, int lane) {
+  constexpr float LARGE = 0x1p56f;            // 128 products of two such stay finite
+  const int key = w.first + 32 * wave, keys = min(key + 32, w.n);
+  const float c2 = IS_BF<T> ? 1.0f : fmaxf(a.c2, 1.0f);                 // float32 keys are scaled
+  if (any_beyond<T, DH>(key, keys, LARGE / c2, lane, [&](int i) { return static_cast<const T*>(a.k) + (w.q0 + i) * a.ld_k + w.hk * DH; }) ||
+      any_beyond<T, DH>(key, keys, LARGE, lane, [&](int i) { return static_cast<const T*>(a.v) + (w.q0 + i) * a.ld_v + w.hk * DH; }))
+    return true;
+  auto rows = [&](int first, int end) {
+    bool stat = false;
+    for (int x = first + lane; __any(x < end); x += 64) {
+      const float* at = a.stat + 2 * ((w.q0 + min(x, end - 1) / a.G) * a.heads + w.hk * a.G + min(x, end - 1) % a.G);
+      stat |= !(fabsf(at[0]) < INFINITY) || !(fabsf(at[1]) < INFINITY);
+    }
+    return __any(stat) ||
+           any_beyond<T, DH>(first, end, LARGE, lane, [&](int x) { return static_cast<const T*>(a.q) + (w.q0 + x / a.G) * a.ld_q + (w.hk * a.G + x % a.G) * DH; }) ||
+           any_beyond<T, DH>(first, end, LARGE, lane, [&](int x) { return static_cast<const T*>(a.d_o) + (w.q0 + x / a.G) * a.ld_do + (w.hk * a.G + x % a.G) * DH; });
+  };
+  const int begin = w.x0 + w.t0 * TILE_ROWS<T, DH>, end = min(w.x0 + w.t1 * TILE_ROWS<T, DH>, w.x1);
+  return rows(max(w.x0 + (lo_a - w.x0) / 32 * 32, begin), min(lo_z, end)) || rows(max(hi_a, begin), min(w.x0 + (hi_z - w.x0 + 31) / 32 * 32, end));
+}
+
+template <class T, int DH>
+__device__ __forceinline__ void dkv_again(const Table& t, const Args& a, bool with_v) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   KeyWork w;
   if (!key_work_of<true>(t, a, formed_anew(blockIdx.x), TILE_ROWS<T, DH>, lane, w)) return;
@@ -652,7 +706,7 @@ __device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
     const int hi = (max(min(a.off[s + 1], (int)w.q0 + w.n), (int)krow + 1) - (int)w.q0) * a.G;
     const int end = min(min(w.x0 + w.t1 * TILE_ROWS<T, DH>, w.x1), hi);
     float kx = 0.0f, ky = 0.0f, vx = 0.0f, vy = 0.0f;
-    for (int x0 = max(w.x0 + w.t0 * TILE_ROWS<T, DH>, key * a.G); x0 < end; x0 += 64) {
+    for (int x0 = max(w.x0 + w.t0 * TILE_ROWS<T, DH>, key * a.G); x0 < end && !(all_nan<DH>(kx, ky, lane) && (!with_v || all_nan<DH>(vx, vy, lane))); x0 += 64) {
       const int x = min(x0 + lane, end - 1), head = w.hk * a.G + x % a.G;
       const int64_t qrow = w.q0 + x / a.G, orow = qrow * a.heads + head;
       const int64_t qat = qrow * a.ld_q + head * DH, gat = qrow * a.ld_do + head * DH;
@@ -661,7 +715,7 @@ __device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
       const float p = exp2_of(fmaf(dot(q + qat, k, DH), a.c2, -a.stat[2 * orow]));
       const float ds = p * (dot(g + gat, v, DH) - a.stat[2 * orow + 1]);
       const uint64_t used = __ballot(x0 + lane < end);
-      add_rows<T, DH>(vx, vy, p, used, g, gat, lane);
+      if (with_v) add_rows<T, DH>(vx, vy, p, used, g, gat, lane);
       add_rows<T, DH>(kx, ky, ds, used, q, qat, lane);
     }
     kx *= a.scale;
@@ -669,10 +723,10 @@ __device__ __forceinline__ void dkv_again(const Table& t, const Args& a) {
     if (a.splits > 1) {
       const int64_t prow = krow * a.kv_heads + w.hk;
       store_lane<float, DH>(a.part + ((2 * w.split) * a.part_rows + prow) * DH, kx, ky, lane);
-      store_lane<float, DH>(a.part + ((2 * w.split + 1) * a.part_rows + prow) * DH, vx, vy, lane);
+      if (with_v) store_lane<float, DH>(a.part + ((2 * w.split + 1) * a.part_rows + prow) * DH, vx, vy, lane);
     } else {
       store_lane<T, DH>(static_cast<T*>(a.out) + krow * a.ld_out + w.hk * DH, kx, ky, lane);
-      store_lane<T, DH>(static_cast<T*>(a.out2) + krow * a.ld_out2 + w.hk * DH, vx, vy, lane);
+      if (with_v) store_lane<T, DH>(static_cast<T*>(a.out2) + krow * a.ld_out2 + w.hk * DH, vx, vy, lane);
     }
   }
 }
@@ -896,7 +950,15 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
       now = after;
     }
   }
-  if (a.again && __syncthreads_or(not_finite<DB>(acc))) {
+  // only what some of a wavefront's rows do not see can have spoilt their sums
+  auto spoilt = [&]() {
+    auto row = [&](int i) -> const T* {
+      const int64_t at = key_at<DH, PAGED>(a, w, true, i, true);
+      return at < 0 ? nullptr : static_cast<const T*>(a.v) + at;
+    };
+    return any_beyond<T, DH>(lo_a, lo_z, INFINITY, lane, row) || any_beyond<T, DH>(hi_a, min(hi_z, o1), INFINITY, lane, row);
+  };
+  if (a.again && __syncthreads_or(__any(not_finite<DB>(acc)) && spoilt())) {
     forward_again<T, DH, PAGED, RAGGED>(t, a, blockIdx.x, gridDim.x, 32 * WR, KB);
     return;
   }
@@ -1040,7 +1102,13 @@ __global__ __launch_bounds__(256, (FEW_PER_CU<T, DH>)) void few_kernel(const Tab
     now = next;
     ti = tn;
   }
-  if (a.again && __syncthreads_or(tt.y > nP && not_finite<DB>(acc))) {
+  auto spoilt = [&]() {                                       // as in the forward kernel
+    return any_beyond<T, DH>(hi_a, w.o1, INFINITY, lane, [&](int i) -> const T* {
+      const int64_t at = key_at<DH, true>(a, w, true, i, true);
+      return at < 0 ? nullptr : static_cast<const T*>(a.v) + at;
+    });
+  };
+  if (a.again && __syncthreads_or(tt.y > nP && __any(not_finite<DB>(acc)) && spoilt())) {
     forward_again<T, DH, true, false>(t, a, block, gridDim.x - given.more_blocks, 32, KB);
     return;
   }
@@ -1333,7 +1401,11 @@ __global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kerne
     a.stat[2 * orow] = l2;
     a.stat[2 * orow + 1] = delta;
   }
-  if (__syncthreads_or(not_finite<DB>(acc))) {
+  auto spoilt = [&]() {                                        // as in the forward kernel
+    auto key = [&](int i) { return static_cast<const T*>(a.k) + key_at<DH, false>(a, w, true, i, false); };
+    return any_beyond<T, DH>(lo_a, lo_z, INFINITY, lane, key) || any_beyond<T, DH>(hi_a, min(hi_z, o1), INFINITY, lane, key);
+  };
+  if (__syncthreads_or(__any(not_finite<DB>(acc)) && spoilt())) {
     float2* const stat = reinterpret_cast<float2*>(lds);     // the tile's rows'
     if (h == 0) stat[32 * wave + lane] = make_float2(l2, delta);
     __syncthreads();
@@ -1499,30 +1571,36 @@ __global__ __launch_bounds__(256, (KEYS_PER_CU<T, DH, EVEN>)) void dkv_kernel(co
     step(ti, std::integral_constant<int, 0>{});
     if (ti + 1 < t1) step(ti + 1, std::integral_constant<int, 1>{});
   }
+  bool again = false, again_v = false;
   if constexpr (OWN) {
     if (split == 0 && h == 0 && a.splits > 1 && w.first + mine < w.n) a.counts[(w.k0 + w.first + mine) * a.kv_heads + hk] = shares;
-    if (__syncthreads_or(not_finite<DB>(dk) || not_finite<DB>(dv))) {
-      dkv_again<T, DH>(t, a);
-      return;
-    }
+    again = __syncthreads_or(__any(not_finite<DB>(dk) || not_finite<DB>(dv)) && dkv_spoilt<T, DH>(a, w, lo_a, lo_z, hi_a, hi_z, wave, lane));
+    if (again) again_v = __syncthreads_or(not_finite<DB>(dv));
   }
   int kl = threadIdx.x & 31;                                 // formed again, as above
   asm volatile("" : "+v"(kl));
   const int key = w.first + wave * 32 + kl;
   const int64_t krow = w.k0 + key;
-  if (key >= w.n) return;
-  if (!OWN && a.mask && a.mask[krow] == 0) {                 // also where such a key holds NaN
+  if (key < w.n) {
+    if (!OWN && a.mask && a.mask[krow] == 0) {               // also where such a key holds NaN
 #pragma unroll
-    for (int b = 0; b < DB; ++b) dk[b] = dv[b] = f32x16{};
+      for (int b = 0; b < DB; ++b) dk[b] = dv[b] = f32x16{};
+    }
+    if (a.splits > 1) {
+      const int64_t prow = krow * a.kv_heads + hk;
+      if (!OWN && split == 0 && h == 0) a.counts[prow] = shares;
+      store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
+      store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
+    } else {
+      store_cols<T, DB>(static_cast<T*>(a.out) + krow * a.ld_out + hk * DH, dk, a.scale, h);
+      store_cols<T, DB>(static_cast<T*>(a.out2) + krow * a.ld_out2 + hk * DH, dv, 1.0f, h);
+    }
   }
-  if (a.splits > 1) {
-    const int64_t prow = krow * a.kv_heads + hk;
-    if (!OWN && split == 0 && h == 0) a.counts[prow] = shares;
-    store_cols<float, DB>(a.part + ((2 * split) * a.part_rows + prow) * DH, dk, a.scale, h);
-    store_cols<float, DB>(a.part + ((2 * split + 1) * a.part_rows + prow) * DH, dv, 1.0f, h);
-  } else {
-    store_cols<T, DB>(static_cast<T*>(a.out) + krow * a.ld_out + hk * DH, dk, a.scale, h);
-    store_cols<T, DB>(static_cast<T*>(a.out2) + krow * a.ld_out2 + hk * DH, dv, 1.0f, h);
+  if constexpr (OWN) {
+    if (again) {                                             // over what was stored, dv only where it is not finite
+      __syncthreads();
+      dkv_again<T, DH>(t, a, again_v);
+    }
   }
 }
 

@@ -140,3 +140,64 @@ def test_split_chunks(wm, dtype, dh, T, shared):
             pool.v[pool.pages[s][slot // 32], :, slot % 32, 3 + (x > 0):6] = x
         pool.k[pool.pages[s][(own[s] - 1) // 32], :, (own[s] - 1) % 32] = float("nan")
     check_cached(wm, dtype, pool, offsets(T), [len(T)] if shared else None, 2, 1, dh)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("G", [1, 3])
+def test_products_that_overflow_elsewhere(wm, dtype, dh, G):
+    """Finite values whose products are not: they stay in their sequence, its rows before them are as without them."""
+    c = make_prefix(dtype, [4], [20, 33, 7, 60], [0], 2 * G, 2, dh, seed=dh)
+    names, place = ("q", "k", "v", "pk", "pv"), (c["off"], c["q_off"], c["p_off"], dh ** -0.5)
+    x, where = {m: c[m] for m in names}, (i32(c["off"]), c["q_off"], c["p_off"])
+    clean = [host(x[m]) for m in names]
+    f = wm.prefix_attention(*x.values(), *where, T_max=60, need_lse=True)
+    given = host(f["o"])
+    want = dict(zip(("dq", "dk", "dv"), Q.prefix_grad(host(c["do"]), *clean, *place, o=given)))
+    spread = dict(zip(("dq", "dk", "dv"), Q.grad_spread(host(c["do"]), *clean, *place, None, given)))
+    a, b = c["off"][1] + 10, c["off"][2]
+    for what in ("q", "do", "v", "k"):
+        y = {**x, "do": c["do"]}
+        y[what] = y[what].clone()
+        y[what][a:b] = torch.where(torch.randn(y[what][a:b].shape, device="cuda") > 0, 3e38, -3e38).to(dt(dtype))
+        got = wm.prefix_attention_grad(y["do"], *[y[m] for m in names], f["o"], f["lse"], *where, T_max=60)
+        for m in want:
+            # rows that see none of them; keys that none of the sequence's rows see (a row's weights and the mean of its score gradients
+            # bring what it sees to all of its keys)
+            far = np.ones(c["off"][-1], bool)
+            far[(a if m == "dq" else c["off"][1]):b] = False
+            t = torch.tensor(far, device="cuda")
+            close(f"{what}: {m}", got[m][t], want[m][far], ATTN[dtype], spread[m][far])
+        if what in "qk":
+            finite = bool(torch.isfinite(got["dq"][a:b].float()).all())
+            assert not finite, what
+
+
+def test_steps_that_are_not_finite_end_soon(wm):
+    """A training step whose values are NaN, or one row's of them: sums that are formed again end where they are NaN, and are formed again
+    only where what some rows do not see can have spoilt them (up to 130 times a finite step's time without both, 4 to 17 with them)."""
+    n, Hq, Hk, dh = 6000, 32, 8, 128
+    off = i32(range(0, n + 1, 1500))
+    q, k, v, do = (torch.randn((n, h, dh), device="cuda").bfloat16() for h in (Hq, Hk, Hk, Hq))
+    none = torch.zeros((0, Hk, dh), device="cuda").bfloat16()
+
+    def step(do, q, k, v):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f = wm.prefix_attention(q, k, v, none, none, off, [0, n], [0, 0], T_max=1500, need_lse=True)
+        wm.prefix_attention_grad(do, q, k, v, none, none, f["o"], f["lse"], off, [0, n], [0, 0], T_max=1500)
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b)
+
+    def row(x):
+        x = x.clone()
+        x[n // 2 + 700] = float("nan")
+        return x
+    nan = lambda x: torch.full_like(x, float("nan"))  # noqa: E731
+    clean = min(step(do, q, k, v) for _ in range(5))
+    for name, x in (("all", (nan(do), nan(q), nan(k), nan(v))), ("do", (nan(do), q, k, v)), ("a row of do", (row(do), q, k, v)),
+                    ("a row of q", (do, row(q), k, v)), ("a row of v", (do, q, k, row(v)))):
+        t = min(step(*x) for _ in range(3))
+        print(f"[not finite] {name}: {t:.2f} ms of {clean:.2f}", flush=True)
+        assert t <= 25 * clean, f"{name}: {t} ms of {clean}"
