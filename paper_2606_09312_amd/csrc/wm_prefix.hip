@@ -138,9 +138,9 @@ __device__ __forceinline__ int page_id(const Args& a, const int32_t* table, int 
 }
 
 // Rows of a matrix (stride ld elements) into a tile: the first n of them, others read as zero.  The buffer ends with the last
-// row, so that what a lane adds to its base is the same for every tile; `some`: of the n only those of `vis`.
-template <class T, int DH, int ROWS, int NT, int NV>
-__device__ __forceinline__ void copy_rows(const T* base, int ld, int n, bool some, const uint64_t (&vis)[NV], T* tile, int tid) {
+// row, so that what a lane adds to its base is the same for every tile.
+template <class T, int DH, int ROWS, int NT>
+__device__ __forceinline__ void copy_rows(const T* base, int ld, int n, T* tile, int tid) {
   using TL = Tile<T, DH>;
   constexpr int N = ROWS * TL::UPR / NT;
   n = min(n, ROWS);
@@ -148,9 +148,7 @@ __device__ __forceinline__ void copy_rows(const T* base, int ld, int n, bool som
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int row = (i * NT + tid) / TL::UPR, unit = ((i * NT + tid) % TL::UPR) ^ TL::swz(row);
-    uint32_t at = (uint32_t)(row * ld * sizeof(T) + unit * 16);
-    if (some) at = (vis[NV > 1 ? row >> 6 : 0] >> (row & 63)) & 1 ? at : BAD;
-    copy16(buf, tile + (size_t)(i * NT + (tid & ~63)) * TL::E, at);
+    copy16(buf, tile + (size_t)(i * NT + (tid & ~63)) * TL::E, (uint32_t)(row * ld * sizeof(T) + unit * 16));
   }
 }
 
@@ -909,7 +907,6 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
     T* const kt = lds + wave * KB * DH;
     T* const vt = TWO ? kt + 32 * DH : kt;
     const int end = min(hi_z, o1);
-    const uint64_t every[1] = {~0ull};
     auto block_of = [&](int first) -> Block {
       if constexpr (PAGED) return paged_block(a, w.own_table, first, end - first, lane);
       else return {first, min(max(end - first, 0), 32), 0, 0};
@@ -920,11 +917,11 @@ __global__ __launch_bounds__(256, (FWD_PER_CU<T, DH, WK>)) void forward_kernel(c
         place = place_of<T, DH>(a, hk, b);
         copy_block<T, DH>(a.k, place, kt, lane);
       }
-      else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.k) + b.first * a.ld_k + hk * DH, (int)a.ld_k, b.n, false, every, kt, lane);
+      else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.k) + b.first * a.ld_k + hk * DH, (int)a.ld_k, b.n, kt, lane);
     };
     auto copy_v = [&](const Block& b) {
       if constexpr (PAGED) copy_block<T, DH>(a.v, place, vt, lane);        // K's block
-      else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.v) + b.first * a.ld_v + hk * DH, (int)a.ld_v, b.n, false, every, vt, lane);
+      else copy_rows<T, DH, 32, 64>(static_cast<const T*>(a.v) + b.first * a.ld_v + hk * DH, (int)a.ld_v, b.n, vt, lane);
     };
     Block now = block_of(max(lo_a, rest) + 32 * wk);
     if (now.n > 0) {
@@ -1269,16 +1266,15 @@ __global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kerne
     constexpr bool TWO = KB >= 64;
     T* const kt = lds + wave * KB * DH;
     T* const vt = TWO ? kt + 32 * DH : kt;
-    const uint64_t every[1] = {~0ull};
     const bool few = P + hi - lo <= FEW;
     const uint64_t which = __ballot(few);
     float sum = 0.0f;
     auto block = [&](const T* k, int64_t ldk, const T* v, int64_t ldv, int n, uint32_t seen) {
-      copy_rows<T, DH, 32, 64>(v, (int)ldv, n, false, every, vt, lane);
+      copy_rows<T, DH, 32, 64>(v, (int)ldv, n, vt, lane);
       wait_counts<0, true>();
       const f32x16 dp = TL::mm_row(vt, 0, gf, lane);
       wait_counts<63, true>();
-      copy_rows<T, DH, 32, 64>(k, (int)ldk, n, false, every, kt, lane);
+      copy_rows<T, DH, 32, 64>(k, (int)ldk, n, kt, lane);
       wait_counts<0, true>();
       f32x16 s = TL::mm_row(kt, 0, qf, lane);
       wait_counts<63, true>();
@@ -1371,9 +1367,8 @@ __global__ __launch_bounds__(256, IS_BF<T> ? DH == 64 ? 3 : 2 : 1) void dq_kerne
     T* const kt = lds + wave * KB * DH;
     T* const vt = TWO ? kt + 32 * DH : kt;
     const int end = min(hi_z, o1);
-    const uint64_t every[1] = {~0ull};
     auto copy_of = [&](const void* x, int64_t ld, int first, T* tile) {
-      copy_rows<T, DH, 32, 64>(static_cast<const T*>(x) + first * ld + w.hk * DH, (int)ld, end - first, false, every, tile, lane);
+      copy_rows<T, DH, 32, 64>(static_cast<const T*>(x) + first * ld + w.hk * DH, (int)ld, end - first, tile, lane);
     };
     int first = max(lo_a, rest);
     if (first < end) copy_of(a.v, a.ld_v, first, vt);
