@@ -175,6 +175,30 @@ def test_many_sequences_and_one_long(wm, S):
             close(f"o of {s}", o[off[s]:off[s + 1], :4], want, ATTN["bf16"])
 
 
+def test_bad_offsets_of_chunks_are_reported(wm):
+    """Offsets that decrease, pass the rows or sequences that pass T_max, where tiles are dealt out by rows: reported, the caches as they
+    were, rows that no sequence has too."""
+    B, n = 40, 300
+    T = [1] * (B - 1) + [n - B + 1]
+    good = offsets(T)
+    kc, vc = (torch.randn((8, 1, 16, 32), device="cuda") for _ in range(2))
+    q = torch.randn((n + 50, 2, 32), device="cuda")
+    pages, lens = i32(np.arange(B * 24).reshape(B, 24) % 8), i32([t + 2 for t in T])
+    keep = kc.clone(), vc.clone()
+    for what, off, rows in (("", good, n), ("length", good[:20] + [0] + good[21:], n), ("offsets", [x - 5 for x in good], n), ("offsets", good, n + 50),
+                            ("length", good[:-2] + [good[-1], good[-2]], n), ("length", good[:5] + [1 << 30] + good[6:], n),
+                            ("length", [0] + [-(1 << 30)] * (B - 1) + [n], n)):
+        st, o = status(), torch.full((n + 50, 2, 32), 7.0, device="cuda")
+        wm.cached_attention(q[:rows], kc, vc, pages, lens, i32(off), T_max=n - B + 1, len_max=300, o=o[:rows], status=st)
+        if what:
+            with pytest.raises(wm.WMError) as e:
+                wm.device_status(st)
+            assert e.value.status == 5 and what in str(e.value), str(e.value)
+        else:
+            wm.device_status(st)
+        assert (o[n:] == 7.0).all() and same_bits(kc, keep[0]) and same_bits(vc, keep[1])
+
+
 # ---- outputs that a program gives ------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gradient_outputs_of_the_caller(wm, dtype):

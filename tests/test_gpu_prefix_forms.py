@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import prefix as Q
-from prefix_util import ATTN, LSE, TURN, Pool, close, dt, frequencies, host, i32, offsets
+from prefix_util import ATTN, LSE, TURN, Pool, close, dt, frequencies, host, i32, offsets, same_bits
 from test_gpu_prefix import check_cached, make_prefix, status
 
 pytestmark = pytest.mark.gpu
@@ -74,6 +74,21 @@ def test_append_many_rows(wm, dtype, interleaved, n, dh, rot, page):
         else:
             assert np.array_equal(host(kc), want[1], equal_nan=True)
         assert np.array_equal(host(vc), want[2], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,rot,interleaved", [(9, 64, False), (9, 20, True), (2051, 64, True), (2051, 6, False)])
+def test_append_turns_queries_in_place(wm, dtype, n, rot, interleaved):
+    lens = lengths(n, n)
+    off, total = offsets(lens), [x + 5 for x in lens]
+    pool = Pool(dtype, 32, 1, 64, total, seed=n)
+    qkv = torch.randn((n, 4, 64), device="cuda").to(dt(dtype))
+    q, k, v = qkv[:, :2], qkv[:, 2:3], qkv[:, 3:]
+    f, before = frequencies(rot), qkv.clone()
+    kw = dict(T_max=max(lens), freq=f, interleaved=interleaved)
+    want = wm.cache_append(k, v, pool.k.clone(), pool.v.clone(), i32(pool.pages), i32(total), i32(off), q=q, **kw)["q"]
+    r = wm.cache_append(k, v, pool.k, pool.v, i32(pool.pages), i32(total), i32(off), q=q, q_out=q, **kw)
+    assert r["q"] is q and same_bits(q, want) and same_bits(qkv[:, 2:], before[:, 2:])
 
 
 # ---- values that are not finite, in split loops ----------------------------------------
