@@ -591,7 +591,10 @@ wm_status wm_cache_append(const wm_append* a, void* q_out, int64_t ld_q_out, voi
  * seg_off[p] .. seg_off[p + 1] (HOST [S + 1] from 0 to B) share them, in pages prefix_pages[p] of the same pool
  * (device int32 [S][prefix_max_pages], [S]).  len_max and prefix_max: no length is greater (the work is
  * divided by them; they need not be exact).  A row that sees no key has o = 0 and lse = -infinity.  Rows
- * behind the last sequence stay.  heads a multiple of kv_heads, at most 1024; scale as in wm_attention. */
+ * behind the last sequence stay.  heads a multiple of kv_heads, at most 1024; scale as in wm_attention.
+ * There is no mask: what is to be hidden is left out of the pages.  As wm_cache_append's positions count slots,
+ * the keys of a program with gaps are turned by wm_rotate, a sequence with its own `first` for every run of shown tokens,
+ * and appended without freq. */
 typedef struct wm_cached {
   wm_cache cache;
   int32_t T_max, len_max, heads, S, prefix_max_pages, prefix_max;

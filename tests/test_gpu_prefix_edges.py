@@ -1,11 +1,11 @@
 """The operators over a shared prefix where their statements are tightest: far positions, lengths of programs that no sequence
 reads, gradients of rows that see few keys, batches of sequences that differ widely,
-outputs that a program gives."""
+outputs that a program gives, hidden keys in a cache."""
 import numpy as np
 import pytest
 
 from oracle import prefix as Q
-from prefix_util import ATTN, Pool, close, dt, host, i32, offsets, same_bits
+from prefix_util import ATTN, Pool, close, dt, frequencies, host, i32, offsets, same_bits
 from test_gpu_prefix import check_cached, make_prefix, run_prefix, status
 
 pytestmark = pytest.mark.gpu
@@ -221,3 +221,32 @@ def test_gradient_outputs_of_the_caller(wm, dtype):
     assert (dqkv[n:] == 7.0).all()
     for m, t in out.items():
         assert r[m] is t and same_bits(*(y[:n] if m in ("dq", "dk", "dv") else y for y in (t, want[m]))), m
+
+
+# ---- hidden keys -----------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_hidden_keys_left_out_of_the_pages(wm, dtype):
+    """Programs with hidden tokens: a mask over packed rows, and in a cache runs of shown tokens turned at their own positions.  Both
+    see the same operands, so they are within twice the attention's tolerance of each other."""
+    P, n, Hq, Hk, dh, page = [40, 23], 5, 4, 2, 64, 16
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(dt(dtype))  # noqa: E731
+    pk, pv, q, k, v = rnd(sum(P), Hk, dh), rnd(sum(P), Hk, dh), rnd(2 * n, Hq, dh), rnd(2 * n, Hk, dh), rnd(2 * n, Hk, dh)
+    mask = (torch.rand(sum(P), generator=g, device="cuda") > 0.4).to(torch.uint8)
+    f, p_off, off = frequencies(dh), offsets(P), i32([0, n, 2 * n])
+    whole = wm.rotate(pk, i32(p_off), f, T_max=max(P))["y"]
+    o = wm.prefix_attention(q, k, v, whole, pv, off, [0, n, 2 * n], p_off, T_max=n, kv_mask=mask)["o"]
+
+    shown = np.nonzero(mask.cpu().numpy())[0]
+    runs = np.split(shown, np.nonzero((np.diff(shown) > 1) | np.isin(shown[1:], p_off))[0] + 1)
+    at = torch.tensor(shown, device="cuda")
+    first = [r[0] - p_off[int(np.searchsorted(p_off, r[0], side="right")) - 1] for r in runs]
+    turned = wm.rotate(pk[at], i32(offsets([len(r) for r in runs])), f, T_max=max(len(r) for r in runs), first=i32(first))["y"]
+    assert same_bits(turned, whole[at])
+    lens = [int(((shown >= a) & (shown < b)).sum()) for a, b in zip(p_off, p_off[1:])]
+    kc, vc = (torch.zeros((10, Hk, page, dh), dtype=dt(dtype), device="cuda") for _ in range(2))
+    table, own = i32(np.arange(6).reshape(2, 3)), i32([[6], [7]])
+    wm.cache_append(turned, pv[at], kc, vc, table, i32(lens), i32(offsets(lens)), T_max=max(lens))
+    wm.cache_append(k, v, kc, vc, own, i32([n, n]), off, T_max=n)
+    c = wm.cached_attention(q, kc, vc, own, i32([n, n]), off, T_max=n, seg_off=[0, 1, 2], prefix_pages=table, prefix_lens=i32(lens))["o"]
+    close("o", c, host(o), 2 * ATTN[dtype])
